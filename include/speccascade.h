@@ -57,6 +57,11 @@ extern "C" {
  * an out-of-range value never reaches the library as an enum. */
 typedef enum { SPC_F32 = 0, SPC_BF16 = 1 } spc_dtype;
 
+/* The further element type of a paged cache's keys and values (spc_kv_cache):
+ * 8-bit floats e4m3 (largest value 448, no infinities) with a float32 scale
+ * per token and head. */
+#define SPC_E4M3 2
+
 /* Deferral rules of Table 1, two constant rules, and the token-specific rules
  * of Section 4.4.  A token rule r(v) marks token v as not acceptable and uses
  * the target of Alg. 6 (TokenSpecCascade) in place of T_delta:
@@ -99,11 +104,13 @@ typedef enum {
   SPC_OK = 0,
   SPC_E_NULL = -1,      /* a required pointer is NULL                                 */
   SPC_E_SHAPE = -2,     /* B < 1, gamma < 1, gamma > SPC_MAX_GAMMA or V < 2 (any B:
-                           large batches run as several launches)                     */
+                           large batches run as several launches), or a cache's,
+                           stride's or chunk's size out of its range                  */
   SPC_E_RULE = -3,      /* a rule id outside spc_rule                                 */
-  SPC_E_PARAM = -4,     /* alpha not finite, temperature not > 0 and finite,
-                           or an unknown dtype                                        */
-  SPC_E_ALIGN = -5,     /* a logit base pointer not 16-byte aligned                   */
+  SPC_E_PARAM = -4,     /* alpha not finite, temperature not > 0 and finite, a
+                           truncation setting out of its range, or an unknown dtype   */
+  SPC_E_ALIGN = -5,     /* a pointer not aligned as its function asks (logits of the
+                           verify and drafter calls: 16 bytes)                        */
   SPC_E_WORKSPACE = -6, /* caller workspace too small or misaligned                   */
   SPC_E_HIP = -7        /* a HIP call failed; spc_last_error() holds its message      */
 } spc_status;
@@ -281,6 +288,184 @@ spc_status spc_draft_sample_ws(const void* logits, int32_t dtype, int32_t B, int
 
 /* Bytes of device workspace one spc_draft_sample_ws call of this shape needs. */
 size_t spc_draft_workspace_bytes(int32_t B, int32_t V, int32_t dtype);
+
+/*
+ * Truncated distributions: softmax(z / T) cut by top-k, top-p and min-p.
+ *
+ * A row's entries are taken in the order of their logits, the largest first
+ * (the lowest index first on a tie).  Each setting keeps a prefix of that
+ * order, and the shortest of the three is kept:
+ *   top_k  the first k entries (0: all)
+ *   top_p  the fewest entries whose mass reaches top_p times the mass of the
+ *          first k (1: all); 0 < top_p <= 1
+ *   min_p  the entries with z >= max z + T ln(min_p), i.e. of at least min_p
+ *          times the largest probability (0: all); 0 <= min_p <= 1
+ * Masked entries (-inf) are never kept.  A NaN counts as -inf, +inf as the
+ * largest finite value.  Masses, their sums and the comparisons are in 64 bits.
+ *
+ * A field of spc_truncation applies to every sequence unless its [B] device
+ * array is given.  An invalid scalar is SPC_E_PARAM; a sequence with an invalid
+ * entry in an array keeps nothing.  Temperature 0 is the greedy step: see the
+ * two functions.
+ */
+typedef struct {
+  float temperature;
+  int32_t top_k;
+  float top_p;
+  float min_p;
+  const float* temp_per_seq;
+  const int32_t* top_k_per_seq;
+  const float* top_p_per_seq;
+  const float* min_p_per_seq;
+} spc_truncation;
+
+/*
+ * spc_sample -- one token for each of B rows from its truncated distribution,
+ * renormalised: the smallest kept v (vocabulary order) whose cumulative mass
+ * exceeds u times the kept total.  Temperature 0: the argmax (lowest index).
+ *
+ *   logits      [B][V], `dtype`, row b at element b * row_stride (>= V); any
+ *               element alignment
+ *   uniforms    [B] float32 in [0, 1); may be NULL only for the batch-wide
+ *               greedy step (temperature 0 and temp_per_seq NULL)
+ *   out_token   [B] int32; -1 for a row that keeps nothing (all entries
+ *               masked, or invalid settings)
+ *   out_logprob [B] float32 or NULL: ln of the token's probability under the
+ *               renormalised kept distribution (0 at temperature 0, -inf
+ *               with token -1)
+ *   out_kept    [B] int32 or NULL: entries kept (1 at temperature 0, 0 with
+ *               token -1)
+ *   workspace   a 256-byte aligned buffer of at least
+ *               spc_truncation_workspace_bytes(B, V, dtype) bytes (its contents
+ *               need no preparation), or NULL for the internal workspace
+ */
+spc_status spc_sample(const void* logits, int32_t dtype, int32_t B, int32_t V,
+                      int64_t row_stride, const spc_truncation* truncation,
+                      const float* uniforms, int32_t* out_token, float* out_logprob,
+                      int32_t* out_kept, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
+/*
+ * spc_truncate -- the truncated distributions as logits, for spc_verify: drafts
+ * drawn by spc_sample follow the target exactly when the drafter's rows are
+ * truncated as the drafts were, and the verifier's as the target asks.
+ *
+ *   logits      [B][rows_per_seq][V], `dtype`, contiguous; any element alignment
+ *   out_logits  the same shape and type: kept entries as they are, the others
+ *               -inf.  May be `logits` itself, but not overlap it otherwise.
+ * Rows of a sequence at temperature 0 are left as they are (the greedy step
+ * reads whole rows); rows of invalid settings become -inf.  The workspace is
+ * that of spc_sample for B * rows_per_seq rows.
+ */
+spc_status spc_truncate(const void* logits, int32_t dtype, int32_t B, int32_t rows_per_seq,
+                        int32_t V, const spc_truncation* truncation, void* out_logits,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace one spc_sample or spc_truncate call of this many
+ * rows needs (0: none, a workspace is then not looked at). */
+size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype);
+
+/*
+ * A paged key/value cache, and the sequences in it.  A page holds page_size
+ * consecutive tokens of one sequence for every key/value head; position t of
+ * sequence b lies in page page_table[b][t / page_size], slot t % page_size.
+ *   k_pages   [num_pages][kv_heads][page_size][head_dim]
+ *   v_pages   [num_pages][kv_heads][head_dim][page_size] (transposed)
+ *   k_scale, v_scale  [num_pages][kv_heads][page_size] float32, for SPC_E4M3
+ *             only: a value is its code times its token's and head's scale
+ *   dtype     SPC_BF16 or SPC_E4M3
+ *   page_size a multiple of 16 (16 .. 1024); head_dim 64, 128 or 256
+ *   page_table [B][table_width] int32 device array
+ *   kv_len    [B] int32 device array: the tokens of a sequence, its new tokens
+ *             included
+ * Page and scale pointers are 16-byte aligned.
+ *
+ * New tokens come as rows.  Without row_start there are rows / B of them for
+ * every sequence, sequence after sequence; with it (a [B+1] int32 device
+ * array, not decreasing) sequence b has rows row_start[b] .. row_start[b+1]-1.
+ * The last of a sequence's n new rows is at position kv_len[b] - 1, the first
+ * at kv_len[b] - n.  Rows before row_start[0] and from row_start[B] on belong
+ * to no sequence: they are not read, and outputs for them are left as they are.
+ *
+ * Rolling back is a smaller kv_len: nothing at or past it is read.  A token
+ * whose page id lies outside [0, num_pages), or whose position lies outside
+ * [0, table_width * page_size), is not in the cache: it is not written, not
+ * read back, and not attended to.
+ */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  float* k_scale;
+  float* v_scale;
+  int32_t dtype;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t kv_heads;
+  int32_t head_dim;
+  const int32_t* page_table;
+  int32_t table_width;
+  const int32_t* kv_len;
+  int32_t B;
+} spc_kv_cache;
+
+/*
+ * spc_kv_write -- the keys and values of new tokens into their pages.
+ *
+ *   k, v        [rows][kv_heads][head_dim], `dtype` (SPC_F32 or SPC_BF16), row r
+ *               at element r * k_stride (v_stride), at least
+ *               kv_heads * head_dim; element-aligned
+ * SPC_BF16 caches round once (to nearest even).  SPC_E4M3 caches hold, for a
+ * token and head, scale = max(amax / 448, 2^-126) with amax the largest
+ * magnitude, and the codes of x / scale rounded to nearest even.  Inputs are
+ * finite (not checked).  Two rows must not share a slot: sequences that share
+ * pages may not write to them in one call.
+ */
+spc_status spc_kv_write(const spc_kv_cache* cache, const void* k, const void* v, int32_t dtype,
+                        int64_t k_stride, int64_t v_stride, int64_t rows,
+                        const int32_t* row_start, hipStream_t stream);
+
+/*
+ * spc_kv_read -- positions 0 .. length - 1 of every sequence as dense rows.
+ *
+ *   out_k, out_v  [B][length][kv_heads][head_dim], `dtype` (SPC_F32 or
+ *               SPC_BF16), 16-byte aligned.  Positions at or past kv_len, or
+ *               not in the cache, are left as they are.
+ */
+spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int32_t dtype,
+                       int32_t length, hipStream_t stream);
+
+/*
+ * spc_kv_attend -- attention of the new tokens over the cache, which holds
+ * them already (spc_kv_write first):
+ *   out = sum_t softmax_t(scale q.k_t) v_t,  t from max(0, s - window + 1) to s
+ * for the new token at position s (window 0: from 0).  A row that sees no
+ * cached token is zero.
+ *
+ *   q           [rows][heads][head_dim] bfloat16, row r at element r * q_stride;
+ *               heads a multiple of kv_heads, head i reading key/value head
+ *               i / (heads / kv_heads); element-aligned
+ *   out         the same, row r at element r * out_stride, 8-byte aligned, the
+ *               stride a multiple of 4
+ *   max_rows    with row_start, the most rows of one sequence (rows of a
+ *               longer one past it are left as they are); else ignored
+ * Scores, softmax statistics and sums are in 32 bits; probabilities enter the
+ * second product in bfloat16.  Cached tokens below kv_len are finite (not
+ * checked); what lies at or past it may be anything.
+ *   workspace   a 256-byte aligned buffer of at least
+ *               spc_kv_workspace_bytes(...) bytes, or NULL for the internal
+ *               per-device workspace (see the conventions above)
+ */
+spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                         int64_t q_stride, int32_t heads, int64_t rows,
+                         const int32_t* row_start, int32_t max_rows, float scale,
+                         int32_t window, void* out, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace one spc_kv_attend call of these sizes needs (its
+ * contents need no preparation); max_rows as there, 0 without row_start.  Of
+ * the cache only its sizes are read. */
+size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                              int32_t max_rows);
 
 /* Bytes of device workspace one call of this shape needs. */
 size_t spc_workspace_bytes(int32_t B, int32_t gamma, int32_t V, int32_t dtype);

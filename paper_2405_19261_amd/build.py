@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libspeccascade.so")
-SOURCES = ["spc_kernels.hip", "spc_api.cpp"]
+SOURCES = ["spc_kernels.hip", "spc_sample.hip", "spc_kv.hip", "spc_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -581,9 +581,284 @@ spc_status draft_impl(const void* logits, int32_t dtype, int32_t B, int32_t V, f
   return SPC_OK;
 }
 
+// Settings of spc_truncation that apply to the whole batch.
+spc_status check_truncation(const spc_truncation* t) {
+  if (!t->temp_per_seq && !(isfinite(t->temperature) && t->temperature >= 0.0f))
+    return fail(SPC_E_PARAM, "temperature must be finite and >= 0 (got %g)",
+                (double)t->temperature);
+  if (!t->top_k_per_seq && t->top_k < 0)
+    return fail(SPC_E_PARAM, "top_k must be >= 0 (got %d)", t->top_k);
+  if (!t->top_p_per_seq && !(t->top_p > 0.0f && t->top_p <= 1.0f))
+    return fail(SPC_E_PARAM, "top_p must be in (0, 1] (got %g)", (double)t->top_p);
+  if (!t->min_p_per_seq && !(t->min_p >= 0.0f && t->min_p <= 1.0f))
+    return fail(SPC_E_PARAM, "min_p must be in [0, 1] (got %g)", (double)t->min_p);
+  return SPC_OK;
+}
+
+spc::TruncParams truncated_rows(const void* logits, int64_t R, int32_t rows_per_seq, int32_t V,
+                                int64_t ld, const spc_truncation* t) {
+  spc::TruncParams P{};
+  P.z = logits;
+  P.R = R;
+  P.rows_per_seq = rows_per_seq;
+  P.V = V;
+  P.ld = ld;
+  P.temp = t->temperature;
+  P.top_k = t->top_k;
+  P.top_p = t->top_p;
+  P.min_p = t->min_p;
+  P.temp_ps = t->temp_per_seq;
+  P.top_k_ps = t->top_k_per_seq;
+  P.top_p_ps = t->top_p_per_seq;
+  P.min_p_ps = t->min_p_per_seq;
+  return P;
+}
+
+spc_status sample_impl(const void* logits, int32_t dtype, int32_t B, int32_t V,
+                       int64_t row_stride, const spc_truncation* t, const float* uniforms,
+                       int32_t* out_token, float* out_logprob, int32_t* out_kept,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  g_err.clear();
+  if (!logits || !t || !out_token) return fail(SPC_E_NULL, "a required pointer is NULL");
+  spc_status st = check_truncation(t);
+  if (st != SPC_OK) return st;
+  if (!uniforms && (t->temp_per_seq || t->temperature != 0.0f))
+    return fail(SPC_E_NULL, "uniforms is NULL");
+  if (B < 1 || V < 2 || row_stride < V)
+    return fail(SPC_E_SHAPE, "bad shape B=%d V=%d row_stride=%lld (need B>=1, V>=2, stride>=V)", B,
+                V, (long long)row_stride);
+  if (dtype != SPC_F32 && dtype != SPC_BF16) return fail(SPC_E_PARAM, "unknown dtype %d", dtype);
+  const int64_t eb = dtype == SPC_BF16 ? 2 : 4;
+  if ((uintptr_t)logits % eb != 0)
+    return fail(SPC_E_ALIGN, "the logits must be aligned to their elements");
+  for (int64_t b0 = 0; b0 < B; b0 += spc::kMaxRows) {
+    spc::TruncParams P =
+        truncated_rows(static_cast<const char*>(logits) + b0 * row_stride * eb,
+                       std::min<int64_t>(B - b0, spc::kMaxRows), 1, V, row_stride, t);
+    P.temp_ps = offset(P.temp_ps, b0);
+    P.top_k_ps = offset(P.top_k_ps, b0);
+    P.top_p_ps = offset(P.top_p_ps, b0);
+    P.min_p_ps = offset(P.min_p_ps, b0);
+    P.uniforms = offset(uniforms, b0);
+    P.out_token = out_token + b0;
+    P.out_logprob = offset(out_logprob, b0);
+    P.out_kept = offset(out_kept, b0);
+    const hipError_t e = spc::launch_truncated(P, dtype, stream);
+    if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  }
+  return SPC_OK;
+}
+
+spc_status truncate_impl(const void* logits, int32_t dtype, int32_t B, int32_t rows_per_seq,
+                         int32_t V, const spc_truncation* t, void* out, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  g_err.clear();
+  if (!logits || !t || !out) return fail(SPC_E_NULL, "a required pointer is NULL");
+  spc_status st = check_truncation(t);
+  if (st != SPC_OK) return st;
+  if (B < 1 || V < 2 || rows_per_seq < 1)
+    return fail(SPC_E_SHAPE, "bad shape B=%d rows_per_seq=%d V=%d (need B>=1, rows>=1, V>=2)", B,
+                rows_per_seq, V);
+  if (dtype != SPC_F32 && dtype != SPC_BF16) return fail(SPC_E_PARAM, "unknown dtype %d", dtype);
+  const int64_t eb = dtype == SPC_BF16 ? 2 : 4;
+  if (((uintptr_t)logits | (uintptr_t)out) % eb != 0)
+    return fail(SPC_E_ALIGN, "the logits must be aligned to their elements");
+  // whole sequences a launch, or parts of one sequence's rows
+  const int64_t step = std::max<int64_t>(1, spc::kMaxRows / rows_per_seq);
+  for (int64_t b0 = 0; b0 < B; b0 += step) {
+    const int64_t nb = std::min<int64_t>(B - b0, step), rows = nb * rows_per_seq;
+    for (int64_t r0 = 0; r0 < rows; r0 += spc::kMaxRows) {
+      const int64_t at = (b0 * rows_per_seq + r0) * V * eb;
+      spc::TruncParams P = truncated_rows(static_cast<const char*>(logits) + at,
+                                          std::min<int64_t>(rows - r0, spc::kMaxRows),
+                                          rows_per_seq, V, V, t);
+      P.out = static_cast<char*>(out) + at;
+      P.out_ld = V;
+      P.temp_ps = offset(P.temp_ps, b0);
+      P.top_k_ps = offset(P.top_k_ps, b0);
+      P.top_p_ps = offset(P.top_p_ps, b0);
+      P.min_p_ps = offset(P.min_p_ps, b0);
+      const hipError_t e = spc::launch_truncated(P, dtype, stream);
+      if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+    }
+  }
+  return SPC_OK;
+}
+
+// The checks every cache call makes of the cache, and its parameters.
+spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
+  if (!c || !c->k_pages || !c->v_pages || !c->page_table || !c->kv_len)
+    return fail(SPC_E_NULL, "a required pointer is NULL");
+  if (c->dtype != SPC_BF16 && c->dtype != SPC_E4M3)
+    return fail(SPC_E_PARAM, "unknown cache dtype %d", c->dtype);
+  const bool f8 = c->dtype == SPC_E4M3;
+  if (f8 && (!c->k_scale || !c->v_scale)) return fail(SPC_E_NULL, "an e4m3 cache needs its scales");
+  if (c->B < 1 || c->B > 65535 || c->num_pages < 1 || c->table_width < 1 || c->kv_heads < 1 ||
+      c->kv_heads > 65535)
+    return fail(SPC_E_SHAPE, "bad cache: B=%d num_pages=%d table_width=%d kv_heads=%d", c->B,
+                c->num_pages, c->table_width, c->kv_heads);
+  if (c->page_size < 16 || c->page_size > 1024 || c->page_size % 16 != 0)
+    return fail(SPC_E_SHAPE, "page_size must be a multiple of 16 from 16 to 1024 (got %d)",
+                c->page_size);
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+    return fail(SPC_E_SHAPE, "head_dim must be 64, 128 or 256 (got %d)", c->head_dim);
+  if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages |
+       (f8 ? (uintptr_t)c->k_scale | (uintptr_t)c->v_scale : 0)) % 16 != 0)
+    return fail(SPC_E_ALIGN, "pages and scales must be 16-byte aligned");
+  if (((uintptr_t)c->page_table | (uintptr_t)c->kv_len) % 4 != 0)
+    return fail(SPC_E_ALIGN, "page_table and kv_len must be 4-byte aligned");
+  P.k = c->k_pages;
+  P.v = c->v_pages;
+  P.k_scale = c->k_scale;
+  P.v_scale = c->v_scale;
+  P.f8 = f8;
+  P.pages = c->num_pages;
+  P.S = c->page_size;
+  P.H = c->kv_heads;
+  P.D = c->head_dim;
+  P.table = c->page_table;
+  P.width = c->table_width;
+  P.len = c->kv_len;
+  P.B = c->B;
+  return SPC_OK;
+}
+
+// The rows of a chunk of new tokens.
+spc_status kv_rows(int64_t rows, const int32_t* row_start, int32_t max_rows, spc::KvParams& P) {
+  if (rows < 1 || rows > (int64_t(1) << 26))
+    return fail(SPC_E_SHAPE, "rows must be from 1 to 2^26 (got %lld)", (long long)rows);
+  if (!row_start && rows % P.B != 0)
+    return fail(SPC_E_SHAPE, "%lld rows do not divide into %d sequences (no row_start)",
+                (long long)rows, P.B);
+  if (row_start && max_rows < 1)
+    return fail(SPC_E_SHAPE, "max_rows must be at least 1 (got %d)", max_rows);
+  P.rows = rows;
+  P.start = row_start;
+  P.n = row_start ? (int32_t)std::min<int64_t>(max_rows, rows) : (int32_t)(rows / P.B);
+  return SPC_OK;
+}
+
+spc_status kv_write_impl(const spc_kv_cache* cache, const void* k, const void* v, int32_t dtype,
+                         int64_t k_stride, int64_t v_stride, int64_t rows,
+                         const int32_t* row_start, hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_params(cache, P);
+  if (st == SPC_OK && (!k || !v)) st = fail(SPC_E_NULL, "a required pointer is NULL");
+  if (st == SPC_OK) st = kv_rows(rows, row_start, 1, P);
+  if (st != SPC_OK) return st;
+  if (dtype != SPC_F32 && dtype != SPC_BF16) return fail(SPC_E_PARAM, "unknown dtype %d", dtype);
+  if (k_stride < (int64_t)P.H * P.D || v_stride < (int64_t)P.H * P.D)
+    return fail(SPC_E_SHAPE, "row strides must be at least kv_heads * head_dim");
+  if (((uintptr_t)k | (uintptr_t)v) % (dtype == SPC_BF16 ? 2 : 4) != 0)
+    return fail(SPC_E_ALIGN, "keys and values must be aligned to their elements");
+  P.k_new = k;
+  P.v_new = v;
+  P.k_stride = k_stride;
+  P.v_stride = v_stride;
+  const hipError_t e = spc::launch_kv_write(P, dtype, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
+spc_status kv_read_impl(const spc_kv_cache* cache, void* out_k, void* out_v, int32_t dtype,
+                        int32_t length, hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  const spc_status st = kv_params(cache, P);
+  if (st != SPC_OK) return st;
+  if (!out_k || !out_v) return fail(SPC_E_NULL, "a required pointer is NULL");
+  if (dtype != SPC_F32 && dtype != SPC_BF16) return fail(SPC_E_PARAM, "unknown dtype %d", dtype);
+  if (length < 1 || length > (1 << 26))
+    return fail(SPC_E_SHAPE, "length must be from 1 to 2^26 (got %d)", length);
+  if (((uintptr_t)out_k | (uintptr_t)out_v) % 16 != 0)
+    return fail(SPC_E_ALIGN, "outputs must be 16-byte aligned");
+  P.k_out = out_k;
+  P.v_out = out_v;
+  P.L = length;
+  const hipError_t e = spc::launch_kv_read(P, dtype, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
+spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                          int64_t q_stride, int32_t heads, int64_t rows,
+                          const int32_t* row_start, int32_t max_rows, float scale, int32_t window,
+                          void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_params(cache, P);
+  if (st == SPC_OK && (!q || !out)) st = fail(SPC_E_NULL, "a required pointer is NULL");
+  if (st == SPC_OK) st = kv_rows(rows, row_start, max_rows, P);
+  if (st != SPC_OK) return st;
+  if (dtype != SPC_BF16) return fail(SPC_E_PARAM, "queries must be bfloat16 (dtype %d)", dtype);
+  if (heads < 1 || heads % P.H != 0)
+    return fail(SPC_E_SHAPE, "heads=%d is no multiple of kv_heads=%d", heads, P.H);
+  if (q_stride < (int64_t)heads * P.D || out_stride < (int64_t)heads * P.D)
+    return fail(SPC_E_SHAPE, "row strides must be at least heads * head_dim");
+  if (!isfinite(scale)) return fail(SPC_E_PARAM, "scale is not finite");
+  if (window < 0) return fail(SPC_E_PARAM, "window must be >= 0 (got %d)", window);
+  if ((uintptr_t)q % 2 != 0 || (uintptr_t)out % 8 != 0 || out_stride % 4 != 0)
+    return fail(SPC_E_ALIGN, "q must be element-aligned, out and its rows 8-byte aligned");
+  P.q = q;
+  P.q_stride = q_stride;
+  P.heads = heads;
+  P.scale = (float)((double)scale * 1.4426950408889634074);
+  P.window = window;
+  P.out = out;
+  P.out_stride = out_stride;
+  const hipError_t e = spc::launch_kv_attend(P, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+spc_status spc_sample(const void* logits, int32_t dtype, int32_t B, int32_t V,
+                      int64_t row_stride, const spc_truncation* truncation,
+                      const float* uniforms, int32_t* out_token, float* out_logprob,
+                      int32_t* out_kept, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream) {
+  return sample_impl(logits, dtype, B, V, row_stride, truncation, uniforms, out_token,
+                     out_logprob, out_kept, workspace, workspace_bytes, stream);
+}
+
+spc_status spc_truncate(const void* logits, int32_t dtype, int32_t B, int32_t rows_per_seq,
+                        int32_t V, const spc_truncation* truncation, void* out_logits,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return truncate_impl(logits, dtype, B, rows_per_seq, V, truncation, out_logits, workspace,
+                       workspace_bytes, stream);
+}
+
+size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype) { return 0; }
+
+spc_status spc_kv_write(const spc_kv_cache* cache, const void* k, const void* v, int32_t dtype,
+                        int64_t k_stride, int64_t v_stride, int64_t rows,
+                        const int32_t* row_start, hipStream_t stream) {
+  return kv_write_impl(cache, k, v, dtype, k_stride, v_stride, rows, row_start, stream);
+}
+
+spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int32_t dtype,
+                       int32_t length, hipStream_t stream) {
+  return kv_read_impl(cache, out_k, out_v, dtype, length, stream);
+}
+
+spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                         int64_t q_stride, int32_t heads, int64_t rows,
+                         const int32_t* row_start, int32_t max_rows, float scale,
+                         int32_t window, void* out, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  return kv_attend_impl(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                        window, out, out_stride, workspace, workspace_bytes, stream);
+}
+
+size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                              int32_t max_rows) {
+  return 0;
+}
 
 spc_status spc_verify(const void* q_logits, const void* p_logits, int32_t dtype,
                       const int32_t* draft_tokens, const float* uniforms, int32_t B,

@@ -175,6 +175,61 @@ hipError_t launch_small(const Params& P, int dtype, hipEvent_t ev_begin,
 hipError_t launch_step(const Params& P, int dtype, bool draw_pass, bool tv_pass, bool job_pass, int job_groups, hipEvent_t ev_begin, hipEvent_t ev_end,
                        hipStream_t stream);
 
+// Rows drawn from, or cut to, their truncated distributions (spc_sample,
+// spc_truncate): R rows of V logits, row stride ld entries; row r has the
+// settings of sequence r / rows_per_seq.  out: the cut logits (row stride
+// out_ld; may be z), or NULL for a draw.
+struct TruncParams {
+  const void* z;
+  void* out;
+  int64_t ld, out_ld, R;
+  int32_t rows_per_seq, V;
+  float temp, top_p, min_p;
+  int32_t top_k;
+  const float* temp_ps;
+  const int32_t* top_k_ps;
+  const float* top_p_ps;
+  const float* min_p_ps;
+  const float* uniforms;
+  int32_t* out_token;
+  float* out_logprob;
+  int32_t* out_kept;
+};
+hipError_t launch_truncated(const TruncParams& P, int dtype, hipStream_t stream);
+
+// A call on a paged key/value cache (spc_kv_*): the cache's pages and the
+// sequences' tables, and the chunk of new tokens.  Row r of the chunk is token
+// r - start(b) of its sequence b: start given, or n rows a sequence.
+struct KvParams {
+  void* k;
+  void* v;                  // keys [page][H][S][D], values [page][H][D][S]
+  float* k_scale;
+  float* v_scale;           // [page][H][S], 8-bit caches
+  int32_t f8, pages, S, H, D;
+  const int32_t* table;     // [B][width]
+  const int32_t* len;       // [B] tokens of the sequence, its new ones included
+  int32_t B, width;
+  const int32_t* start;     // [B + 1] or NULL
+  int64_t rows;
+  int32_t n;                // rows per sequence (start: the most of one sequence)
+  // spc_kv_write, spc_kv_read: dense keys and values
+  const void* k_new;
+  const void* v_new;
+  int64_t k_stride, v_stride;
+  void* k_out;
+  void* v_out;
+  int32_t L;                // positions read back
+  // spc_kv_attend
+  const void* q;
+  void* out;
+  int64_t q_stride, out_stride;
+  int32_t heads, window;
+  float scale;              // of q.k, times log2(e)
+};
+hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
+hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
+hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream);
+
 // Enqueue a kernel writing `bytes` zero bytes at `ptr` (a multiple of 4, ptr
 // 4-byte aligned): a fill a graph capture may record.
 hipError_t launch_fill_zero(void* ptr, size_t bytes, hipStream_t stream);

@@ -15,7 +15,7 @@ import torch
 LIB_PATH = os.environ.get("SPC_LIB_PATH") or os.path.join(
     os.path.dirname(os.path.abspath(__file__)), "libspeccascade.so")
 
-SPC_F32, SPC_BF16 = 0, 1
+SPC_F32, SPC_BF16, SPC_E4M3 = 0, 1, 2
 SPC_RULE_CHOW, SPC_RULE_DIFF, SPC_RULE_OPT, SPC_RULE_ALWAYS, SPC_RULE_NEVER = range(5)
 SPC_RULE_TOKEN_V1, SPC_RULE_TOKEN_V2, SPC_RULE_TOKEN_V3 = 5, 6, 7
 SPC_RULE_LOSSY, SPC_RULE_BILD, SPC_RULE_CHOWLOG, SPC_RULE_DIFFLOG, SPC_RULE_OPTLOG = range(8, 13)
@@ -34,6 +34,21 @@ class ExArgs(ctypes.Structure):
                 ("workspace", _P), ("workspace_bytes", ctypes.c_size_t),
                 ("rules_present", ctypes.c_uint32), ("ev_tiles_begin", _P),
                 ("ev_tiles_end", _P)]
+
+
+class Truncation(ctypes.Structure):
+    """spc_truncation."""
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", _I32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("temp_per_seq", _P), ("top_k_per_seq", _P),
+                ("top_p_per_seq", _P), ("min_p_per_seq", _P)]
+
+
+class KvCache(ctypes.Structure):
+    """spc_kv_cache."""
+    _fields_ = [("k_pages", _P), ("v_pages", _P), ("k_scale", _P), ("v_scale", _P),
+                ("dtype", _I32), ("num_pages", _I32), ("page_size", _I32), ("kv_heads", _I32),
+                ("head_dim", _I32), ("page_table", _P), ("table_width", _I32), ("kv_len", _P),
+                ("B", _I32)]
 
 
 class SpcError(RuntimeError):
@@ -76,6 +91,23 @@ def lib():
         L.spc_draft_sample_ws.restype = ctypes.c_int
         L.spc_draft_workspace_bytes.argtypes = [_I32, _I32, ctypes.c_int]
         L.spc_draft_workspace_bytes.restype = ctypes.c_size_t
+        cut, cache, i64 = ctypes.POINTER(Truncation), ctypes.POINTER(KvCache), ctypes.c_int64
+        L.spc_sample.argtypes = [_P, _I32, _I32, _I32, i64, cut, _P, _P, _P, _P, _P,
+                                 ctypes.c_size_t, _P]
+        L.spc_sample.restype = ctypes.c_int
+        L.spc_truncate.argtypes = [_P, _I32, _I32, _I32, _I32, cut, _P, _P, ctypes.c_size_t, _P]
+        L.spc_truncate.restype = ctypes.c_int
+        L.spc_truncation_workspace_bytes.argtypes = [i64, _I32, _I32]
+        L.spc_truncation_workspace_bytes.restype = ctypes.c_size_t
+        L.spc_kv_write.argtypes = [cache, _P, _P, _I32, i64, i64, i64, _P, _P]
+        L.spc_kv_write.restype = ctypes.c_int
+        L.spc_kv_read.argtypes = [cache, _P, _P, _I32, _I32, _P]
+        L.spc_kv_read.restype = ctypes.c_int
+        L.spc_kv_attend.argtypes = [cache, _P, _I32, i64, _I32, i64, _P, _I32, ctypes.c_float,
+                                    _I32, _P, i64, _P, ctypes.c_size_t, _P]
+        L.spc_kv_attend.restype = ctypes.c_int
+        L.spc_kv_workspace_bytes.argtypes = [cache, _I32, i64, _I32]
+        L.spc_kv_workspace_bytes.restype = ctypes.c_size_t
         L.spc_workspace_bytes.argtypes = [_I32, _I32, _I32, ctypes.c_int]
         L.spc_workspace_bytes.restype = ctypes.c_size_t
         L.spc_workspace_zero_bytes.argtypes = [_I32, _I32, _I32, ctypes.c_int]
@@ -263,6 +295,216 @@ def spc_draft_sample(logits, temperature, uniforms=None, temp_per_seq=None, out=
                                          workspace.numel() * workspace.element_size(),
                                          _stream(stream)))
     return tok
+
+
+def _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq, top_p_per_seq,
+                min_p_per_seq, dev, B):
+    _check_arg("temp_per_seq", temp_per_seq, torch.float32, dev, (B,))
+    _check_arg("top_k_per_seq", top_k_per_seq, torch.int32, dev, (B,))
+    _check_arg("top_p_per_seq", top_p_per_seq, torch.float32, dev, (B,))
+    _check_arg("min_p_per_seq", min_p_per_seq, torch.float32, dev, (B,))
+    return Truncation(float(temperature), int(top_k), float(top_p), float(min_p),
+                      _ptr(temp_per_seq), _ptr(top_k_per_seq), _ptr(top_p_per_seq),
+                      _ptr(min_p_per_seq))
+
+
+def _workspace(workspace, dev):
+    """(address, bytes) of a caller workspace; (None, 0) for the library's own."""
+    if workspace is None:
+        return None, 0
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def spc_sample(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, *,
+               temp_per_seq=None, top_k_per_seq=None, top_p_per_seq=None, min_p_per_seq=None,
+               out=None, out_logprob=None, out_kept=None, workspace=None, stream=None):
+    """One token per row of ``logits`` [B, V] (float32 or bfloat16; rows may
+    be strided, a row's entries are not) from softmax(z / T) cut by top-k,
+    top-p and min-p, at ``uniforms`` [B] (float32).  Returns the tokens [B]
+    int32 (``out`` if given; -1 where nothing is kept).  ``out_logprob`` [B]
+    float32 and ``out_kept`` [B] int32 receive the token's log-probability
+    under the kept distribution and the number of entries kept."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be a [B, V] tensor")
+    B, V = logits.shape
+    if logits.stride(1) != 1 or (B > 1 and logits.stride(0) < V):
+        raise ValueError("the entries of a row of logits must be contiguous, rows not overlap")
+    dev = logits.device
+    _check_arg("uniforms", uniforms, torch.float32, dev, (B,))
+    _check_arg("out_logprob", out_logprob, torch.float32, dev, (B,))
+    _check_arg("out_kept", out_kept, torch.int32, dev, (B,))
+    cut = _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq,
+                      top_p_per_seq, min_p_per_seq, dev, B)
+    tok = out if out is not None else torch.empty(B, dtype=torch.int32, device=dev)
+    _check_arg("out", tok, torch.int32, dev, (B,))
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().spc_sample(_ptr(logits), _dtype_code(logits), B, V,
+                            logits.stride(0) if B > 1 else V, cut, _ptr(uniforms), _ptr(tok),
+                            _ptr(out_logprob), _ptr(out_kept), ws, nbytes, _stream(stream)))
+    return tok
+
+
+def spc_truncate(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, *, temp_per_seq=None,
+                 top_k_per_seq=None, top_p_per_seq=None, min_p_per_seq=None, out=None,
+                 workspace=None, stream=None):
+    """``logits`` [B, rows, V] or [B, V] (float32 or bfloat16, contiguous)
+    with the entries that top-k, top-p and min-p leave out set to -inf: the
+    rows ``spc_verify`` reads when drafts were drawn by ``spc_sample``.
+    Returns ``out`` (a new tensor unless given; it may be ``logits``)."""
+    if logits.dim() not in (2, 3) or not logits.is_contiguous():
+        raise ValueError("logits must be a contiguous [B, rows, V] or [B, V] tensor")
+    B, V = logits.shape[0], logits.shape[-1]
+    dev = logits.device
+    cut = _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq,
+                      top_p_per_seq, min_p_per_seq, dev, B)
+    if out is None:
+        out = torch.empty_like(logits)
+    _check_arg("out", out, logits.dtype, dev, logits.shape)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().spc_truncate(_ptr(logits), _dtype_code(logits), B,
+                              logits.shape[1] if logits.dim() == 3 else 1, V, cut, _ptr(out), ws,
+                              nbytes, _stream(stream)))
+    return out
+
+
+def spc_truncation_workspace_bytes(rows, V, dtype_code):
+    return lib().spc_truncation_workspace_bytes(rows, V, dtype_code)
+
+
+def _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale):
+    if k_pages.dim() != 4 or v_pages.dim() != 4:
+        raise ValueError("k_pages must be [pages, heads, page_size, dim], v_pages "
+                         "[pages, heads, dim, page_size]")
+    n, H, S, D = k_pages.shape
+    dev = k_pages.device
+    if k_pages.dtype == torch.bfloat16:
+        code = SPC_BF16
+        if k_scale is not None or v_scale is not None:
+            raise ValueError("a bfloat16 cache has no scales")
+    elif k_pages.dtype == torch.float8_e4m3fn:
+        code = SPC_E4M3
+        if k_scale is None or v_scale is None:
+            raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
+    else:
+        raise TypeError(f"pages must be bfloat16 or float8_e4m3fn, not {k_pages.dtype}")
+    _check_arg("k_pages", k_pages, k_pages.dtype, dev)
+    _check_arg("v_pages", v_pages, k_pages.dtype, dev, (n, H, D, S))
+    _check_arg("k_scale", k_scale, torch.float32, dev, (n, H, S))
+    _check_arg("v_scale", v_scale, torch.float32, dev, (n, H, S))
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B, pages of a sequence]")
+    B = page_table.shape[0]
+    _check_arg("page_table", page_table, torch.int32, dev)
+    _check_arg("kv_len", kv_len, torch.int32, dev, (B,))
+    return KvCache(_ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), code, n, S, H, D,
+                   _ptr(page_table), page_table.shape[1], _ptr(kv_len), B)
+
+
+def _kv_rows(name, t, dev, B, row_start, dim):
+    """(rows, heads, stride between rows) of new tokens: [B, n, heads, dim],
+    or [rows, heads, dim] with row_start.  Rows may be strided (a slice of a
+    fused projection); the heads of a row are contiguous."""
+    if row_start is not None:
+        _check_arg("q_start", row_start, torch.int32, dev, (B + 1,))
+    if t.dim() != (3 if row_start is not None else 4):
+        raise ValueError(f"{name} must be [B, n, heads, dim], or [rows, heads, dim] with q_start")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}, not {t.device}")
+    heads, d = t.shape[-2:]
+    if d != dim:
+        raise ValueError(f"{name} must have {dim} dimensions a head, not {d}")
+    if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != d):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    if row_start is not None:
+        rows, stride = t.shape[0], t.stride(0)
+    else:
+        if t.shape[0] != B:
+            raise ValueError(f"{name} must hold {B} sequences, not {t.shape[0]}")
+        n = t.shape[1]
+        rows, stride = B * n, t.stride(1) if n > 1 else t.stride(0)
+        if n > 1 and B > 1 and t.stride(0) != n * stride:
+            raise ValueError(f"the rows of {name} must be evenly spaced over the batch")
+    return rows, heads, heads * d if rows == 1 else stride
+
+
+def spc_kv_write(k, v, k_pages, v_pages, page_table, kv_len, *, k_scale=None, v_scale=None,
+                 q_start=None, stream=None):
+    """The keys and values of new tokens (float32 or bfloat16, [B, n, heads,
+    dim], or [rows, heads, dim] with ``q_start`` [B + 1]) into the pages of
+    their sequences: bfloat16 pages, or float8_e4m3fn with ``k_scale`` and
+    ``v_scale``.  The last new token of sequence b is at ``kv_len[b]`` - 1."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    dev = k_pages.device
+    rows, heads, ks = _kv_rows("k", k, dev, cache.B, q_start, cache.head_dim)
+    vrows, vheads, vs = _kv_rows("v", v, dev, cache.B, q_start, cache.head_dim)
+    if rows != vrows or not heads == vheads == cache.kv_heads or k.dtype != v.dtype:
+        raise ValueError("k and v must have the same rows and type, and the cache's heads")
+    if rows == 0:
+        return
+    _check(lib().spc_kv_write(cache, _ptr(k), _ptr(v), _dtype_code(k), ks, vs, rows,
+                              _ptr(q_start), _stream(stream)))
+
+
+def spc_kv_read(k_pages, v_pages, page_table, kv_len, length=None, *, k_scale=None, v_scale=None,
+                dtype=torch.bfloat16, out=None, stream=None):
+    """Positions 0 .. ``length`` - 1 of every sequence as dense keys and
+    values [B, length, heads, dim] in ``dtype`` (float32 or bfloat16).
+    ``out``: a pair to write instead; positions past ``kv_len`` keep what they
+    hold (new tensors: zero)."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if out is None:
+        if length is None:
+            raise ValueError("length or out must be given")
+        shape = (cache.B, length, cache.kv_heads, cache.head_dim)
+        out = tuple(torch.zeros(shape, dtype=dtype, device=k_pages.device) for _ in range(2))
+    k, v = out
+    if length is None:
+        length = k.shape[1]
+    shape = (cache.B, length, cache.kv_heads, cache.head_dim)
+    _check_arg("out", k, k.dtype, k_pages.device, shape)
+    _check_arg("out", v, k.dtype, k_pages.device, shape)
+    if length == 0:
+        return k, v
+    _check(lib().spc_kv_read(cache, _ptr(k), _ptr(v), _dtype_code(k), length, _stream(stream)))
+    return k, v
+
+
+def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window=0, k_scale=None,
+                  v_scale=None, q_start=None, max_q=None, out=None, workspace=None, stream=None):
+    """Attention of new tokens, whose keys and values the cache holds
+    already, over the cache: ``q`` bfloat16 [B, n, heads, dim], or [rows,
+    heads, dim] with ``q_start`` [B + 1] and ``max_q`` (the most rows of one
+    sequence; None: all rows).  ``scale`` None: 1 / sqrt(dim).  ``window`` > 0:
+    only the last ``window`` tokens.  Returns ``out`` (as ``q``)."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    dev = k_pages.device
+    rows, heads, qs = _kv_rows("q", q, dev, cache.B, q_start, cache.head_dim)
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"q must be bfloat16, not {q.dtype}")
+    if out is None:  # (rows of no sequence stay zero)
+        out = (torch.empty if q_start is None else torch.zeros)(q.shape, dtype=q.dtype, device=dev)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have the shape and type of q")
+    orows, _, os_ = _kv_rows("out", out, dev, cache.B, q_start, cache.head_dim)
+    if rows == 0:
+        return out
+    if max_q is None:
+        max_q = rows
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().spc_kv_attend(cache, _ptr(q), SPC_BF16, qs, heads, rows, _ptr(q_start),
+                               int(max_q), cache.head_dim ** -0.5 if scale is None else
+                               float(scale), int(window), _ptr(out), os_, ws, nbytes,
+                               _stream(stream)))
+    return out
+
+
+def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=0, *,
+                           k_scale=None, v_scale=None):
+    """Bytes of workspace an spc_kv_attend call of this cache and chunk needs."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    return lib().spc_kv_workspace_bytes(cache, heads, rows, max_q)
 
 
 def spc_workspace_bytes(B, gamma, V, dtype_code):
