@@ -90,13 +90,39 @@ __device__ __forceinline__ uint64_t fixed_point(double x, double scale) {
   return (uint64_t)__double_as_longlong(m) & 0xfffffffffffffull;
 }
 
+
+// Inclusive sums over a wavefront (DPP row shifts and broadcasts; 64-bit
+// values as two halves).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp(uint64_t x) {
+  return (uint64_t)dpp<CTRL, ROWS>((uint32_t)x) |
+         (uint64_t)dpp<CTRL, ROWS>((uint32_t)(x >> 32)) << 32;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double x) {
+  return __longlong_as_double((long long)dpp<CTRL, ROWS>((uint64_t)__double_as_longlong(x)));
+}
 template <class T>
-__device__ __forceinline__ T wave_incl_scan(T v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
+__device__ __forceinline__ T wave_incl_scan(T v) {
+  v += dpp<0x111, 0xf>(v);  // row_shr
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);  // row_bcast 15, 31
+  v += dpp<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {  // in lane 63
+  v = max(v, dpp<0x111, 0xf>(v));
+  v = max(v, dpp<0x112, 0xf>(v));
+  v = max(v, dpp<0x114, 0xf>(v));
+  v = max(v, dpp<0x118, 0xf>(v));
+  v = max(v, dpp<0x142, 0xa>(v));
+  v = max(v, dpp<0x143, 0xc>(v));
   return v;
 }
 
@@ -137,53 +163,19 @@ __device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) {
   return Cut{a.key, min(a.idx, b.idx)};
 }
 
-// Row entries read from memory at every pass.  Thread t's lane load i covers
-// entries (i kNT + t) VW ..; sub-chunk i kNW + wave is a wavefront's lane load.
+
+// ------------------------------------------------------------------ rows
+// Row entries, in 16-byte lane loads.  Thread t's lane load i covers entries
+// (i kNT + t) VW ..; sub-chunk i kNW + wave is a wavefront's lane load.
 template <int DT>
-struct ScanRow {
-  const char* row;
-  int32_t V;
+struct RowOf {
   static constexpr int VW = Elem<DT>::VW;
-  __device__ __forceinline__ int loads() const { return (int)(((int64_t)V + kNT * VW - 1) / (kNT * VW)); }
-  // f(entry, logit, the entry's bits) over the thread's entries of lane loads [i0, i1)
-  template <class F>
-  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
-    for (int i = i0; i < i1; ++i) {
-      const int64_t e0 = ((int64_t)i * kNT + threadIdx.x) * VW;
-      uint32_t w[4];
-      int n = 0;
-      if (e0 < V) n = load(e0, w);
-#pragma unroll
-      for (int e = 0; e < VW; ++e)
-        if (e < n) f(e0 + e, value(w, e), bits(w, e));
-    }
-  }
-  // the lane load at entry e0 < V; the number of its entries
-  __device__ __forceinline__ int load(int64_t e0, uint32_t (&w)[4]) const {
-    const int n = (int)min((int64_t)VW, (int64_t)V - e0);
-    const char* a = row + e0 * Elem<DT>::EB;
-    if (n == VW) {
-      w4 v;
-      if constexpr (DT == 1) v = *reinterpret_cast<const w4a2*>(a);
-      else v = *reinterpret_cast<const w4a4*>(a);
-      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (DT == 1) {
-          const uint16_t* s = reinterpret_cast<const uint16_t*>(a);
-          w[j] = (2 * j < n ? (uint32_t)s[2 * j] : 0xff80u) |
-                 ((2 * j + 1 < n ? (uint32_t)s[2 * j + 1] : 0xff80u) << 16);
-        } else {
-          w[j] = j < n ? reinterpret_cast<const uint32_t*>(a)[j] : 0xff800000u;
-        }
-      }
-    }
-    return n;
-  }
   static __device__ __forceinline__ uint32_t bits(const uint32_t (&w)[4], int e) {
     if constexpr (DT == 1) return (e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu;
     else return w[e];
+  }
+  static __device__ __forceinline__ float of_bits(uint32_t b) {
+    return clean(__uint_as_float(DT == 1 ? b << 16 : b));
   }
   static __device__ __forceinline__ float value(const uint32_t (&w)[4], int e) {
     if constexpr (DT == 1)
@@ -191,14 +183,124 @@ struct ScanRow {
     else return clean(__uint_as_float(w[e]));
   }
 };
+// The lane load at entry e0 < V of a row in memory, -inf behind its end; the
+// number of its entries.
+template <int DT>
+__device__ __forceinline__ int load_lane(const char* row, int64_t e0, int32_t V,
+                                         uint32_t (&w)[4]) {
+  constexpr int VW = Elem<DT>::VW;
+  const int n = (int)min((int64_t)VW, (int64_t)V - e0);
+  const char* a = row + e0 * Elem<DT>::EB;
+  if (n == VW) {
+    w4 v;
+    if constexpr (DT == 1) v = *reinterpret_cast<const w4a2*>(a);
+    else v = *reinterpret_cast<const w4a4*>(a);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (DT == 1) {
+        const uint16_t* s = reinterpret_cast<const uint16_t*>(a);
+        w[j] = (2 * j < n ? (uint32_t)s[2 * j] : 0xff80u) |
+               ((2 * j + 1 < n ? (uint32_t)s[2 * j + 1] : 0xff80u) << 16);
+      } else {
+        w[j] = j < n ? reinterpret_cast<const uint32_t*>(a)[j] : 0xff800000u;
+      }
+    }
+  }
+  return n;
+}
+
+// A row read from memory at every pass.
+template <int DT>
+struct ScanRow : RowOf<DT> {
+  using RowOf<DT>::VW;
+  const char* row;
+  int32_t V;
+  __device__ __forceinline__ ScanRow(const char* r, int32_t v) : row(r), V(v) {}
+  __device__ __forceinline__ int loads() const {
+    return (int)(((int64_t)V + kNT * VW - 1) / (kNT * VW));
+  }
+  __device__ __forceinline__ int load(int64_t e0, uint32_t (&w)[4]) const {
+    return load_lane<DT>(row, e0, V, w);
+  }
+  // f(entry, logit, the entry's bits) over the thread's entries of lane loads [i0, i1)
+  template <class F>
+  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
+    for (int i = i0; i < i1; ++i) {
+      const int64_t e0 = ((int64_t)i * kNT + threadIdx.x) * VW;
+      if (e0 >= V) continue;
+      uint32_t w[4];
+      const int n = load(e0, w);
+#pragma unroll
+      for (int e = 0; e < VW; ++e)
+        if (e < n) f(e0 + e, RowOf<DT>::value(w, e), RowOf<DT>::bits(w, e));
+    }
+  }
+};
+
+// A row of at most kHeld entries held in LDS, lane load after lane load; what
+// lies behind its end is -inf, which no pass counts.
+constexpr int kHeld = 32768;
+template <int DT>
+struct HeldRow : RowOf<DT> {
+  using RowOf<DT>::VW;
+  const w4* lds;
+  int32_t V;
+  __device__ __forceinline__ HeldRow(const w4* l, int32_t v) : lds(l), V(v) {}
+  __device__ __forceinline__ int loads() const { return (V + kNT * VW - 1) / (kNT * VW); }
+  __device__ __forceinline__ int load(int64_t e0, uint32_t (&w)[4]) const {
+    const w4 v = lds[e0 / VW];
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    return (int)min((int64_t)VW, (int64_t)V - e0);
+  }
+  template <class F>
+  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
+    for (int i = i0; i < i1; ++i) {
+      const int e0 = (i * kNT + (int)threadIdx.x) * VW;
+      uint32_t w[4];
+      load(e0, w);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) f(e0 + e, RowOf<DT>::value(w, e), RowOf<DT>::bits(w, e));
+    }
+  }
+};
+
+// Entries of a row taken out of it.
+struct Item {
+  uint32_t bits;
+  int32_t idx;
+};
+template <int DT>
+struct ItemRow : RowOf<DT> {
+  const Item* item;
+  int32_t V, n;  // of a row of V entries
+  __device__ __forceinline__ ItemRow(const Item* i, int32_t v, int32_t m) : item(i), V(v), n(m) {}
+  __device__ __forceinline__ int loads() const { return (n + kNT - 1) / kNT; }
+  template <class F>
+  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
+    for (int i = i0; i < i1; ++i) {
+      const int j = i * kNT + (int)threadIdx.x;
+      if (j >= n) continue;
+      const Item x = item[j];
+      f(x.idx, RowOf<DT>::of_bits(x.bits), x.bits);
+    }
+  }
+};
+
+// ------------------------------------------------------------------ the cut
+constexpr int kItems = 1024;   // entries of the bins in question held in LDS
+constexpr int kRanked = 256;   // as many are ranked against each other
 
 struct Shared {
   uint64_t mass[kBins];
   uint32_t cnt[kBins];
-  uint64_t wave64[kNW];
+  double edge[kBins];          // 2^(-i/16)
+  Item items[kItems];
   double waved[kNW];
+  uint64_t wave64[kNW];
   uint32_t wave32[kNW];
-  uint32_t red[2];
+  uint32_t n_items, n_kept;
   // first_reaching's answer
   int32_t found, last;
   uint32_t above_cnt, in_cnt;
@@ -206,30 +308,29 @@ struct Shared {
   // the draw's
   uint64_t before;
   int32_t token;
-  uint32_t token_key;
+  float token_z;
 };
 
-// Fixed-point scales for rows of V entries: a bin's mass (V terms under
-// 0.0444) and the draw's weights (V terms of at most 1) stay under 2^63.
-__device__ __forceinline__ int log2_ceil(int32_t V) { return 32 - __builtin_clz((uint32_t)(V - 1) | 1u); }
-__device__ __forceinline__ int mass_bits(int32_t V) { return min(51, 67 - log2_ceil(V)); }
-__device__ __forceinline__ int draw_bits(int32_t V) { return min(50, 62 - log2_ceil(V)); }
+__device__ __forceinline__ int log2_ceil(int32_t V) {
+  return 32 - __builtin_clz((uint32_t)(V - 1) | 1u);
+}
+// Fixed-point scales: sums of V terms of at most 2^(1/16) stay under 2^63,
+// and a term under 2^51.
+__device__ __forceinline__ int sum_bits(int32_t V) { return min(50, 61 - log2_ceil(V)); }
+// The masses of the bins of at most kHeld entries: 16 bits of count above 48 of
+// mass (kHeld terms under 0.0444 2^37).
+constexpr int kPackBits = 37;
 
-// A wavefront's maximum or minimum over the block, of unsigned values.
 template <bool MAX>
 __device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    const uint32_t o = __shfl_xor(x, d);
-    x = MAX ? max(x, o) : min(x, o);
-  }
-  if ((threadIdx.x & 63) == 0) S.wave32[threadIdx.x >> 6] = x;
+  x = wave_max(MAX ? x : ~x);
+  if ((threadIdx.x & 63) == 63) S.wave32[threadIdx.x >> 6] = x;
   __syncthreads();
   x = S.wave32[0];
 #pragma unroll
-  for (int i = 1; i < kNW; ++i) x = MAX ? max(x, S.wave32[i]) : min(x, S.wave32[i]);
+  for (int i = 1; i < kNW; ++i) x = max(x, S.wave32[i]);
   __syncthreads();
-  return x;
+  return MAX ? x : ~x;
 }
 
 // Counts c and masses m, one of each per thread, in thread order: the first
@@ -239,8 +340,8 @@ __device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
 __device__ __forceinline__ int first_reaching(Shared& S, uint32_t c, double m, bool by_mass,
                                               uint32_t want_c, double want_m) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t ci = wave_incl_scan(c, lane);
-  double mi = wave_incl_scan(m, lane);
+  const uint32_t ci = wave_incl_scan(c);
+  const double mi = wave_incl_scan(m);
   if (lane == 63) {
     S.wave32[wave] = ci;
     S.waved[wave] = mi;
@@ -252,15 +353,22 @@ __device__ __forceinline__ int first_reaching(Shared& S, uint32_t c, double m, b
   __syncthreads();
   uint32_t bc = 0;
   double bm = 0;
-  for (int i = 0; i < wave; ++i) {
-    bc += S.wave32[i];
-    bm += S.waved[i];
+#pragma unroll
+  for (int i = 0; i < kNW; ++i) {
+    const uint32_t x = S.wave32[i];
+    const double y = S.waved[i];
+    bc += i < wave ? x : 0u;
+    bm += i < wave ? y : 0.0;
   }
-  double me = __shfl_up(mi, 1);
+  double me = dpp<0x138, 0xf>(mi);  // wave_shr: the lane before
   if (lane == 0) me = 0;
-  const bool here = c != 0 && (by_mass ? bm + mi >= want_m : bc + ci >= want_c);
-  if (here) atomicMin(&S.found, (int)threadIdx.x);
-  if (c != 0) atomicMax(&S.last, (int)threadIdx.x);
+  const bool some = c != 0;
+  const bool here = some && (by_mass ? bm + mi >= want_m : bc + ci >= want_c);
+  const uint64_t any = __ballot(here), all = __ballot(some);
+  if (lane == 0) {
+    if (any) atomicMin(&S.found, (wave << 6) + __builtin_ctzll(any));
+    if (all) atomicMax(&S.last, (wave << 6) + 63 - __builtin_clzll(all));
+  }
   __syncthreads();
   const int at = S.found == kNoIndex ? S.last : S.found;
   if ((int)threadIdx.x == at) {
@@ -273,20 +381,129 @@ __device__ __forceinline__ int first_reaching(Shared& S, uint32_t c, double m, b
   return at;
 }
 
-// Where a sum over entries in the order of x (ascending) reaches what is
-// wanted: the value of x, the sums before it and those of the entries at it.
+// What first_reaching found, before S is used again.
 struct Reached {
+  int at;
+  uint32_t above_cnt, in_cnt;
+  double above_mass, in_mass;
+};
+__device__ __forceinline__ Reached reach(Shared& S, uint32_t c, double m, bool by_mass,
+                                         uint32_t want_c, double want_m) {
+  Reached r;
+  r.at = first_reaching(S, c, m, by_mass, want_c, want_m);
+  r.above_cnt = S.above_cnt;
+  r.in_cnt = S.in_cnt;
+  r.above_mass = S.above_mass;
+  r.in_mass = S.in_mass;
+  __syncthreads();
+  return r;
+}
+
+// The bin of t below a row's top bin.
+__device__ __forceinline__ int bin_of(double top, double t) {
+  return (int)fmin(top - floor(t), (double)(kBins - 1));
+}
+
+// The fixed point of a row's bin masses, 2^bits and its inverse.
+struct Unit {
+  double scale, inv;
+};
+template <bool PACK>
+__device__ __forceinline__ Unit bin_unit(int32_t V) {
+  const int bits = PACK ? kPackBits : sum_bits(V);
+  return Unit{exp2((double)bits), exp2((double)-bits)};
+}
+// The mass of an entry relative to its bin's lower edge, rounded as the bins
+// hold it: sums over entries and over bins then agree where no rounding need
+// part them (a row of equal logits, say, and its half).
+__device__ __forceinline__ double entry_mass(double f, const Unit& u) {
+  return 1.0 + (double)fixed_point(frac_mass(f), u.scale) * u.inv;
+}
+
+// Adds an entry to the bins.
+template <bool PACK>
+__device__ __forceinline__ void add_to_bins(Shared& S, float z, double c, double top,
+                                            double scale) {
+  if (!(z > -__builtin_huge_valf())) return;
+  const double t = (double)z * c, b = floor(t);
+  const int bin = (int)fmin(top - b, (double)(kBins - 1));
+  // (a bin without mass needs none of it, but every lane takes the same path)
+  const uint64_t m = bin < kBins - 1 ? fixed_point(frac_mass(t - b), scale) : 0;
+  if constexpr (PACK) {
+    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)(m + (1ull << 48)));
+  } else {
+    atomicAdd(&S.cnt[bin], 1u);
+    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)m);
+  }
+}
+
+// What a row's bins say about its cut.  Bins are counted down from the top.
+struct Plan {
+  int32_t kbin;      // the bin top-k ends in, or -1
+  uint32_t k_need;   // entries it keeps of that bin
+  double k_above;    // mass of the bins above it, or (kbin = -1) of all
+  int32_t plo, phi;  // the bins top-p may end in, or -1 (not before plo, if k ends inside its bin)
+  double p_above;    // mass of the bins above plo
+  uint32_t items;    // entries in those bins
+};
+
+// n entries of mass m (relative to the top bin's lower edge): thread i's bin i.
+// key_bin: the bin of min-p's cut (kBins: none).
+__device__ __forceinline__ Plan make_plan(Shared& S, const Ask& a, int32_t V, uint32_t n,
+                                          double m, int key_bin) {
+  Plan p{-1, 0, 0.0, -1, -1, 0.0, 0};
+  const bool by_p = a.p < 1.0f;
+  // (no count is reached without top-k: the last filled bin, whose sums are the row's)
+  const Reached k = reach(S, n, m, false, a.k > 0 && a.k < V ? (uint32_t)a.k : 0xffffffffu, 0.0);
+  const bool by_k = a.k > 0 && a.k < V && (uint32_t)a.k <= k.above_cnt + k.in_cnt;
+  double lo, hi;  // bounds of the mass of the first k
+  if (by_k) {
+    p.kbin = k.at;
+    p.k_need = (uint32_t)a.k - k.above_cnt;
+    p.k_above = lo = k.above_mass;
+    hi = k.above_mass + k.in_mass;
+  } else {
+    p.k_above = lo = hi = k.above_mass + k.in_mass;
+  }
+  if (by_p) {
+    // (sums over bins and sums over entries differ in rounding: far less than 2^-30)
+    const Reached l = reach(S, n, m, true, 0u, (double)a.p * lo * (1.0 - 0x1p-30));
+    const Reached h = reach(S, n, m, true, 0u, (double)a.p * hi * (1.0 + 0x1p-30));
+    p.plo = l.at;
+    p.phi = h.at;
+    p.p_above = l.above_mass;
+  }
+  // min-p's cut lies above them: they do not matter
+  if (by_p ? key_bin < p.plo : by_k && key_bin < p.kbin) {
+    p.kbin = p.plo = p.phi = -1;
+  } else {
+    const int i = (int)threadIdx.x;
+    const bool in = i == p.kbin || (i >= p.plo && i <= p.phi && p.plo >= 0);
+    const Reached r = reach(S, in ? n : 0u, 0.0, false, 0xffffffffu, 0.0);
+    p.items = r.at < 0 ? 0u : r.above_cnt + r.in_cnt;
+  }
+  return p;
+}
+__device__ __forceinline__ bool in_question(const Plan& p, int bin) {
+  return bin == p.kbin || (bin >= p.plo && bin <= p.phi && p.plo >= 0);
+}
+
+// Where a sum over entries in ascending x reaches what is wanted: the value of
+// x, the sums before it and those of the entries at it.
+// take(key, entry, x): whether an entry takes part, and its x in [lo, hi].
+// Masses are relative to the edge of bin `first` (no entry lies above it).  1024
+// ranges of x a pass, at most four passes.
+struct Narrowed {
   uint32_t x, above_cnt, in_cnt;
   double above_mass, in_mass;
 };
-
-// take(key, entry, x): whether an entry takes part, and its x in [lo, hi].
-// Masses are 2^(f/16) per entry.  1024 ranges of x a pass, at most four passes.
 template <class Row, class Take>
-__device__ Reached narrow(Shared& S, const Row& row, double c, int mb, uint32_t lo, uint32_t hi,
-                          bool by_mass, uint32_t want_c, double want_m, Take&& take) {
-  Reached r{0, 0, 0, 0.0, 0.0};
-  const double scale = exp2((double)mb), unscale = exp2((double)-mb);
+__device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, double top,
+                                        int first, const Unit& unit, uint32_t lo, uint32_t hi, bool masses, bool by_mass,
+                                        uint32_t want_c, double want_m, Take take) {
+  Narrowed r{0, 0, 0, 0.0, 0.0};
+  const int sb = sum_bits(row.V);
+  const double scale = exp2((double)sb), unscale = exp2((double)-sb);
   for (;;) {
     const uint32_t span = hi - lo;
     const int shift = max(0, 22 - (span ? __builtin_clz(span) : 32));
@@ -297,23 +514,26 @@ __device__ Reached narrow(Shared& S, const Row& row, double c, int mb, uint32_t 
       const uint32_t key = key_of(z);
       uint32_t x;
       if (!take(key, e, x) || x < lo || x > hi) return;
-      const double t = (double)z * c;
       atomicAdd(&S.cnt[(x - lo) >> shift], 1u);
-      atomicAdd((unsigned long long*)&S.mass[(x - lo) >> shift],
-                (unsigned long long)fixed_point(frac_mass(t - floor(t)), scale));
+      if (masses) {
+        const double t = (double)z * c, b = floor(t);
+        const int bin = (int)fmin(top - b, (double)(kBins - 1));
+        atomicAdd((unsigned long long*)&S.mass[(x - lo) >> shift],
+                  (unsigned long long)fixed_point(entry_mass(t - b, unit) * S.edge[bin - first],
+                                                  scale));
+      }
     });
     __syncthreads();
     const uint32_t n = S.cnt[threadIdx.x];
-    const double m = (double)n + (double)S.mass[threadIdx.x] * unscale;
-    const int at = first_reaching(S, n, m, by_mass, want_c - r.above_cnt, want_m - r.above_mass);
-    if (at < 0) return r;  // (nothing takes part: no caller asks that)
-    r.above_cnt += S.above_cnt;
-    r.above_mass += S.above_mass;
-    r.in_cnt = S.in_cnt;
-    r.in_mass = S.in_mass;
-    lo += (uint32_t)at << shift;
+    const Reached f = reach(S, n, (double)S.mass[threadIdx.x] * unscale, by_mass,
+                            want_c - r.above_cnt, want_m - r.above_mass);
+    if (f.at < 0) return r;  // (nothing takes part: no caller asks that)
+    r.above_cnt += f.above_cnt;
+    r.above_mass += f.above_mass;
+    r.in_cnt = f.in_cnt;
+    r.in_mass = f.in_mass;
+    lo += (uint32_t)f.at << shift;
     hi = min(hi, lo + ((1u << shift) - 1u));
-    __syncthreads();
     if (shift == 0) {
       r.x = lo;
       return r;
@@ -321,330 +541,483 @@ __device__ Reached narrow(Shared& S, const Row& row, double c, int mb, uint32_t 
   }
 }
 
-// The cut of `want_c` entries (or the fewest whose mass reaches want_m) of the
-// bin `bin` below the row's maximum, and the mass they have (relative to the
-// bin's lower edge).
+// The cut that keeps want_c entries (or the fewest whose mass reaches want_m,
+// relative to the edge of `first`) of bins first .. last, and their mass.
 template <class Row>
-__device__ Cut cut_in_bin(Shared& S, const Row& row, double c, double top, int bin, int mb,
-                          bool by_mass, uint32_t want_c, double want_m, double& mass) {
-  // the bin's keys: a range, as the bins are monotone in the key
+__device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, double top,
+                                        const Unit& unit, int first, int last, bool by_mass, uint32_t want_c, double want_m,
+                                        double& mass) {
+  // the bins' keys: a range, as bins are monotone in the key
   uint32_t lo = 0xffffffffu, hi = 0;
   row.each(0, row.loads(), [&](int64_t, float z, uint32_t) {
     const uint32_t key = key_of(z);
     if (key < kKeyLowest) return;
-    const double d = top - floor((double)z * c);
-    if (d >= (double)bin && (bin == kBins - 1 || d < (double)(bin + 1))) {
+    const int b = bin_of(top, (double)z * c);
+    if (b >= first && b <= last) {
       lo = min(lo, key);
       hi = max(hi, key);
     }
   });
   lo = block_extreme<false>(S, lo);
   hi = block_extreme<true>(S, hi);
-  const Reached v = narrow(S, row, c, mb, ~hi, ~lo, by_mass, want_c, want_m,
-                           [&](uint32_t key, int64_t, uint32_t& x) {
-                             x = ~key;
-                             return key >= kKeyLowest;
-                           });
+  const Narrowed v = narrow(S, row, c, top, first, unit, ~hi, ~lo, true, by_mass, want_c, want_m,
+                            [](uint32_t key, int64_t, uint32_t& x) {
+                              x = ~key;
+                              return true;
+                            });
   const uint32_t key = ~v.x;
   // of the entries at that key, the first `need` by index
   const double each = v.in_mass / (double)v.in_cnt;
   uint32_t need;
   if (by_mass) {
     const double n = ceil((want_m - v.above_mass) / each);
-    need = n < 1.0 ? 1u : n > (double)v.in_cnt ? v.in_cnt : (uint32_t)n;
+    need = n >= (double)v.in_cnt ? v.in_cnt : n > 1.0 ? (uint32_t)n : 1u;
   } else {
     need = min(want_c - v.above_cnt, v.in_cnt);
   }
   mass = v.above_mass + each * (double)need;
   if (need == v.in_cnt) return Cut{key, kNoIndex};
-  const Reached i = narrow(S, row, c, mb, 0u, (uint32_t)(row.V - 1), false, need, 0.0,
-                           [&](uint32_t k, int64_t e, uint32_t& x) {
-                             x = (uint32_t)e;
-                             return k == key;
-                           });
+  const Narrowed i = narrow(S, row, c, top, first, unit, 0u, (uint32_t)(row.V - 1), false, false, need, 0.0,
+                            [key](uint32_t k, int64_t e, uint32_t& x) {
+                              x = (uint32_t)e;
+                              return k == key;
+                            });
   return Cut{key, (int32_t)i.x};
 }
 
-// The cut of a row whose largest logit is `zmax` (finite).
+// The cut by top-k and top-p, from the entries of the bins in question (or all
+// entries of the row).
 template <class Row>
-__device__ Cut cut_of(Shared& S, const Row& row, const Ask& a, float zmax) {
+__device__ __forceinline__ Cut resolve(Shared& S, const Row& row, const Ask& a, double top,
+                                       const Unit& unit, const Plan& p) {
   Cut cut{kKeyLowest, kNoIndex};
-  // min-p: the lowest float not below max z + T ln(min_p)
+  double whole = p.k_above;
+  if (p.kbin >= 0) {
+    double part;
+    cut = cut_in_bins(S, row, a.c, top, unit, p.kbin, p.kbin, false, p.k_need, 0.0, part);
+    if (p.kbin < kBins - 1) whole += part * S.edge[p.kbin];
+  }
+  if (p.plo >= 0) {
+    double part;
+    const double want = ((double)a.p * whole - p.p_above) / S.edge[p.plo];
+    cut = tighter(cut, cut_in_bins(S, row, a.c, top, unit, p.plo, p.phi, true, 0u, want, part));
+  }
+  return cut;
+}
+
+// The same for at most kRanked entries in LDS: each entry's place in the order
+// is counted against all others, and the sums run over the places.
+template <int DT>
+__device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double top,
+                                              const Unit& unit, const Plan& p, int n) {
+  using Row = RowOf<DT>;
+  const int j = (int)threadIdx.x;
+  uint32_t* order = S.cnt;  // place -> entry (no bin is in use)
+  if (j < n) {
+    const Item x = S.items[j];
+    const uint32_t key = key_of(Row::of_bits(x.bits));
+    uint32_t place = 0;
+    for (int i = 0; i < n; ++i) {
+      const Item y = S.items[i];
+      const uint32_t k = key_of(Row::of_bits(y.bits));
+      place += k > key || (k == key && y.idx < x.idx);
+    }
+    order[place] = (uint32_t)j;
+  }
+  __syncthreads();
+  float z = 0.0f;
+  int bin = -2;
+  double mass = 0.0;
+  if (j < n) {
+    z = Row::of_bits(S.items[order[j]].bits);
+    const double t = (double)z * a.c;
+    bin = bin_of(top, t);
+    mass = entry_mass(t - floor(t), unit);
+  }
+  const auto at = [&](int place) {
+    const Item x = S.items[order[place]];
+    return Cut{key_of(Row::of_bits(x.bits)), x.idx};
+  };
+  Cut cut{kKeyLowest, kNoIndex};
+  double whole = p.k_above;
+  if (p.kbin >= 0) {
+    const bool in = bin == p.kbin;
+    const Reached r = reach(S, in ? 1u : 0u, in ? mass : 0.0, false, p.k_need, 0.0);
+    cut = at(r.at);
+    if (p.kbin < kBins - 1) whole += (r.above_mass + r.in_mass) * S.edge[p.kbin];
+  }
+  if (p.plo >= 0) {
+    const bool in = bin >= p.plo && bin <= p.phi;
+    const Reached r = reach(S, in ? 1u : 0u, in ? mass * S.edge[bin - p.plo] : 0.0, true, 0u,
+                            ((double)a.p * whole - p.p_above) / S.edge[p.plo]);
+    cut = tighter(cut, at(r.at));
+  }
+  __syncthreads();
+  return cut;
+}
+
+// min-p's cut: the lowest float not below max z + T ln(min_p).
+__device__ __forceinline__ Cut min_p_cut(const Ask& a, float zmax) {
+  Cut cut{kKeyLowest, kNoIndex};
   const double zmin = (double)zmax + a.logm;
   if (zmin > (double)of_key(kKeyLowest)) {
     uint32_t k = key_of((float)zmin + 0.0f);
     if ((double)of_key(k) < zmin) ++k;
     cut.key = max(cut.key, k);
   }
-  const bool by_k = a.k > 0 && a.k < row.V, by_p = a.p < 1.0f;
-  if (!by_k && !by_p) return cut;
-  const double top = floor((double)zmax * a.c);
-  const int mb = mass_bits(row.V);
-  const double scale = exp2((double)mb);
+  return cut;
+}
+__device__ __forceinline__ int cut_bin(const Ask& a, const Cut& c, double top) {
+  return c.key > kKeyLowest ? bin_of(top, (double)of_key(c.key) * a.c) : kBins;
+}
+
+__device__ __forceinline__ void fill_edges(Shared& S) {
+  S.edge[threadIdx.x] = exp2(-(double)threadIdx.x * 0.0625);
+}
+
+// The cut of a row in one workgroup; zmax its largest logit (finite).  PACK:
+// at most kHeld entries.
+template <bool PACK, int DT, class Row>
+__device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const Ask& a, float zmax,
+                                      double top) {
+  const Cut floor_cut = min_p_cut(a, zmax);
+  if (!(a.k > 0 && a.k < row.V) && a.p >= 1.0f) return floor_cut;
+  const Unit unit = bin_unit<PACK>(row.V);
   S.cnt[threadIdx.x] = 0;
   S.mass[threadIdx.x] = 0;
+  if (threadIdx.x == 0) S.n_items = 0;
   __syncthreads();
-  row.each(0, row.loads(), [&](int64_t, float z, uint32_t) {
-    if (!(z > -__builtin_huge_valf())) return;
-    const double t = (double)z * a.c, b = floor(t);
-    const int bin = (int)fmin(top - b, (double)(kBins - 1));
-    atomicAdd(&S.cnt[bin], 1u);
-    if (bin < kBins - 1)
-      atomicAdd((unsigned long long*)&S.mass[bin],
-                (unsigned long long)fixed_point(frac_mass(t - b), scale));
+  row.each(0, row.loads(),
+           [&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top, unit.scale); });
+  __syncthreads();
+  uint64_t m = S.mass[threadIdx.x];
+  const uint32_t n = PACK ? (uint32_t)(m >> 48) : S.cnt[threadIdx.x];
+  if (PACK) m &= (1ull << 48) - 1;
+  const double mass = threadIdx.x == kBins - 1
+                          ? 0.0
+                          : ((double)n + (double)m * unit.inv) * S.edge[threadIdx.x];
+  const Plan p = make_plan(S, a, row.V, n, mass, cut_bin(a, floor_cut, top));
+  if (p.kbin < 0 && p.plo < 0) return floor_cut;
+  if (p.items > (uint32_t)kItems) return tighter(floor_cut, resolve(S, row, a, top, unit, p));
+  row.each(0, row.loads(), [&](int64_t e, float z, uint32_t bits) {
+    if (z > -__builtin_huge_valf() && in_question(p, bin_of(top, (double)z * a.c))) {
+      const uint32_t at = atomicAdd(&S.n_items, 1u);
+      if (at < (uint32_t)kItems) S.items[at] = Item{bits, (int32_t)e};
+    }
   });
   __syncthreads();
-  const uint32_t n = S.cnt[threadIdx.x];
-  const double edge = exp2(-(double)threadIdx.x * 0.0625);
-  const double m = threadIdx.x == kBins - 1
-                       ? 0.0
-                       : ((double)n + (double)S.mass[threadIdx.x] * exp2((double)-mb)) * edge;
-  // the mass of the first k entries (of all of them)
-  double whole = 0.0;
-  if (by_k) {
-    const int kbin = first_reaching(S, n, m, false, (uint32_t)a.k, 0.0);
-    const uint32_t above = S.above_cnt, in = S.in_cnt;
-    const double k_above = S.above_mass, in_mass = S.in_mass;
-    __syncthreads();
-    if ((uint32_t)a.k > above + in) {  // the row has fewer
-      whole = k_above + in_mass;
-    } else {
-      double part;
-      cut = tighter(cut, cut_in_bin(S, row, a.c, top, kbin, mb, false, (uint32_t)a.k - above, 0.0,
-                                    part));
-      whole = k_above + (kbin == kBins - 1 ? 0.0 : part * exp2(-(double)kbin * 0.0625));
-    }
-  }
-  if (!by_p) return cut;
-  if (!by_k) {
-    (void)first_reaching(S, n, m, false, 0xffffffffu, 0.0);  // (the last filled bin)
-    whole = S.above_mass + S.in_mass;
-    __syncthreads();
-  }
-  const double want = (double)a.p * whole;
-  const int pbin = first_reaching(S, n, m, true, 0u, want);
-  const double above = S.above_mass;
-  __syncthreads();
-  double part;
-  return tighter(cut, cut_in_bin(S, row, a.c, top, pbin, mb, true, 0u,
-                                 (want - above) * exp2((double)pbin * 0.0625), part));
+  if (p.items <= (uint32_t)kRanked)
+    return tighter(floor_cut, resolve_ranked<DT>(S, a, top, unit, p, (int)p.items));
+  return tighter(floor_cut,
+                 resolve(S, ItemRow<DT>(S.items, row.V, (int)p.items), a, top, unit, p));
 }
 
-// Weight of an entry in the draw.
-__device__ __forceinline__ uint64_t weight(float z, double c, double zmax, double scale) {
-  return fixed_point(exp2(((double)z - zmax) * c * 0.0625), scale);
+// ------------------------------------------------------------------ the draw
+// Weight of an entry: 2^((t - top)/16), 64 octaves below the top none.
+__device__ __forceinline__ uint64_t weight(const Shared& S, float z, double c, double top,
+                                           double scale) {
+  const double t = (double)z * c, b = floor(t);
+  const int bin = (int)fmin(top - b, (double)(kBins - 1));
+  return bin < kBins - 1 ? fixed_point((1.0 + frac_mass(t - b)) * S.edge[bin], scale) : 0;
 }
 
-// The kept token at which the cumulative weight in vocabulary order exceeds
-// u times the total; `total` is set to the total.  S.token and its key.
-template <class Row>
-__device__ void draw(Shared& S, const Row& row, const Cut& cut, double c, float zmax, float u,
-                     double& total) {
-  constexpr int VW = Row::VW;
+// From sums of G sub-chunks each in S.mass (thread i: sub-chunks lo + i G ..):
+// the place of thr in them.  Returns the total.
+__device__ __forceinline__ uint64_t find_sum(Shared& S, bool first, float u, uint64_t& thr,
+                                             int& at) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const double zm = (double)zmax;
-  const double scale = exp2((double)draw_bits(row.V));
-  int64_t lo = 0, n = ((int64_t)row.V + 64 * VW - 1) / (64 * VW);  // sub-chunks
-  uint64_t thr = 0;
-  bool first = true;
-  for (;;) {
-    const int64_t G = (n + kBins - 1) / kBins;  // sub-chunks to a sum
-    S.mass[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = (int)(lo / kNW); i <= (int)((lo + n - 1) / kNW); ++i) {
-      const int64_t sub = (int64_t)i * kNW + wave;
-      uint64_t s = 0;
-      if (sub >= lo && sub < lo + n)
-        row.each(i, i + 1, [&](int64_t e, float z, uint32_t) {
-          if (kept(cut, key_of(z), e)) s += weight(z, c, zm, scale);
-        });
-      if (__any(s != 0)) {
+  const uint64_t own = S.mass[threadIdx.x];
+  uint64_t in = wave_incl_scan(own);
+  if (lane == 63) S.wave64[wave] = in;
+  __syncthreads();
+  uint64_t base = 0, sum = 0;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) s += __shfl_xor((unsigned long long)s, d);
-        if (lane == 0) atomicAdd((unsigned long long*)&S.mass[(sub - lo) / G], (unsigned long long)s);
-      }
-    }
-    __syncthreads();
-    const uint64_t own = S.mass[threadIdx.x];
-    uint64_t in = wave_incl_scan((unsigned long long)own, lane);
-    if (lane == 63) S.wave64[wave] = in;
-    if (threadIdx.x == 0) S.found = kNoIndex;
-    __syncthreads();
-    uint64_t base = 0, sum = 0;
-#pragma unroll
-    for (int i = 0; i < kNW; ++i) {
-      if (i < wave) base += S.wave64[i];
-      sum += S.wave64[i];
-    }
-    in += base;
-    if (first) {
-      const double x = fmin((double)u * (double)sum, (double)sum);
-      thr = x > 0.0 ? min((uint64_t)x, sum - 1) : 0;
-      total = (double)sum / scale;
-      first = false;
-    }
-    if (in > thr && in - own <= thr) {  // one thread
-      S.found = (int)threadIdx.x;
-      S.before = in - own;
-    }
-    __syncthreads();
-    const int g = S.found;
-    thr -= S.before;
-    lo += (int64_t)g * G;
-    n = min(G, n - (int64_t)g * G);
-    __syncthreads();
-    if (G == 1) break;
+  for (int i = 0; i < kNW; ++i) {
+    const uint64_t x = S.wave64[i];
+    base += i < wave ? x : 0;
+    sum += x;
   }
-  if (wave == 0) {
-    const int64_t e0 = (lo * 64 + lane) * VW;
-    uint32_t w[4];
-    const int ne = e0 < row.V ? row.load(e0, w) : 0;
-    uint64_t s = 0;
+  in += base;
+  if (first) {
+    const double x = fmin((double)u * (double)sum, (double)sum);
+    thr = x > 0.0 ? min((uint64_t)x, sum - 1) : 0;
+  }
+  if (in > thr && in - own <= thr) {  // one thread
+    S.found = (int)threadIdx.x;
+    S.before = in - own;
+  }
+  __syncthreads();
+  at = S.found;
+  thr -= S.before;
+  return sum;
+}
+
+// The kept token at weight thr of sub-chunk `sub` of a row (the first
+// wavefront's): S.token and its logit.
+template <class Row>
+__device__ __forceinline__ void pick(Shared& S, const Row& row, const Cut& cut, double c,
+                                     double top, double scale, int64_t sub, uint64_t thr) {
+  constexpr int VW = Row::VW;
+  const int lane = threadIdx.x & 63;
+  const int64_t e0 = (sub * 64 + lane) * VW;
+  uint32_t w[4];
+  const int ne = e0 < row.V ? row.load(e0, w) : 0;
+  uint64_t ws[VW], s = 0;
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    ws[e] = 0;
+    if (e < ne) {
+      const float z = Row::value(w, e);
+      if (kept(cut, key_of(z), e0 + e)) ws[e] = weight(S, z, c, top, scale);
+    }
+    s += ws[e];
+  }
+  const uint64_t in = wave_incl_scan(s);
+  if (in > thr && in - s <= thr) {  // one lane
+    uint64_t at = in - s;
+    bool done = false;
 #pragma unroll
     for (int e = 0; e < VW; ++e) {
-      if (e >= ne) continue;
-      const float z = Row::value(w, e);
-      if (kept(cut, key_of(z), e0 + e)) s += weight(z, c, zm, scale);
-    }
-    const uint64_t in = wave_incl_scan((unsigned long long)s, lane);
-    if (in > thr && in - s <= thr) {
-      uint64_t at = in - s;
-      bool done = false;
-#pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        if (e >= ne || done) continue;
-        const float z = Row::value(w, e);
-        if (!kept(cut, key_of(z), e0 + e)) continue;
-        at += weight(z, c, zm, scale);
-        if (at > thr) {
-          S.token = (int)(e0 + e);
-          S.token_key = key_of(z);
-          done = true;
-        }
+      at += ws[e];
+      if (!done && at > thr) {
+        done = true;
+        S.token = (int)(e0 + e);
+        S.token_z = Row::value(w, e);
       }
     }
+  }
+}
+
+// Sums of the kept weights of sub-chunks [lo, lo + n) of a row, G to a sum;
+// the entries kept are counted in S.n_kept if `count`.
+template <class Row>
+__device__ __forceinline__ void sum_subs(Shared& S, const Row& row, const Cut& cut, double c,
+                                         double top, double scale, int64_t lo, int64_t n, int64_t G,
+                                         bool count) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  S.mass[threadIdx.x] = 0;
+  if (threadIdx.x == 0) S.n_kept = 0;
+  __syncthreads();
+  uint32_t k = 0;
+  for (int i = (int)(lo / kNW); i <= (int)((lo + n - 1) / kNW); ++i) {
+    const int64_t sub = (int64_t)i * kNW + wave;
+    if (sub < lo || sub >= lo + n) continue;
+    uint64_t s = 0;
+    uint32_t mine = 0;
+    row.each(i, i + 1, [&](int64_t e, float z, uint32_t) {
+      if (kept(cut, key_of(z), e)) {
+        s += weight(S, z, c, top, scale);
+        ++mine;
+      }
+    });
+    if (__any(mine != 0)) {
+      s = wave_incl_scan(s);
+      if (lane == 63)
+        atomicAdd((unsigned long long*)&S.mass[(sub - lo) / G], (unsigned long long)s);
+      k += mine;
+    }
+  }
+  if (count && __any(k != 0)) {
+    k = wave_incl_scan(k);
+    if (lane == 63) atomicAdd(&S.n_kept, k);
   }
   __syncthreads();
 }
 
-// A workgroup per row, which it reads from memory at every pass.
-template <int DT>
-__global__ void __launch_bounds__(kNT) k_sample(TruncParams P) {
-  __shared__ Shared S;
-  const int64_t r = blockIdx.x;
-  const ScanRow<DT> row{static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V};
-  const Ask a = ask_of(P, r);
-  float zmax = -__builtin_huge_valf();
-  row.each(0, row.loads(), [&](int64_t, float z, uint32_t) { zmax = fmaxf(zmax, z); });
-  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
-  zmax = of_key(kmax);
-  if (!a.valid || kmax < kKeyLowest) {
-    if (threadIdx.x == 0) {
-      P.out_token[r] = -1;
-      if (P.out_kept) P.out_kept[r] = 0;
-      if (P.out_logprob) P.out_logprob[r] = -__builtin_huge_valf();
-    }
-    return;
-  }
-  if (a.greedy) {
-    uint32_t first = 0xffffffffu;
-    row.each(0, row.loads(), [&](int64_t e, float z, uint32_t) {
-      if (key_of(z) == kmax) first = min(first, (uint32_t)e);
-    });
-    first = block_extreme<false>(S, first);
-    if (threadIdx.x == 0) {
-      P.out_token[r] = (int32_t)first;
-      if (P.out_kept) P.out_kept[r] = 1;
-      if (P.out_logprob) P.out_logprob[r] = 0.0f;
-    }
-    return;
-  }
-  const Cut cut = cut_of(S, row, a, zmax);
-  if (P.out_kept) {
-    if (threadIdx.x == 0) S.red[0] = 0;
+// The draw among sub-chunks [lo, lo + n), whose weights are known to hold thr.
+template <class Row>
+__device__ __forceinline__ void draw_within(Shared& S, const Row& row, const Cut& cut, double c,
+                                            double top, double scale, int64_t lo, int64_t n,
+                                            uint64_t thr) {
+  while (n > 1) {
+    const int64_t G = (n + kBins - 1) / kBins;
     __syncthreads();
-    uint32_t n = 0;
-    row.each(0, row.loads(), [&](int64_t e, float z, uint32_t) { n += kept(cut, key_of(z), e); });
-#pragma unroll
-    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-    if ((threadIdx.x & 63) == 0) atomicAdd(&S.red[0], n);
-    __syncthreads();
+    sum_subs(S, row, cut, c, top, scale, lo, n, G, false);
+    int at;
+    (void)find_sum(S, false, 0.0f, thr, at);
+    lo += (int64_t)at * G;
+    n = min(G, n - (int64_t)at * G);
   }
-  double total;
-  draw(S, row, cut, a.c, zmax, P.uniforms[r], total);
+  if (threadIdx.x < 64) pick(S, row, cut, c, top, scale, lo, thr);
+  __syncthreads();
+}
+
+__device__ __forceinline__ void no_token(const TruncParams& P, int64_t r) {
+  if (threadIdx.x == 0) {
+    P.out_token[r] = -1;
+    if (P.out_kept) P.out_kept[r] = 0;
+    if (P.out_logprob) P.out_logprob[r] = -__builtin_huge_valf();
+  }
+}
+__device__ __forceinline__ void greedy_token(const TruncParams& P, int64_t r, uint32_t token) {
+  if (threadIdx.x == 0) {
+    P.out_token[r] = (int32_t)token;
+    if (P.out_kept) P.out_kept[r] = 1;
+    if (P.out_logprob) P.out_logprob[r] = 0.0f;
+  }
+}
+__device__ __forceinline__ void drawn_token(const TruncParams& P, int64_t r, const Shared& S,
+                                            const Ask& a, double top, double total,
+                                            uint32_t n_kept) {
   if (threadIdx.x == 0) {
     P.out_token[r] = S.token;
-    if (P.out_kept) P.out_kept[r] = (int32_t)S.red[0];
+    if (P.out_kept) P.out_kept[r] = (int32_t)n_kept;
     if (P.out_logprob)
-      P.out_logprob[r] = (float)(((double)of_key(S.token_key) - (double)zmax) * a.c * kLn2by16 -
-                                 log(total));
+      P.out_logprob[r] = (float)(((double)S.token_z * a.c - top) * kLn2by16 - log(total));
   }
+}
+
+// The draw of a row in one workgroup.
+template <class Row>
+__device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r, const Row& row,
+                                     const Cut& cut, const Ask& a, double top) {
+  const double scale = exp2((double)sum_bits(row.V));
+  const int64_t n = ((int64_t)row.V + 64 * Row::VW - 1) / (64 * Row::VW);
+  const int64_t G = (n + kBins - 1) / kBins;
+  sum_subs(S, row, cut, a.c, top, scale, 0, n, G, true);
+  uint64_t thr = 0;
+  int at;
+  const uint64_t sum = find_sum(S, true, P.uniforms[r], thr, at);
+  const uint32_t n_kept = S.n_kept;
+  draw_within(S, row, cut, a.c, top, scale, (int64_t)at * G, min(G, n - (int64_t)at * G), thr);
+  drawn_token(P, r, S, a, top, (double)sum / scale, n_kept);
 }
 
 // The row's entries outside `cut` as -inf, the others as they are (all of
 // them with `whole`, none with `none`).
-template <class Row, int DT>
-__device__ void write_cut(const Row& row, char* out, const Cut& cut, bool whole, bool none) {
-  constexpr int VW = Row::VW;
+template <int DT, class Row>
+__device__ __forceinline__ void write_lane(const Row& row, char* out, int64_t e0,
+                                           const uint32_t (&w)[4], int n, const Cut& cut,
+                                           bool whole, bool none) {
+  constexpr int VW = Elem<DT>::VW;
+  uint32_t o[4];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    const bool k = !none && (whole || kept(cut, key_of(Row::value(w, e)), e0 + e));
+    if constexpr (DT == 1) {
+      const uint32_t b = k ? Row::bits(w, e) : 0xff80u;
+      o[e >> 1] = (e & 1) ? o[e >> 1] | (b << 16) : b;
+    } else {
+      o[e] = k ? w[e] : 0xff800000u;
+    }
+  }
+  char* a = out + e0 * Elem<DT>::EB;
+  if (n == VW) {
+    const w4 v{o[0], o[1], o[2], o[3]};
+    if constexpr (DT == 1) *reinterpret_cast<w4a2*>(a) = v;
+    else *reinterpret_cast<w4a4*>(a) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < VW; ++e)
+      if (e < n) {
+        if constexpr (DT == 1) reinterpret_cast<uint16_t*>(a)[e] = (uint16_t)Row::bits(o, e);
+        else reinterpret_cast<uint32_t*>(a)[e] = o[e];
+      }
+  }
+}
+template <int DT, class Row>
+__device__ __forceinline__ void write_cut(const Row& row, char* out, const Cut& cut, bool whole,
+                                          bool none) {
+  constexpr int VW = Elem<DT>::VW;
   for (int i = 0; i < row.loads(); ++i) {
     const int64_t e0 = ((int64_t)i * kNT + threadIdx.x) * VW;
     if (e0 >= row.V) continue;
-    uint32_t w[4], o[4];
+    uint32_t w[4];
     const int n = row.load(e0, w);
-#pragma unroll
-    for (int e = 0; e < VW; ++e) {
-      const bool k = !none && (whole || kept(cut, key_of(Row::value(w, e)), e0 + e));
-      if constexpr (DT == 1) {
-        const uint32_t b = k ? Row::bits(w, e) : 0xff80u;
-        o[e >> 1] = (e & 1) ? o[e >> 1] | (b << 16) : b;
-      } else {
-        o[e] = k ? w[e] : 0xff800000u;
-      }
-    }
-    char* a = out + e0 * Elem<DT>::EB;
-    if (n == VW) {
-      const w4 v{o[0], o[1], o[2], o[3]};
-      if constexpr (DT == 1) *reinterpret_cast<w4a2*>(a) = v;
-      else *reinterpret_cast<w4a4*>(a) = v;
-    } else {
-#pragma unroll
-      for (int e = 0; e < VW; ++e)
-        if (e < n) {
-          if constexpr (DT == 1) reinterpret_cast<uint16_t*>(a)[e] = (uint16_t)Row::bits(o, e);
-          else reinterpret_cast<uint32_t*>(a)[e] = o[e];
-        }
-    }
+    write_lane<DT>(row, out, e0, w, n, cut, whole, none);
   }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kNT) k_truncate(TruncParams P) {
+// One row by one workgroup.
+template <bool PACK, int DT, bool CUT, class Row>
+__device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t r, const Row& row,
+                                        float zmax) {
+  const Ask a = ask_of(P, r / P.rows_per_seq);
+  fill_edges(S);
+  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
+  zmax = of_key(kmax);
+  const bool none = !a.valid || kmax < kKeyLowest;
+  const double top = floor((double)zmax * a.c);
+  if constexpr (CUT) {
+    Cut cut{kKeyLowest, kNoIndex};
+    if (!none && !a.greedy) cut = cut_of<PACK, DT>(S, row, a, zmax, top);
+    __syncthreads();
+    write_cut<DT>(row, static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB, cut,
+                  a.valid && a.greedy, none);
+  } else if (none) {
+    no_token(P, r);
+  } else if (a.greedy) {
+    uint32_t first = 0xffffffffu;
+    row.each(0, row.loads(), [&](int64_t e, float z, uint32_t) {
+      if (key_of(z) == kmax) first = min(first, (uint32_t)e);
+    });
+    greedy_token(P, r, block_extreme<false>(S, first));
+  } else {
+    const Cut cut = cut_of<PACK, DT>(S, row, a, zmax, top);
+    draw(S, P, r, row, cut, a, top);
+  }
+}
+
+// A workgroup per row, which it reads from memory at every pass.
+template <int DT, bool CUT>
+__global__ void __launch_bounds__(kNT) k_trunc_scan(TruncParams P) {
   __shared__ Shared S;
   const int64_t r = blockIdx.x;
-  const ScanRow<DT> row{static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V};
-  char* out = static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB;
-  const Ask a = ask_of(P, r / P.rows_per_seq);
+  const ScanRow<DT> row(static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V);
   float zmax = -__builtin_huge_valf();
   row.each(0, row.loads(), [&](int64_t, float z, uint32_t) { zmax = fmaxf(zmax, z); });
-  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
-  const bool none = !a.valid || kmax < kKeyLowest, whole = a.greedy;
-  Cut cut{kKeyLowest, kNoIndex};
-  if (!none && !whole) cut = cut_of(S, row, a, of_key(kmax));
-  __syncthreads();
-  write_cut<ScanRow<DT>, DT>(row, out, cut, whole, none);
+  one_row<false, DT, CUT>(S, P, r, row, zmax);
+}
+
+// A workgroup per row, which it holds in LDS: U lane loads a thread.
+template <int DT, int U, bool CUT>
+__global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
+  constexpr int VW = Elem<DT>::VW;
+  __shared__ Shared S;
+  __shared__ w4 held[U * kNT];
+  const int64_t r = blockIdx.x;
+  const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
+  constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
+  float zmax = -__builtin_huge_valf();
+  uint32_t w[U][4];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int e0 = (i * kNT + (int)threadIdx.x) * VW;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[i][j] = kPad;
+    if (e0 < P.V) load_lane<DT>(src, e0, P.V, w[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+#pragma unroll
+    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::value(w[i], e));
+    held[i * kNT + threadIdx.x] = w4{w[i][0], w[i][1], w[i][2], w[i][3]};
+  }
+  one_row<true, DT, CUT>(S, P, r, HeldRow<DT>(held, P.V), zmax);
+}
+
+template <int DT, bool CUT>
+void launch_rows(const TruncParams& P, hipStream_t stream) {
+  constexpr int N = kNT * Elem<DT>::VW;  // entries of a lane load of a workgroup
+  const dim3 grid((uint32_t)P.R), block(kNT);
+  if (P.V <= N) k_trunc_held<DT, 1, CUT><<<grid, block, 0, stream>>>(P);
+  else if (P.V <= 2 * N) k_trunc_held<DT, 2, CUT><<<grid, block, 0, stream>>>(P);
+  else if (P.V <= 4 * N) k_trunc_held<DT, 4, CUT><<<grid, block, 0, stream>>>(P);
+  else if (P.V <= kHeld) {
+    if constexpr (DT == 0) k_trunc_held<DT, 8, CUT><<<grid, block, 0, stream>>>(P);
+  } else k_trunc_scan<DT, CUT><<<grid, block, 0, stream>>>(P);
 }
 
 }  // namespace
 
 // (P.R at most kMaxRows)
 hipError_t launch_truncated(const TruncParams& P, int dtype, hipStream_t stream) {
-  const dim3 grid((uint32_t)P.R), block(kNT);
-  if (P.out) {
-    if (dtype == SPC_BF16) k_truncate<1><<<grid, block, 0, stream>>>(P);
-    else k_truncate<0><<<grid, block, 0, stream>>>(P);
+  if (dtype == SPC_BF16) {
+    if (P.out) launch_rows<1, true>(P, stream);
+    else launch_rows<1, false>(P, stream);
   } else {
-    if (dtype == SPC_BF16) k_sample<1><<<grid, block, 0, stream>>>(P);
-    else k_sample<0><<<grid, block, 0, stream>>>(P);
+    if (P.out) launch_rows<0, true>(P, stream);
+    else launch_rows<0, false>(P, stream);
   }
   return hipGetLastError();
 }
