@@ -91,6 +91,10 @@ __device__ __forceinline__ uint64_t fixed_point(double x, double scale) {
 }
 
 
+__device__ __forceinline__ int wave_id() {
+  return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+}
+
 // Inclusive sums over a wavefront (DPP row shifts and broadcasts; 64-bit
 // values as two halves).
 template <int CTRL, int ROWS>
@@ -149,24 +153,23 @@ __device__ __forceinline__ Ask ask_of(const TruncParams& P, int64_t seq) {
   return a;
 }
 
-// The kept entries of a row: key above `key`, or equal with index <= `idx`.
+// The kept entries of a row: logit above z, or equal with index <= idx.
+constexpr float kLowest = -3.40282347e38f;  // the lowest finite float
 struct Cut {
-  uint32_t key;
+  float z;
   int32_t idx;
 };
-__device__ __forceinline__ bool kept(const Cut& c, uint32_t key, int64_t idx) {
-  return key > c.key || (key == c.key && idx <= c.idx);
+__device__ __forceinline__ bool kept(const Cut& c, float z, int64_t idx) {
+  return z > c.z || (z == c.z && idx <= c.idx);
 }
 // The more restrictive of two cuts.
 __device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) {
-  if (a.key != b.key) return a.key > b.key ? a : b;
-  return Cut{a.key, min(a.idx, b.idx)};
+  if (a.z != b.z) return a.z > b.z ? a : b;
+  return Cut{a.z, min(a.idx, b.idx)};
 }
 
 
 // ------------------------------------------------------------------ rows
-// Row entries, in 16-byte lane loads.  Thread t's lane load i covers entries
-// (i kNT + t) VW ..; sub-chunk i kNW + wave is a wavefront's lane load.
 template <int DT>
 struct RowOf {
   static constexpr int VW = Elem<DT>::VW;
@@ -211,7 +214,8 @@ __device__ __forceinline__ int load_lane(const char* row, int64_t e0, int32_t V,
   return n;
 }
 
-// A row read from memory at every pass.
+// A row read from memory at every pass: thread t's lane load i covers entries
+// (i kNT + t) VW ...
 template <int DT>
 struct ScanRow : RowOf<DT> {
   using RowOf<DT>::VW;
@@ -224,10 +228,14 @@ struct ScanRow : RowOf<DT> {
   __device__ __forceinline__ int load(int64_t e0, uint32_t (&w)[4]) const {
     return load_lane<DT>(row, e0, V, w);
   }
-  // f(entry, logit, the entry's bits) over the thread's entries of lane loads [i0, i1)
+  __device__ __forceinline__ float at(int64_t e) const {
+    return RowOf<DT>::of_bits(DT == 1 ? reinterpret_cast<const uint16_t*>(row)[e]
+                                      : reinterpret_cast<const uint32_t*>(row)[e]);
+  }
+  // f(entry, logit, the entry's bits) over the thread's entries
   template <class F>
-  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
-    for (int i = i0; i < i1; ++i) {
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int i = 0; i < loads(); ++i) {
       const int64_t e0 = ((int64_t)i * kNT + threadIdx.x) * VW;
       if (e0 >= V) continue;
       uint32_t w[4];
@@ -239,12 +247,15 @@ struct ScanRow : RowOf<DT> {
   }
 };
 
-// A row of at most kHeld entries held in LDS, lane load after lane load; what
-// lies behind its end is -inf, which no pass counts.
+// A row (or a slice of one) of at most kHeld entries held in LDS, in order; what
+// lies behind its end is -inf, which no pass counts.  Thread t's entries are
+// the E from t E on, its lane loads taken from another place on by each thread
+// so that a wavefront's reads spread over the banks.
 constexpr int kHeld = 32768;
-template <int DT>
+template <int DT, int U>
 struct HeldRow : RowOf<DT> {
   using RowOf<DT>::VW;
+  static constexpr int E = U * VW;
   const w4* lds;
   int32_t V;
   __device__ __forceinline__ HeldRow(const w4* l, int32_t v) : lds(l), V(v) {}
@@ -254,10 +265,15 @@ struct HeldRow : RowOf<DT> {
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     return (int)min((int64_t)VW, (int64_t)V - e0);
   }
+  __device__ __forceinline__ float at(int64_t e) const {
+    return RowOf<DT>::of_bits(DT == 1 ? reinterpret_cast<const uint16_t*>(lds)[e]
+                                      : reinterpret_cast<const uint32_t*>(lds)[e]);
+  }
   template <class F>
-  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
-    for (int i = i0; i < i1; ++i) {
-      const int e0 = (i * kNT + (int)threadIdx.x) * VW;
+  __device__ __forceinline__ void each(F&& f) const {
+    if ((int)threadIdx.x * E >= V) return;
+    for (int j = 0; j < U; ++j) {
+      const int e0 = (int)threadIdx.x * E + ((j + (int)threadIdx.x) & (U - 1)) * VW;
       uint32_t w[4];
       load(e0, w);
 #pragma unroll
@@ -276,12 +292,9 @@ struct ItemRow : RowOf<DT> {
   const Item* item;
   int32_t V, n;  // of a row of V entries
   __device__ __forceinline__ ItemRow(const Item* i, int32_t v, int32_t m) : item(i), V(v), n(m) {}
-  __device__ __forceinline__ int loads() const { return (n + kNT - 1) / kNT; }
   template <class F>
-  __device__ __forceinline__ void each(int i0, int i1, F&& f) const {
-    for (int i = i0; i < i1; ++i) {
-      const int j = i * kNT + (int)threadIdx.x;
-      if (j >= n) continue;
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int j = (int)threadIdx.x; j < n; j += kNT) {
       const Item x = item[j];
       f(x.idx, RowOf<DT>::of_bits(x.bits), x.bits);
     }
@@ -292,6 +305,12 @@ struct ItemRow : RowOf<DT> {
 constexpr int kItems = 1024;   // entries of the bins in question held in LDS
 constexpr int kRanked = 256;   // as many are ranked against each other
 
+struct Found {
+  int32_t state, at;  // 2: reached, 1: the last entry, 0: no entry
+  uint32_t above_cnt, in_cnt;
+  double above_mass, in_mass;
+};
+
 struct Shared {
   uint64_t mass[kBins];
   uint32_t cnt[kBins];
@@ -300,15 +319,11 @@ struct Shared {
   double waved[kNW];
   uint64_t wave64[kNW];
   uint32_t wave32[kNW];
-  uint32_t n_items, n_kept;
-  // first_reaching's answer
-  int32_t found, last;
-  uint32_t above_cnt, in_cnt;
-  double above_mass, in_mass;
+  uint32_t n_items;
+  Found found[2][kNW];
   // the draw's
+  int32_t sum_at;
   uint64_t before;
-  int32_t token;
-  float token_z;
 };
 
 __device__ __forceinline__ int log2_ceil(int32_t V) {
@@ -326,77 +341,85 @@ __device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
   x = wave_max(MAX ? x : ~x);
   if ((threadIdx.x & 63) == 63) S.wave32[threadIdx.x >> 6] = x;
   __syncthreads();
-  x = S.wave32[0];
-#pragma unroll
-  for (int i = 1; i < kNW; ++i) x = max(x, S.wave32[i]);
+  x = wave_max(S.wave32[threadIdx.x & 15]);
+  x = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
   __syncthreads();
   return MAX ? x : ~x;
 }
 
-// Counts c and masses m, one of each per thread, in thread order: the first
-// thread at which the inclusive sum reaches what is wanted (want_c entries, or
-// with by_mass a mass of want_m), else the last thread with c != 0; -1 if there
-// is none.  S holds the sums before that thread and its own.
-__device__ __forceinline__ int first_reaching(Shared& S, uint32_t c, double m, bool by_mass,
-                                              uint32_t want_c, double want_m) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// One value per wavefront, summed over the wavefronts before this one.  Every
+// wavefront scans the 16 sums in its first lanes; `slot` alternates between
+// calls, so that one barrier a call is enough.
+template <class T>
+__device__ __forceinline__ T lane_value(T v, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    return (T)__builtin_amdgcn_readlane((int)v, lane);
+  } else {
+    const uint64_t x = __builtin_bit_cast(uint64_t, v);
+    const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane)
+                           << 32;
+    return __builtin_bit_cast(T, y);
+  }
+}
+template <class T>
+__device__ __forceinline__ T row_incl_scan(T v) {  // over 16 lanes
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  return v;
+}
+
+// Counts c and masses m, one of each per thread, summed in thread order.
+struct Sums {
+  uint32_t c, upto_c;
+  double m, upto_m, before_m;  // inclusive, exclusive
+};
+__device__ __forceinline__ Sums sums_of(Shared& S, uint32_t c, double m) {
+  const int lane = threadIdx.x & 63, wave = wave_id();
   const uint32_t ci = wave_incl_scan(c);
   const double mi = wave_incl_scan(m);
   if (lane == 63) {
     S.wave32[wave] = ci;
     S.waved[wave] = mi;
   }
-  if (threadIdx.x == 0) {
-    S.found = kNoIndex;
-    S.last = -1;
-  }
   __syncthreads();
-  uint32_t bc = 0;
-  double bm = 0;
-#pragma unroll
-  for (int i = 0; i < kNW; ++i) {
-    const uint32_t x = S.wave32[i];
-    const double y = S.waved[i];
-    bc += i < wave ? x : 0u;
-    bm += i < wave ? y : 0.0;
-  }
+  const uint32_t wc = row_incl_scan(S.wave32[lane & 15]);
+  const double wm = row_incl_scan(S.waved[lane & 15]);
+  const uint32_t bc = wave ? lane_value(wc, wave - 1) : 0u;
+  const double bm = wave ? lane_value(wm, wave - 1) : 0.0;
   double me = dpp<0x138, 0xf>(mi);  // wave_shr: the lane before
   if (lane == 0) me = 0;
-  const bool some = c != 0;
-  const bool here = some && (by_mass ? bm + mi >= want_m : bc + ci >= want_c);
-  const uint64_t any = __ballot(here), all = __ballot(some);
-  if (lane == 0) {
-    if (any) atomicMin(&S.found, (wave << 6) + __builtin_ctzll(any));
-    if (all) atomicMax(&S.last, (wave << 6) + 63 - __builtin_clzll(all));
-  }
   __syncthreads();
-  const int at = S.found == kNoIndex ? S.last : S.found;
-  if ((int)threadIdx.x == at) {
-    S.above_cnt = bc + ci - c;
-    S.above_mass = bm + me;
-    S.in_cnt = c;
-    S.in_mass = m;
-  }
-  __syncthreads();
-  return at;
+  return Sums{c, bc + ci, m, bm + mi, bm + me};
 }
 
-// What first_reaching found, before S is used again.
+// The first thread whose sum up to it reaches want_c entries (by_mass: a mass
+// of want_m), or the last thread with an entry; -1 if there is none.  And the
+// sums before that thread, and its own.  `slot` differs from the last call's.
 struct Reached {
   int at;
   uint32_t above_cnt, in_cnt;
   double above_mass, in_mass;
 };
-__device__ __forceinline__ Reached reach(Shared& S, uint32_t c, double m, bool by_mass,
+__device__ __forceinline__ Reached reach(Shared& S, int slot, const Sums& x, bool by_mass,
                                          uint32_t want_c, double want_m) {
-  Reached r;
-  r.at = first_reaching(S, c, m, by_mass, want_c, want_m);
-  r.above_cnt = S.above_cnt;
-  r.in_cnt = S.in_cnt;
-  r.above_mass = S.above_mass;
-  r.in_mass = S.in_mass;
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const bool some = x.c != 0;
+  const uint64_t any = __ballot(some && (by_mass ? x.upto_m >= want_m : x.upto_c >= want_c));
+  const uint64_t all = __ballot(some);
+  const int mine = any ? __builtin_ctzll(any) : all ? 63 - __builtin_clzll(all) : 0;
+  if (lane == mine)
+    S.found[slot][wave] = Found{any ? 2 : all ? 1 : 0, (int)threadIdx.x, x.upto_c - x.c, x.c,
+                                x.before_m, x.m};
   __syncthreads();
-  return r;
+  const int state = S.found[slot][lane & 15].state;
+  const uint32_t yes = (uint32_t)__ballot(state == 2) & 0xffffu;
+  const uint32_t may = (uint32_t)__ballot(state == 1) & 0xffffu;
+  if (!(yes | may)) return Reached{-1, 0, 0, 0.0, 0.0};
+  const Found f = S.found[slot][yes ? __builtin_ctz(yes) : 31 - __builtin_clz(may)];
+  return Reached{f.at, f.above_cnt, f.in_cnt, f.above_mass, f.in_mass};
 }
 
 // The bin of t below a row's top bin.
@@ -453,8 +476,9 @@ __device__ __forceinline__ Plan make_plan(Shared& S, const Ask& a, int32_t V, ui
                                           double m, int key_bin) {
   Plan p{-1, 0, 0.0, -1, -1, 0.0, 0};
   const bool by_p = a.p < 1.0f;
+  const Sums x = sums_of(S, n, m);
   // (no count is reached without top-k: the last filled bin, whose sums are the row's)
-  const Reached k = reach(S, n, m, false, a.k > 0 && a.k < V ? (uint32_t)a.k : 0xffffffffu, 0.0);
+  const Reached k = reach(S, 0, x, false, a.k > 0 && a.k < V ? (uint32_t)a.k : 0xffffffffu, 0.0);
   const bool by_k = a.k > 0 && a.k < V && (uint32_t)a.k <= k.above_cnt + k.in_cnt;
   double lo, hi;  // bounds of the mass of the first k
   if (by_k) {
@@ -462,30 +486,58 @@ __device__ __forceinline__ Plan make_plan(Shared& S, const Ask& a, int32_t V, ui
     p.k_need = (uint32_t)a.k - k.above_cnt;
     p.k_above = lo = k.above_mass;
     hi = k.above_mass + k.in_mass;
+    p.items = k.in_cnt;
   } else {
     p.k_above = lo = hi = k.above_mass + k.in_mass;
   }
   if (by_p) {
     // (sums over bins and sums over entries differ in rounding: far less than 2^-30)
-    const Reached l = reach(S, n, m, true, 0u, (double)a.p * lo * (1.0 - 0x1p-30));
-    const Reached h = reach(S, n, m, true, 0u, (double)a.p * hi * (1.0 + 0x1p-30));
+    const Reached l = reach(S, 1, x, true, 0u, (double)a.p * lo * (1.0 - 0x1p-30));
+    const Reached h = reach(S, 0, x, true, 0u, (double)a.p * hi * (1.0 + 0x1p-30));
     p.plo = l.at;
     p.phi = h.at;
     p.p_above = l.above_mass;
+    p.items = h.above_cnt + h.in_cnt - l.above_cnt + (p.phi < p.kbin ? p.items : 0u);
   }
   // min-p's cut lies above them: they do not matter
   if (by_p ? key_bin < p.plo : by_k && key_bin < p.kbin) {
     p.kbin = p.plo = p.phi = -1;
-  } else {
-    const int i = (int)threadIdx.x;
-    const bool in = i == p.kbin || (i >= p.plo && i <= p.phi && p.plo >= 0);
-    const Reached r = reach(S, in ? n : 0u, 0.0, false, 0xffffffffu, 0.0);
-    p.items = r.at < 0 ? 0u : r.above_cnt + r.in_cnt;
+    p.items = 0;
   }
   return p;
 }
-__device__ __forceinline__ bool in_question(const Plan& p, int bin) {
-  return bin == p.kbin || (bin >= p.plo && bin <= p.phi && p.plo >= 0);
+
+// The lowest float whose t is at least `edge` (t is monotone in the logit).
+__device__ __forceinline__ float lowest_at(double edge, double c) {
+  const double g = fmin(fmax(edge / c, (double)kLowest), -(double)kLowest);
+  uint32_t k = key_of((float)g + 0.0f);
+  while (k > kKeyLowest && floor((double)of_key(k - 1) * c) >= edge) --k;
+  while (k < ~kKeyLowest && floor((double)of_key(k) * c) < edge) ++k;
+  return of_key(k);
+}
+// The logits of bins first .. last: lo <= z < hi.
+struct Range {
+  float lo, hi;
+};
+__device__ __forceinline__ Range range_of(int first, int last, double top, double c) {
+  Range r;
+  r.lo = last >= kBins - 1 ? kLowest : lowest_at(top - last, c);
+  r.hi = first <= 0 ? __builtin_huge_valf() : lowest_at(top - first + 1.0, c);
+  return r;
+}
+// The logits of the bins in question: two ranges.
+struct Question {
+  Range k, p;
+};
+__device__ __forceinline__ Question question_of(const Plan& p, double top, double c) {
+  const Range none{__builtin_huge_valf(), -__builtin_huge_valf()};
+  Question q{none, none};
+  if (p.kbin >= 0) q.k = range_of(p.kbin, p.kbin, top, c);
+  if (p.plo >= 0) q.p = range_of(p.plo, p.phi, top, c);
+  return q;
+}
+__device__ __forceinline__ bool asked(const Question& q, float z) {
+  return (z >= q.k.lo && z < q.k.hi) || (z >= q.p.lo && z < q.p.hi);
 }
 
 // Where a sum over entries in ascending x reaches what is wanted: the value of
@@ -502,6 +554,7 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
                                         int first, const Unit& unit, uint32_t lo, uint32_t hi, bool masses, bool by_mass,
                                         uint32_t want_c, double want_m, Take take) {
   Narrowed r{0, 0, 0, 0.0, 0.0};
+  int slot = 0;
   const int sb = sum_bits(row.V);
   const double scale = exp2((double)sb), unscale = exp2((double)-sb);
   for (;;) {
@@ -510,7 +563,7 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
     S.cnt[threadIdx.x] = 0;
     S.mass[threadIdx.x] = 0;
     __syncthreads();
-    row.each(0, row.loads(), [&](int64_t e, float z, uint32_t) {
+    row.each([&](int64_t e, float z, uint32_t) {
       const uint32_t key = key_of(z);
       uint32_t x;
       if (!take(key, e, x) || x < lo || x > hi) return;
@@ -525,8 +578,8 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
     });
     __syncthreads();
     const uint32_t n = S.cnt[threadIdx.x];
-    const Reached f = reach(S, n, (double)S.mass[threadIdx.x] * unscale, by_mass,
-                            want_c - r.above_cnt, want_m - r.above_mass);
+    const Reached f = reach(S, slot ^= 1, sums_of(S, n, (double)S.mass[threadIdx.x] * unscale),
+                            by_mass, want_c - r.above_cnt, want_m - r.above_mass);
     if (f.at < 0) return r;  // (nothing takes part: no caller asks that)
     r.above_cnt += f.above_cnt;
     r.above_mass += f.above_mass;
@@ -547,15 +600,13 @@ template <class Row>
 __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, double top,
                                         const Unit& unit, int first, int last, bool by_mass, uint32_t want_c, double want_m,
                                         double& mass) {
-  // the bins' keys: a range, as bins are monotone in the key
+  // the keys there are in the bins
+  const Range in = range_of(first, last, top, c);
   uint32_t lo = 0xffffffffu, hi = 0;
-  row.each(0, row.loads(), [&](int64_t, float z, uint32_t) {
-    const uint32_t key = key_of(z);
-    if (key < kKeyLowest) return;
-    const int b = bin_of(top, (double)z * c);
-    if (b >= first && b <= last) {
-      lo = min(lo, key);
-      hi = max(hi, key);
+  row.each([&](int64_t, float z, uint32_t) {
+    if (z >= in.lo && z < in.hi) {
+      lo = min(lo, key_of(z));
+      hi = max(hi, key_of(z));
     }
   });
   lo = block_extreme<false>(S, lo);
@@ -576,13 +627,13 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
     need = min(want_c - v.above_cnt, v.in_cnt);
   }
   mass = v.above_mass + each * (double)need;
-  if (need == v.in_cnt) return Cut{key, kNoIndex};
+  if (need == v.in_cnt) return Cut{of_key(key), kNoIndex};
   const Narrowed i = narrow(S, row, c, top, first, unit, 0u, (uint32_t)(row.V - 1), false, false, need, 0.0,
                             [key](uint32_t k, int64_t e, uint32_t& x) {
                               x = (uint32_t)e;
                               return k == key;
                             });
-  return Cut{key, (int32_t)i.x};
+  return Cut{of_key(key), (int32_t)i.x};
 }
 
 // The cut by top-k and top-p, from the entries of the bins in question (or all
@@ -590,7 +641,7 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
 template <class Row>
 __device__ __forceinline__ Cut resolve(Shared& S, const Row& row, const Ask& a, double top,
                                        const Unit& unit, const Plan& p) {
-  Cut cut{kKeyLowest, kNoIndex};
+  Cut cut{kLowest, kNoIndex};
   double whole = p.k_above;
   if (p.kbin >= 0) {
     double part;
@@ -636,20 +687,20 @@ __device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double to
   }
   const auto at = [&](int place) {
     const Item x = S.items[order[place]];
-    return Cut{key_of(Row::of_bits(x.bits)), x.idx};
+    return Cut{Row::of_bits(x.bits), x.idx};
   };
-  Cut cut{kKeyLowest, kNoIndex};
+  Cut cut{kLowest, kNoIndex};
   double whole = p.k_above;
   if (p.kbin >= 0) {
     const bool in = bin == p.kbin;
-    const Reached r = reach(S, in ? 1u : 0u, in ? mass : 0.0, false, p.k_need, 0.0);
+    const Reached r = reach(S, 0, sums_of(S, in ? 1u : 0u, in ? mass : 0.0), false, p.k_need, 0.0);
     cut = at(r.at);
     if (p.kbin < kBins - 1) whole += (r.above_mass + r.in_mass) * S.edge[p.kbin];
   }
   if (p.plo >= 0) {
     const bool in = bin >= p.plo && bin <= p.phi;
-    const Reached r = reach(S, in ? 1u : 0u, in ? mass * S.edge[bin - p.plo] : 0.0, true, 0u,
-                            ((double)a.p * whole - p.p_above) / S.edge[p.plo]);
+    const Reached r = reach(S, 1, sums_of(S, in ? 1u : 0u, in ? mass * S.edge[bin - p.plo] : 0.0),
+                            true, 0u, ((double)a.p * whole - p.p_above) / S.edge[p.plo]);
     cut = tighter(cut, at(r.at));
   }
   __syncthreads();
@@ -658,28 +709,28 @@ __device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double to
 
 // min-p's cut: the lowest float not below max z + T ln(min_p).
 __device__ __forceinline__ Cut min_p_cut(const Ask& a, float zmax) {
-  Cut cut{kKeyLowest, kNoIndex};
+  Cut cut{kLowest, kNoIndex};
   const double zmin = (double)zmax + a.logm;
-  if (zmin > (double)of_key(kKeyLowest)) {
+  if (zmin > (double)kLowest) {
     uint32_t k = key_of((float)zmin + 0.0f);
     if ((double)of_key(k) < zmin) ++k;
-    cut.key = max(cut.key, k);
+    cut.z = of_key(k);
   }
   return cut;
 }
 __device__ __forceinline__ int cut_bin(const Ask& a, const Cut& c, double top) {
-  return c.key > kKeyLowest ? bin_of(top, (double)of_key(c.key) * a.c) : kBins;
+  return c.z > kLowest ? bin_of(top, (double)c.z * a.c) : kBins;
 }
 
 __device__ __forceinline__ void fill_edges(Shared& S) {
   S.edge[threadIdx.x] = exp2(-(double)threadIdx.x * 0.0625);
 }
 
-// The cut of a row in one workgroup; zmax its largest logit (finite).  PACK:
-// at most kHeld entries.
+// The cut of a row in one workgroup; zmax its largest logit (finite), `whole` the
+// row in memory.  PACK: at most kHeld entries.
 template <bool PACK, int DT, class Row>
-__device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const Ask& a, float zmax,
-                                      double top) {
+__device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const ScanRow<DT>& whole,
+                                      const Ask& a, float zmax, double top) {
   const Cut floor_cut = min_p_cut(a, zmax);
   if (!(a.k > 0 && a.k < row.V) && a.p >= 1.0f) return floor_cut;
   const Unit unit = bin_unit<PACK>(row.V);
@@ -687,8 +738,7 @@ __device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const Ask& a, f
   S.mass[threadIdx.x] = 0;
   if (threadIdx.x == 0) S.n_items = 0;
   __syncthreads();
-  row.each(0, row.loads(),
-           [&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top, unit.scale); });
+  row.each([&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top, unit.scale); });
   __syncthreads();
   uint64_t m = S.mass[threadIdx.x];
   const uint32_t n = PACK ? (uint32_t)(m >> 48) : S.cnt[threadIdx.x];
@@ -698,9 +748,10 @@ __device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const Ask& a, f
                           : ((double)n + (double)m * unit.inv) * S.edge[threadIdx.x];
   const Plan p = make_plan(S, a, row.V, n, mass, cut_bin(a, floor_cut, top));
   if (p.kbin < 0 && p.plo < 0) return floor_cut;
-  if (p.items > (uint32_t)kItems) return tighter(floor_cut, resolve(S, row, a, top, unit, p));
-  row.each(0, row.loads(), [&](int64_t e, float z, uint32_t bits) {
-    if (z > -__builtin_huge_valf() && in_question(p, bin_of(top, (double)z * a.c))) {
+  if (p.items > (uint32_t)kItems) return tighter(floor_cut, resolve(S, whole, a, top, unit, p));
+  const Question q = question_of(p, top, a.c);
+  row.each([&](int64_t e, float z, uint32_t bits) {
+    if (asked(q, z)) {
       const uint32_t at = atomicAdd(&S.n_items, 1u);
       if (at < (uint32_t)kItems) S.items[at] = Item{bits, (int32_t)e};
     }
@@ -721,125 +772,63 @@ __device__ __forceinline__ uint64_t weight(const Shared& S, float z, double c, d
   return bin < kBins - 1 ? fixed_point((1.0 + frac_mass(t - b)) * S.edge[bin], scale) : 0;
 }
 
-// From sums of G sub-chunks each in S.mass (thread i: sub-chunks lo + i G ..):
-// the place of thr in them.  Returns the total.
-__device__ __forceinline__ uint64_t find_sum(Shared& S, bool first, float u, uint64_t& thr,
-                                             int& at) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t own = S.mass[threadIdx.x];
+// Weights `own`, one per thread in vocabulary order: the thread at which their
+// sum exceeds thr (first: thr is set to u times the total); thr becomes what is
+// left of it there.  Returns the total.
+__device__ __forceinline__ uint64_t find_sum(Shared& S, uint64_t own, bool first, float u,
+                                             uint64_t& thr, int& at) {
+  const int lane = threadIdx.x & 63, wave = wave_id();
   uint64_t in = wave_incl_scan(own);
   if (lane == 63) S.wave64[wave] = in;
   __syncthreads();
-  uint64_t base = 0, sum = 0;
-#pragma unroll
-  for (int i = 0; i < kNW; ++i) {
-    const uint64_t x = S.wave64[i];
-    base += i < wave ? x : 0;
-    sum += x;
-  }
-  in += base;
+  const uint64_t ws = row_incl_scan(S.wave64[lane & 15]);
+  const uint64_t sum = lane_value(ws, 15);
+  in += wave ? lane_value(ws, wave - 1) : 0;
   if (first) {
     const double x = fmin((double)u * (double)sum, (double)sum);
     thr = x > 0.0 ? min((uint64_t)x, sum - 1) : 0;
   }
   if (in > thr && in - own <= thr) {  // one thread
-    S.found = (int)threadIdx.x;
+    S.sum_at = (int)threadIdx.x;
     S.before = in - own;
   }
   __syncthreads();
-  at = S.found;
+  at = S.sum_at;
   thr -= S.before;
   return sum;
 }
 
-// The kept token at weight thr of sub-chunk `sub` of a row (the first
-// wavefront's): S.token and its logit.
+// The kept token at weight thr of entries [lo, lo + n) of a row, which have that
+// much: each thread sums a share of them, until a share is one entry.
 template <class Row>
-__device__ __forceinline__ void pick(Shared& S, const Row& row, const Cut& cut, double c,
-                                     double top, double scale, int64_t sub, uint64_t thr) {
-  constexpr int VW = Row::VW;
-  const int lane = threadIdx.x & 63;
-  const int64_t e0 = (sub * 64 + lane) * VW;
-  uint32_t w[4];
-  const int ne = e0 < row.V ? row.load(e0, w) : 0;
-  uint64_t ws[VW], s = 0;
-#pragma unroll
-  for (int e = 0; e < VW; ++e) {
-    ws[e] = 0;
-    if (e < ne) {
-      const float z = Row::value(w, e);
-      if (kept(cut, key_of(z), e0 + e)) ws[e] = weight(S, z, c, top, scale);
-    }
-    s += ws[e];
-  }
-  const uint64_t in = wave_incl_scan(s);
-  if (in > thr && in - s <= thr) {  // one lane
-    uint64_t at = in - s;
-    bool done = false;
-#pragma unroll
-    for (int e = 0; e < VW; ++e) {
-      at += ws[e];
-      if (!done && at > thr) {
-        done = true;
-        S.token = (int)(e0 + e);
-        S.token_z = Row::value(w, e);
-      }
-    }
-  }
-}
-
-// Sums of the kept weights of sub-chunks [lo, lo + n) of a row, G to a sum;
-// the entries kept are counted in S.n_kept if `count`.
-template <class Row>
-__device__ __forceinline__ void sum_subs(Shared& S, const Row& row, const Cut& cut, double c,
-                                         double top, double scale, int64_t lo, int64_t n, int64_t G,
-                                         bool count) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  S.mass[threadIdx.x] = 0;
-  if (threadIdx.x == 0) S.n_kept = 0;
-  __syncthreads();
-  uint32_t k = 0;
-  for (int i = (int)(lo / kNW); i <= (int)((lo + n - 1) / kNW); ++i) {
-    const int64_t sub = (int64_t)i * kNW + wave;
-    if (sub < lo || sub >= lo + n) continue;
+__device__ __forceinline__ int64_t draw_among(Shared& S, const Row& row, const Cut& cut, double c,
+                                              double top, double scale, int64_t lo, int64_t n,
+                                              uint64_t thr) {
+  for (;;) {
+    const int64_t q = (n + kNT - 1) / kNT;
+    const int64_t e0 = (int64_t)threadIdx.x * q, e1 = min(e0 + q, n);
     uint64_t s = 0;
-    uint32_t mine = 0;
-    row.each(i, i + 1, [&](int64_t e, float z, uint32_t) {
-      if (kept(cut, key_of(z), e)) {
-        s += weight(S, z, c, top, scale);
-        ++mine;
-      }
-    });
-    if (__any(mine != 0)) {
-      s = wave_incl_scan(s);
-      if (lane == 63)
-        atomicAdd((unsigned long long*)&S.mass[(sub - lo) / G], (unsigned long long)s);
-      k += mine;
+    for (int64_t e = lo + e0; e < lo + e1; ++e) {
+      const float z = row.at(e);
+      if (kept(cut, z, e)) s += weight(S, z, c, top, scale);
     }
+    int at;
+    (void)find_sum(S, s, false, 0.0f, thr, at);
+    lo += (int64_t)at * q;
+    n = min(q, n - (int64_t)at * q);
+    __syncthreads();
+    if (q == 1) return lo;
   }
-  if (count && __any(k != 0)) {
-    k = wave_incl_scan(k);
-    if (lane == 63) atomicAdd(&S.n_kept, k);
-  }
-  __syncthreads();
 }
 
-// The draw among sub-chunks [lo, lo + n), whose weights are known to hold thr.
-template <class Row>
-__device__ __forceinline__ void draw_within(Shared& S, const Row& row, const Cut& cut, double c,
-                                            double top, double scale, int64_t lo, int64_t n,
-                                            uint64_t thr) {
-  while (n > 1) {
-    const int64_t G = (n + kBins - 1) / kBins;
-    __syncthreads();
-    sum_subs(S, row, cut, c, top, scale, lo, n, G, false);
-    int at;
-    (void)find_sum(S, false, 0.0f, thr, at);
-    lo += (int64_t)at * G;
-    n = min(G, n - (int64_t)at * G);
-  }
-  if (threadIdx.x < 64) pick(S, row, cut, c, top, scale, lo, thr);
+// Entries kept, over the block.
+__device__ __forceinline__ uint32_t block_sum(Shared& S, uint32_t k) {
+  k = wave_incl_scan(k);
+  if ((threadIdx.x & 63) == 63) S.wave32[threadIdx.x >> 6] = k;
   __syncthreads();
+  k = lane_value(row_incl_scan(S.wave32[threadIdx.x & 15]), 15);
+  __syncthreads();
+  return k;
 }
 
 __device__ __forceinline__ void no_token(const TruncParams& P, int64_t r) {
@@ -856,31 +845,88 @@ __device__ __forceinline__ void greedy_token(const TruncParams& P, int64_t r, ui
     if (P.out_logprob) P.out_logprob[r] = 0.0f;
   }
 }
-__device__ __forceinline__ void drawn_token(const TruncParams& P, int64_t r, const Shared& S,
-                                            const Ask& a, double top, double total,
+__device__ __forceinline__ void drawn_token(const TruncParams& P, int64_t r, int64_t token,
+                                            float z, const Ask& a, double top, double total,
                                             uint32_t n_kept) {
   if (threadIdx.x == 0) {
-    P.out_token[r] = S.token;
+    P.out_token[r] = (int32_t)token;
     if (P.out_kept) P.out_kept[r] = (int32_t)n_kept;
     if (P.out_logprob)
-      P.out_logprob[r] = (float)(((double)S.token_z * a.c - top) * kLn2by16 - log(total));
+      P.out_logprob[r] = (float)(((double)z * a.c - top) * kLn2by16 - log(total));
   }
 }
 
-// The draw of a row in one workgroup.
-template <class Row>
-__device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r, const Row& row,
-                                     const Cut& cut, const Ask& a, double top) {
+// The weight of a thread's kept entries of a held row, and their number.  The
+// weights are taken one of each thread at a time: few of a thread's entries are
+// kept as a rule, and some of every wavefront's.
+template <int DT, int U>
+__device__ __forceinline__ uint64_t held_weight(const Shared& S, const HeldRow<DT, U>& row,
+                                                int64_t first, const Cut& cut, const Ask& a,
+                                                double top, double scale, uint32_t& n) {
+  constexpr int VW = Elem<DT>::VW, E = HeldRow<DT, U>::E;
+  static_assert(E <= 32, "a bit for each of a thread's entries");
+  uint32_t mask = 0;
+  if ((int)threadIdx.x * E < row.V)
+    for (int j = 0; j < U; ++j) {
+      const int at = ((j + (int)threadIdx.x) & (U - 1)) * VW, e0 = (int)threadIdx.x * E + at;
+      uint32_t w[4], bits = 0;
+      row.load(e0, w);
+#pragma unroll
+      for (int e = 0; e < VW; ++e)
+        bits |= (kept(cut, RowOf<DT>::value(w, e), first + e0 + e) ? 1u : 0u) << e;
+      mask |= bits << at;
+    }
+  n = __popc(mask);
+  uint64_t s = 0;
+  while (mask) {
+    const int e = __builtin_ctz(mask);
+    mask &= mask - 1;
+    s += weight(S, row.at((int)threadIdx.x * E + e), a.c, top, scale);
+  }
+  return s;
+}
+
+// The draw of a row in one workgroup: held, or read from memory.
+template <int DT, int U>
+__device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
+                                     const HeldRow<DT, U>& row, const Cut& cut, const Ask& a,
+                                     double top) {
+  constexpr int E = HeldRow<DT, U>::E;
   const double scale = exp2((double)sum_bits(row.V));
-  const int64_t n = ((int64_t)row.V + 64 * Row::VW - 1) / (64 * Row::VW);
-  const int64_t G = (n + kBins - 1) / kBins;
-  sum_subs(S, row, cut, a.c, top, scale, 0, n, G, true);
+  uint32_t n;
+  const uint64_t s = held_weight(S, row, 0, cut, a, top, scale, n);
+  const uint32_t n_kept = P.out_kept ? block_sum(S, n) : 0;
   uint64_t thr = 0;
   int at;
-  const uint64_t sum = find_sum(S, true, P.uniforms[r], thr, at);
-  const uint32_t n_kept = S.n_kept;
-  draw_within(S, row, cut, a.c, top, scale, (int64_t)at * G, min(G, n - (int64_t)at * G), thr);
-  drawn_token(P, r, S, a, top, (double)sum / scale, n_kept);
+  const uint64_t sum = find_sum(S, s, true, P.uniforms[r], thr, at);
+  __syncthreads();
+  const int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * E,
+                                   min(E, row.V - at * E), thr);
+  drawn_token(P, r, token, row.at(token), a, top, (double)sum / scale, n_kept);
+}
+template <int DT>
+__device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
+                                     const ScanRow<DT>& row, const Cut& cut, const Ask& a,
+                                     double top) {
+  const double scale = exp2((double)sum_bits(row.V));
+  const int64_t q = ((int64_t)row.V + kNT - 1) / kNT, e0 = (int64_t)threadIdx.x * q;
+  uint32_t n = 0;
+  uint64_t s = 0;
+  for (int64_t e = e0; e < min(e0 + q, (int64_t)row.V); ++e) {
+    const float z = row.at(e);
+    if (kept(cut, z, e)) {
+      s += weight(S, z, a.c, top, scale);
+      ++n;
+    }
+  }
+  const uint32_t n_kept = P.out_kept ? block_sum(S, n) : 0;
+  uint64_t thr = 0;
+  int at;
+  const uint64_t sum = find_sum(S, s, true, P.uniforms[r], thr, at);
+  __syncthreads();
+  const int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * q,
+                                   min(q, row.V - (int64_t)at * q), thr);
+  drawn_token(P, r, token, row.at(token), a, top, (double)sum / scale, n_kept);
 }
 
 // The row's entries outside `cut` as -inf, the others as they are (all of
@@ -893,7 +939,7 @@ __device__ __forceinline__ void write_lane(const Row& row, char* out, int64_t e0
   uint32_t o[4];
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
-    const bool k = !none && (whole || kept(cut, key_of(Row::value(w, e)), e0 + e));
+    const bool k = !none && (whole || kept(cut, Row::value(w, e), e0 + e));
     if constexpr (DT == 1) {
       const uint32_t b = k ? Row::bits(w, e) : 0xff80u;
       o[e >> 1] = (e & 1) ? o[e >> 1] | (b << 16) : b;
@@ -931,7 +977,7 @@ __device__ __forceinline__ void write_cut(const Row& row, char* out, const Cut& 
 // One row by one workgroup.
 template <bool PACK, int DT, bool CUT, class Row>
 __device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t r, const Row& row,
-                                        float zmax) {
+                                        const ScanRow<DT>& mem, float zmax) {
   const Ask a = ask_of(P, r / P.rows_per_seq);
   fill_edges(S);
   const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
@@ -939,8 +985,8 @@ __device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t
   const bool none = !a.valid || kmax < kKeyLowest;
   const double top = floor((double)zmax * a.c);
   if constexpr (CUT) {
-    Cut cut{kKeyLowest, kNoIndex};
-    if (!none && !a.greedy) cut = cut_of<PACK, DT>(S, row, a, zmax, top);
+    Cut cut{kLowest, kNoIndex};
+    if (!none && !a.greedy) cut = cut_of<PACK, DT>(S, row, mem, a, zmax, top);
     __syncthreads();
     write_cut<DT>(row, static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB, cut,
                   a.valid && a.greedy, none);
@@ -948,12 +994,12 @@ __device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t
     no_token(P, r);
   } else if (a.greedy) {
     uint32_t first = 0xffffffffu;
-    row.each(0, row.loads(), [&](int64_t e, float z, uint32_t) {
+    row.each([&](int64_t e, float z, uint32_t) {
       if (key_of(z) == kmax) first = min(first, (uint32_t)e);
     });
     greedy_token(P, r, block_extreme<false>(S, first));
   } else {
-    const Cut cut = cut_of<PACK, DT>(S, row, a, zmax, top);
+    const Cut cut = cut_of<PACK, DT>(S, row, mem, a, zmax, top);
     draw(S, P, r, row, cut, a, top);
   }
 }
@@ -965,8 +1011,8 @@ __global__ void __launch_bounds__(kNT) k_trunc_scan(TruncParams P) {
   const int64_t r = blockIdx.x;
   const ScanRow<DT> row(static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V);
   float zmax = -__builtin_huge_valf();
-  row.each(0, row.loads(), [&](int64_t, float z, uint32_t) { zmax = fmaxf(zmax, z); });
-  one_row<false, DT, CUT>(S, P, r, row, zmax);
+  row.each([&](int64_t, float z, uint32_t) { zmax = fmaxf(zmax, z); });
+  one_row<false, DT, CUT>(S, P, r, row, row, zmax);
 }
 
 // A workgroup per row, which it holds in LDS: U lane loads a thread.
@@ -993,7 +1039,7 @@ __global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
     for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::value(w[i], e));
     held[i * kNT + threadIdx.x] = w4{w[i][0], w[i][1], w[i][2], w[i][3]};
   }
-  one_row<true, DT, CUT>(S, P, r, HeldRow<DT>(held, P.V), zmax);
+  one_row<true, DT, CUT>(S, P, r, HeldRow<DT, U>(held, P.V), ScanRow<DT>(src, P.V), zmax);
 }
 
 template <int DT, bool CUT>
