@@ -614,6 +614,103 @@ spc::TruncParams truncated_rows(const void* logits, int64_t R, int32_t rows_per_
   return P;
 }
 
+// How rows of V entries are taken: held by a workgroup, or in slices of
+// `loads` lane loads a thread, `rows` of them a launch.
+struct TruncLayout {
+  int32_t slices = 0, loads = 0;
+  int64_t rows = spc::kMaxRows;
+  size_t max, bins, weights, kept, plans, items, total = 0;
+};
+TruncLayout trunc_layout(int64_t R, int32_t V, int32_t dtype) {
+  TruncLayout L;
+  L.rows = std::min<int64_t>(R, spc::kMaxRows);
+  if (V <= spc::kTruncHeld) return L;
+  L.loads = 4;
+  L.slices = (int32_t)(((int64_t)V + spc::trunc_slice_elems(dtype, L.loads) - 1) /
+                       spc::trunc_slice_elems(dtype, L.loads));
+  const size_t row = (size_t)L.slices * (8 * spc::kTruncBins + 8 * 16 + 8) +
+                     spc::trunc_plan_bytes() + spc::kTruncItems * spc::trunc_item_bytes();
+  L.rows = std::max<int64_t>(1, std::min<int64_t>(L.rows, (size_t(256) << 20) / row));
+  size_t o = 0;
+  const auto part = [&](size_t bytes) {
+    const size_t at = o;
+    o = align_up(o + bytes * (size_t)L.rows, 256);
+    return at;
+  };
+  L.bins = part((size_t)L.slices * 8 * spc::kTruncBins);
+  L.weights = part((size_t)L.slices * 8 * 16);
+  L.max = part((size_t)L.slices * 4);
+  L.kept = part((size_t)L.slices * 4);
+  L.plans = part(spc::trunc_plan_bytes());
+  L.items = part(spc::kTruncItems * spc::trunc_item_bytes());
+  L.total = o;
+  return L;
+}
+
+// A workspace of `bytes`: the caller's, or from the internal one behind its
+// counter region, which stays as it is.
+spc_status plain_workspace(void* caller, size_t caller_bytes, size_t bytes, hipStream_t stream,
+                           char** out) {
+  if (caller) {
+    if (caller_bytes < bytes || (uintptr_t)caller % 256 != 0)
+      return fail(SPC_E_WORKSPACE, "workspace of %zu bytes (need %zu, 256-byte aligned)",
+                  caller_bytes, bytes);
+    *out = static_cast<char*>(caller);
+    return SPC_OK;
+  }
+  const size_t zero = spc::ws_layout(1, 1, 2, SPC_BF16).zero_end;
+  const spc_status st = internal_workspace(zero + bytes, zero, stream, out);
+  if (st == SPC_OK) *out += zero;
+  return st;
+}
+
+// Rows [r0, ...) of a call, a launch's worth at a time: `base` holds the call's
+// pointers, settings arrays of sequences from 0.
+spc_status truncated_impl(const spc::TruncParams& base, int32_t dtype, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream) {
+  const TruncLayout L = trunc_layout(base.R, base.V, dtype);
+  char* ws = nullptr;
+  if (L.total) {
+    const spc_status st = plain_workspace(workspace, workspace_bytes, L.total, stream, &ws);
+    if (st != SPC_OK) return st;
+  }
+  const int64_t eb = dtype == SPC_BF16 ? 2 : 4, per = base.rows_per_seq;
+  // whole sequences a launch, or parts of one sequence's rows
+  const int64_t step = std::max<int64_t>(1, L.rows / per) * per;
+  for (int64_t s0 = 0; s0 < base.R; s0 += step) {
+    const int64_t s1 = std::min(base.R, s0 + step);
+    for (int64_t r0 = s0; r0 < s1; r0 += L.rows) {
+      spc::TruncParams P = base;
+      const int64_t b0 = s0 / per;
+      P.R = std::min(s1 - r0, L.rows);
+      P.z = static_cast<const char*>(base.z) + r0 * base.ld * eb;
+      if (base.out) P.out = static_cast<char*>(base.out) + r0 * base.out_ld * eb;
+      P.temp_ps = offset(base.temp_ps, b0);
+      P.top_k_ps = offset(base.top_k_ps, b0);
+      P.top_p_ps = offset(base.top_p_ps, b0);
+      P.min_p_ps = offset(base.min_p_ps, b0);
+      P.uniforms = offset(base.uniforms, r0);
+      P.out_token = offset(base.out_token, r0);
+      P.out_logprob = offset(base.out_logprob, r0);
+      P.out_kept = offset(base.out_kept, r0);
+      if (L.total) {
+        P.slices = L.slices;
+        P.slice_loads = L.loads;
+        P.items_max = spc::kTruncItems;
+        P.slice_bins = reinterpret_cast<uint64_t*>(ws + L.bins);
+        P.sub_weight = reinterpret_cast<uint64_t*>(ws + L.weights);
+        P.slice_max = reinterpret_cast<float*>(ws + L.max);
+        P.slice_kept = reinterpret_cast<uint32_t*>(ws + L.kept);
+        P.row_plan = ws + L.plans;
+        P.items = ws + L.items;
+      }
+      const hipError_t e = spc::launch_truncated(P, dtype, stream);
+      if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+    }
+  }
+  return SPC_OK;
+}
+
 spc_status sample_impl(const void* logits, int32_t dtype, int32_t B, int32_t V,
                        int64_t row_stride, const spc_truncation* t, const float* uniforms,
                        int32_t* out_token, float* out_logprob, int32_t* out_kept,
@@ -631,22 +728,12 @@ spc_status sample_impl(const void* logits, int32_t dtype, int32_t B, int32_t V,
   const int64_t eb = dtype == SPC_BF16 ? 2 : 4;
   if ((uintptr_t)logits % eb != 0)
     return fail(SPC_E_ALIGN, "the logits must be aligned to their elements");
-  for (int64_t b0 = 0; b0 < B; b0 += spc::kMaxRows) {
-    spc::TruncParams P =
-        truncated_rows(static_cast<const char*>(logits) + b0 * row_stride * eb,
-                       std::min<int64_t>(B - b0, spc::kMaxRows), 1, V, row_stride, t);
-    P.temp_ps = offset(P.temp_ps, b0);
-    P.top_k_ps = offset(P.top_k_ps, b0);
-    P.top_p_ps = offset(P.top_p_ps, b0);
-    P.min_p_ps = offset(P.min_p_ps, b0);
-    P.uniforms = offset(uniforms, b0);
-    P.out_token = out_token + b0;
-    P.out_logprob = offset(out_logprob, b0);
-    P.out_kept = offset(out_kept, b0);
-    const hipError_t e = spc::launch_truncated(P, dtype, stream);
-    if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
-  }
-  return SPC_OK;
+  spc::TruncParams P = truncated_rows(logits, B, 1, V, row_stride, t);
+  P.uniforms = uniforms;
+  P.out_token = out_token;
+  P.out_logprob = out_logprob;
+  P.out_kept = out_kept;
+  return truncated_impl(P, dtype, workspace, workspace_bytes, stream);
 }
 
 spc_status truncate_impl(const void* logits, int32_t dtype, int32_t B, int32_t rows_per_seq,
@@ -663,26 +750,10 @@ spc_status truncate_impl(const void* logits, int32_t dtype, int32_t B, int32_t r
   const int64_t eb = dtype == SPC_BF16 ? 2 : 4;
   if (((uintptr_t)logits | (uintptr_t)out) % eb != 0)
     return fail(SPC_E_ALIGN, "the logits must be aligned to their elements");
-  // whole sequences a launch, or parts of one sequence's rows
-  const int64_t step = std::max<int64_t>(1, spc::kMaxRows / rows_per_seq);
-  for (int64_t b0 = 0; b0 < B; b0 += step) {
-    const int64_t nb = std::min<int64_t>(B - b0, step), rows = nb * rows_per_seq;
-    for (int64_t r0 = 0; r0 < rows; r0 += spc::kMaxRows) {
-      const int64_t at = (b0 * rows_per_seq + r0) * V * eb;
-      spc::TruncParams P = truncated_rows(static_cast<const char*>(logits) + at,
-                                          std::min<int64_t>(rows - r0, spc::kMaxRows),
-                                          rows_per_seq, V, V, t);
-      P.out = static_cast<char*>(out) + at;
-      P.out_ld = V;
-      P.temp_ps = offset(P.temp_ps, b0);
-      P.top_k_ps = offset(P.top_k_ps, b0);
-      P.top_p_ps = offset(P.top_p_ps, b0);
-      P.min_p_ps = offset(P.min_p_ps, b0);
-      const hipError_t e = spc::launch_truncated(P, dtype, stream);
-      if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
-    }
-  }
-  return SPC_OK;
+  spc::TruncParams P = truncated_rows(logits, (int64_t)B * rows_per_seq, rows_per_seq, V, V, t);
+  P.out = out;
+  P.out_ld = V;
+  return truncated_impl(P, dtype, workspace, workspace_bytes, stream);
 }
 
 // The checks every cache call makes of the cache, and its parameters.
@@ -833,7 +904,10 @@ spc_status spc_truncate(const void* logits, int32_t dtype, int32_t B, int32_t ro
                        workspace_bytes, stream);
 }
 
-size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype) { return 0; }
+size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype) {
+  if (rows < 1 || V < 2 || (dtype != SPC_F32 && dtype != SPC_BF16)) return 0;
+  return trunc_layout(rows, V, dtype).total;
+}
 
 spc_status spc_kv_write(const spc_kv_cache* cache, const void* k, const void* v, int32_t dtype,
                         int64_t k_stride, int64_t v_stride, int64_t rows,

@@ -194,7 +194,22 @@ struct TruncParams {
   int32_t* out_token;
   float* out_logprob;
   int32_t* out_kept;
+  // rows of more than kTruncHeld entries: `slices` of them a row (0: a
+  // workgroup holds the row), slice_loads lane loads a thread each, and the
+  // workspace of a launch's R rows
+  int32_t slices, slice_loads;
+  int32_t items_max;         // entries of a row's list
+  float* slice_max;          // [R][slices]
+  uint64_t* slice_bins;      // [R][slices][kTruncBins]
+  uint64_t* sub_weight;      // [R][slices][16]
+  uint32_t* slice_kept;      // [R][slices]
+  void* row_plan;            // [R] of trunc_plan_bytes()
+  void* items;               // [R][items_max] of trunc_item_bytes()
 };
+constexpr int kTruncHeld = 32768, kTruncBins = 1024, kTruncItems = 8192;
+int trunc_slice_elems(int dtype, int loads);  // entries of a slice
+size_t trunc_plan_bytes();
+size_t trunc_item_bytes();
 hipError_t launch_truncated(const TruncParams& P, int dtype, hipStream_t stream);
 
 // A call on a paged key/value cache (spc_kv_*): the cache's pages and the

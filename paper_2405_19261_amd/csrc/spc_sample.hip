@@ -41,7 +41,7 @@ namespace {
 
 constexpr int kNT = 1024;  // threads of a workgroup
 constexpr int kNW = kNT / 64;
-constexpr int kBins = 1024;
+constexpr int kBins = kTruncBins;
 constexpr double kBinsPerNat = 23.083120654223414518;  // 16 log2(e)
 constexpr double kLn2by16 = 0.043321698784996581839;   // ln(2) / 16
 constexpr int kNoIndex = 0x7fffffff;
@@ -247,11 +247,10 @@ struct ScanRow : RowOf<DT> {
   }
 };
 
-// A row (or a slice of one) of at most kHeld entries held in LDS, in order; what
+// A row (or a slice of one) of at most kTruncHeld entries held in LDS, in order; what
 // lies behind its end is -inf, which no pass counts.  Thread t's entries are
 // the E from t E on, its lane loads taken from another place on by each thread
 // so that a wavefront's reads spread over the banks.
-constexpr int kHeld = 32768;
 template <int DT, int U>
 struct HeldRow : RowOf<DT> {
   using RowOf<DT>::VW;
@@ -332,8 +331,8 @@ __device__ __forceinline__ int log2_ceil(int32_t V) {
 // Fixed-point scales: sums of V terms of at most 2^(1/16) stay under 2^63,
 // and a term under 2^51.
 __device__ __forceinline__ int sum_bits(int32_t V) { return min(50, 61 - log2_ceil(V)); }
-// The masses of the bins of at most kHeld entries: 16 bits of count above 48 of
-// mass (kHeld terms under 0.0444 2^37).
+// The masses of the bins of at most kTruncHeld entries: 16 bits of count above 48 of
+// mass (kTruncHeld terms under 0.0444 2^37).
 constexpr int kPackBits = 37;
 
 template <bool MAX>
@@ -727,7 +726,7 @@ __device__ __forceinline__ void fill_edges(Shared& S) {
 }
 
 // The cut of a row in one workgroup; zmax its largest logit (finite), `whole` the
-// row in memory.  PACK: at most kHeld entries.
+// row in memory.  PACK: at most kTruncHeld entries.
 template <bool PACK, int DT, class Row>
 __device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const ScanRow<DT>& whole,
                                       const Ask& a, float zmax, double top) {
@@ -1004,17 +1003,6 @@ __device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t
   }
 }
 
-// A workgroup per row, which it reads from memory at every pass.
-template <int DT, bool CUT>
-__global__ void __launch_bounds__(kNT) k_trunc_scan(TruncParams P) {
-  __shared__ Shared S;
-  const int64_t r = blockIdx.x;
-  const ScanRow<DT> row(static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V);
-  float zmax = -__builtin_huge_valf();
-  row.each([&](int64_t, float z, uint32_t) { zmax = fmaxf(zmax, z); });
-  one_row<false, DT, CUT>(S, P, r, row, row, zmax);
-}
-
 // A workgroup per row, which it holds in LDS: U lane loads a thread.
 template <int DT, int U, bool CUT>
 __global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
@@ -1042,19 +1030,281 @@ __global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
   one_row<true, DT, CUT>(S, P, r, HeldRow<DT, U>(held, P.V), ScanRow<DT>(src, P.V), zmax);
 }
 
+// ------------------------------------------------------------------ long rows
+// Rows of more than kTruncHeld entries are cut into slices, a workgroup to each, in
+// four launches: the slices' bins; the row's plan from them; the slices again,
+// for what is kept for sure and the entries in question; and the row's end.
+
+// Bins of a slice, relative to the slice's own maximum: bins lie on one grid
+// for the whole row, so that a row's bins are sums of its slices'.
+template <int DT, int U>
+__global__ void __launch_bounds__(kNT) k_slice_bins(TruncParams P) {
+  constexpr int VW = Elem<DT>::VW;
+  constexpr int64_t N = (int64_t)kNT * U * VW;
+  __shared__ Shared S;
+  const int s = blockIdx.x;
+  const int64_t r = blockIdx.y;
+  const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
+  constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
+  uint32_t w[U][4];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int64_t e0 = s * N + (i * kNT + (int)threadIdx.x) * VW;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[i][j] = kPad;
+    if (e0 < P.V) load_lane<DT>(src, e0, P.V, w[i]);
+  }
+  S.mass[threadIdx.x] = 0;
+  float zmax = -__builtin_huge_valf();
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::value(w[i], e));
+  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
+  zmax = of_key(kmax);
+  if (threadIdx.x == 0) P.slice_max[r * P.slices + s] = zmax;
+  const Ask a = ask_of(P, r / P.rows_per_seq);
+  if (!a.valid || a.greedy || kmax < kKeyLowest || (!(a.k > 0 && a.k < P.V) && a.p >= 1.0f)) return;
+  const double top = floor((double)zmax * a.c);
+  const Unit unit = bin_unit<true>(P.V);
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int e = 0; e < VW; ++e)
+      add_to_bins<true>(S, RowOf<DT>::value(w[i], e), a.c, top, unit.scale);
+  __syncthreads();
+  P.slice_bins[(r * P.slices + s) * kBins + threadIdx.x] = S.mass[threadIdx.x];
+}
+
+enum RowMode : int32_t { kRowNone, kRowGreedy, kRowCut, kRowScan };
+struct RowPlan {
+  int32_t mode;
+  float zmax, floor_z, sure_z;  // min-p's cut; entries not below sure_z are kept
+  double top;
+  Plan plan;
+  Question q;
+  uint32_t n_items, first;      // entries put into the list; the argmax (greedy rows)
+};
+
+__global__ void __launch_bounds__(kNT) k_slice_plan(TruncParams P) {
+  __shared__ Shared S;
+  const int64_t r = blockIdx.x;
+  const float* maxima = P.slice_max + r * P.slices;
+  float zmax = -__builtin_huge_valf();
+  for (int s = (int)threadIdx.x; s < P.slices; s += kNT) zmax = fmaxf(zmax, maxima[s]);
+  fill_edges(S);
+  if (threadIdx.x == 0) S.n_items = 0;
+  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
+  zmax = of_key(kmax);
+  const Ask a = ask_of(P, r / P.rows_per_seq);
+  RowPlan R{};
+  R.mode = !a.valid || kmax < kKeyLowest ? kRowNone : a.greedy ? kRowGreedy : kRowCut;
+  R.zmax = zmax;
+  R.first = 0xffffffffu;
+  R.plan.kbin = R.plan.plo = -1;
+  if (R.mode == kRowCut) {
+    R.top = floor((double)zmax * a.c);
+    const Cut floor_cut = min_p_cut(a, zmax);
+    R.sure_z = R.floor_z = floor_cut.z;
+    if ((a.k > 0 && a.k < P.V) || a.p < 1.0f) {
+      const uint64_t* bins = P.slice_bins + r * P.slices * kBins;
+      const int i = (int)threadIdx.x;
+      uint32_t n = 0;
+      uint64_t m = 0;
+#pragma unroll 4
+      for (int s = 0; s < P.slices; ++s) {
+        const float zs = maxima[s];
+        if (zs < kLowest) continue;
+        const int shift = (int)fmin(R.top - floor((double)zs * a.c), (double)(kBins - 1));
+        const uint64_t* b = bins + (int64_t)s * kBins;
+        if (i < kBins - 1 && i >= shift) {
+          const uint64_t x = b[i - shift];
+          n += (uint32_t)(x >> 48);
+          m += x & ((1ull << 48) - 1);
+        }
+        // the row's last bin takes all that the shift moves there
+        if (i + shift >= kBins - 1) atomicAdd(&S.n_items, (uint32_t)(b[i] >> 48));
+      }
+      __syncthreads();
+      if (i == kBins - 1) n = S.n_items;
+      const Unit unit = bin_unit<true>(P.V);
+      const double mass = i == kBins - 1 ? 0.0 : ((double)n + (double)m * unit.inv) * S.edge[i];
+      R.plan = make_plan(S, a, P.V, n, mass, cut_bin(a, floor_cut, R.top));
+      R.q = question_of(R.plan, R.top, a.c);
+      if (R.plan.items > (uint32_t)P.items_max) R.mode = kRowScan;
+      if (R.plan.plo >= 0) R.sure_z = fmaxf(R.floor_z, R.q.p.hi);
+      else if (R.plan.kbin >= 0) R.sure_z = fmaxf(R.floor_z, R.q.k.hi);
+    }
+  }
+  if (threadIdx.x == 0) reinterpret_cast<RowPlan*>(P.row_plan)[r] = R;
+}
+
+template <int DT, int U, bool CUT>
+__global__ void __launch_bounds__(kNT) k_slice_keep(TruncParams P) {
+  constexpr int VW = Elem<DT>::VW;
+  constexpr int64_t N = (int64_t)kNT * U * VW;
+  __shared__ Shared S;
+  __shared__ w4 held[U * kNT];
+  const int s = blockIdx.x;
+  const int64_t r = blockIdx.y;
+  RowPlan* plan = reinterpret_cast<RowPlan*>(P.row_plan) + r;
+  const int mode = plan->mode;
+  if (mode == kRowScan || (!CUT && mode == kRowNone)) return;
+  const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
+  constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
+  const Ask a = ask_of(P, r / P.rows_per_seq);
+  fill_edges(S);
+  const Cut sure{plan->sure_z, kNoIndex};
+  const Question q = plan->q;
+  const bool ask = plan->plan.kbin >= 0 || plan->plan.plo >= 0;
+  char* out = CUT ? static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB : nullptr;
+  const ScanRow<DT> row(src, P.V);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int64_t e0 = s * N + (i * kNT + (int)threadIdx.x) * VW;
+    uint32_t w[4] = {kPad, kPad, kPad, kPad};
+    if (e0 < P.V) {
+      const int n = load_lane<DT>(src, e0, P.V, w);
+      if (CUT) write_lane<DT>(row, out, e0, w, n, sure, mode == kRowGreedy, mode == kRowNone);
+    }
+    held[i * kNT + threadIdx.x] = w4{w[0], w[1], w[2], w[3]};
+  }
+  __syncthreads();
+  const int left = (int)min(N, P.V - s * N);
+  const HeldRow<DT, U> mine(held, left);
+  if (mode == kRowCut && ask) {
+    // the entries in question, to the row's list
+    Item* list = reinterpret_cast<Item*>(P.items) + r * P.items_max;
+    mine.each([&](int64_t e, float z, uint32_t bits) {
+      if (asked(q, z)) {
+        const uint32_t at = atomicAdd(&plan->n_items, 1u);
+        if (at < (uint32_t)P.items_max) list[at] = Item{bits, (int32_t)(s * N + e)};
+      }
+    });
+  }
+  if constexpr (!CUT) {
+    if (mode == kRowGreedy) {
+      mine.each([&](int64_t e, float z, uint32_t) {
+        if (z == plan->zmax) atomicMin(&plan->first, (uint32_t)(s * N + e));
+      });
+      return;
+    }
+    uint32_t n;
+    uint64_t x = held_weight(S, mine, s * N, sure, a, plan->top, exp2((double)sum_bits(P.V)), n);
+    x = wave_incl_scan(x);
+    if ((threadIdx.x & 63) == 63)
+      P.sub_weight[(r * P.slices + s) * kNW + (threadIdx.x >> 6)] = x;
+    n = block_sum(S, n);
+    if (threadIdx.x == 0) P.slice_kept[r * P.slices + s] = n;
+  }
+}
+
+template <int DT, bool CUT>
+__global__ void __launch_bounds__(kNT) k_slice_end(TruncParams P, int sub) {
+  __shared__ Shared S;
+  const int64_t r = blockIdx.x;
+  const RowPlan R = reinterpret_cast<const RowPlan*>(P.row_plan)[r];
+  const ScanRow<DT> row(static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V);
+  if (R.mode == kRowScan) {
+    one_row<false, DT, CUT>(S, P, r, row, row, R.zmax);
+    return;
+  }
+  if (R.mode == kRowNone) {
+    if (!CUT) no_token(P, r);
+    return;
+  }
+  if (R.mode == kRowGreedy) {
+    if (!CUT) greedy_token(P, r, R.first);
+    return;
+  }
+  const Ask a = ask_of(P, r / P.rows_per_seq);
+  const bool ask = R.plan.kbin >= 0 || R.plan.plo >= 0;
+  if (CUT && !ask) return;
+  fill_edges(S);
+  const Item* list = reinterpret_cast<const Item*>(P.items) + r * P.items_max;
+  const int n_items = ask ? (int)R.plan.items : 0;
+  Cut cut{R.floor_z, kNoIndex};
+  if (ask) {
+    const Unit unit = bin_unit<true>(P.V);
+    if (n_items <= kItems) {
+      if ((int)threadIdx.x < n_items) S.items[threadIdx.x] = list[threadIdx.x];
+      __syncthreads();
+      cut = tighter(cut, n_items <= kRanked
+                             ? resolve_ranked<DT>(S, a, R.top, unit, R.plan, n_items)
+                             : resolve(S, ItemRow<DT>(S.items, P.V, n_items), a, R.top, unit, R.plan));
+    } else {
+      __syncthreads();
+      cut = tighter(cut, resolve(S, ItemRow<DT>(list, P.V, n_items), a, R.top, unit, R.plan));
+    }
+  }
+  if constexpr (CUT) {
+    char* out = static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB;
+    for (int i = (int)threadIdx.x; i < n_items; i += kNT) {
+      const Item x = list[i];
+      if (!kept(cut, RowOf<DT>::of_bits(x.bits), x.idx)) continue;
+      if constexpr (DT == 1) reinterpret_cast<uint16_t*>(out)[x.idx] = (uint16_t)x.bits;
+      else reinterpret_cast<uint32_t*>(out)[x.idx] = x.bits;
+    }
+  } else {
+    // weights by groups of G sub-chunks of `sub` entries
+    const double scale = exp2((double)sum_bits(P.V));
+    const int64_t subs = ((int64_t)P.V + sub - 1) / sub, G = (subs + kNT - 1) / kNT;
+    const uint64_t* weights = P.sub_weight + r * P.slices * kNW;
+    uint64_t own = 0;
+    for (int64_t g = threadIdx.x * G; g < min((threadIdx.x + 1) * G, subs); ++g) own += weights[g];
+    uint32_t n = 0;
+    for (int i = (int)threadIdx.x; i < P.slices; i += kNT) n += P.slice_kept[r * P.slices + i];
+    __syncthreads();
+    S.mass[threadIdx.x] = own;
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < n_items; i += kNT) {
+      const Item x = list[i];
+      const float z = RowOf<DT>::of_bits(x.bits);
+      if (!kept(cut, z, x.idx)) continue;
+      ++n;
+      atomicAdd((unsigned long long*)&S.mass[x.idx / (sub * G)],
+                (unsigned long long)weight(S, z, a.c, R.top, scale));
+    }
+    n = block_sum(S, n);
+    uint64_t thr = 0;
+    int at;
+    const uint64_t sum = find_sum(S, S.mass[threadIdx.x], true, P.uniforms[r], thr, at);
+    __syncthreads();
+    const int64_t lo = (int64_t)at * G * sub;
+    const int64_t token =
+        draw_among(S, row, cut, a.c, R.top, scale, lo, min(G * sub, P.V - lo), thr);
+    drawn_token(P, r, token, row.at(token), a, R.top, (double)sum / scale, n);
+  }
+}
+
+template <int DT, int U, bool CUT>
+void launch_slices(const TruncParams& P, hipStream_t stream) {
+  const dim3 grid((uint32_t)P.slices, (uint32_t)P.R), rows((uint32_t)P.R), block(kNT);
+  k_slice_bins<DT, U><<<grid, block, 0, stream>>>(P);
+  k_slice_plan<<<rows, block, 0, stream>>>(P);
+  k_slice_keep<DT, U, CUT><<<grid, block, 0, stream>>>(P);
+  k_slice_end<DT, CUT><<<rows, block, 0, stream>>>(P, 64 * U * Elem<DT>::VW);
+}
+
 template <int DT, bool CUT>
 void launch_rows(const TruncParams& P, hipStream_t stream) {
   constexpr int N = kNT * Elem<DT>::VW;  // entries of a lane load of a workgroup
   const dim3 grid((uint32_t)P.R), block(kNT);
-  if (P.V <= N) k_trunc_held<DT, 1, CUT><<<grid, block, 0, stream>>>(P);
+  if (P.slices) {
+    if (P.slice_loads == 1) launch_slices<DT, 1, CUT>(P, stream);
+    else if (P.slice_loads == 2) launch_slices<DT, 2, CUT>(P, stream);
+    else launch_slices<DT, 4, CUT>(P, stream);
+  } else if (P.V <= N) k_trunc_held<DT, 1, CUT><<<grid, block, 0, stream>>>(P);
   else if (P.V <= 2 * N) k_trunc_held<DT, 2, CUT><<<grid, block, 0, stream>>>(P);
   else if (P.V <= 4 * N) k_trunc_held<DT, 4, CUT><<<grid, block, 0, stream>>>(P);
-  else if (P.V <= kHeld) {
-    if constexpr (DT == 0) k_trunc_held<DT, 8, CUT><<<grid, block, 0, stream>>>(P);
-  } else k_trunc_scan<DT, CUT><<<grid, block, 0, stream>>>(P);
+  else if constexpr (DT == 0) k_trunc_held<DT, 8, CUT><<<grid, block, 0, stream>>>(P);
 }
 
 }  // namespace
+
+int trunc_slice_elems(int dtype, int loads) { return kNT * loads * (dtype == SPC_BF16 ? 8 : 4); }
+size_t trunc_plan_bytes() { return sizeof(RowPlan); }
+size_t trunc_item_bytes() { return sizeof(Item); }
 
 // (P.R at most kMaxRows)
 hipError_t launch_truncated(const TruncParams& P, int dtype, hipStream_t stream) {
