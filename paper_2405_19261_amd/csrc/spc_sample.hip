@@ -71,25 +71,39 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 }
 constexpr uint32_t kKeyLowest = 0x00800000u;  // key of the lowest finite float
 
-// 2^(f/16) - 1 for f in [0, 1): the series of e^x - 1 (x < 0.0434; the next
-// term is under 4e-16).
+// 2^(f/16) - 1 for f in [0, 1), the series of e^x - 1 at x = f ln(2)/16 < 0.0434.
+// In bins, which hold it in units of 2^-37 or less: to the sixth power, the rest
+// under 6e-14.  In weights: to the seventh, the rest under 4e-16.
+constexpr double kF1 = kLn2by16, kF2 = kF1 * kLn2by16 / 2, kF3 = kF2 * kLn2by16 / 3,
+                 kF4 = kF3 * kLn2by16 / 4, kF5 = kF4 * kLn2by16 / 5, kF6 = kF5 * kLn2by16 / 6,
+                 kF7 = kF6 * kLn2by16 / 7;
 __device__ __forceinline__ double frac_mass(double f) {
-  const double x = f * kLn2by16;
-  double r = 1.0 / 5040;
-  r = fma(r, x, 1.0 / 720);
-  r = fma(r, x, 1.0 / 120);
-  r = fma(r, x, 1.0 / 24);
-  r = fma(r, x, 1.0 / 6);
-  r = fma(r, x, 0.5);
-  r = fma(r, x, 1.0);
-  return r * x;
+  double r = fma(kF7, f, kF6);
+  r = fma(r, f, kF5);
+  r = fma(r, f, kF4);
+  r = fma(r, f, kF3);
+  r = fma(r, f, kF2);
+  r = fma(r, f, kF1);
+  return r * f;
 }
 // rint(x 2^s) of 0 <= x 2^s < 2^51 as an integer.
+constexpr double kTwo52 = 4503599627370496.0;
 __device__ __forceinline__ uint64_t fixed_point(double x, double scale) {
-  const double m = fma(x, scale, 4503599627370496.0);  // + 2^52
+  const double m = fma(x, scale, kTwo52);
   return (uint64_t)__double_as_longlong(m) & 0xfffffffffffffull;
 }
-
+// The units of 2^-BITS in 2^(f/16) - 1, above the bits of 2^52.
+template <int BITS>
+__device__ __forceinline__ uint64_t frac_units(double f) {
+  constexpr double s = (double)(1ull << BITS);
+  double r = fma(kF6 * s, f, kF5 * s);
+  r = fma(r, f, kF4 * s);
+  r = fma(r, f, kF3 * s);
+  r = fma(r, f, kF2 * s);
+  r = fma(r, f, kF1 * s);
+  return (uint64_t)__double_as_longlong(fma(r, f, kTwo52));
+}
+constexpr uint64_t kTwo52Bits = 0x4330000000000000ull;
 
 __device__ __forceinline__ int wave_id() {
   return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -180,10 +194,13 @@ struct RowOf {
   static __device__ __forceinline__ float of_bits(uint32_t b) {
     return clean(__uint_as_float(DT == 1 ? b << 16 : b));
   }
-  static __device__ __forceinline__ float value(const uint32_t (&w)[4], int e) {
+  static __device__ __forceinline__ float raw(const uint32_t (&w)[4], int e) {
     if constexpr (DT == 1)
-      return clean(__uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16));
-    else return clean(__uint_as_float(w[e]));
+      return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+    else return __uint_as_float(w[e]);
+  }
+  static __device__ __forceinline__ float value(const uint32_t (&w)[4], int e) {
+    return clean(raw(w, e));
   }
 };
 // The lane load at entry e0 < V of a row in memory, -inf behind its end; the
@@ -320,6 +337,7 @@ struct Shared {
   uint32_t wave32[kNW];
   uint32_t n_items;
   Found found[2][kNW];
+  Cut cut;                     // resolve_ranked's answer
   // the draw's
   int32_t sum_at;
   uint64_t before;
@@ -331,8 +349,8 @@ __device__ __forceinline__ int log2_ceil(int32_t V) {
 // Fixed-point scales: sums of V terms of at most 2^(1/16) stay under 2^63,
 // and a term under 2^51.
 __device__ __forceinline__ int sum_bits(int32_t V) { return min(50, 61 - log2_ceil(V)); }
-// The masses of the bins of at most kTruncHeld entries: 16 bits of count above 48 of
-// mass (kTruncHeld terms under 0.0444 2^37).
+// Bin masses are sums of units of 2^-37; of at most kTruncHeld entries they take
+// 48 bits (kTruncHeld terms under 0.0444 2^37) under 16 of count.
 constexpr int kPackBits = 37;
 
 template <bool MAX>
@@ -426,36 +444,28 @@ __device__ __forceinline__ int bin_of(double top, double t) {
   return (int)fmin(top - floor(t), (double)(kBins - 1));
 }
 
-// The fixed point of a row's bin masses, 2^bits and its inverse.
-struct Unit {
-  double scale, inv;
-};
-template <bool PACK>
-__device__ __forceinline__ Unit bin_unit(int32_t V) {
-  const int bits = PACK ? kPackBits : sum_bits(V);
-  return Unit{exp2((double)bits), exp2((double)-bits)};
-}
 // The mass of an entry relative to its bin's lower edge, rounded as the bins
 // hold it: sums over entries and over bins then agree where no rounding need
 // part them (a row of equal logits, say, and its half).
-__device__ __forceinline__ double entry_mass(double f, const Unit& u) {
-  return 1.0 + (double)fixed_point(frac_mass(f), u.scale) * u.inv;
+constexpr double kUnit = 1.0 / (double)(1ull << kPackBits);
+__device__ __forceinline__ double entry_mass(double f) {
+  return 1.0 + (double)(frac_units<kPackBits>(f) - kTwo52Bits) * kUnit;
 }
 
-// Adds an entry to the bins.
+// Adds an entry (as it is stored) to the bins; the last bin's mass is not used.
+// PACK: at most kTruncHeld entries, count and mass in one word.
 template <bool PACK>
-__device__ __forceinline__ void add_to_bins(Shared& S, float z, double c, double top,
-                                            double scale) {
-  if (!(z > -__builtin_huge_valf())) return;
-  const double t = (double)z * c, b = floor(t);
-  const int bin = (int)fmin(top - b, (double)(kBins - 1));
-  // (a bin without mass needs none of it, but every lane takes the same path)
-  const uint64_t m = bin < kBins - 1 ? fixed_point(frac_mass(t - b), scale) : 0;
+__device__ __forceinline__ void add_to_bins(Shared& S, float z, double c, double top) {
+  if (!(z > -__builtin_huge_valf())) return;  // (NaN neither)
+  const double t = (double)fminf(z, -kLowest) * c, b = floor(t);
+  const uint32_t bin = min((uint32_t)(int)(top - b), (uint32_t)(kBins - 1));
+  const uint64_t m = frac_units<kPackBits>(t - b);
   if constexpr (PACK) {
-    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)(m + (1ull << 48)));
+    atomicAdd((unsigned long long*)&S.mass[bin],
+              (unsigned long long)(m + ((1ull << 48) - kTwo52Bits)));
   } else {
     atomicAdd(&S.cnt[bin], 1u);
-    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)m);
+    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)(m - kTwo52Bits));
   }
 }
 
@@ -518,22 +528,24 @@ __device__ __forceinline__ float lowest_at(double edge, double c) {
 struct Range {
   float lo, hi;
 };
-__device__ __forceinline__ Range range_of(int first, int last, double top, double c) {
-  Range r;
-  r.lo = last >= kBins - 1 ? kLowest : lowest_at(top - last, c);
-  r.hi = first <= 0 ? __builtin_huge_valf() : lowest_at(top - first + 1.0, c);
-  return r;
-}
 // The logits of the bins in question: two ranges.
 struct Question {
   Range k, p;
 };
+// (the four edges in four lanes)
 __device__ __forceinline__ Question question_of(const Plan& p, double top, double c) {
-  const Range none{__builtin_huge_valf(), -__builtin_huge_valf()};
-  Question q{none, none};
-  if (p.kbin >= 0) q.k = range_of(p.kbin, p.kbin, top, c);
-  if (p.plo >= 0) q.p = range_of(p.plo, p.phi, top, c);
-  return q;
+  const int lane = threadIdx.x & 63;
+  const bool of_k = lane < 2, low = !(lane & 1);
+  const int first = of_k ? p.kbin : p.plo, last = of_k ? p.kbin : p.phi;
+  float z;
+  if (first < 0) z = low ? __builtin_huge_valf() : -__builtin_huge_valf();
+  else if (low && last >= kBins - 1) z = kLowest;
+  else if (!low && first == 0) z = __builtin_huge_valf();
+  else z = lowest_at(low ? top - last : top - first + 1.0, c);
+  const auto lane_z = [z](int i) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(z), i));
+  };
+  return Question{{lane_z(0), lane_z(1)}, {lane_z(2), lane_z(3)}};
 }
 __device__ __forceinline__ bool asked(const Question& q, float z) {
   return (z >= q.k.lo && z < q.k.hi) || (z >= q.p.lo && z < q.p.hi);
@@ -550,7 +562,7 @@ struct Narrowed {
 };
 template <class Row, class Take>
 __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, double top,
-                                        int first, const Unit& unit, uint32_t lo, uint32_t hi, bool masses, bool by_mass,
+                                        int first, uint32_t lo, uint32_t hi, bool masses, bool by_mass,
                                         uint32_t want_c, double want_m, Take take) {
   Narrowed r{0, 0, 0, 0.0, 0.0};
   int slot = 0;
@@ -571,7 +583,7 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
         const double t = (double)z * c, b = floor(t);
         const int bin = (int)fmin(top - b, (double)(kBins - 1));
         atomicAdd((unsigned long long*)&S.mass[(x - lo) >> shift],
-                  (unsigned long long)fixed_point(entry_mass(t - b, unit) * S.edge[bin - first],
+                  (unsigned long long)fixed_point(entry_mass(t - b) * S.edge[bin - first],
                                                   scale));
       }
     });
@@ -597,10 +609,10 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
 // relative to the edge of `first`) of bins first .. last, and their mass.
 template <class Row>
 __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, double top,
-                                        const Unit& unit, int first, int last, bool by_mass, uint32_t want_c, double want_m,
+                                        int first, int last, bool by_mass, uint32_t want_c, double want_m,
                                         double& mass) {
   // the keys there are in the bins
-  const Range in = range_of(first, last, top, c);
+  const Range in = question_of(Plan{-1, 0, 0.0, first, last, 0.0, 0}, top, c).p;
   uint32_t lo = 0xffffffffu, hi = 0;
   row.each([&](int64_t, float z, uint32_t) {
     if (z >= in.lo && z < in.hi) {
@@ -610,7 +622,7 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
   });
   lo = block_extreme<false>(S, lo);
   hi = block_extreme<true>(S, hi);
-  const Narrowed v = narrow(S, row, c, top, first, unit, ~hi, ~lo, true, by_mass, want_c, want_m,
+  const Narrowed v = narrow(S, row, c, top, first, ~hi, ~lo, true, by_mass, want_c, want_m,
                             [](uint32_t key, int64_t, uint32_t& x) {
                               x = ~key;
                               return true;
@@ -627,7 +639,7 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
   }
   mass = v.above_mass + each * (double)need;
   if (need == v.in_cnt) return Cut{of_key(key), kNoIndex};
-  const Narrowed i = narrow(S, row, c, top, first, unit, 0u, (uint32_t)(row.V - 1), false, false, need, 0.0,
+  const Narrowed i = narrow(S, row, c, top, first, 0u, (uint32_t)(row.V - 1), false, false, need, 0.0,
                             [key](uint32_t k, int64_t e, uint32_t& x) {
                               x = (uint32_t)e;
                               return k == key;
@@ -639,71 +651,113 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
 // entries of the row).
 template <class Row>
 __device__ __forceinline__ Cut resolve(Shared& S, const Row& row, const Ask& a, double top,
-                                       const Unit& unit, const Plan& p) {
+                                       const Plan& p) {
   Cut cut{kLowest, kNoIndex};
   double whole = p.k_above;
   if (p.kbin >= 0) {
     double part;
-    cut = cut_in_bins(S, row, a.c, top, unit, p.kbin, p.kbin, false, p.k_need, 0.0, part);
+    cut = cut_in_bins(S, row, a.c, top, p.kbin, p.kbin, false, p.k_need, 0.0, part);
     if (p.kbin < kBins - 1) whole += part * S.edge[p.kbin];
   }
   if (p.plo >= 0) {
     double part;
     const double want = ((double)a.p * whole - p.p_above) / S.edge[p.plo];
-    cut = tighter(cut, cut_in_bins(S, row, a.c, top, unit, p.plo, p.phi, true, 0u, want, part));
+    cut = tighter(cut, cut_in_bins(S, row, a.c, top, p.plo, p.phi, true, 0u, want, part));
   }
   return cut;
 }
 
 // The same for at most kRanked entries in LDS: each entry's place in the order
-// is counted against all others, and the sums run over the places.
+// is counted against all others, by the whole workgroup; the sums over the
+// places are the first wavefront's, four places a lane.
 template <int DT>
-__device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double top,
-                                              const Unit& unit, const Plan& p, int n) {
+__device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double top, const Plan& p,
+                                              int n) {
   using Row = RowOf<DT>;
-  const int j = (int)threadIdx.x;
-  uint32_t* order = S.cnt;  // place -> entry (no bin is in use)
+  static_assert(kRanked == 256 && kNT == 4 * kRanked, "four threads an entry, four entries a lane");
+  uint32_t* place = S.cnt;            // (no bin is in use)
+  uint32_t* order = S.cnt + kRanked;
+  const int j = (int)threadIdx.x & (kRanked - 1);
+  if (threadIdx.x < kRanked) place[j] = 0;
+  __syncthreads();
   if (j < n) {
     const Item x = S.items[j];
-    const uint32_t key = key_of(Row::of_bits(x.bits));
-    uint32_t place = 0;
-    for (int i = 0; i < n; ++i) {
+    const float z = Row::of_bits(x.bits);
+    uint32_t c = 0;
+    for (int i = (int)threadIdx.x / kRanked; i < n; i += kNT / kRanked) {
       const Item y = S.items[i];
-      const uint32_t k = key_of(Row::of_bits(y.bits));
-      place += k > key || (k == key && y.idx < x.idx);
+      const float zy = Row::of_bits(y.bits);
+      c += zy > z || (zy == z && y.idx < x.idx);
     }
-    order[place] = (uint32_t)j;
+    if (c) atomicAdd(&place[j], c);
   }
   __syncthreads();
-  float z = 0.0f;
-  int bin = -2;
-  double mass = 0.0;
-  if (j < n) {
-    z = Row::of_bits(S.items[order[j]].bits);
-    const double t = (double)z * a.c;
-    bin = bin_of(top, t);
-    mass = entry_mass(t - floor(t), unit);
-  }
-  const auto at = [&](int place) {
-    const Item x = S.items[order[place]];
-    return Cut{Row::of_bits(x.bits), x.idx};
-  };
-  Cut cut{kLowest, kNoIndex};
-  double whole = p.k_above;
-  if (p.kbin >= 0) {
-    const bool in = bin == p.kbin;
-    const Reached r = reach(S, 0, sums_of(S, in ? 1u : 0u, in ? mass : 0.0), false, p.k_need, 0.0);
-    cut = at(r.at);
-    if (p.kbin < kBins - 1) whole += (r.above_mass + r.in_mass) * S.edge[p.kbin];
-  }
-  if (p.plo >= 0) {
-    const bool in = bin >= p.plo && bin <= p.phi;
-    const Reached r = reach(S, 1, sums_of(S, in ? 1u : 0u, in ? mass * S.edge[bin - p.plo] : 0.0),
-                            true, 0u, ((double)a.p * whole - p.p_above) / S.edge[p.plo]);
-    cut = tighter(cut, at(r.at));
+  if ((int)threadIdx.x < n) order[place[j]] = (uint32_t)j;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int lane = (int)threadIdx.x;
+    int bin[4];
+    double mass[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bin[e] = -2;
+      mass[e] = 0.0;
+      if (4 * lane + e < n) {
+        const double t = (double)Row::of_bits(S.items[order[4 * lane + e]].bits) * a.c;
+        bin[e] = bin_of(top, t);
+        mass[e] = entry_mass(t - floor(t));
+      }
+    }
+    // the place in bins first .. last that reaches what is wanted (else their last)
+    const auto reach_place = [&](int first, int last, bool by_mass, double want) {
+      double sum = 0.0, own[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = bin[e] >= first && bin[e] <= last;
+        own[e] = !in ? 0.0 : by_mass ? mass[e] * S.edge[bin[e] - first] : 1.0;
+        sum += own[e];
+      }
+      const double in = wave_incl_scan(sum);
+      double before = dpp<0x138, 0xf>(in);  // wave_shr: the lane before
+      if (lane == 0) before = 0.0;
+      const uint64_t yes = __ballot(sum > 0.0 && in >= want), some = __ballot(sum > 0.0);
+      const int at = yes ? __builtin_ctzll(yes) : 63 - __builtin_clzll(some | 1);
+      int e_at = -1;
+      double s = before;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (own[e] > 0.0 && (e_at < 0 || s < want)) {
+          e_at = e;
+          s += own[e];
+        }
+      }
+      return 4 * at + __builtin_amdgcn_readlane(e_at, at);
+    };
+    Cut cut{kLowest, kNoIndex};
+    double whole = p.k_above;
+    const auto cut_at = [&](int at) {
+      const Item x = S.items[order[max(at, 0)]];
+      return Cut{Row::of_bits(x.bits), x.idx};
+    };
+    if (p.kbin >= 0) {
+      const int at = reach_place(p.kbin, p.kbin, false, (double)p.k_need);
+      cut = cut_at(at);
+      if (p.kbin < kBins - 1) {  // the mass of the bin's entries up to there
+        double m = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (bin[e] == p.kbin && 4 * lane + e <= at) m += mass[e];
+        m = lane_value(wave_incl_scan(m), 63);
+        whole += m * S.edge[p.kbin];
+      }
+    }
+    if (p.plo >= 0)
+      cut = tighter(cut, cut_at(reach_place(p.plo, p.phi, true,
+                                            ((double)a.p * whole - p.p_above) / S.edge[p.plo])));
+    if (lane == 0) S.cut = cut;
   }
   __syncthreads();
-  return cut;
+  return S.cut;
 }
 
 // min-p's cut: the lowest float not below max z + T ln(min_p).
@@ -732,22 +786,21 @@ __device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const ScanRow<D
                                       const Ask& a, float zmax, double top) {
   const Cut floor_cut = min_p_cut(a, zmax);
   if (!(a.k > 0 && a.k < row.V) && a.p >= 1.0f) return floor_cut;
-  const Unit unit = bin_unit<PACK>(row.V);
   S.cnt[threadIdx.x] = 0;
   S.mass[threadIdx.x] = 0;
   if (threadIdx.x == 0) S.n_items = 0;
   __syncthreads();
-  row.each([&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top, unit.scale); });
+  row.each([&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top); });
   __syncthreads();
   uint64_t m = S.mass[threadIdx.x];
   const uint32_t n = PACK ? (uint32_t)(m >> 48) : S.cnt[threadIdx.x];
   if (PACK) m &= (1ull << 48) - 1;
   const double mass = threadIdx.x == kBins - 1
                           ? 0.0
-                          : ((double)n + (double)m * unit.inv) * S.edge[threadIdx.x];
+                          : ((double)n + (double)m * kUnit) * S.edge[threadIdx.x];
   const Plan p = make_plan(S, a, row.V, n, mass, cut_bin(a, floor_cut, top));
   if (p.kbin < 0 && p.plo < 0) return floor_cut;
-  if (p.items > (uint32_t)kItems) return tighter(floor_cut, resolve(S, whole, a, top, unit, p));
+  if (p.items > (uint32_t)kItems) return tighter(floor_cut, resolve(S, whole, a, top, p));
   const Question q = question_of(p, top, a.c);
   row.each([&](int64_t e, float z, uint32_t bits) {
     if (asked(q, z)) {
@@ -757,9 +810,9 @@ __device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const ScanRow<D
   });
   __syncthreads();
   if (p.items <= (uint32_t)kRanked)
-    return tighter(floor_cut, resolve_ranked<DT>(S, a, top, unit, p, (int)p.items));
+    return tighter(floor_cut, resolve_ranked<DT>(S, a, top, p, (int)p.items));
   return tighter(floor_cut,
-                 resolve(S, ItemRow<DT>(S.items, row.V, (int)p.items), a, top, unit, p));
+                 resolve(S, ItemRow<DT>(S.items, row.V, (int)p.items), a, top, p));
 }
 
 // ------------------------------------------------------------------ the draw
@@ -1066,12 +1119,11 @@ __global__ void __launch_bounds__(kNT) k_slice_bins(TruncParams P) {
   const Ask a = ask_of(P, r / P.rows_per_seq);
   if (!a.valid || a.greedy || kmax < kKeyLowest || (!(a.k > 0 && a.k < P.V) && a.p >= 1.0f)) return;
   const double top = floor((double)zmax * a.c);
-  const Unit unit = bin_unit<true>(P.V);
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
     for (int e = 0; e < VW; ++e)
-      add_to_bins<true>(S, RowOf<DT>::value(w[i], e), a.c, top, unit.scale);
+      add_to_bins<true>(S, RowOf<DT>::raw(w[i], e), a.c, top);
   __syncthreads();
   P.slice_bins[(r * P.slices + s) * kBins + threadIdx.x] = S.mass[threadIdx.x];
 }
@@ -1093,7 +1145,6 @@ __global__ void __launch_bounds__(kNT) k_slice_plan(TruncParams P) {
   float zmax = -__builtin_huge_valf();
   for (int s = (int)threadIdx.x; s < P.slices; s += kNT) zmax = fmaxf(zmax, maxima[s]);
   fill_edges(S);
-  if (threadIdx.x == 0) S.n_items = 0;
   const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
   zmax = of_key(kmax);
   const Ask a = ask_of(P, r / P.rows_per_seq);
@@ -1109,26 +1160,35 @@ __global__ void __launch_bounds__(kNT) k_slice_plan(TruncParams P) {
     if ((a.k > 0 && a.k < P.V) || a.p < 1.0f) {
       const uint64_t* bins = P.slice_bins + r * P.slices * kBins;
       const int i = (int)threadIdx.x;
-      uint32_t n = 0;
+      uint32_t n = 0, rest = 0;
       uint64_t m = 0;
-#pragma unroll 4
-      for (int s = 0; s < P.slices; ++s) {
-        const float zs = maxima[s];
-        if (zs < kLowest) continue;
-        const int shift = (int)fmin(R.top - floor((double)zs * a.c), (double)(kBins - 1));
-        const uint64_t* b = bins + (int64_t)s * kBins;
-        if (i < kBins - 1 && i >= shift) {
-          const uint64_t x = b[i - shift];
-          n += (uint32_t)(x >> 48);
-          m += x & ((1ull << 48) - 1);
+      // kNT slices' shifts at a time (in S.cnt), then their bins
+      for (int s0 = 0; s0 < P.slices; s0 += kNT) {
+        const int ns = min(P.slices - s0, kNT);
+        __syncthreads();
+        if (i < ns) {
+          const float zs = maxima[s0 + i];  // (a slice of nothing: nowhere)
+          S.cnt[i] = zs < kLowest ? (uint32_t)kBins
+                                  : min((uint32_t)(int)(R.top - floor((double)zs * a.c)),
+                                        (uint32_t)(kBins - 1));
         }
-        // the row's last bin takes all that the shift moves there
-        if (i + shift >= kBins - 1) atomicAdd(&S.n_items, (uint32_t)(b[i] >> 48));
+        __syncthreads();
+#pragma unroll 8
+        for (int s = 0; s < ns; ++s) {
+          const int shift = (int)S.cnt[s];
+          const uint64_t* b = bins + (int64_t)(s0 + s) * kBins;
+          const uint64_t x = b[max(i - shift, 0)], y = b[i];
+          if (i >= shift && i < kBins - 1) {
+            n += (uint32_t)(x >> 48);
+            m += x & ((1ull << 48) - 1);
+          }
+          // the row's last bin takes all that the shift moves there
+          if (shift < kBins && i + shift >= kBins - 1) rest += (uint32_t)(y >> 48);
+        }
       }
-      __syncthreads();
-      if (i == kBins - 1) n = S.n_items;
-      const Unit unit = bin_unit<true>(P.V);
-      const double mass = i == kBins - 1 ? 0.0 : ((double)n + (double)m * unit.inv) * S.edge[i];
+      rest = block_sum(S, rest);
+      if (i == kBins - 1) n = rest;
+      const double mass = i == kBins - 1 ? 0.0 : ((double)n + (double)m * kUnit) * S.edge[i];
       R.plan = make_plan(S, a, P.V, n, mass, cut_bin(a, floor_cut, R.top));
       R.q = question_of(R.plan, R.top, a.c);
       if (R.plan.items > (uint32_t)P.items_max) R.mode = kRowScan;
@@ -1225,16 +1285,15 @@ __global__ void __launch_bounds__(kNT) k_slice_end(TruncParams P, int sub) {
   const int n_items = ask ? (int)R.plan.items : 0;
   Cut cut{R.floor_z, kNoIndex};
   if (ask) {
-    const Unit unit = bin_unit<true>(P.V);
     if (n_items <= kItems) {
       if ((int)threadIdx.x < n_items) S.items[threadIdx.x] = list[threadIdx.x];
       __syncthreads();
       cut = tighter(cut, n_items <= kRanked
-                             ? resolve_ranked<DT>(S, a, R.top, unit, R.plan, n_items)
-                             : resolve(S, ItemRow<DT>(S.items, P.V, n_items), a, R.top, unit, R.plan));
+                             ? resolve_ranked<DT>(S, a, R.top, R.plan, n_items)
+                             : resolve(S, ItemRow<DT>(S.items, P.V, n_items), a, R.top, R.plan));
     } else {
       __syncthreads();
-      cut = tighter(cut, resolve(S, ItemRow<DT>(list, P.V, n_items), a, R.top, unit, R.plan));
+      cut = tighter(cut, resolve(S, ItemRow<DT>(list, P.V, n_items), a, R.top, R.plan));
     }
   }
   if constexpr (CUT) {
