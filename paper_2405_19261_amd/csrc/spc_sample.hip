@@ -167,14 +167,17 @@ __device__ __forceinline__ Ask ask_of(const TruncParams& P, int64_t seq) {
   return a;
 }
 
-// The kept entries of a row: logit above z, or equal with index <= idx.
+// The kept entries of a row: logit above z, or equal with index <= idx.  Logits
+// are compared as they are stored: a NaN is never kept, and +inf is not above
+// a cut at the largest finite value.
 constexpr float kLowest = -3.40282347e38f;  // the lowest finite float
 struct Cut {
   float z;
   int32_t idx;
 };
 __device__ __forceinline__ bool kept(const Cut& c, float z, int64_t idx) {
-  return z > c.z || (z == c.z && idx <= c.idx);
+  const float above = c.z == -kLowest ? __builtin_huge_valf() : c.z;  // uniform
+  return z > above || (z >= c.z && idx <= c.idx);
 }
 // The more restrictive of two cuts.
 __device__ __forceinline__ Cut tighter(const Cut& a, const Cut& b) {
@@ -249,7 +252,7 @@ struct ScanRow : RowOf<DT> {
     return RowOf<DT>::of_bits(DT == 1 ? reinterpret_cast<const uint16_t*>(row)[e]
                                       : reinterpret_cast<const uint32_t*>(row)[e]);
   }
-  // f(entry, logit, the entry's bits) over the thread's entries
+  // f(entry, logit as stored, its bits) over the thread's entries
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
     for (int i = 0; i < loads(); ++i) {
@@ -259,7 +262,7 @@ struct ScanRow : RowOf<DT> {
       const int n = load(e0, w);
 #pragma unroll
       for (int e = 0; e < VW; ++e)
-        if (e < n) f(e0 + e, RowOf<DT>::value(w, e), RowOf<DT>::bits(w, e));
+        if (e < n) f(e0 + e, RowOf<DT>::raw(w, e), RowOf<DT>::bits(w, e));
     }
   }
 };
@@ -293,7 +296,7 @@ struct HeldRow : RowOf<DT> {
       uint32_t w[4];
       load(e0, w);
 #pragma unroll
-      for (int e = 0; e < VW; ++e) f(e0 + e, RowOf<DT>::value(w, e), RowOf<DT>::bits(w, e));
+      for (int e = 0; e < VW; ++e) f(e0 + e, RowOf<DT>::raw(w, e), RowOf<DT>::bits(w, e));
     }
   }
 };
@@ -353,14 +356,18 @@ __device__ __forceinline__ int sum_bits(int32_t V) { return min(50, 61 - log2_ce
 // 48 bits (kTruncHeld terms under 0.0444 2^37) under 16 of count.
 constexpr int kPackBits = 37;
 
-template <bool MAX>
-__device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
-  x = wave_max(MAX ? x : ~x);
-  if ((threadIdx.x & 63) == 63) S.wave32[threadIdx.x >> 6] = x;
+__device__ __forceinline__ uint32_t block_max(uint32_t* wave32, uint32_t x) {
+  x = wave_max(x);
+  if ((threadIdx.x & 63) == 63) wave32[threadIdx.x >> 6] = x;
   __syncthreads();
-  x = wave_max(S.wave32[threadIdx.x & 15]);
+  x = wave_max(wave32[threadIdx.x & 15]);
   x = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
   __syncthreads();
+  return x;
+}
+template <bool MAX>
+__device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
+  x = block_max(S.wave32, MAX ? x : ~x);
   return MAX ? x : ~x;
 }
 
@@ -452,20 +459,56 @@ __device__ __forceinline__ double entry_mass(double f) {
   return 1.0 + (double)(frac_units<kPackBits>(f) - kTwo52Bits) * kUnit;
 }
 
-// Adds an entry (as it is stored) to the bins; the last bin's mass is not used.
-// PACK: at most kTruncHeld entries, count and mass in one word.
-template <bool PACK>
-__device__ __forceinline__ void add_to_bins(Shared& S, float z, double c, double top) {
-  if (!(z > -__builtin_huge_valf())) return;  // (NaN neither)
+// The bin of an entry (as it is stored), which is neither -inf nor NaN, and the
+// units of its mass above 2^52's bits.  (The last bin's mass is not used.)
+__device__ __forceinline__ uint32_t bin_and_units(float z, double c, double top, uint64_t& m) {
   const double t = (double)fminf(z, -kLowest) * c, b = floor(t);
-  const uint32_t bin = min((uint32_t)(int)(top - b), (uint32_t)(kBins - 1));
-  const uint64_t m = frac_units<kPackBits>(t - b);
-  if constexpr (PACK) {
-    atomicAdd((unsigned long long*)&S.mass[bin],
-              (unsigned long long)(m + ((1ull << 48) - kTwo52Bits)));
+  m = frac_units<kPackBits>(t - b);
+  return min((uint32_t)(int)(top - b), (uint32_t)(kBins - 1));
+}
+constexpr uint64_t kOnePacked = (1ull << 48) - kTwo52Bits;
+
+// Entries of a bfloat16 row take few values: those of magnitudes 2^-6 to 2^6 are
+// counted by value, and each value met enters its bin once, as often as it was
+// met.  A count is a few integer operations and one 32-bit add in LDS, where
+// the mass of an entry is about 20 operations in 64 bits (65.5M entries: k_slice_bins
+// 80 us entry by entry).  Others go to their bins one by one.
+constexpr uint32_t kMagFirst = 0x3c80, kMags = 12 * 128, kValues = 2 * kMags;
+// Adds an entry to the bins of at most kTruncHeld entries.
+__device__ __forceinline__ void add_packed(uint64_t* mass, float z, double c, double top) {
+  if (!(z > -__builtin_huge_valf())) return;
+  uint64_t m;
+  const uint32_t bin = bin_and_units(z, c, top, m);
+  atomicAdd((unsigned long long*)&mass[bin], (unsigned long long)(m + kOnePacked));
+}
+// To the bins of any number: counts apart.
+__device__ __forceinline__ void add_unpacked(Shared& S, float z, double c, double top) {
+  if (!(z > -__builtin_huge_valf())) return;
+  uint64_t m;
+  const uint32_t bin = bin_and_units(z, c, top, m);
+  atomicAdd(&S.cnt[bin], 1u);
+  atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)(m - kTwo52Bits));
+}
+
+__device__ __forceinline__ void add_value(uint64_t* mass, uint32_t* values, uint32_t h, double c,
+                                          double top) {
+  const uint32_t m = (h & 0x7fffu) - kMagFirst;
+  if (m < kMags) {
+    atomicAdd(&values[m + (h >> 15) * kMags], 1u);
   } else {
-    atomicAdd(&S.cnt[bin], 1u);
-    atomicAdd((unsigned long long*)&S.mass[bin], (unsigned long long)(m - kTwo52Bits));
+    add_packed(mass, __uint_as_float(h << 16), c, top);
+  }
+}
+// The counted values into their bins (between barriers).
+__device__ __forceinline__ void add_values(uint64_t* mass, const uint32_t* values, double c,
+                                           double top) {
+  for (uint32_t i = threadIdx.x; i < kValues; i += kNT) {
+    const uint64_t n = values[i];
+    if (!n) continue;
+    const uint32_t h = i < kMags ? i + kMagFirst : (i - kMags + kMagFirst) | 0x8000u;
+    uint64_t m;
+    const uint32_t bin = bin_and_units(__uint_as_float(h << 16), c, top, m);
+    atomicAdd((unsigned long long*)&mass[bin], (unsigned long long)((m + kOnePacked) * n));
   }
 }
 
@@ -524,7 +567,8 @@ __device__ __forceinline__ float lowest_at(double edge, double c) {
   while (k < ~kKeyLowest && floor((double)of_key(k) * c) < edge) ++k;
   return of_key(k);
 }
-// The logits of bins first .. last: lo <= z < hi.
+// The logits of bins first .. last: lo <= z, not z >= hi (NaN: no bound; +inf too
+// is under it).
 struct Range {
   float lo, hi;
 };
@@ -538,9 +582,9 @@ __device__ __forceinline__ Question question_of(const Plan& p, double top, doubl
   const bool of_k = lane < 2, low = !(lane & 1);
   const int first = of_k ? p.kbin : p.plo, last = of_k ? p.kbin : p.phi;
   float z;
-  if (first < 0) z = low ? __builtin_huge_valf() : -__builtin_huge_valf();
+  if (first < 0) z = low ? __builtin_nanf("") : 0.0f;  // (no logit is >= NaN)
   else if (low && last >= kBins - 1) z = kLowest;
-  else if (!low && first == 0) z = __builtin_huge_valf();
+  else if (!low && first == 0) z = __builtin_nanf("");
   else z = lowest_at(low ? top - last : top - first + 1.0, c);
   const auto lane_z = [z](int i) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(z), i));
@@ -548,7 +592,7 @@ __device__ __forceinline__ Question question_of(const Plan& p, double top, doubl
   return Question{{lane_z(0), lane_z(1)}, {lane_z(2), lane_z(3)}};
 }
 __device__ __forceinline__ bool asked(const Question& q, float z) {
-  return (z >= q.k.lo && z < q.k.hi) || (z >= q.p.lo && z < q.p.hi);
+  return (z >= q.k.lo && !(z >= q.k.hi)) || (z >= q.p.lo && !(z >= q.p.hi));
 }
 
 // Where a sum over entries in ascending x reaches what is wanted: the value of
@@ -574,7 +618,8 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
     S.cnt[threadIdx.x] = 0;
     S.mass[threadIdx.x] = 0;
     __syncthreads();
-    row.each([&](int64_t e, float z, uint32_t) {
+    row.each([&](int64_t e, float raw, uint32_t) {
+      const float z = clean(raw);
       const uint32_t key = key_of(z);
       uint32_t x;
       if (!take(key, e, x) || x < lo || x > hi) return;
@@ -615,9 +660,10 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
   const Range in = question_of(Plan{-1, 0, 0.0, first, last, 0.0, 0}, top, c).p;
   uint32_t lo = 0xffffffffu, hi = 0;
   row.each([&](int64_t, float z, uint32_t) {
-    if (z >= in.lo && z < in.hi) {
-      lo = min(lo, key_of(z));
-      hi = max(hi, key_of(z));
+    if (z >= in.lo && !(z >= in.hi)) {
+      const uint32_t key = key_of(clean(z));
+      lo = min(lo, key);
+      hi = max(hi, key);
     }
   });
   lo = block_extreme<false>(S, lo);
@@ -782,15 +828,26 @@ __device__ __forceinline__ void fill_edges(Shared& S) {
 // The cut of a row in one workgroup; zmax its largest logit (finite), `whole` the
 // row in memory.  PACK: at most kTruncHeld entries.
 template <bool PACK, int DT, class Row>
-__device__ __forceinline__ Cut cut_of(Shared& S, const Row& row, const ScanRow<DT>& whole,
-                                      const Ask& a, float zmax, double top) {
+__device__ __forceinline__ Cut cut_of(Shared& S, uint32_t* values, const Row& row,
+                                      const ScanRow<DT>& whole, const Ask& a, float zmax,
+                                      double top) {
   const Cut floor_cut = min_p_cut(a, zmax);
   if (!(a.k > 0 && a.k < row.V) && a.p >= 1.0f) return floor_cut;
   S.cnt[threadIdx.x] = 0;
   S.mass[threadIdx.x] = 0;
   if (threadIdx.x == 0) S.n_items = 0;
+  if constexpr (PACK && DT == 1)
+    for (uint32_t i = threadIdx.x; i < kValues; i += kNT) values[i] = 0;
   __syncthreads();
-  row.each([&](int64_t, float z, uint32_t) { add_to_bins<PACK>(S, z, a.c, top); });
+  if constexpr (PACK && DT == 1) {
+    row.each([&](int64_t, float, uint32_t h) { add_value(S.mass, values, h, a.c, top); });
+    __syncthreads();
+    add_values(S.mass, values, a.c, top);
+  } else if constexpr (PACK) {
+    row.each([&](int64_t, float z, uint32_t) { add_packed(S.mass, z, a.c, top); });
+  } else {
+    row.each([&](int64_t, float z, uint32_t) { add_unpacked(S, z, a.c, top); });
+  }
   __syncthreads();
   uint64_t m = S.mass[threadIdx.x];
   const uint32_t n = PACK ? (uint32_t)(m >> 48) : S.cnt[threadIdx.x];
@@ -925,7 +982,7 @@ __device__ __forceinline__ uint64_t held_weight(const Shared& S, const HeldRow<D
       row.load(e0, w);
 #pragma unroll
       for (int e = 0; e < VW; ++e)
-        bits |= (kept(cut, RowOf<DT>::value(w, e), first + e0 + e) ? 1u : 0u) << e;
+        bits |= (kept(cut, RowOf<DT>::raw(w, e), first + e0 + e) ? 1u : 0u) << e;
       mask |= bits << at;
     }
   n = __popc(mask);
@@ -991,7 +1048,7 @@ __device__ __forceinline__ void write_lane(const Row& row, char* out, int64_t e0
   uint32_t o[4];
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
-    const bool k = !none && (whole || kept(cut, Row::value(w, e), e0 + e));
+    const bool k = !none && (whole || kept(cut, Row::raw(w, e), e0 + e));
     if constexpr (DT == 1) {
       const uint32_t b = k ? Row::bits(w, e) : 0xff80u;
       o[e >> 1] = (e & 1) ? o[e >> 1] | (b << 16) : b;
@@ -1028,17 +1085,17 @@ __device__ __forceinline__ void write_cut(const Row& row, char* out, const Cut& 
 
 // One row by one workgroup.
 template <bool PACK, int DT, bool CUT, class Row>
-__device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t r, const Row& row,
-                                        const ScanRow<DT>& mem, float zmax) {
+__device__ __forceinline__ void one_row(Shared& S, uint32_t* values, const TruncParams& P, int64_t r,
+                                        const Row& row, const ScanRow<DT>& mem, float zmax) {
   const Ask a = ask_of(P, r / P.rows_per_seq);
   fill_edges(S);
-  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
+  const uint32_t kmax = block_extreme<true>(S, key_of(clean(zmax)));
   zmax = of_key(kmax);
   const bool none = !a.valid || kmax < kKeyLowest;
   const double top = floor((double)zmax * a.c);
   if constexpr (CUT) {
     Cut cut{kLowest, kNoIndex};
-    if (!none && !a.greedy) cut = cut_of<PACK, DT>(S, row, mem, a, zmax, top);
+    if (!none && !a.greedy) cut = cut_of<PACK, DT>(S, values, row, mem, a, zmax, top);
     __syncthreads();
     write_cut<DT>(row, static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB, cut,
                   a.valid && a.greedy, none);
@@ -1047,11 +1104,11 @@ __device__ __forceinline__ void one_row(Shared& S, const TruncParams& P, int64_t
   } else if (a.greedy) {
     uint32_t first = 0xffffffffu;
     row.each([&](int64_t e, float z, uint32_t) {
-      if (key_of(z) == kmax) first = min(first, (uint32_t)e);
+      if (z >= zmax) first = min(first, (uint32_t)e);
     });
     greedy_token(P, r, block_extreme<false>(S, first));
   } else {
-    const Cut cut = cut_of<PACK, DT>(S, row, mem, a, zmax, top);
+    const Cut cut = cut_of<PACK, DT>(S, values, row, mem, a, zmax, top);
     draw(S, P, r, row, cut, a, top);
   }
 }
@@ -1062,6 +1119,7 @@ __global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
   constexpr int VW = Elem<DT>::VW;
   __shared__ Shared S;
   __shared__ w4 held[U * kNT];
+  __shared__ uint32_t values[DT == 1 ? kValues : 1];
   const int64_t r = blockIdx.x;
   const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
   constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
@@ -1077,10 +1135,10 @@ __global__ void __launch_bounds__(kNT) k_trunc_held(TruncParams P) {
 #pragma unroll
   for (int i = 0; i < U; ++i) {
 #pragma unroll
-    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::value(w[i], e));
+    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::raw(w[i], e));
     held[i * kNT + threadIdx.x] = w4{w[i][0], w[i][1], w[i][2], w[i][3]};
   }
-  one_row<true, DT, CUT>(S, P, r, HeldRow<DT, U>(held, P.V), ScanRow<DT>(src, P.V), zmax);
+  one_row<true, DT, CUT>(S, values, P, r, HeldRow<DT, U>(held, P.V), ScanRow<DT>(src, P.V), zmax);
 }
 
 // ------------------------------------------------------------------ long rows
@@ -1094,7 +1152,8 @@ template <int DT, int U>
 __global__ void __launch_bounds__(kNT) k_slice_bins(TruncParams P) {
   constexpr int VW = Elem<DT>::VW;
   constexpr int64_t N = (int64_t)kNT * U * VW;
-  __shared__ Shared S;
+  __shared__ uint64_t bins[kBins];
+  __shared__ uint32_t values[DT == 1 ? kValues : 1], wave32[kNW];
   const int s = blockIdx.x;
   const int64_t r = blockIdx.y;
   const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
@@ -1107,13 +1166,15 @@ __global__ void __launch_bounds__(kNT) k_slice_bins(TruncParams P) {
     for (int j = 0; j < 4; ++j) w[i][j] = kPad;
     if (e0 < P.V) load_lane<DT>(src, e0, P.V, w[i]);
   }
-  S.mass[threadIdx.x] = 0;
+  bins[threadIdx.x] = 0;
+  if constexpr (DT == 1)
+    for (uint32_t i = threadIdx.x; i < kValues; i += kNT) values[i] = 0;
   float zmax = -__builtin_huge_valf();
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::value(w[i], e));
-  const uint32_t kmax = block_extreme<true>(S, key_of(zmax));
+    for (int e = 0; e < VW; ++e) zmax = fmaxf(zmax, RowOf<DT>::raw(w[i], e));
+  const uint32_t kmax = block_max(wave32, key_of(clean(zmax)));
   zmax = of_key(kmax);
   if (threadIdx.x == 0) P.slice_max[r * P.slices + s] = zmax;
   const Ask a = ask_of(P, r / P.rows_per_seq);
@@ -1122,10 +1183,16 @@ __global__ void __launch_bounds__(kNT) k_slice_bins(TruncParams P) {
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int e = 0; e < VW; ++e)
-      add_to_bins<true>(S, RowOf<DT>::raw(w[i], e), a.c, top);
+    for (int e = 0; e < VW; ++e) {
+      if constexpr (DT == 1) add_value(bins, values, RowOf<DT>::bits(w[i], e), a.c, top);
+      else add_packed(bins, RowOf<DT>::raw(w[i], e), a.c, top);
+    }
   __syncthreads();
-  P.slice_bins[(r * P.slices + s) * kBins + threadIdx.x] = S.mass[threadIdx.x];
+  if constexpr (DT == 1) {
+    add_values(bins, values, a.c, top);
+    __syncthreads();
+  }
+  P.slice_bins[(r * P.slices + s) * kBins + threadIdx.x] = bins[threadIdx.x];
 }
 
 enum RowMode : int32_t { kRowNone, kRowGreedy, kRowCut, kRowScan };
@@ -1192,8 +1259,10 @@ __global__ void __launch_bounds__(kNT) k_slice_plan(TruncParams P) {
       R.plan = make_plan(S, a, P.V, n, mass, cut_bin(a, floor_cut, R.top));
       R.q = question_of(R.plan, R.top, a.c);
       if (R.plan.items > (uint32_t)P.items_max) R.mode = kRowScan;
-      if (R.plan.plo >= 0) R.sure_z = fmaxf(R.floor_z, R.q.p.hi);
-      else if (R.plan.kbin >= 0) R.sure_z = fmaxf(R.floor_z, R.q.k.hi);
+      if (R.plan.plo >= 0 || R.plan.kbin >= 0) {
+        const float hi = R.plan.plo >= 0 ? R.q.p.hi : R.q.k.hi;
+        R.sure_z = hi == hi ? fmaxf(R.floor_z, hi) : __builtin_huge_valf();  // (inf: none)
+      }
     }
   }
   if (threadIdx.x == 0) reinterpret_cast<RowPlan*>(P.row_plan)[r] = R;
@@ -1214,7 +1283,8 @@ __global__ void __launch_bounds__(kNT) k_slice_keep(TruncParams P) {
   constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
   const Ask a = ask_of(P, r / P.rows_per_seq);
   fill_edges(S);
-  const Cut sure{plan->sure_z, kNoIndex};
+  const float sure_z = plan->sure_z;
+  const Cut sure{sure_z, sure_z <= -kLowest ? kNoIndex : -1};
   const Question q = plan->q;
   const bool ask = plan->plan.kbin >= 0 || plan->plan.plo >= 0;
   char* out = CUT ? static_cast<char*>(P.out) + r * P.out_ld * Elem<DT>::EB : nullptr;
@@ -1245,7 +1315,7 @@ __global__ void __launch_bounds__(kNT) k_slice_keep(TruncParams P) {
   if constexpr (!CUT) {
     if (mode == kRowGreedy) {
       mine.each([&](int64_t e, float z, uint32_t) {
-        if (z == plan->zmax) atomicMin(&plan->first, (uint32_t)(s * N + e));
+        if (z >= plan->zmax) atomicMin(&plan->first, (uint32_t)(s * N + e));
       });
       return;
     }
@@ -1266,7 +1336,7 @@ __global__ void __launch_bounds__(kNT) k_slice_end(TruncParams P, int sub) {
   const RowPlan R = reinterpret_cast<const RowPlan*>(P.row_plan)[r];
   const ScanRow<DT> row(static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB, P.V);
   if (R.mode == kRowScan) {
-    one_row<false, DT, CUT>(S, P, r, row, row, R.zmax);
+    one_row<false, DT, CUT>(S, nullptr, P, r, row, row, R.zmax);
     return;
   }
   if (R.mode == kRowNone) {
