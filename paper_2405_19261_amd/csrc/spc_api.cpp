@@ -852,6 +852,26 @@ spc_status kv_read_impl(const spc_kv_cache* cache, void* out_k, void* out_v, int
   return SPC_OK;
 }
 
+// How an attention is cut: rows a workgroup takes, the most shares of the keys,
+// and the workspace the shares need.
+struct AttendLayout {
+  int32_t tile_rows, splits;
+  size_t bytes;
+};
+AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t D,
+                           int64_t tokens) {
+  AttendLayout L;
+  const int64_t rows = n * (heads / H);
+  L.tile_rows = rows <= 16 ? 16 : rows <= 32 || D > 128 ? 32 : 64;
+  const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
+  // shares of at least 512 keys, up to four workgroups to a compute unit
+  const int64_t most = std::max<int64_t>(1, tokens / 512);
+  L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
+                                                     (int64_t)64, 65535 / B}));
+  L.bytes = L.splits > 1 ? (size_t)(groups * L.splits * L.tile_rows) * (size_t)(D + 2) * 4 : 0;
+  return L;
+}
+
 spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtype,
                           int64_t q_stride, int32_t heads, int64_t rows,
                           const int32_t* row_start, int32_t max_rows, float scale, int32_t window,
@@ -879,6 +899,16 @@ spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtyp
   P.window = window;
   P.out = out;
   P.out_stride = out_stride;
+  const AttendLayout L =
+      attend_layout(P.B, P.H, heads, P.n, P.D, (int64_t)P.width * P.S);
+  P.tile_rows = L.tile_rows;
+  P.splits = L.splits;
+  if (L.bytes) {
+    char* ws = nullptr;
+    st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
+    if (st != SPC_OK) return st;
+    P.part = reinterpret_cast<float*>(ws);
+  }
   const hipError_t e = spc::launch_kv_attend(P, stream);
   if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
   return SPC_OK;
@@ -931,7 +961,13 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
 
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
                               int32_t max_rows) {
-  return 0;
+  if (!cache || cache->B < 1 || cache->kv_heads < 1 || heads < 1 || rows < 1 ||
+      heads % cache->kv_heads != 0 || cache->table_width < 1 || cache->page_size < 1)
+    return 0;
+  const int64_t n = max_rows > 0 ? std::min<int64_t>(max_rows, rows) : rows / cache->B;
+  return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
+                       (int64_t)cache->table_width * cache->page_size)
+      .bytes;
 }
 
 spc_status spc_verify(const void* q_logits, const void* p_logits, int32_t dtype,

@@ -240,6 +240,9 @@ struct KvParams {
   int64_t q_stride, out_stride;
   int32_t heads, window;
   float scale;              // of q.k, times log2(e)
+  int32_t tile_rows;        // rows (new token, query head) a workgroup takes: 16, 32 or 64
+  int32_t splits;           // most shares the keys are cut into
+  float* part;              // [B * splits][H][row tiles][tile_rows][D + 2], splits > 1
 };
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);

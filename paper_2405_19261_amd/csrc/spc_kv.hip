@@ -184,109 +184,282 @@ __device__ __forceinline__ void first_of(Frag<F8>& f, int n) {
   }
 }
 
-// Attention of 16 rows by one wavefront.  The rows of a key/value head are the
-// pairs (new token i, query head g of the head's group), i first.  Scores are
-// taken transposed, S^T = K Q^T, in tiles of 32 keys: lane 16 j + c then holds
-// row c's scores of keys 8 j .. 8 j + 7, which is what the second product
-// O^T = V^T P^T wants of it as right operand: neither P nor the running
-// maximum and sum of a row ever moves between lanes but for the row's own
-// reductions over j.  Statistics and O are held in 32 bits; P is rounded to
-// bfloat16 (by at most 2^-8) for the matrix unit, its sum is of the values before that.
-template <int D, bool F8>
-__global__ void __launch_bounds__(64) k_kv_attend(KvParams P) {
+// ------------------------------------------------------------------ attention
+// The rows of a key/value head are the pairs (new token i, query head g of the
+// head's group), i first; a workgroup takes 16 MT of them and a share of the
+// keys, its four wavefronts every fourth tile of 32 keys.  Scores are taken
+// transposed, S^T = K Q^T: lane 16 j + c then holds row c's scores of keys
+// 8 j .. 8 j + 7 of a tile, which is what the second product O^T = V^T P^T wants
+// as right operand, so neither P nor the running statistics of a row move
+// between lanes but for the row's own reductions over j, and these only when
+// its maximum grows.  Keys and values are read once per workgroup, straight to
+// registers.  Statistics and O are held in 32 bits; P is rounded to bfloat16
+// (by at most 2^-8) for the matrix unit, its sum is of the values before that.
+constexpr int kAttendWaves = 4;
+constexpr int kSplitTiles = 4 * kAttendWaves;  // tiles a share of the keys has at least
+
+// The keys that rows [r0, r1) of a chunk see, in tiles of 32: [begin, end).
+struct Span {
+  int64_t begin;  // a multiple of 32
+  int32_t tiles, shares, per;  // shares of `per` tiles
+};
+__device__ __forceinline__ Span span_of(const KvParams& P, int64_t len, int n, int64_t i0,
+                                        int64_t i1, int splits) {
+  const int64_t there = min(len, (int64_t)P.width * P.S);
+  const int64_t end = min(there, len - n + i1 + 1);
+  int64_t begin = P.window > 0 ? max(len - n + i0 - P.window + 1, (int64_t)0) : 0;
+  begin &= ~(int64_t)31;
+  Span s;
+  s.begin = begin;
+  s.tiles = end > begin ? (int32_t)((end - begin + 31) / 32) : 0;
+  s.shares = max(1, min(splits, s.tiles / kSplitTiles));
+  s.per = (s.tiles + s.shares - 1) / s.shares;
+  return s;
+}
+
+template <int D, bool F8, int MT>
+__global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
   constexpr int kC = D / 32, kM = D / 16;
-  const int b = blockIdx.z, h = blockIdx.y;
-  const int lane = threadIdx.x, c16 = lane & 15, j = lane >> 4;
+  constexpr int kPad = 4;
+  __shared__ float o_lds[kAttendWaves][16][D + kPad];
+  __shared__ float m_lds[kAttendWaves][16], l_lds[kAttendWaves][16];
+  const int share = blockIdx.z % P.splits, b = blockIdx.z / P.splits, h = blockIdx.y;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Chunk ch = chunk_of(P, b);
   const int G = P.heads / P.H;
-  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)blockIdx.x * 16;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)blockIdx.x * (16 * MT);
   if (r0 >= rows) return;
-  const int64_t r = min(r0 + c16, rows - 1);
-  const bool live = r0 + c16 < rows;
-  const int i = (int)(r / G), g = (int)(r % G);
-  const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
-  bf16x8 q[kC];
-#pragma unroll
-  for (int c = 0; c < kC; ++c)
-    q[c] = __builtin_bit_cast(bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(
-                                          static_cast<const uint16_t*>(P.q) + q_at + 32 * c + 8 * j)));
   const int64_t len = P.len[b];
-  const int64_t there = min(len, (int64_t)P.width * P.S);  // tokens the table holds
-  const int64_t last = len - ch.n + i;                     // the row's own position
-  const int64_t first = P.window > 0 ? last - P.window + 1 : 0;
-  // keys of the tile's first and last row bound the loop
-  const int64_t i_end = (min(r0 + 16, rows) - 1) / G;
-  const int64_t end = min(there, len - ch.n + i_end + 1);
-  const int64_t begin = P.window > 0 ? max(len - ch.n + r0 / G - P.window + 1, (int64_t)0) : 0;
-  f32x4 o[kM] = {};
-  float m = kNegInf, l = 0.0f;
-  for (int64_t t0 = begin & ~(int64_t)31; t0 < end; t0 += 32) {
-    // the pages of this lane's key (as a row of K) and of its eight keys
-    const int64_t tk = t0 + 8 * (c16 >> 2) + (c16 & 3), ts = t0 + 8 * j;
-    const int pk = tk < there ? page_of(P, b, tk) : -1;
-    const int ps = ts < there ? page_of(P, b, ts) : -1;
-    const int64_t hk = ((int64_t)max(pk, 0) * P.H + h) * P.S * D + (pk < 0 ? 0 : tk % P.S) * D;
+  const int64_t i0 = r0 / G, i1 = (min(r0 + 16 * MT, rows) - 1) / G;
+  const Span span = span_of(P, len, ch.n, i0, i1, P.splits);
+  if (share >= span.shares) return;
+  const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
+  const int64_t there = min(len, (int64_t)P.width * P.S);
+
+  bf16x8 q[MT][kC];
+  int32_t last[MT], first[MT];  // the keys a row sees, from span.begin
+  const int64_t pos0 = len - ch.n - span.begin;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int64_t r = min(r0 + 16 * mt + c16, rows - 1);
+    const int i = (int)(r / G), g = (int)(r % G);
+    const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+      q[mt][c] = __builtin_bit_cast(
+          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at +
+                                                          32 * c + 8 * j)));
+    last[mt] = (int32_t)(pos0 + i);
+    first[mt] = P.window > 0 ? last[mt] - P.window + 1 : 0;
+  }
+  const int32_t limit = (int32_t)(there - span.begin);
+  // a tile between these is seen whole by every row
+  const int32_t all_from = P.window > 0 ? (int32_t)(pos0 + i1) - P.window + 1 : 0;
+  const int32_t all_to = min((int32_t)(pos0 + i0) + 1, limit);
+
+  f32x4 o[MT][kM] = {};
+  float m[MT], l[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = kNegInf;
+    l[mt] = 0.0f;
+  }
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  // the page of tile-relative key t, or -1
+  const auto page_at = [&](int32_t t) {
+    if (t >= limit) return -1;
+    const int p = table[(span.begin + t) / P.S];
+    return p >= 0 && p < P.pages ? p : -1;
+  };
+  int tile = tile0 + wave;
+  // the pages of this lane's key (as a row of K) and of its eight keys
+  int pk = tile < tile1 ? page_at(32 * tile + 8 * (c16 >> 2)) : -1;
+  int ps = tile < tile1 ? page_at(32 * tile + 8 * j) : -1;
+  for (; tile < tile1; tile += kAttendWaves) {
+    const int32_t t0 = 32 * tile, ts = t0 + 8 * j;
+    const int slot_k = (int)((span.begin + t0 + 8 * (c16 >> 2)) % P.S) + (c16 & 3);
+    const int slot = (int)((span.begin + ts) % P.S);
+    const int64_t hk = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D + 8 * j;
     const int64_t hs = (int64_t)max(ps, 0) * P.H + h;
-    f32x4 s[2] = {};
+    Frag<F8> kf[2][kC], vf[kM];
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int c = 0; c < kC; ++c)
-        s[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            widen(load_frag<F8>(P.k, hk + (pk < 0 ? 0 : 4 * half) * D + 32 * c + 8 * j)), q[c],
-            s[half], 0, 0, 0);
-    float x[8], vs[8];
-    const int slot = (int)(ts % P.S);
+      for (int c = 0; c < kC; ++c) kf[half][c] = load_frag<F8>(P.k, hk + 4 * half * D + 32 * c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float k_scale = P.scale;
-      vs[e] = 1.0f;
-      if constexpr (F8) {
-        k_scale *= P.k_scale[hs * P.S + slot + e];
-        vs[e] = P.v_scale[hs * P.S + slot + e];
+    for (int mt = 0; mt < kM; ++mt)
+      vf[mt] = load_frag<F8>(P.v, (hs * D + 16 * mt + c16) * P.S + slot);
+    f32x4 ks[2], vs[2];
+    if constexpr (F8) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        ks[half] = *reinterpret_cast<const f32x4*>(P.k_scale + hs * P.S + slot + 4 * half);
+        vs[half] = *reinterpret_cast<const f32x4*>(P.v_scale + hs * P.S + slot + 4 * half);
       }
-      const int64_t t = ts + e;
-      const bool seen = ps >= 0 && t < there && t <= last && t >= first;
-      x[e] = seen ? s[e >> 2][e & 3] * k_scale : kNegInf;
-      if (!seen) vs[e] = 0.0f;
     }
-    float mx = x[0];
+    const bool whole = t0 >= all_from && t0 + 32 <= all_to && !__any((pk | ps) < 0);
+    const int ps_now = ps;
+    // the next tile's pages
+    const int next = tile + kAttendWaves;
+    pk = next < tile1 ? page_at(32 * next + 8 * (c16 >> 2)) : -1;
+    ps = next < tile1 ? page_at(32 * next + 8 * j) : -1;
+
+    bf16x8 p[MT];
+    f32x4 s[MT][2];
 #pragma unroll
-    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m, mx);
-    const float base = m_new == kNegInf ? 0.0f : m_new;  // (nothing seen yet)
-    const float fade = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    l *= fade;
-    bf16x8 p;
+    for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float w = __builtin_amdgcn_exp2f(x[e] - base);
-      l += w;
-      p[e] = (__bf16)(w * vs[e]);
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const bf16x8 k8 = widen(kf[half][c]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][half], 0, 0, 0);
+      }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = s[mt][e >> 2][e & 3] * P.scale;
+        if constexpr (F8) x[e] *= ks[e >> 2][e & 3];
+      }
+      if (!whole) {  // uniform
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int32_t t = ts + e;
+          if (!(ps_now >= 0 && t < limit && t <= last[mt] && t >= first[mt])) x[e] = kNegInf;
+        }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                       fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m[mt])) {  // some row's maximum grows
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m[mt], mx);
+        const float fade = m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[mt] - m_new);
+        m[mt] = m_new;
+        l[mt] *= fade;
+#pragma unroll
+        for (int d = 0; d < kM; ++d) o[mt][d] *= fade;
+      }
+      const float base = m[mt] == kNegInf ? 0.0f : m[mt];  // (nothing seen yet)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float w = __builtin_amdgcn_exp2f(x[e] - base);
+        l[mt] += w;
+        if constexpr (F8) w = w > 0.0f ? w * vs[e >> 2][e & 3] : 0.0f;  // (a scale may be junk)
+        p[mt][e] = (__bf16)w;
+      }
     }
-    const int live_keys = ps < 0 ? 0 : (int)min(there - ts, (int64_t)8);
+    if (!whole) {  // what lies behind the last key may be anything, NaN too
+      const int live = ps_now < 0 ? 0 : limit - ts;
 #pragma unroll
-    for (int mt = 0; mt < kM; ++mt) {
-      Frag<F8> v = load_frag<F8>(P.v, (hs * D + 16 * mt + c16) * P.S + slot);
-      first_of<F8>(v, live_keys);  // what lies behind may be anything, NaN too
-      o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(v), p, o[mt] * fade, 0, 0, 0);
+      for (int d = 0; d < kM; ++d) first_of<F8>(vf[d], live);
+    }
+#pragma unroll
+    for (int d = 0; d < kM; ++d) {
+      const bf16x8 v8 = widen(vf[d]);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt], o[mt][d], 0, 0, 0);
     }
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (!live) return;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* out = static_cast<uint16_t*>(P.out) + (ch.first + i) * P.out_stride + (int64_t)(h * G + g) * D;
+
+  // join the wavefronts, 16 rows at a time; a share that is all of its keys ends
+  // here, others leave O, the maximum and the sum to k_kv_join
+  const bool alone = span.shares == 1;
+  float* part = P.part + ((((int64_t)blockIdx.z * P.H + h) * gridDim.x + blockIdx.x) * (16 * MT)) *
+                             (int64_t)(D + 2);
 #pragma unroll
-  for (int mt = 0; mt < kM; ++mt) {
-    bf16x4 y;
+  for (int mt = 0; mt < MT; ++mt) {
+    l[mt] += __shfl_xor(l[mt], 16);
+    l[mt] += __shfl_xor(l[mt], 32);
+    if (mt) __syncthreads();
+    if (j == 0) {
+      m_lds[wave][c16] = m[mt];
+      l_lds[wave][c16] = l[mt];
+    }
+    __syncthreads();
+    float top = m_lds[0][c16];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[mt][e] * inv);
-    *reinterpret_cast<u32x2a2*>(out + 16 * mt + 4 * j) = __builtin_bit_cast(u32x2, y);
+    for (int w = 1; w < kAttendWaves; ++w) top = fmaxf(top, m_lds[w][c16]);
+    const float fade = m[mt] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m[mt] - top);
+#pragma unroll
+    for (int d = 0; d < kM; ++d)
+      *reinterpret_cast<f32x4*>(&o_lds[wave][c16][16 * d + 4 * j]) = o[mt][d] * fade;
+    __syncthreads();
+    for (int k = (int)threadIdx.x; k < 16 * (D / 4); k += 64 * kAttendWaves) {
+      const int row = k / (D / 4), d = k % (D / 4) * 4;
+      const int64_t r = r0 + 16 * mt + row;
+      if (r >= rows) continue;
+      float t = m_lds[0][row];
+#pragma unroll
+      for (int w = 1; w < kAttendWaves; ++w) t = fmaxf(t, m_lds[w][row]);
+      float sum = 0.0f;
+      f32x4 y{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < kAttendWaves; ++w) {
+        if (m_lds[w][row] != kNegInf)
+          sum += l_lds[w][row] * __builtin_amdgcn_exp2f(m_lds[w][row] - t);
+        y += *reinterpret_cast<const f32x4*>(&o_lds[w][row][d]);
+      }
+      if (alone) {
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const int i = (int)(r / G), g = (int)(r % G);
+        bf16x4 z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(P.out) + (ch.first + i) * P.out_stride +
+                                  (int64_t)(h * G + g) * D + d) = __builtin_bit_cast(u32x2, z);
+      } else {
+        float* to = part + (int64_t)(16 * mt + row) * (D + 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[2 + d + e] = y[e];
+        if (d == 0) {
+          to[0] = t;
+          to[1] = sum;
+        }
+      }
+    }
   }
+}
+
+// The shares of a row joined, in their order: a wavefront a row.
+template <int D>
+__global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63;
+  const Chunk ch = chunk_of(P, b);
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  const int64_t x = r / tile_rows, tiles_x = ((int64_t)P.n * G + tile_rows - 1) / tile_rows;
+  const int64_t r0 = x * tile_rows;
+  const Span span = span_of(P, P.len[b], ch.n, r0 / G, (min(r0 + tile_rows, rows) - 1) / G, P.splits);
+  if (span.shares == 1) return;
+  const auto part = [&](int s) {
+    return P.part + (((((int64_t)b * P.splits + s) * P.H + h) * tiles_x + x) * tile_rows + (r - r0)) *
+                        (int64_t)(D + 2);
+  };
+  float top = kNegInf;
+  for (int s = 0; s < span.shares; ++s) top = fmaxf(top, part(s)[0]);
+  constexpr int E = D / 64;
+  float sum = 0.0f, y[E] = {};
+  for (int s = 0; s < span.shares; ++s) {
+    const float* p = part(s);
+    const float fade = p[0] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(p[0] - top);
+    sum += p[1] * fade;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] += p[2 + lane * E + e] * fade;
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const int i = (int)(r / G), g = (int)(r % G);
+  __bf16* out = static_cast<__bf16*>(P.out) + (ch.first + i) * P.out_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[lane * E + e] = (__bf16)(y[e] * inv);
 }
 
 }  // namespace
@@ -316,19 +489,23 @@ hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream) {
 }
 
 namespace {
-template <int D>
+template <int D, bool F8>
 void attend(const KvParams& P, hipStream_t stream) {
-  const int G = P.heads / P.H;
-  const dim3 grid((uint32_t)(((int64_t)P.n * G + 15) / 16), P.H, P.B), block(64);
-  if (P.f8) k_kv_attend<D, true><<<grid, block, 0, stream>>>(P);
-  else k_kv_attend<D, false><<<grid, block, 0, stream>>>(P);
+  const int64_t rows = (int64_t)P.n * (P.heads / P.H);
+  const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows), P.H, P.B * P.splits);
+  const dim3 block(64 * kAttendWaves);
+  if (P.tile_rows == 16) k_kv_attend<D, F8, 1><<<grid, block, 0, stream>>>(P);
+  else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
+  else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
+  if (P.splits > 1)
+    k_kv_join<D><<<dim3((uint32_t)((rows + 3) / 4), P.H, P.B), 256, 0, stream>>>(P, P.tile_rows);
 }
 }  // namespace
 
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream) {
-  if (P.D == 64) attend<64>(P, stream);
-  else if (P.D == 128) attend<128>(P, stream);
-  else attend<256>(P, stream);
+  if (P.D == 64) P.f8 ? attend<64, true>(P, stream) : attend<64, false>(P, stream);
+  else if (P.D == 128) P.f8 ? attend<128, true>(P, stream) : attend<128, false>(P, stream);
+  else P.f8 ? attend<256, true>(P, stream) : attend<256, false>(P, stream);
   return hipGetLastError();
 }
 
