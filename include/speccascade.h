@@ -375,7 +375,8 @@ size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype);
  *             only: a value is its code times its token's and head's scale
  *   dtype     SPC_BF16 or SPC_E4M3
  *   page_size a multiple of 16 (16 .. 1024); head_dim 64, 128 or 256
- *   page_table [B][table_width] int32 device array
+ *   page_table [B][table_width] int32 device array; table_width * page_size
+ *             is at most 2^30
  *   kv_len    [B] int32 device array: the tokens of a sequence, its new tokens
  *             included
  * Page and scale pointers are 16-byte aligned.

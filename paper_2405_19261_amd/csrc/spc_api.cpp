@@ -771,6 +771,9 @@ spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
   if (c->page_size < 16 || c->page_size > 1024 || c->page_size % 16 != 0)
     return fail(SPC_E_SHAPE, "page_size must be a multiple of 16 from 16 to 1024 (got %d)",
                 c->page_size);
+  if ((int64_t)c->table_width * c->page_size > (int64_t(1) << 30))
+    return fail(SPC_E_SHAPE, "table_width * page_size must be at most 2^30 (got %d * %d)",
+                c->table_width, c->page_size);
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
     return fail(SPC_E_SHAPE, "head_dim must be 64, 128 or 256 (got %d)", c->head_dim);
   if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages |
@@ -789,6 +792,9 @@ spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
   P.D = c->head_dim;
   P.table = c->page_table;
   P.width = c->table_width;
+  const uint32_t u = (uint32_t)c->page_size / 16;  // at most 64
+  // ceil(2^32 / u): with g < 2^26 the product is g / u and less than 1 / u more
+  P.s16_magic = u > 1 ? (uint32_t)(((uint64_t(1) << 32) + u - 1) / u) : 0;
   P.len = c->kv_len;
   P.B = c->B;
   return SPC_OK;

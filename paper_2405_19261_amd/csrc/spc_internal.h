@@ -223,6 +223,7 @@ struct KvParams {
   int32_t f8, pages, S, H, D;
   const int32_t* table;     // [B][width]
   const int32_t* len;       // [B] tokens of the sequence, its new ones included
+  uint32_t s16_magic;       // t / S = (t / 16) s16_magic / 2^32 for t < 2^30 (0: S = 16)
   int32_t B, width;
   const int32_t* start;     // [B + 1] or NULL
   int64_t rows;

@@ -51,7 +51,7 @@ __device__ __forceinline__ int sequence_of(const KvParams& P, int64_t r) {
 // The page of position t of sequence b, or -1: past the table, or no page.
 __device__ __forceinline__ int page_of(const KvParams& P, int b, int64_t t) {
   if (t < 0 || t >= (int64_t)P.width * P.S) return -1;
-  const int p = P.table[(int64_t)b * P.width + t / P.S];
+  const int p = P.table[(int64_t)b * P.width + (int)t / P.S];
   return p >= 0 && p < P.pages ? p : -1;
 }
 
@@ -145,80 +145,75 @@ __global__ void __launch_bounds__(256) k_kv_read(KvParams P) {
   }
 }
 
-// Eight consecutive cached values as bfloat16 (exact for e4m3).
+// Sixteen bytes of the cache: eight bfloat16 or sixteen e4m3 values.
+__device__ __forceinline__ u32x4 load16(const void* p, int64_t bytes) {
+  return *reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + bytes);
+}
+// The step-th eight values of them as bfloat16 (exact for e4m3).
 template <bool F8>
-struct Frag {
-  uint32_t w[F8 ? 2 : 4];
-};
-template <bool F8>
-__device__ __forceinline__ Frag<F8> load_frag(const void* p, int64_t i) {
-  Frag<F8> f;
+__device__ __forceinline__ bf16x8 widen(const u32x4& w, int step) {
   if constexpr (F8) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p) + i);
-    f.w[0] = x.x; f.w[1] = x.y;
+    const uint32_t lo = w[2 * step], hi = w[2 * step + 1];
+    const u32x4 y{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true))};
+    return __builtin_bit_cast(bf16x8, y);
   } else {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i);
-    f.w[0] = x.x; f.w[1] = x.y; f.w[2] = x.z; f.w[3] = x.w;
+    return __builtin_bit_cast(bf16x8, w);
   }
-  return f;
 }
-__device__ __forceinline__ bf16x8 widen(const Frag<false>& f) {
-  const u32x4 x{f.w[0], f.w[1], f.w[2], f.w[3]};
-  return __builtin_bit_cast(bf16x8, x);
-}
-__device__ __forceinline__ bf16x8 widen(const Frag<true>& f) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.w[0], 1.0f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.w[0], 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.w[1], 1.0f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.w[1], 1.0f, true);
-  return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-}
-// The first `n` of eight values, zeros behind them (n may be negative).
+// The first n values, zeros behind them (n may be negative).
 template <bool F8>
-__device__ __forceinline__ void first_of(Frag<F8>& f, int n) {
+__device__ __forceinline__ void first_of(u32x4& w, int n) {
   constexpr int kPer = F8 ? 4 : 2, kBits = 32 / kPer;
 #pragma unroll
-  for (int j = 0; j < 8 / kPer; ++j) {
-    const int m = n - j * kPer;
-    f.w[j] = m >= kPer ? f.w[j] : m <= 0 ? 0u : f.w[j] & ((1u << (m * kBits)) - 1u);
+  for (int j = 0; j < 4; ++j) {
+    const int m = min(max(n - j * kPer, 0), kPer) * kBits;
+    w[j] &= m == 32 ? 0xffffffffu : (1u << m) - 1u;
   }
 }
 
 // ------------------------------------------------------------------ attention
 // The rows of a key/value head are the pairs (new token i, query head g of the
 // head's group), i first; a workgroup takes 16 MT of them and a share of the
-// keys, its four wavefronts every fourth tile of 32 keys.  Scores are taken
-// transposed, S^T = K Q^T: lane 16 j + c then holds row c's scores of keys
-// 8 j .. 8 j + 7 of a tile, which is what the second product O^T = V^T P^T wants
-// as right operand, so neither P nor the running statistics of a row move
-// between lanes but for the row's own reductions over j, and these only when
-// its maximum grows.  Keys and values are read once per workgroup, straight to
-// registers.  Statistics and O are held in 32 bits; P is rounded to bfloat16
-// (by at most 2^-8) for the matrix unit, its sum is of the values before that.
+// keys, its four wavefronts every fourth tile of T keys.  Scores are taken
+// transposed, S^T = K Q^T, sixteen keys at a time, so chosen that lane 16 j + c
+// holds row c's scores of T/4 consecutive keys, which is what the second product
+// O^T = V^T P^T wants as right operand: neither P nor the running statistics of
+// a row move between lanes but for the row's own reductions over j, and these
+// only when its maximum grows.  Keys and values are read once per workgroup,
+// straight to registers, sixteen bytes a lane: with 8-bit values a lane's bytes
+// are two steps of the products, so there T = 64, else 32.  Which dimension
+// stands where in Q K^T does not matter so long as Q is loaded alike.
+// Statistics and O are held in 32 bits; P is rounded to bfloat16 (by at most
+// 2^-8) for the matrix unit, its sum is of the values before that.
 constexpr int kAttendWaves = 4;
-constexpr int kSplitTiles = 4 * kAttendWaves;  // tiles a share of the keys has at least
+constexpr int kShareKeys = 512;  // a share of the keys has at least as many
 
-// The keys that rows [r0, r1) of a chunk see, in tiles of 32: [begin, end).
+// The keys that rows of a chunk's tokens i0 .. i1 see: tiles of T from `begin`
+// (a multiple of T), cut into shares of `per` tiles.
 struct Span {
-  int64_t begin;  // a multiple of 32
-  int32_t tiles, shares, per;  // shares of `per` tiles
+  int32_t begin, tiles, shares, per;
 };
-__device__ __forceinline__ Span span_of(const KvParams& P, int64_t len, int n, int64_t i0,
-                                        int64_t i1, int splits) {
-  const int64_t there = min(len, (int64_t)P.width * P.S);
-  const int64_t end = min(there, len - n + i1 + 1);
-  int64_t begin = P.window > 0 ? max(len - n + i0 - P.window + 1, (int64_t)0) : 0;
-  begin &= ~(int64_t)31;
+template <int T>
+__device__ __forceinline__ Span span_of(const KvParams& P, int32_t len, int n, int i0, int i1,
+                                        int splits) {
+  const int32_t end = min(min(len, P.width * P.S), len - n + i1 + 1);
   Span s;
-  s.begin = begin;
-  s.tiles = end > begin ? (int32_t)((end - begin + 31) / 32) : 0;
-  s.shares = max(1, min(splits, s.tiles / kSplitTiles));
+  s.begin = P.window > 0 ? max(len - n + i0 - P.window + 1, 0) & ~(T - 1) : 0;
+  s.tiles = end > s.begin ? (end - s.begin + T - 1) / T : 0;
+  s.shares = max(1, min(splits, s.tiles / (kShareKeys / T)));
   s.per = (s.tiles + s.shares - 1) / s.shares;
   return s;
 }
 
 template <int D, bool F8, int MT>
 __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
+  constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
+  constexpr int kQuarters = T / 16, kG = T / 4;  // score tiles; a lane's keys
+  constexpr int kL = D * EB / 64;                // 16-byte loads of a key row by four lanes
+  constexpr int kSteps = 2 / EB;                 // matrix steps in 16 bytes
   constexpr int kC = D / 32, kM = D / 16;
   constexpr int kPad = 4;
   __shared__ float o_lds[kAttendWaves][16][D + kPad];
@@ -230,33 +225,32 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
   const int G = P.heads / P.H;
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)blockIdx.x * (16 * MT);
   if (r0 >= rows) return;
-  const int64_t len = P.len[b];
-  const int64_t i0 = r0 / G, i1 = (min(r0 + 16 * MT, rows) - 1) / G;
-  const Span span = span_of(P, len, ch.n, i0, i1, P.splits);
+  const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S);
+  const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
+  const Span span = span_of<T>(P, len, ch.n, i0, i1, P.splits);
   if (share >= span.shares) return;
   const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
-  const int64_t there = min(len, (int64_t)P.width * P.S);
+  const int32_t pos0 = len - ch.n;
 
   bf16x8 q[MT][kC];
-  int32_t last[MT], first[MT];  // the keys a row sees, from span.begin
-  const int64_t pos0 = len - ch.n - span.begin;
+  int32_t last[MT], first[MT];  // the keys a row sees
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int64_t r = min(r0 + 16 * mt + c16, rows - 1);
     const int i = (int)(r / G), g = (int)(r % G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
-    for (int c = 0; c < kC; ++c)
+    for (int c = 0; c < kC; ++c) {
+      const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
       q[mt][c] = __builtin_bit_cast(
-          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at +
-                                                          32 * c + 8 * j)));
-    last[mt] = (int32_t)(pos0 + i);
+          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+    }
+    last[mt] = pos0 + i;
     first[mt] = P.window > 0 ? last[mt] - P.window + 1 : 0;
   }
-  const int32_t limit = (int32_t)(there - span.begin);
-  // a tile between these is seen whole by every row
-  const int32_t all_from = P.window > 0 ? (int32_t)(pos0 + i1) - P.window + 1 : 0;
-  const int32_t all_to = min((int32_t)(pos0 + i0) + 1, limit);
+  // a tile within these is seen whole by every row
+  const int32_t all_from = P.window > 0 ? pos0 + i1 - P.window + 1 : 0;
+  const int32_t all_to = min(pos0 + i0 + 1, there);
 
   f32x4 o[MT][kM] = {};
   float m[MT], l[MT];
@@ -266,75 +260,107 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
     l[mt] = 0.0f;
   }
   const int32_t* table = P.table + (int64_t)b * P.width;
-  // the page of tile-relative key t, or -1
+  // the page index of a position in the table, and the page there (or -1)
+  const auto index_of = [&](uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  };
   const auto page_at = [&](int32_t t) {
-    if (t >= limit) return -1;
-    const int p = table[(span.begin + t) / P.S];
-    return p >= 0 && p < P.pages ? p : -1;
+    const int p = table[index_of((uint32_t)min(t, there - 1))];
+    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
+  };
+  // where this lane reads of a tile at t0: a row of K, and its own keys of V
+  const int key = kG * (c16 >> 2);
+  struct Where {
+    int64_t k, v;  // bytes
+    int64_t scale;
+    int ps, any;
+  };
+  const auto where = [&](int32_t t0, int pk, int ps) {
+    const uint32_t tk = (uint32_t)(t0 + key), ts = (uint32_t)(t0 + kG * j);
+    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
+    const int slot = (int)(ts - index_of(ts) * (uint32_t)P.S);
+    const int64_t hk = (int64_t)max(pk, 0) * P.H + h, hs = (int64_t)max(ps, 0) * P.H + h;
+    Where w;
+    w.k = ((hk * P.S + slot_k) * D) * EB + 16 * j;
+    w.v = ((hs * D + c16) * P.S + slot) * EB;
+    w.scale = hs * P.S + slot;
+    w.ps = ps;
+    w.any = __any((pk | ps) < 0);
+    return w;
+  };
+  u32x4 kf[kQuarters][kL];
+  const auto load_k = [&](const Where& w) {
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd)
+#pragma unroll
+      for (int c = 0; c < kL; ++c) kf[qd][c] = load16(P.k, w.k + 4 * qd * D * EB + 64 * c);
   };
   int tile = tile0 + wave;
-  // the pages of this lane's key (as a row of K) and of its eight keys
-  int pk = tile < tile1 ? page_at(32 * tile + 8 * (c16 >> 2)) : -1;
-  int ps = tile < tile1 ? page_at(32 * tile + 8 * j) : -1;
+  Where now{};
+  if (tile < tile1) {
+    const int32_t t0 = span.begin + T * tile;
+    now = where(t0, page_at(t0 + key), page_at(t0 + kG * j));
+    load_k(now);
+  }
   for (; tile < tile1; tile += kAttendWaves) {
-    const int32_t t0 = 32 * tile, ts = t0 + 8 * j;
-    const int slot_k = (int)((span.begin + t0 + 8 * (c16 >> 2)) % P.S) + (c16 & 3);
-    const int slot = (int)((span.begin + ts) % P.S);
-    const int64_t hk = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D + 8 * j;
-    const int64_t hs = (int64_t)max(ps, 0) * P.H + h;
-    Frag<F8> kf[2][kC], vf[kM];
+    const int32_t t0 = span.begin + T * tile, ts = t0 + kG * j;
+    // the next tile's pages
+    const int32_t tn = t0 + T * kAttendWaves;
+    const bool more = tile + kAttendWaves < tile1;
+    int pk = -1, ps = -1;
+    if (more) {
+      pk = page_at(tn + key);
+      ps = page_at(tn + kG * j);
+    }
+    u32x4 vf[kM];
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int c = 0; c < kC; ++c) kf[half][c] = load_frag<F8>(P.k, hk + 4 * half * D + 32 * c);
-#pragma unroll
-    for (int mt = 0; mt < kM; ++mt)
-      vf[mt] = load_frag<F8>(P.v, (hs * D + 16 * mt + c16) * P.S + slot);
-    f32x4 ks[2], vs[2];
+    for (int d = 0; d < kM; ++d) vf[d] = load16(P.v, now.v + (int64_t)(16 * d) * P.S * EB);
+    f32x4 ks[kQuarters], vs[kQuarters];
     if constexpr (F8) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        ks[half] = *reinterpret_cast<const f32x4*>(P.k_scale + hs * P.S + slot + 4 * half);
-        vs[half] = *reinterpret_cast<const f32x4*>(P.v_scale + hs * P.S + slot + 4 * half);
+      for (int qd = 0; qd < kQuarters; ++qd) {
+        ks[qd] = *reinterpret_cast<const f32x4*>(P.k_scale + now.scale + 4 * qd);
+        vs[qd] = *reinterpret_cast<const f32x4*>(P.v_scale + now.scale + 4 * qd);
       }
     }
-    const bool whole = t0 >= all_from && t0 + 32 <= all_to && !__any((pk | ps) < 0);
-    const int ps_now = ps;
-    // the next tile's pages
-    const int next = tile + kAttendWaves;
-    pk = next < tile1 ? page_at(32 * next + 8 * (c16 >> 2)) : -1;
-    ps = next < tile1 ? page_at(32 * next + 8 * j) : -1;
-
-    bf16x8 p[MT];
-    f32x4 s[MT][2];
+    f32x4 s[MT][kQuarters];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+      for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        const bf16x8 k8 = widen(kf[half][c]);
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) {
+        const bf16x8 k8 = widen<F8>(kf[qd][c / kSteps], c % kSteps);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          s[mt][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][half], 0, 0, 0);
+          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
       }
+    const bool whole = t0 >= all_from && t0 + T <= all_to && !now.any;
+    const bool page = now.ps >= 0;
+    if (more) {
+      now = where(tn, pk, ps);
+      load_k(now);
+    }
+    bf16x8 p[MT][kSteps];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      float x[8];
+      float x[kG];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kG; ++e) {
         x[e] = s[mt][e >> 2][e & 3] * P.scale;
         if constexpr (F8) x[e] *= ks[e >> 2][e & 3];
       }
       if (!whole) {  // uniform
+        const int32_t hi = page ? min(there - 1, last[mt]) : -1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int32_t t = ts + e;
-          if (!(ps_now >= 0 && t < limit && t <= last[mt] && t >= first[mt])) x[e] = kNegInf;
-        }
+        for (int e = 0; e < kG; ++e)
+          x[e] = ((ts + e <= hi) & (ts + e >= first[mt])) ? x[e] : kNegInf;
       }
-      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                       fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      float mx = x[0];
+#pragma unroll
+      for (int e = 1; e < kG; ++e) mx = fmaxf(mx, x[e]);
       if (__any(mx > m[mt])) {  // some row's maximum grows
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -347,25 +373,30 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
       }
       const float base = m[mt] == kNegInf ? 0.0f : m[mt];  // (nothing seen yet)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kG; ++e) {
         float w = __builtin_amdgcn_exp2f(x[e] - base);
         l[mt] += w;
-        if constexpr (F8) w = w > 0.0f ? w * vs[e >> 2][e & 3] : 0.0f;  // (a scale may be junk)
-        p[mt][e] = (__bf16)w;
+        if constexpr (F8) {
+          w *= vs[e >> 2][e & 3];
+          if (!whole) w = x[e] > kNegInf ? w : 0.0f;  // (an unseen key's scale may be junk)
+        }
+        p[mt][e >> 3][e & 7] = (__bf16)w;
       }
     }
     if (!whole) {  // what lies behind the last key may be anything, NaN too
-      const int live = ps_now < 0 ? 0 : limit - ts;
+      const int live = page ? there - ts : 0;
 #pragma unroll
       for (int d = 0; d < kM; ++d) first_of<F8>(vf[d], live);
     }
 #pragma unroll
-    for (int d = 0; d < kM; ++d) {
-      const bf16x8 v8 = widen(vf[d]);
+    for (int d = 0; d < kM; ++d)
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt], o[mt][d], 0, 0, 0);
-    }
+      for (int step = 0; step < kSteps; ++step) {
+        const bf16x8 v8 = widen<F8>(vf[d], step);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][step], o[mt][d], 0, 0, 0);
+      }
   }
 
   // join the wavefronts, 16 rows at a time; a share that is all of its keys ends
@@ -428,7 +459,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
 }
 
 // The shares of a row joined, in their order: a wavefront a row.
-template <int D>
+template <int D, int T>
 __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
   const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63;
   const Chunk ch = chunk_of(P, b);
@@ -438,7 +469,7 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
   if (r >= rows) return;
   const int64_t x = r / tile_rows, tiles_x = ((int64_t)P.n * G + tile_rows - 1) / tile_rows;
   const int64_t r0 = x * tile_rows;
-  const Span span = span_of(P, P.len[b], ch.n, r0 / G, (min(r0 + tile_rows, rows) - 1) / G, P.splits);
+  const Span span = span_of<T>(P, max(P.len[b], 0), ch.n, (int)(r0 / G), (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
   if (span.shares == 1) return;
   const auto part = [&](int s) {
     return P.part + (((((int64_t)b * P.splits + s) * P.H + h) * tiles_x + x) * tile_rows + (r - r0)) *
@@ -498,7 +529,7 @@ void attend(const KvParams& P, hipStream_t stream) {
   else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
   else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
   if (P.splits > 1)
-    k_kv_join<D><<<dim3((uint32_t)((rows + 3) / 4), P.H, P.B), 256, 0, stream>>>(P, P.tile_rows);
+    k_kv_join<D, F8 ? 64 : 32><<<dim3((uint32_t)((rows + 3) / 4), P.H, P.B), 256, 0, stream>>>(P, P.tile_rows);
 }
 }  // namespace
 

@@ -82,7 +82,7 @@ BAD_CACHES = [
     (dict(kv_len=None), -1), (dict(dtype=spc.SPC_E4M3), -1),
     (dict(dtype=spc.SPC_E4M3, k_scale=OK), -1), (dict(dtype=0), -4), (dict(dtype=3), -4),
     (dict(B=0), -2), (dict(B=65536), -2), (dict(num_pages=0), -2), (dict(table_width=0), -2),
-    (dict(kv_heads=0), -2), (dict(page_size=8), -2), (dict(page_size=24), -2),
+    (dict(table_width=(1 << 26) + 1), -2), (dict(kv_heads=0), -2), (dict(page_size=8), -2), (dict(page_size=24), -2),
     (dict(page_size=2048), -2), (dict(page_size=0), -2), (dict(head_dim=96), -2),
     (dict(head_dim=0), -2), (dict(k_pages=OK + 8), -5), (dict(v_pages=OK + 2), -5),
     (dict(page_table=OK + 2), -5), (dict(kv_len=OK + 1), -5),
