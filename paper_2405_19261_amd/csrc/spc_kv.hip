@@ -209,7 +209,7 @@ __device__ __forceinline__ Span span_of(const KvParams& P, int32_t len, int n, i
 }
 
 template <int D, bool F8, int MT>
-__global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
+__global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) && D <= 128 ? 2 : 1) k_kv_attend(KvParams P) {
   constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
   constexpr int kQuarters = T / 16, kG = T / 4;  // score tiles; a lane's keys
   constexpr int kL = D * EB / 64;                // 16-byte loads of a key row by four lanes
@@ -218,12 +218,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
   constexpr int kPad = 4;
   __shared__ float o_lds[kAttendWaves][16][D + kPad];
   __shared__ float m_lds[kAttendWaves][16], l_lds[kAttendWaves][16];
-  const int share = blockIdx.z % P.splits, b = blockIdx.z / P.splits, h = blockIdx.y;
+  // Workgroups are dealt to the 8 dies in turn: those of one sequence and head
+  // (and share of its keys) go to one die, whose cache then holds their keys, the
+  // row tiles that see most keys first.
+  const uint32_t tiles_x = (uint32_t)(((int64_t)P.n * (P.heads / P.H) + 16 * MT - 1) / (16 * MT));
+  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
+  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  if (group >= (uint32_t)(P.H * P.B * P.splits)) return;
+  const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
   const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Chunk ch = chunk_of(P, b);
   const int G = P.heads / P.H;
-  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)blockIdx.x * (16 * MT);
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * (16 * MT);
   if (r0 >= rows) return;
   const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S);
   const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
@@ -337,6 +344,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
         for (int mt = 0; mt < MT; ++mt)
           s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
       }
+    if constexpr (F8) {
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) ks[qd] *= P.scale;
+    }
     const bool whole = t0 >= all_from && t0 + T <= all_to && !now.any;
     const bool page = now.ps >= 0;
     if (more) {
@@ -349,8 +360,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
       float x[kG];
 #pragma unroll
       for (int e = 0; e < kG; ++e) {
-        x[e] = s[mt][e >> 2][e & 3] * P.scale;
-        if constexpr (F8) x[e] *= ks[e >> 2][e & 3];
+        if constexpr (F8) x[e] = s[mt][e >> 2][e & 3] * ks[e >> 2][e & 3];
+        else x[e] = s[mt][e >> 2][e & 3] * P.scale;
       }
       if (!whole) {  // uniform
         const int32_t hi = page ? min(there - 1, last[mt]) : -1;
@@ -402,7 +413,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_kv_attend(KvParams P) {
   // join the wavefronts, 16 rows at a time; a share that is all of its keys ends
   // here, others leave O, the maximum and the sum to k_kv_join
   const bool alone = span.shares == 1;
-  float* part = P.part + ((((int64_t)blockIdx.z * P.H + h) * gridDim.x + blockIdx.x) * (16 * MT)) *
+  float* part = P.part + ((((int64_t)z * P.H + h) * tiles_x + tile_x) * (16 * MT)) *
                              (int64_t)(D + 2);
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -523,7 +534,8 @@ namespace {
 template <int D, bool F8>
 void attend(const KvParams& P, hipStream_t stream) {
   const int64_t rows = (int64_t)P.n * (P.heads / P.H);
-  const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows), P.H, P.B * P.splits);
+  const int64_t groups = ((int64_t)P.H * P.B * P.splits + 7) / 8 * 8;
+  const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups));
   const dim3 block(64 * kAttendWaves);
   if (P.tile_rows == 16) k_kv_attend<D, F8, 1><<<grid, block, 0, stream>>>(P);
   else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
