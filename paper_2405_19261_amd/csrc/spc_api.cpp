@@ -868,7 +868,7 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
                            int64_t tokens) {
   AttendLayout L;
   const int64_t rows = n * (heads / H);
-  L.tile_rows = rows <= 16 ? 16 : rows <= 32 || D > 128 ? 32 : 64;
+  L.tile_rows = rows <= 16 ? 16 : rows <= 32 || (D > 128 && rows <= 64) ? 32 : rows <= 64 ? 64 : 128;
   const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
   // shares of at least 512 keys, up to four workgroups to a compute unit
   const int64_t most = std::max<int64_t>(1, tokens / 512);

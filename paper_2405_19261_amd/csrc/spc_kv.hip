@@ -469,6 +469,241 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
   }
 }
 
+// The same for chunks of many rows: a workgroup takes 128, each wavefront 32 of
+// its own over all of the share's keys, so that a tile of keys and values is
+// read once for 128 rows. Tiles pass through LDS, in the order the lanes of the
+// products want them (a wavefront's read is 1 KiB in a row, without conflicts),
+// double-buffered: the next tile's are written behind the products of this one
+// and the loads of the one after it are then under way.  What bounds it is the
+// LDS, whose reads of a tile take as long as the products of 32 rows with it,
+// and the softmax's vector instructions; with 64 rows a wavefront, whose O fills
+// the registers of a whole SIMD, nothing hides them.
+template <int D, bool F8>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
+  constexpr int MT = 2, kRows = 16 * MT * kAttendWaves;
+  constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
+  constexpr int kQuarters = T / 16, kG = T / 4;
+  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32, kM = D / 16;
+  constexpr int kFrags = kQuarters * kL + kM;        // of 1 KiB: K's, then V's
+  constexpr int kMine = kFrags / kAttendWaves;       // that a wavefront brings
+  static_assert(kQuarters * kL % kAttendWaves == 0 && kM % kAttendWaves == 0, "whole shares");
+  __shared__ u32x4 frags[2][kFrags][64];
+  __shared__ float scales[2][2][F8 ? T : 1];         // of keys, of values
+  const uint32_t tiles_x = (uint32_t)(((int64_t)P.n * (P.heads / P.H) + kRows - 1) / kRows);
+  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
+  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  if (group >= (uint32_t)(P.H * P.B * P.splits)) return;
+  const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Chunk ch = chunk_of(P, b);
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * kRows;
+  if (r0 >= rows) return;
+  const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S), pos0 = len - ch.n;
+  const Span span = span_of<T>(P, len, ch.n, (int)(r0 / G), (int)((min(r0 + kRows, rows) - 1) / G),
+                               P.splits);
+  if (share >= span.shares) return;
+  const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
+
+  // this wavefront's rows (the last row again behind the end)
+  const int64_t w0 = r0 + 16 * MT * wave;
+  bf16x8 q[MT][kC];
+  int32_t last[MT], first[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int64_t r = min(w0 + 16 * mt + c16, rows - 1);
+    const int i = (int)(r / G), g = (int)(r % G);
+    const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
+      q[mt][c] = __builtin_bit_cast(
+          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+    }
+    last[mt] = pos0 + i;
+    first[mt] = P.window > 0 ? last[mt] - P.window + 1 : 0;
+  }
+  const int i0 = (int)(min(w0, rows - 1) / G), i1 = (int)((min(w0 + 16 * MT, rows) - 1) / G);
+  const int32_t all_from = P.window > 0 ? pos0 + i1 - P.window + 1 : 0;
+  const int32_t all_to = min(pos0 + i0 + 1, there);
+
+  f32x4 o[MT][kM] = {};
+  float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  const auto index_of = [&](uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  };
+  const auto page_at = [&](int32_t t) {
+    const int p = table[index_of((uint32_t)min(t, there - 1))];
+    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
+  };
+  const int key = kG * (c16 >> 2);
+  // the fragments this wavefront brings of a tile at t0, and a lane's scale
+  u32x4 mine[kMine];
+  float my_scale = 0.0f;
+  int page_next = -1, page_now = -1;  // the page of this lane's own keys
+  const auto bring = [&](int32_t t0) {
+    const int pk = page_at(t0 + key), ps = page_at(t0 + kG * j);
+    const uint32_t tk = (uint32_t)(t0 + key), ts = (uint32_t)(t0 + kG * j);
+    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
+    const int slot = (int)(ts - index_of(ts) * (uint32_t)P.S);
+    const int64_t hk = (int64_t)max(pk, 0) * P.H + h, hs = (int64_t)max(ps, 0) * P.H + h;
+    const int64_t at_k = (hk * P.S + slot_k) * D * EB + 16 * j;
+    const int64_t at_v = ((hs * D + c16) * P.S + slot) * EB;
+    page_next = ps;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int f = wave + i * kAttendWaves;
+      if (i < kQuarters * kL / kAttendWaves)
+        mine[i] = load16(P.k, at_k + (f / kL) * 4 * D * EB + f % kL * 64);
+      else
+        mine[i] = load16(P.v, at_v + (int64_t)(16 * (f - kQuarters * kL)) * P.S * EB);
+    }
+    if constexpr (F8) {
+      if (threadIdx.x < 2 * T) {  // a thread a key and kind
+        const uint32_t t = (uint32_t)t0 + threadIdx.x % T;
+        const int p = page_at((int32_t)t);
+        const int64_t at = ((int64_t)max(p, 0) * P.H + h) * P.S + (t - index_of(t) * (uint32_t)P.S);
+        my_scale = p < 0 ? 0.0f : threadIdx.x < T ? P.k_scale[at] * P.scale : P.v_scale[at];
+      }
+    }
+  };
+  const auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) frags[buf][wave + i * kAttendWaves][lane] = mine[i];
+    if constexpr (F8)
+      if (threadIdx.x < 2 * T) scales[buf][threadIdx.x / T][threadIdx.x % T] = my_scale;
+  };
+  if (tile0 < tile1) {
+    bring(span.begin + T * tile0);
+    put(0);
+    page_now = page_next;
+    if (tile0 + 1 < tile1) bring(span.begin + T * (tile0 + 1));
+  }
+  __syncthreads();
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int buf = (tile - tile0) & 1;
+    const int32_t t0 = span.begin + T * tile, ts = t0 + kG * j;
+    f32x4 s[MT][kQuarters];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd)
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const bf16x8 k8 = widen<F8>(frags[buf][qd * kL + c / kSteps][lane], c % kSteps);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
+      }
+    const bool whole = t0 >= all_from && t0 + T <= all_to && !__any(page_now < 0);
+    bf16x8 p[MT][kSteps];
+    float x[MT][kG], mx[MT];
+    bool grows = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        if constexpr (F8) x[mt][e] = s[mt][e >> 2][e & 3] * scales[buf][0][kG * j + e];
+        else x[mt][e] = s[mt][e >> 2][e & 3] * P.scale;
+      }
+      if (!whole) {  // uniform
+        const int32_t hi = page_now >= 0 ? min(there - 1, last[mt]) : -1;
+#pragma unroll
+        for (int e = 0; e < kG; ++e)
+          x[mt][e] = ((ts + e <= hi) & (ts + e >= first[mt])) ? x[mt][e] : kNegInf;
+      }
+      mx[mt] = x[mt][0];
+#pragma unroll
+      for (int e = 1; e < kG; ++e) mx[mt] = fmaxf(mx[mt], x[mt][e]);
+      grows |= mx[mt] > m[mt];
+    }
+    if (__any(grows)) {  // some row's maximum grows
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        mx[mt] = fmaxf(mx[mt], __shfl_xor(mx[mt], 16));
+        mx[mt] = fmaxf(mx[mt], __shfl_xor(mx[mt], 32));
+        const float m_new = fmaxf(m[mt], mx[mt]);
+        const float fade = m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[mt] - m_new);
+        m[mt] = m_new;
+        l[mt] *= fade;
+#pragma unroll
+        for (int d = 0; d < kM; ++d) o[mt][d] *= fade;
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const float base = m[mt] == kNegInf ? 0.0f : m[mt];  // (nothing seen yet)
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        float w = __builtin_amdgcn_exp2f(x[mt][e] - base);
+        l[mt] += w;
+        if constexpr (F8) {
+          w *= scales[buf][1][kG * j + e];
+          if (!whole) w = x[mt][e] > kNegInf ? w : 0.0f;  // (an unseen key's scale may be junk)
+        }
+        p[mt][e >> 3][e & 7] = (__bf16)w;
+      }
+    }
+    const int live = page_now >= 0 ? there - ts : 0;
+#pragma unroll
+    for (int d = 0; d < kM; ++d) {
+      u32x4 v = frags[buf][kQuarters * kL + d][lane];
+      if (!whole) first_of<F8>(v, live);  // what lies behind the last key may be anything, NaN too
+#pragma unroll
+      for (int step = 0; step < kSteps; ++step) {
+        const bf16x8 v8 = widen<F8>(v, step);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][step], o[mt][d], 0, 0, 0);
+      }
+    }
+    // (the buffer written here was last read before the last barrier)
+    if (tile + 1 < tile1) {
+      put(buf ^ 1);
+      page_now = page_next;
+      if (tile + 2 < tile1) bring(t0 + 2 * T);
+    }
+    __syncthreads();
+  }
+
+  const bool alone = span.shares == 1;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    l[mt] += __shfl_xor(l[mt], 16);
+    l[mt] += __shfl_xor(l[mt], 32);
+    const int64_t r = w0 + 16 * mt + c16;
+    if (r >= rows) continue;
+    if (alone) {
+      const float inv = l[mt] > 0.0f ? 1.0f / l[mt] : 0.0f;
+      const int i = (int)(r / G), g = (int)(r % G);
+      uint16_t* out = static_cast<uint16_t*>(P.out) + (ch.first + i) * P.out_stride +
+                      (int64_t)(h * G + g) * D + 4 * j;
+#pragma unroll
+      for (int d = 0; d < kM; ++d) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[mt][d][e] * inv);
+        *reinterpret_cast<u32x2*>(out + 16 * d) = __builtin_bit_cast(u32x2, y);
+      }
+    } else {
+      float* to = P.part + ((((int64_t)z * P.H + h) * tiles_x + tile_x) * kRows + (r - r0)) *
+                               (int64_t)(D + 2);
+#pragma unroll
+      for (int d = 0; d < kM; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[2 + 16 * d + 4 * j + e] = o[mt][d][e];
+      if (j == 0) {
+        to[0] = m[mt];
+        to[1] = l[mt];
+      }
+    }
+  }
+}
+
 // The shares of a row joined, in their order: a wavefront a row.
 template <int D, int T>
 __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
@@ -539,6 +774,7 @@ void attend(const KvParams& P, hipStream_t stream) {
   const dim3 block(64 * kAttendWaves);
   if (P.tile_rows == 16) k_kv_attend<D, F8, 1><<<grid, block, 0, stream>>>(P);
   else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
+  else if (P.tile_rows == 128) k_kv_attend_rows<D, F8><<<grid, block, 0, stream>>>(P);
   else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
   if (P.splits > 1)
     k_kv_join<D, F8 ? 64 : 32><<<dim3((uint32_t)((rows + 3) / 4), P.H, P.B), 256, 0, stream>>>(P, P.tile_rows);
