@@ -469,6 +469,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
   }
 }
 
+// Keys in a tile of k_kv_attend_rows.
+constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
+
 // The same for chunks of many rows: a workgroup takes 128, each wavefront 32 of
 // its own over all of the share's keys, so that a tile of keys and values is
 // read once for 128 rows. Tiles pass through LDS, in the order the lanes of the
@@ -481,12 +484,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
 template <int D, bool F8>
 __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
   constexpr int MT = 2, kRows = 16 * MT * kAttendWaves;
-  constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
+  constexpr int EB = F8 ? 1 : 2, T = rows_tile(D, F8);
   constexpr int kQuarters = T / 16, kG = T / 4;
   constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32, kM = D / 16;
-  constexpr int kFrags = kQuarters * kL + kM;        // of 1 KiB: K's, then V's
+  constexpr int kVL = T * EB / 64;                   // 16-byte loads of a lane's keys of V
+  constexpr int kFrags = kQuarters * kL + kM * kVL;  // of 1 KiB: K's, then V's
   constexpr int kMine = kFrags / kAttendWaves;       // that a wavefront brings
-  static_assert(kQuarters * kL % kAttendWaves == 0 && kM % kAttendWaves == 0, "whole shares");
+  static_assert(kQuarters * kL % kAttendWaves == 0 && kM * kVL % kAttendWaves == 0, "whole shares");
   __shared__ u32x4 frags[2][kFrags][64];
   __shared__ float scales[2][2][F8 ? T : 1];         // of keys, of values
   const uint32_t tiles_x = (uint32_t)(((int64_t)P.n * (P.heads / P.H) + kRows - 1) / kRows);
@@ -558,7 +562,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
       if (i < kQuarters * kL / kAttendWaves)
         mine[i] = load16(P.k, at_k + (f / kL) * 4 * D * EB + f % kL * 64);
       else
-        mine[i] = load16(P.v, at_v + (int64_t)(16 * (f - kQuarters * kL)) * P.S * EB);
+        mine[i] = load16(P.v, at_v + (int64_t)(16 * ((f - kQuarters * kL) / kVL)) * P.S * EB +
+                                  (f - kQuarters * kL) % kVL * 16);
     }
     if constexpr (F8) {
       if (threadIdx.x < 2 * T) {  // a thread a key and kind
@@ -600,7 +605,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
           s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
       }
     const bool whole = t0 >= all_from && t0 + T <= all_to && !__any(page_now < 0);
-    bf16x8 p[MT][kSteps];
+    bf16x8 p[MT][kG / 8];
     float x[MT][kG], mx[MT];
     bool grows = false;
 #pragma unroll
@@ -650,17 +655,21 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     }
     const int live = page_now >= 0 ? there - ts : 0;
 #pragma unroll
-    for (int d = 0; d < kM; ++d) {
-      u32x4 v = frags[buf][kQuarters * kL + d][lane];
-      if (!whole) first_of<F8>(v, live);  // what lies behind the last key may be anything, NaN too
+    for (int d = 0; d < kM; ++d)
 #pragma unroll
-      for (int step = 0; step < kSteps; ++step) {
-        const bf16x8 v8 = widen<F8>(v, step);
+      for (int part = 0; part < kVL; ++part) {
+        u32x4 v = frags[buf][kQuarters * kL + d * kVL + part][lane];
+        // what lies behind the last key may be anything, NaN too
+        if (!whole) first_of<F8>(v, live - part * 8);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][step], o[mt][d], 0, 0, 0);
+        for (int step = 0; step < kSteps; ++step) {
+          const bf16x8 v8 = widen<F8>(v, step);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][part * kSteps + step],
+                                                               o[mt][d], 0, 0, 0);
+        }
       }
-    }
     // (the buffer written here was last read before the last barrier)
     if (tile + 1 < tile1) {
       put(buf ^ 1);
@@ -776,8 +785,11 @@ void attend(const KvParams& P, hipStream_t stream) {
   else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
   else if (P.tile_rows == 128) k_kv_attend_rows<D, F8><<<grid, block, 0, stream>>>(P);
   else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
-  if (P.splits > 1)
-    k_kv_join<D, F8 ? 64 : 32><<<dim3((uint32_t)((rows + 3) / 4), P.H, P.B), 256, 0, stream>>>(P, P.tile_rows);
+  if (P.splits > 1) {
+    const dim3 join((uint32_t)((rows + 3) / 4), P.H, P.B);
+    if (P.tile_rows == 128) k_kv_join<D, rows_tile(D, F8)><<<join, 256, 0, stream>>>(P, 128);
+    else k_kv_join<D, F8 ? 64 : 32><<<join, 256, 0, stream>>>(P, P.tile_rows);
+  }
 }
 }  // namespace
 
