@@ -122,14 +122,15 @@ __device__ __forceinline__ u32x4 load16(const void* p, int64_t bytes) {
 // Chunks of many rows: a workgroup takes 64 rows of a head, a wavefront a row at
 // a time, and turns the values around in LDS, so that eight tokens of a dimension
 // are one store (16 bytes, or 8 of 8 bits) where the page has them all; one by
-// one they are 64 stores of 2 bytes to as many lines (8000 rows of 8 heads of
-// 128: 37 us so, 13 us with the tiles).
+// one they are 64 stores of 2 bytes to as many lines (4500 float32 rows of 8
+// heads of 128 into bfloat16: 37 us so, 20 us with the tiles, 12 at the rate of
+// a copy).
 template <int SRC, bool F8, int D>
 __global__ void __launch_bounds__(256) k_kv_write_tile(KvParams P) {
   constexpr int E = D / 64, kRow = 66;  // an odd number of words between dimensions
   typedef typename std::conditional<F8, uint8_t, uint16_t>::type T;
   __shared__ T turned[D * kRow];
-  __shared__ int32_t pages[64], slots[64];
+  __shared__ int32_t pages[64], slots[64], whole[9];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
   const int64_t r0 = (int64_t)blockIdx.x * 64;
   const int n = (int)min(P.rows - r0, (int64_t)64);
@@ -146,48 +147,65 @@ __global__ void __launch_bounds__(256) k_kv_write_tile(KvParams P) {
     slots[lane] = slot;
   }
   __syncthreads();
-  for (int i = wave; i < n; i += 4) {
-    const int page = pages[i];
-    if (page < 0) continue;  // (a wavefront's)
-    const int64_t head = (int64_t)page * P.H + h, line = head * P.S + slots[i];
+  // kAtOnce rows of a wavefront at a time: their loads are under way together
+  constexpr int kAtOnce = 4;
+  for (int i0 = wave * kAtOnce; i0 < n; i0 += 4 * kAtOnce) {
+    float x[kAtOnce][2][E];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const int64_t at = (r0 + i) * (which ? P.v_stride : P.k_stride) + (int64_t)h * D;
-      float x[E], amax = 0.0f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        x[e] = source<SRC>(which ? P.v_new : P.k_new, at + e * 64 + lane);
-        amax = fmaxf(amax, fabsf(x[e]));
-      }
-      float scale = 1.0f;
-      if constexpr (F8) {
-#pragma unroll
-        for (int d = 32; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
-        scale = fmaxf(amax / kF8Max, 1.17549435e-38f);
-        if (lane == 0) (which ? P.v_scale : P.k_scale)[line] = scale;
-      }
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t r = r0 + min(i0 + k, n - 1);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        T y;
-        if constexpr (F8) y = to_f8(x[e] / scale);
-        else y = __builtin_bit_cast(uint16_t, (__bf16)x[e]);
-        if (which) turned[(e * 64 + lane) * kRow + i] = y;
-        else static_cast<T*>(P.k)[line * D + e * 64 + lane] = y;
+        x[k][0][e] = source<SRC>(P.k_new, r * P.k_stride + (int64_t)h * D + e * 64 + lane);
+        x[k][1][e] = source<SRC>(P.v_new, r * P.v_stride + (int64_t)h * D + e * 64 + lane);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k, page = i < n ? pages[i] : -1;
+      if (page < 0) continue;  // (a wavefront's)
+      const int64_t line = ((int64_t)page * P.H + h) * P.S + slots[i];
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        float scale = 1.0f;
+        if constexpr (F8) {
+          float amax = 0.0f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) amax = fmaxf(amax, fabsf(x[k][which][e]));
+#pragma unroll
+          for (int d = 32; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+          scale = fmaxf(amax / kF8Max, 1.17549435e-38f);
+          if (lane == 0) (which ? P.v_scale : P.k_scale)[line] = scale;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          T y;
+          if constexpr (F8) y = to_f8(x[k][which][e] / scale);
+          else y = __builtin_bit_cast(uint16_t, (__bf16)x[k][which][e]);
+          if (which) turned[(e * 64 + lane) * kRow + i] = y;
+          else static_cast<T*>(P.k)[line * D + e * 64 + lane] = y;
+        }
       }
     }
   }
   __syncthreads();
-  // values: 9 groups of eight slots cover 64 rows; group g of a row run starts at
-  // the row whose slot is a multiple of eight
+  // values: 9 groups of eight slots cover 64 rows; a group that starts at a slot
+  // which is a multiple of eight and lies in one page is one store a dimension
   const int lead = slots[0] & 7;
-  for (int k = (int)threadIdx.x; k < D * 9; k += 256) {
-    const int g = k % 9, d = k / 9, i0 = g * 8 - lead;
-    const T* src = turned + d * kRow;
-    T* dst = static_cast<T*>(P.v);
+  if (threadIdx.x < 9) {
+    const int i0 = (int)threadIdx.x * 8 - lead;
     bool one = i0 >= 0 && i0 + 8 <= n && pages[i0] >= 0 && (slots[i0] & 7) == 0;
     if (one)
       for (int e = 1; e < 8; ++e)
         one &= pages[i0 + e] == pages[i0] && slots[i0 + e] == slots[i0] + e;
+    whole[threadIdx.x] = one;
+  }
+  __syncthreads();
+  for (int k = (int)threadIdx.x; k < D * 9; k += 256) {
+    const int g = k % 9, d = k / 9, i0 = g * 8 - lead;
+    const T* src = turned + d * kRow;
+    T* dst = static_cast<T*>(P.v);
+    const bool one = whole[g];
     if (one) {
       T* to = dst + (((int64_t)pages[i0] * P.H + h) * D + d) * P.S + slots[i0];
       uint32_t w[F8 ? 2 : 4];

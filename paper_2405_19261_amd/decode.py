@@ -20,7 +20,14 @@ next-token logits given the last token and its position.  A real language
 model conditions on the whole prefix through its KV cache; rolling back is
 then truncating that cache to t + j* + 1.  ``SyntheticLM`` is such a callable
 with seeded logits, standing in for the paper's drafter/verifier pairs,
-whose weights are not used here.
+whose weights are not used here.  ``ContextLM`` adds a paged KV cache to it:
+its logits depend on every token before them through one attention layer
+(``spc_kv_write``, ``spc_kv_attend``), one token at a time as a drafter and
+gamma + 1 at a time as a verifier.
+
+With ``top_k``, ``top_p`` or ``min_p`` the drafts come from the drafter's
+truncated distribution (``spc_sample``) and the verification sees both models'
+rows truncated alike (``spc_truncate``), so that it still is exact.
 
 The backend does the sampling and verification.  ``GpuBackend`` calls the C
 library; a test may pass any object with the same two methods.
@@ -55,9 +62,68 @@ class SyntheticLM:
         t = scale * self.table.cpu() + sigma * torch.randn(self.rows, self.V, generator=g)
         return SyntheticLM(self.V, self.rows, dtype=self.dtype, device=self.device, table=t)
 
-    def __call__(self, last_tokens, positions):
+    def row_of(self, last_tokens, positions):
         h = (last_tokens.long() * 1000003 + positions.long() * 7919) % self.rows
-        return self.logits_table.index_select(0, h.to(self.device))
+        return h.to(self.device)
+
+    def __call__(self, last_tokens, positions):
+        return self.logits_table.index_select(0, self.row_of(last_tokens, positions))
+
+
+class ContextLM:
+    """A SyntheticLM whose logits also depend on the tokens before the last
+    one: ``base``'s row plus ``mix`` times a projection of one attention layer
+    over a paged KV cache of its own.  A token's query, key and value are rows
+    of seeded tables picked as its logit row is, by a hash of (token,
+    position).  The cache holds up to ``max_len`` tokens of each of ``B``
+    sequences in pages of ``page_size``, in bfloat16 or (``cache_dtype``
+    torch.float8_e4m3fn) quantised as it is written.
+
+    A call takes n tokens of every sequence, [B * n] (sequence by sequence,
+    at consecutive positions), writes their keys and values and attends from
+    all of them.  A position that comes again overwrites what it held, and a
+    call reads no further than its last position: rolling back needs no more
+    than going on from an earlier position."""
+
+    def __init__(self, base, B, max_len, heads=4, kv_heads=2, head_dim=64, page_size=16,
+                 cache_dtype=torch.bfloat16, mix=1.0, seed=0):
+        self.base, self.B, self.V, self.device = base, B, base.V, base.device
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        g = torch.Generator(device="cpu").manual_seed(seed)
+
+        def table(*shape, s=1.0):
+            return (torch.randn(*shape, generator=g) * s).to(self.device, torch.bfloat16)
+
+        self.q_table = table(base.rows, heads, head_dim)
+        self.k_table = table(base.rows, kv_heads, head_dim)
+        self.v_table = table(base.rows, kv_heads, head_dim)
+        self.project = table(heads * head_dim, base.V, s=mix * (heads * head_dim) ** -0.5)
+        width = (max_len + page_size - 1) // page_size
+        # pages in a seeded order, as an allocator leaves them after a while
+        self.page_table = torch.randperm(B * width, generator=g).view(B, width).to(
+            self.device, torch.int32)
+        shape = (B * width, kv_heads, page_size, head_dim)
+        self.k_pages = torch.zeros(shape, device=self.device, dtype=cache_dtype)
+        self.v_pages = torch.zeros((B * width, kv_heads, head_dim, page_size), device=self.device,
+                                   dtype=cache_dtype)
+        self.scales = {}
+        if cache_dtype == torch.float8_e4m3fn:
+            self.scales = {k: torch.zeros(shape[:3], device=self.device)
+                           for k in ("k_scale", "v_scale")}
+
+    def __call__(self, last_tokens, positions):
+        B, n = self.B, last_tokens.numel() // self.B
+        row = self.base.row_of(last_tokens, positions)
+
+        def of(t):
+            return t.index_select(0, row).view(B, n, t.shape[1], t.shape[2])
+
+        kv_len = (positions.view(B, n)[:, -1] + 1).to(torch.int32)
+        cache = (self.k_pages, self.v_pages, self.page_table, kv_len)
+        spc.spc_kv_write(of(self.k_table), of(self.v_table), *cache, **self.scales)
+        o = spc.spc_kv_attend(of(self.q_table), *cache, **self.scales)
+        z = torch.matmul(o.view(B * n, -1), self.project)
+        return self.base.logits_table.index_select(0, row) + z.to(self.base.dtype)
 
 
 class GpuBackend:
@@ -68,11 +134,18 @@ class GpuBackend:
     rule, alpha and temperature the calls take the scalar forms, so the
     library launches only the kernels that rule needs (no argmax at T > 0);
     otherwise the per-sequence arrays go with the ``rules_present`` mask of
-    the rules they hold."""
+    the rules they hold.
+
+    ``truncate`` (called before ``prepare`` where the rounds are truncated)
+    takes top_k, top_p and min_p as [B] tensors."""
 
     def __init__(self):
         self._scalar = None
         self._rules_present = 0
+        self._cut = None
+
+    def truncate(self, top_k, top_p, min_p):
+        self._cut = dict(top_k_per_seq=top_k, top_p_per_seq=top_p, min_p_per_seq=min_p)
 
     def prepare(self, rule, alpha, temperature):
         r, a, t = rule.cpu(), alpha.cpu(), temperature.cpu()
@@ -81,12 +154,17 @@ class GpuBackend:
         self._scalar = (int(r[0]), float(a[0]), float(t[0])) if same else None
 
     def draft_sample(self, logits, temperature, uniforms):
+        if self._cut is not None:
+            return spc.spc_sample(logits, uniforms, temp_per_seq=temperature, **self._cut)
         if self._scalar is not None:
             T = self._scalar[2]
             return spc.spc_draft_sample(logits, T, uniforms=uniforms if T > 0 else None)
         return spc.spc_draft_sample(logits, 0.0, uniforms=uniforms, temp_per_seq=temperature)
 
     def verify(self, q, p, drafts, uniforms, rule, alpha, temperature):
+        if self._cut is not None:
+            q = spc.spc_truncate(q, temp_per_seq=temperature, **self._cut)
+            p = spc.spc_truncate(p, temp_per_seq=temperature, **self._cut)
         if self._scalar is not None:
             acc, tok, _ = spc.spc_verify_ex(q, p, drafts, uniforms, *self._scalar)
         else:
@@ -109,13 +187,17 @@ class DecodeResult:
 
 
 def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, temperature,
-                seed=0, backend=None, rounds_inputs=None, graph=False):
+                seed=0, backend=None, rounds_inputs=None, graph=False, top_k=0, top_p=1.0,
+                min_p=0.0):
     """Run ``rounds`` rounds of GenSpecSample for B sequences whose last
     prefix token is ``first_tokens`` [B] (at position 0).  ``rule``,
     ``alpha`` and ``temperature`` are scalars or [B] tensors (temperature 0:
     greedy).  Uniforms come from a torch.Generator seeded with ``seed``;
     ``rounds_inputs`` (a list), when given, receives each round's inputs so a
-    test can replay them through another backend.
+    test can replay them through another backend.  ``top_k``, ``top_p`` and
+    ``min_p`` (scalars or [B] tensors; 0, 1 and 0 leave a distribution whole)
+    truncate both models' distributions; the backend then needs a ``truncate``
+    method, which gets them as [B] tensors.
 
     The rounds run without waiting for the device: emitted tokens are
     scattered into a device buffer (a round writes its gamma+1 candidates at
@@ -145,6 +227,10 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
     rule_t = per_seq(rule, torch.int32)
     alpha_t = per_seq(alpha, torch.float32)
     temp_t = per_seq(temperature, torch.float32)
+    whole = (0, 1.0, 0.0)
+    if any(torch.is_tensor(x) or x != w for x, w in zip((top_k, top_p, min_p), whole)):
+        backend.truncate(per_seq(top_k, torch.int32), per_seq(top_p, torch.float32),
+                         per_seq(min_p, torch.float32))
     if hasattr(backend, "prepare"):
         backend.prepare(rule_t, alpha_t, temp_t)
     gen = torch.Generator(device=dev).manual_seed(seed)
@@ -240,4 +326,4 @@ def synthetic_pair(V, seed=0, dtype=torch.bfloat16, device="cuda", rows=64):
     return p.derive(scale=0.8, sigma=1.0, seed=seed + 1), p
 
 
-__all__ = ["SyntheticLM", "GpuBackend", "DecodeResult", "spec_decode", "synthetic_pair"]
+__all__ = ["SyntheticLM", "ContextLM", "GpuBackend", "DecodeResult", "spec_decode", "synthetic_pair"]
