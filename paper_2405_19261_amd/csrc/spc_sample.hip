@@ -71,6 +71,9 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 }
 constexpr uint32_t kKeyLowest = 0x00800000u;  // key of the lowest finite float
 
+__device__ __forceinline__ double pow2(int e) {  // -1022 <= e <= 1023
+  return __longlong_as_double((long long)(1023 + e) << 52);
+}
 // 2^(f/16) - 1 for f in [0, 1), the series of e^x - 1 at x = f ln(2)/16 < 0.0434.
 // In bins, which hold it in units of 2^-37 or less: to the sixth power, the rest
 // under 6e-14.  In weights: to the seventh, the rest under 4e-16.
@@ -611,7 +614,7 @@ __device__ __noinline__ Narrowed narrow(Shared& S, const Row& row, double c, dou
   Narrowed r{0, 0, 0, 0.0, 0.0};
   int slot = 0;
   const int sb = sum_bits(row.V);
-  const double scale = exp2((double)sb), unscale = exp2((double)-sb);
+  const double scale = pow2(sb), unscale = pow2(-sb);
   for (;;) {
     const uint32_t span = hi - lo;
     const int shift = max(0, 22 - (span ? __builtin_clz(span) : 32));
@@ -821,8 +824,15 @@ __device__ __forceinline__ int cut_bin(const Ask& a, const Cut& c, double top) {
   return c.z > kLowest ? bin_of(top, (double)c.z * a.c) : kBins;
 }
 
+// 2^-(i/16): a product of at most four roots of 2 and a power (within 2^-50).
 __device__ __forceinline__ void fill_edges(Shared& S) {
-  S.edge[threadIdx.x] = exp2(-(double)threadIdx.x * 0.0625);
+  const int i = (int)threadIdx.x;
+  double x = pow2(-(i >> 4));
+  x *= i & 8 ? 0.70710678118654752440 : 1.0;
+  x *= i & 4 ? 0.84089641525371454303 : 1.0;
+  x *= i & 2 ? 0.91700404320467123174 : 1.0;
+  x *= i & 1 ? 0.95760328069857364694 : 1.0;
+  S.edge[i] = x;
 }
 
 // The cut of a row in one workgroup; zmax its largest logit (finite), `whole` the
@@ -1001,7 +1011,7 @@ __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
                                      const HeldRow<DT, U>& row, const Cut& cut, const Ask& a,
                                      double top) {
   constexpr int E = HeldRow<DT, U>::E;
-  const double scale = exp2((double)sum_bits(row.V));
+  const double scale = pow2(sum_bits(row.V));
   uint32_t n;
   const uint64_t s = held_weight(S, row, 0, cut, a, top, scale, n);
   const uint32_t n_kept = P.out_kept ? block_sum(S, n) : 0;
@@ -1017,7 +1027,7 @@ template <int DT>
 __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
                                      const ScanRow<DT>& row, const Cut& cut, const Ask& a,
                                      double top) {
-  const double scale = exp2((double)sum_bits(row.V));
+  const double scale = pow2(sum_bits(row.V));
   const int64_t q = ((int64_t)row.V + kNT - 1) / kNT, e0 = (int64_t)threadIdx.x * q;
   uint32_t n = 0;
   uint64_t s = 0;
@@ -1282,7 +1292,7 @@ __global__ void __launch_bounds__(kNT) k_slice_keep(TruncParams P) {
   const char* src = static_cast<const char*>(P.z) + r * P.ld * Elem<DT>::EB;
   constexpr uint32_t kPad = DT == 1 ? 0xff80ff80u : 0xff800000u;
   const Ask a = ask_of(P, r / P.rows_per_seq);
-  fill_edges(S);
+  if (!CUT) fill_edges(S);
   const float sure_z = plan->sure_z;
   const Cut sure{sure_z, sure_z <= -kLowest ? kNoIndex : -1};
   const Question q = plan->q;
@@ -1320,7 +1330,7 @@ __global__ void __launch_bounds__(kNT) k_slice_keep(TruncParams P) {
       return;
     }
     uint32_t n;
-    uint64_t x = held_weight(S, mine, s * N, sure, a, plan->top, exp2((double)sum_bits(P.V)), n);
+    uint64_t x = held_weight(S, mine, s * N, sure, a, plan->top, pow2(sum_bits(P.V)), n);
     x = wave_incl_scan(x);
     if ((threadIdx.x & 63) == 63)
       P.sub_weight[(r * P.slices + s) * kNW + (threadIdx.x >> 6)] = x;
@@ -1376,7 +1386,7 @@ __global__ void __launch_bounds__(kNT) k_slice_end(TruncParams P, int sub) {
     }
   } else {
     // weights by groups of G sub-chunks of `sub` entries
-    const double scale = exp2((double)sum_bits(P.V));
+    const double scale = pow2(sum_bits(P.V));
     const int64_t subs = ((int64_t)P.V + sub - 1) / sub, G = (subs + kNT - 1) / kNT;
     const uint64_t* weights = P.sub_weight + r * P.slices * kNW;
     uint64_t own = 0;
