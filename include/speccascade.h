@@ -385,7 +385,7 @@ size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype);
  * every sequence, sequence after sequence; with it (a [B+1] int32 device
  * array, not decreasing) sequence b has rows row_start[b] .. row_start[b+1]-1.
  * The last of a sequence's n new rows is at position kv_len[b] - 1, the first
- * at kv_len[b] - n.  Rows before row_start[0] and from row_start[B] on belong
+ * at kv_len[b] - n.  A call takes at most 2^24 rows.  Rows before row_start[0] and from row_start[B] on belong
  * to no sequence: they are not read, and outputs for them are left as they are.
  *
  * Rolling back is a smaller kv_len: nothing at or past it is read.  A token

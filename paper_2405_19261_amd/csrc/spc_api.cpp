@@ -581,6 +581,17 @@ spc_status draft_impl(const void* logits, int32_t dtype, int32_t B, int32_t V, f
   return SPC_OK;
 }
 
+// A call's body: nothing it throws (a failed allocation of the host's) passes
+// the C interface.
+template <class F>
+spc_status guarded(F&& body) noexcept {
+  try {
+    return body();
+  } catch (...) {
+    return SPC_E_HIP;
+  }
+}
+
 // Settings of spc_truncation that apply to the whole batch.
 spc_status check_truncation(const spc_truncation* t) {
   if (!t->temp_per_seq && !(isfinite(t->temperature) && t->temperature >= 0.0f))
@@ -750,6 +761,10 @@ spc_status truncate_impl(const void* logits, int32_t dtype, int32_t B, int32_t r
   const int64_t eb = dtype == SPC_BF16 ? 2 : 4;
   if (((uintptr_t)logits | (uintptr_t)out) % eb != 0)
     return fail(SPC_E_ALIGN, "the logits must be aligned to their elements");
+  const uintptr_t from = (uintptr_t)logits, to = (uintptr_t)out,
+                  bytes = (uintptr_t)B * (uintptr_t)rows_per_seq * (uintptr_t)V * (uintptr_t)eb;
+  if (from != to && from < to + bytes && to < from + bytes)
+    return fail(SPC_E_PARAM, "out_logits overlaps logits without being it");
   spc::TruncParams P = truncated_rows(logits, (int64_t)B * rows_per_seq, rows_per_seq, V, V, t);
   P.out = out;
   P.out_ld = V;
@@ -802,8 +817,8 @@ spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
 
 // The rows of a chunk of new tokens.
 spc_status kv_rows(int64_t rows, const int32_t* row_start, int32_t max_rows, spc::KvParams& P) {
-  if (rows < 1 || rows > (int64_t(1) << 26))
-    return fail(SPC_E_SHAPE, "rows must be from 1 to 2^26 (got %lld)", (long long)rows);
+  if (rows < 1 || rows > (int64_t(1) << 24))
+    return fail(SPC_E_SHAPE, "rows must be from 1 to 2^24 (got %lld)", (long long)rows);
   if (!row_start && rows % P.B != 0)
     return fail(SPC_E_SHAPE, "%lld rows do not divide into %d sequences (no row_start)",
                 (long long)rows, P.B);
@@ -909,6 +924,10 @@ spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtyp
       attend_layout(P.B, P.H, heads, P.n, P.D, (int64_t)P.width * P.S);
   P.tile_rows = L.tile_rows;
   P.splits = L.splits;
+  const int64_t tiles = ((int64_t)P.n * (heads / P.H) + L.tile_rows - 1) / L.tile_rows;
+  if (tiles * (((int64_t)P.H * P.B * L.splits + 7) / 8 * 8) >= (int64_t(1) << 24))
+    return fail(SPC_E_SHAPE, "%d rows of each of %d sequences are too many for one call%s", P.n,
+                P.B, row_start ? ": pass max_rows" : "");
   if (L.bytes) {
     char* ws = nullptr;
     st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
@@ -929,15 +948,19 @@ spc_status spc_sample(const void* logits, int32_t dtype, int32_t B, int32_t V,
                       const float* uniforms, int32_t* out_token, float* out_logprob,
                       int32_t* out_kept, void* workspace, size_t workspace_bytes,
                       hipStream_t stream) {
-  return sample_impl(logits, dtype, B, V, row_stride, truncation, uniforms, out_token,
-                     out_logprob, out_kept, workspace, workspace_bytes, stream);
+  return guarded([&] {
+    return sample_impl(logits, dtype, B, V, row_stride, truncation, uniforms, out_token,
+                       out_logprob, out_kept, workspace, workspace_bytes, stream);
+  });
 }
 
 spc_status spc_truncate(const void* logits, int32_t dtype, int32_t B, int32_t rows_per_seq,
                         int32_t V, const spc_truncation* truncation, void* out_logits,
                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  return truncate_impl(logits, dtype, B, rows_per_seq, V, truncation, out_logits, workspace,
-                       workspace_bytes, stream);
+  return guarded([&] {
+    return truncate_impl(logits, dtype, B, rows_per_seq, V, truncation, out_logits, workspace,
+                         workspace_bytes, stream);
+  });
 }
 
 size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype) {
@@ -948,12 +971,16 @@ size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype) {
 spc_status spc_kv_write(const spc_kv_cache* cache, const void* k, const void* v, int32_t dtype,
                         int64_t k_stride, int64_t v_stride, int64_t rows,
                         const int32_t* row_start, hipStream_t stream) {
-  return kv_write_impl(cache, k, v, dtype, k_stride, v_stride, rows, row_start, stream);
+  return guarded([&] {
+    return kv_write_impl(cache, k, v, dtype, k_stride, v_stride, rows, row_start, stream);
+  });
 }
 
 spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int32_t dtype,
                        int32_t length, hipStream_t stream) {
-  return kv_read_impl(cache, out_k, out_v, dtype, length, stream);
+  return guarded([&] {
+    return kv_read_impl(cache, out_k, out_v, dtype, length, stream);
+  });
 }
 
 spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
@@ -961,8 +988,10 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
                          const int32_t* row_start, int32_t max_rows, float scale,
                          int32_t window, void* out, int64_t out_stride, void* workspace,
                          size_t workspace_bytes, hipStream_t stream) {
-  return kv_attend_impl(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
-                        window, out, out_stride, workspace, workspace_bytes, stream);
+  return guarded([&] {
+    return kv_attend_impl(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                          window, out, out_stride, workspace, workspace_bytes, stream);
+  });
 }
 
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,

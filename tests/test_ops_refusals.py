@@ -56,6 +56,7 @@ def test_sample_refusals(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(z=None), -1), (dict(out=None), -1), (dict(cut=None), -1), (dict(B=0), -2),
     (dict(rows=0), -2), (dict(V=1), -2), (dict(dtype=-1), -4), (dict(out=OK + 2), -5),
+    (dict(out=OK + 4), -4), (dict(out=OK - 47996), -4),  # overlapping, not the same
 ] + [(dict(cut=cut(**c)), -4) for c in BAD_CUTS])
 def test_truncate_refusals(kw, status):
     assert truncate(**kw) == status
@@ -121,7 +122,7 @@ def test_cache_refusals(kw, status):
 @pytest.mark.parametrize("call,kw,status", [
     (write, dict(k=None), -1), (write, dict(v=None), -1), (write, dict(dtype=2), -4),
     (write, dict(ks=255), -2), (write, dict(vs=0), -2), (write, dict(rows=0), -2),
-    (write, dict(rows=7), -2), (write, dict(rows=(1 << 26) + 1, start=OK), -2),
+    (write, dict(rows=7), -2), (write, dict(rows=(1 << 24) + 1, start=OK), -2),
     (write, dict(k=OK + 2), -5), (write, dict(dtype=spc.SPC_BF16, v=OK + 1), -5),
     (read, dict(k=None), -1), (read, dict(v=None), -1), (read, dict(dtype=2), -4),
     (read, dict(n=0), -2), (read, dict(n=(1 << 26) + 1), -2), (read, dict(v=OK + 4), -5),
@@ -129,6 +130,7 @@ def test_cache_refusals(kw, status):
     (attend, dict(heads=7), -2), (attend, dict(heads=0), -2), (attend, dict(qs=1023), -2),
     (attend, dict(os=1000), -2), (attend, dict(rows=5), -2), (attend, dict(start=OK, most=0), -2),
     (attend, dict(scale=NAN), -4), (attend, dict(scale=INF), -4), (attend, dict(window=-1), -4),
+    (attend, dict(rows=1 << 24, start=OK, most=1 << 24, heads=64, qs=8192, os=8192), -2),
     (attend, dict(q=OK + 1), -5), (attend, dict(out=OK + 4), -5), (attend, dict(os=1026), -5),
 ])
 def test_cache_call_refusals(call, kw, status):
@@ -203,6 +205,20 @@ def test_binding_refuses_shapes_types_and_layouts():
         spc.spc_kv_read(k, v, table, n)                     # neither length nor out
     with pytest.raises(ValueError):
         spc.spc_kv_read(k, v, table, n, 5, out=(new, new))
+
+
+def test_binding_refuses_host_tensors():
+    """Nothing of the host's reaches a kernel."""
+    z, u = torch.zeros(3, 50), torch.zeros(3)
+    k, v = pages()
+    table, n = torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    new = torch.zeros((3, 2, 2, 64))
+    for call in (lambda: spc.spc_sample(z, u), lambda: spc.spc_truncate(z, top_k=3),
+                 lambda: spc.spc_kv_write(new, new, k, v, table, n),
+                 lambda: spc.spc_kv_read(k, v, table, n, 5),
+                 lambda: spc.spc_kv_attend(new.bfloat16(), k, v, table, n)):
+        with pytest.raises(ValueError, match="current HIP device"):
+            call()
 
 
 def test_binding_takes_empty_chunks():
