@@ -880,15 +880,15 @@ struct AttendLayout {
   size_t bytes;
 };
 AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t D,
-                           int64_t tokens) {
+                           int64_t tokens, bool f8) {
   AttendLayout L;
   const int64_t rows = n * (heads / H);
   L.tile_rows = rows <= 16 ? 16 : rows <= 32 || (D > 128 && rows <= 64) ? 32 : rows <= 64 ? 64 : 128;
   const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
-  // shares of at least 512 keys, up to four workgroups to a compute unit
-  const int64_t most = std::max<int64_t>(1, tokens / 512);
+  // up to four workgroups to a compute unit
+  const int64_t most = std::max<int64_t>(1, tokens / spc::kv_share_keys(L.tile_rows, f8));
   L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
-                                                     (int64_t)64, 65535 / B}));
+                                                     (int64_t)spc::kKvShares, 65535 / B}));
   L.bytes = L.splits > 1 ? (size_t)(groups * L.splits * L.tile_rows) * (size_t)(D + 2) * 4 : 0;
   return L;
 }
@@ -921,7 +921,7 @@ spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtyp
   P.out = out;
   P.out_stride = out_stride;
   const AttendLayout L =
-      attend_layout(P.B, P.H, heads, P.n, P.D, (int64_t)P.width * P.S);
+      attend_layout(P.B, P.H, heads, P.n, P.D, (int64_t)P.width * P.S, P.f8);
   P.tile_rows = L.tile_rows;
   P.splits = L.splits;
   const int64_t tiles = ((int64_t)P.n * (heads / P.H) + L.tile_rows - 1) / L.tile_rows;
@@ -1001,7 +1001,7 @@ size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t 
     return 0;
   const int64_t n = max_rows > 0 ? std::min<int64_t>(max_rows, rows) : rows / cache->B;
   return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
-                       (int64_t)cache->table_width * cache->page_size)
+                       (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
       .bytes;
 }
 

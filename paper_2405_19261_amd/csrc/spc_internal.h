@@ -247,6 +247,8 @@ struct KvParams {
 };
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
+constexpr int kKvShares = 128;                // shares the keys of a row are cut into, at most
+int kv_share_keys(int tile_rows, bool f8);  // keys that a share of them has at least
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream);
 
 // Enqueue a kernel writing `bytes` zero bytes at `ptr` (a multiple of 4, ptr

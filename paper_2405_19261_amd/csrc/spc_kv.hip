@@ -368,21 +368,26 @@ __device__ __forceinline__ void first_of(u32x4& w, int n) {
 // Statistics and O are held in 32 bits; P is rounded to bfloat16 (by at most
 // 2^-8) for the matrix unit, its sum is of the values before that.
 constexpr int kAttendWaves = 4;
-constexpr int kShareKeys = 512;  // a share of the keys has at least as many
+// A share of the keys has at least as many: a tile for each wavefront, or in
+// k_kv_attend_rows, whose wavefronts take every tile together, 512.  (One token
+// over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of 512, 6.9 in shares
+// of 128, and the join 4.4.)
+
+constexpr int share_keys(int tile_rows, bool f8) { return tile_rows > 64 ? 512 : f8 ? 256 : 128; }
 
 // The keys that rows of a chunk's tokens i0 .. i1 see: tiles of T from `begin`
 // (a multiple of T), cut into shares of `per` tiles.
 struct Span {
   int32_t begin, tiles, shares, per;
 };
-template <int T>
+template <int T, int MIN>
 __device__ __forceinline__ Span span_of(const KvParams& P, int32_t len, int n, int i0, int i1,
                                         int splits) {
   const int32_t end = min(min(len, P.width * P.S), len - n + i1 + 1);
   Span s;
   s.begin = P.window > 0 ? max(len - n + i0 - P.window + 1, 0) & ~(T - 1) : 0;
   s.tiles = end > s.begin ? (end - s.begin + T - 1) / T : 0;
-  s.shares = max(1, min(splits, s.tiles / (kShareKeys / T)));
+  s.shares = max(1, min(splits, s.tiles / (MIN / T)));
   s.per = (s.tiles + s.shares - 1) / s.shares;
   return s;
 }
@@ -413,7 +418,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
   if (r0 >= rows) return;
   const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S);
   const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
-  const Span span = span_of<T>(P, len, ch.n, i0, i1, P.splits);
+  const Span span = span_of<T, share_keys(16 * MT, F8)>(P, len, ch.n, i0, i1, P.splits);
   if (share >= span.shares) return;
   const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
   const int32_t pos0 = len - ch.n;
@@ -684,7 +689,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * kRows;
   if (r0 >= rows) return;
   const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S), pos0 = len - ch.n;
-  const Span span = span_of<T>(P, len, ch.n, (int)(r0 / G), (int)((min(r0 + kRows, rows) - 1) / G),
+  const Span span = span_of<T, share_keys(kRows, F8)>(P, len, ch.n, (int)(r0 / G), (int)((min(r0 + kRows, rows) - 1) / G),
                                P.splits);
   if (share >= span.shares) return;
   const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
@@ -893,7 +898,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
 }
 
 // The shares of a row joined, in their order: a wavefront a row.
-template <int D, int T>
+template <int D, int T, int MIN>
 __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
   const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63;
   const Chunk ch = chunk_of(P, b);
@@ -903,22 +908,41 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
   if (r >= rows) return;
   const int64_t x = r / tile_rows, tiles_x = ((int64_t)P.n * G + tile_rows - 1) / tile_rows;
   const int64_t r0 = x * tile_rows;
-  const Span span = span_of<T>(P, max(P.len[b], 0), ch.n, (int)(r0 / G), (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
+  const Span span = span_of<T, MIN>(P, max(P.len[b], 0), ch.n, (int)(r0 / G), (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
   if (span.shares == 1) return;
   const auto part = [&](int s) {
     return P.part + (((((int64_t)b * P.splits + s) * P.H + h) * tiles_x + x) * tile_rows + (r - r0)) *
                         (int64_t)(D + 2);
   };
-  float top = kNegInf;
-  for (int s = 0; s < span.shares; ++s) top = fmaxf(top, part(s)[0]);
-  constexpr int E = D / 64;
-  float sum = 0.0f, y[E] = {};
-  for (int s = 0; s < span.shares; ++s) {
-    const float* p = part(s);
-    const float fade = p[0] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(p[0] - top);
-    sum += p[1] * fade;
+  // the shares' maxima and sums, a lane a share (two: at most kKvShares)
+  static_assert(kKvShares == 128, "two a lane");
+  const float m0 = lane < span.shares ? part(lane)[0] : kNegInf;
+  const float m1 = lane + 64 < span.shares ? part(lane + 64)[0] : kNegInf;
+  float sum = lane < span.shares ? part(lane)[1] : 0.0f;
+  float sum1 = lane + 64 < span.shares ? part(lane + 64)[1] : 0.0f;
+  float top = fmaxf(m0, m1);
 #pragma unroll
-    for (int e = 0; e < E; ++e) y[e] += p[2 + lane * E + e] * fade;
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float f0 = m0 == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m0 - top);
+  const float f1 = m1 == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m1 - top);
+  sum = sum * f0 + sum1 * f1;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  constexpr int E = D / 64;
+  float y[E] = {};
+  for (int s0 = 0; s0 < span.shares; s0 += 8) {  // eight shares' values under way together
+    float v[8][E];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = part(min(s0 + k, span.shares - 1))[2 + lane * E + e];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int s = s0 + k;
+      const float fade = s < span.shares ? __shfl(s < 64 ? f0 : f1, s & 63) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] += v[k][e] * fade;
+    }
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   const int i = (int)(r / G), g = (int)(r % G);
@@ -977,11 +1001,13 @@ void attend(const KvParams& P, hipStream_t stream) {
   else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
   if (P.splits > 1) {
     const dim3 join((uint32_t)((rows + 3) / 4), P.H, P.B);
-    if (P.tile_rows == 128) k_kv_join<D, rows_tile(D, F8)><<<join, 256, 0, stream>>>(P, 128);
-    else k_kv_join<D, F8 ? 64 : 32><<<join, 256, 0, stream>>>(P, P.tile_rows);
+    if (P.tile_rows == 128) k_kv_join<D, rows_tile(D, F8), share_keys(128, F8)><<<join, 256, 0, stream>>>(P, 128);
+    else k_kv_join<D, F8 ? 64 : 32, share_keys(64, F8)><<<join, 256, 0, stream>>>(P, P.tile_rows);
   }
 }
 }  // namespace
+
+int kv_share_keys(int tile_rows, bool f8) { return share_keys(tile_rows, f8); }
 
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream) {
   if (P.D == 64) P.f8 ? attend<64, true>(P, stream) : attend<64, false>(P, stream);
