@@ -451,7 +451,8 @@ spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int3
  *               longer one past it are left as they are); else ignored
  * Scores, softmax statistics and sums are in 32 bits; probabilities enter the
  * second product in bfloat16.  Cached tokens below kv_len are finite (not
- * checked); what lies at or past it may be anything.
+ * checked: a NaN in one makes the rows that see it NaN, and may make rows NaN
+ * that do not); what lies at or past kv_len may be anything.
  *   workspace   a 256-byte aligned buffer of at least
  *               spc_kv_workspace_bytes(...) bytes, or NULL for the internal
  *               per-device workspace (see the conventions above)

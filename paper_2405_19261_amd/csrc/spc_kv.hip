@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
         l[mt] += w;
         if constexpr (F8) {
           w *= vs[e >> 2][e & 3];
-          if (!whole) w = x[e] > kNegInf ? w : 0.0f;  // (an unseen key's scale may be junk)
+          if (!whole) w = x[e] == kNegInf ? 0.0f : w;  // (an unseen key's scale may be junk)
         }
         p[mt][e >> 3][e & 7] = (__bf16)w;
       }
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) 
         y += *reinterpret_cast<const f32x4*>(&o_lds[w][row][d]);
       }
       if (alone) {
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         const int i = (int)(r / G), g = (int)(r % G);
         bf16x4 z;
 #pragma unroll
@@ -832,7 +832,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
         l[mt] += w;
         if constexpr (F8) {
           w *= scales[buf][1][kG * j + e];
-          if (!whole) w = x[mt][e] > kNegInf ? w : 0.0f;  // (an unseen key's scale may be junk)
+          if (!whole) w = x[mt][e] == kNegInf ? 0.0f : w;  // (an unseen key's scale may be junk)
         }
         p[mt][e >> 3][e & 7] = (__bf16)w;
       }
@@ -871,7 +871,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     const int64_t r = w0 + 16 * mt + c16;
     if (r >= rows) continue;
     if (alone) {
-      const float inv = l[mt] > 0.0f ? 1.0f / l[mt] : 0.0f;
+      const float inv = l[mt] == 0.0f ? 0.0f : 1.0f / l[mt];
       const int i = (int)(r / G), g = (int)(r % G);
       uint16_t* out = static_cast<uint16_t*>(P.out) + (ch.first + i) * P.out_stride +
                       (int64_t)(h * G + g) * D + 4 * j;
@@ -944,7 +944,7 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
       for (int e = 0; e < E; ++e) y[e] += v[k][e] * fade;
     }
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int i = (int)(r / G), g = (int)(r % G);
   __bf16* out = static_cast<__bf16*>(P.out) + (ch.first + i) * P.out_stride + (int64_t)(h * G + g) * D;
 #pragma unroll

@@ -244,6 +244,28 @@ def test_attend_strided_queries_and_outputs(f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n,L", [(1, 40), (3, 700), (40, 300), (140, 300)])
+def test_a_nan_that_a_row_sees_is_its_answer(n, L, f8):
+    """A NaN among the keys or values a row sees is not lost: the row (the value's
+    dimension of it) is NaN, wherever in a tile the key lies."""
+    H, heads, D, S = 1, 4, 128, 16
+    cache = ops_oracle.Cache(2, (L + S - 1) // S, H, D, S, f8, DEV)
+    fill(cache, [L, L], 3)
+    at = L - n  # the first row's own position: every row sees it
+    page, slot = int(cache.table[0, at // S]), at % S
+    nan = torch.tensor(0x7f, dtype=torch.uint8) if f8 else torch.tensor(float("nan"), dtype=BF16)
+    cache.k[page, 0, slot, 5:6].view(torch.uint8 if f8 else BF16).fill_(nan.item())
+    page, slot = int(cache.table[1, at // S]), at % S
+    cache.v[page, 0, 7, slot:slot + 1].view(torch.uint8 if f8 else BF16).fill_(nan.item())
+    q = randn((2, n, heads, D), 4).to(DEV)
+    out = spc.spc_kv_attend(q, *cache.args(i32([L, L])), **cache.scales()).float()
+    assert bool(out[0].isnan().all())
+    assert bool(out[1, ..., 7].isnan().all())
+    rest = torch.cat([out[1, ..., :7], out[1, ..., 8:]], -1)
+    assert not bool(rest.isnan().any())
+
+
+@pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("s,scale", [(12.0, None), (1.0, 0.0), (1.0, -0.3), (0.01, 1.0)])
 def test_attend_scales_and_peaked_scores(s, scale, f8):
     """Scores of hundreds (a softmax of one key), equal scores, a negative scale."""
