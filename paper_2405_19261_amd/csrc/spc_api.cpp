@@ -625,10 +625,10 @@ spc::TruncParams truncated_rows(const void* logits, int64_t R, int32_t rows_per_
   return P;
 }
 
-// How rows of V entries are taken: held by a workgroup, or in slices of
-// `loads` lane loads a thread, `rows` of them a launch.
+// How rows of V entries are taken: held by a workgroup, or in slices; `rows` of
+// them a launch.
 struct TruncLayout {
-  int32_t slices = 0, loads = 0;
+  int32_t slices = 0;
   int64_t rows = spc::kMaxRows;
   size_t max, bins, weights, kept, plans, items, total = 0;
 };
@@ -636,9 +636,8 @@ TruncLayout trunc_layout(int64_t R, int32_t V, int32_t dtype) {
   TruncLayout L;
   L.rows = std::min<int64_t>(R, spc::kMaxRows);
   if (V <= spc::kTruncHeld) return L;
-  L.loads = 4;
-  L.slices = (int32_t)(((int64_t)V + spc::trunc_slice_elems(dtype, L.loads) - 1) /
-                       spc::trunc_slice_elems(dtype, L.loads));
+  const int64_t slice = spc::trunc_slice_elems(dtype);
+  L.slices = (int32_t)((V + slice - 1) / slice);
   const size_t row = (size_t)L.slices * (8 * spc::kTruncBins + 8 * 16 + 8) +
                      spc::trunc_plan_bytes() + spc::kTruncItems * spc::trunc_item_bytes();
   L.rows = std::max<int64_t>(1, std::min<int64_t>(L.rows, (size_t(256) << 20) / row));
@@ -706,7 +705,6 @@ spc_status truncated_impl(const spc::TruncParams& base, int32_t dtype, void* wor
       P.out_kept = offset(base.out_kept, r0);
       if (L.total) {
         P.slices = L.slices;
-        P.slice_loads = L.loads;
         P.items_max = spc::kTruncItems;
         P.slice_bins = reinterpret_cast<uint64_t*>(ws + L.bins);
         P.sub_weight = reinterpret_cast<uint64_t*>(ws + L.weights);

@@ -1,5 +1,5 @@
 // spc_internal.h -- structures shared by the C interface (spc_api.cpp) and the
-// gfx950 kernels (spc_kernels.hip).  Not part of the public interface.
+// gfx950 kernels (spc_kernels.hip, spc_sample.hip, spc_kv.hip).  Not part of the public interface.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -194,10 +194,9 @@ struct TruncParams {
   int32_t* out_token;
   float* out_logprob;
   int32_t* out_kept;
-  // rows of more than kTruncHeld entries: `slices` of them a row (0: a
-  // workgroup holds the row), slice_loads lane loads a thread each, and the
-  // workspace of a launch's R rows
-  int32_t slices, slice_loads;
+  // rows of more than kTruncHeld entries: slices of a row (0: a workgroup holds
+  // the row), and the workspace of a launch's R rows
+  int32_t slices;
   int32_t items_max;         // entries of a row's list
   float* slice_max;          // [R][slices]
   uint64_t* slice_bins;      // [R][slices][kTruncBins]
@@ -207,7 +206,7 @@ struct TruncParams {
   void* items;               // [R][items_max] of trunc_item_bytes()
 };
 constexpr int kTruncHeld = 32768, kTruncBins = 1024, kTruncItems = 8192;
-int trunc_slice_elems(int dtype, int loads);  // entries of a slice
+int trunc_slice_elems(int dtype);  // entries of a slice
 size_t trunc_plan_bytes();
 size_t trunc_item_bytes();
 hipError_t launch_truncated(const TruncParams& P, int dtype, hipStream_t stream);
