@@ -905,8 +905,12 @@ __device__ __forceinline__ uint64_t find_sum(Shared& S, uint64_t own, bool first
   const uint64_t sum = lane_value(ws, 15);
   in += wave ? lane_value(ws, wave - 1) : 0;
   if (first) {
-    const double x = fmin((double)u * (double)sum, (double)sum);
-    thr = x > 0.0 ? min((uint64_t)x, sum - 1) : 0;
+    // floor(u sum), exactly (u is a float32, 2^56 u an integer but for u under
+    // 2^-32): a uniform that falls on the border between two tokens is decided
+    // as the definition says, in a row of equal weights too
+    const uint64_t x = u > 0.0f ? (uint64_t)(fmin((double)u, 1.0) * 0x1p56) : 0;
+    const uint64_t at_u = (uint64_t)__umul64hi(sum, x) << 8 | (sum * x) >> 56;
+    thr = at_u < sum ? at_u : sum - 1;
   }
   if (in > thr && in - own <= thr) {  // one thread
     S.sum_at = (int)threadIdx.x;

@@ -289,6 +289,58 @@ def test_attend_long_caches(B, n, L, H, heads, f8):
     assert torch.equal(a, spc.spc_kv_attend(q, *cache.args(i32(lens)), **cache.scales()))
 
 
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("B,n,L,H,heads,D,window", [(1, 70, 6000, 1, 2, 64, 0), (2, 130, 3000, 1, 1, 128, 0),
+                                                    (1, 33, 5000, 1, 4, 256, 0), (1, 65, 4000, 1, 2, 64, 2500)])
+def test_many_rows_over_shares_of_the_keys(B, n, L, H, heads, D, window, f8):
+    S = 32
+    cache = ops_oracle.Cache(B, (L + S - 1) // S, H, D, S, f8, DEV)
+    lens = [L - 401 * b for b in range(B)]
+    fill(cache, lens, 3)
+    check_attend(cache, randn((B, n, heads, D), 4).to(DEV), lens, window=window)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n,heads", [(3, 2), (20, 2), (90, 2), (1, 64)])
+@pytest.mark.parametrize("S", [16, 48, 1024])
+def test_attend_around_missing_pages(S, n, heads, f8):
+    """Pages missing at the start, in the middle and at the end, for every kernel."""
+    B, H, D, width = 3, 1, 64, 1 + 400 // S
+    cache = ops_oracle.Cache(B, width + 1, H, D, S, f8, DEV, seed=S)
+    lens = [min(400, S * width), n, min(371, S * width)]
+    fill(cache, lens, 5)
+    for b, at in ((0, 0), (0, width // 2), (2, width - 1)):
+        cache.table[b, at] = -5 if at else cache.pages + 7
+    check_attend(cache, randn((B, n, heads, D), 6).to(DEV), lens)
+
+
+def test_a_capture_that_needs_a_larger_workspace_is_refused():
+    """As for the verify calls: the call says so, and an eager call first mends it."""
+    spc.spc_release()
+    B, H, heads, D, S, L = 1, 1, 2, 64, 16, 4000
+    cache = ops_oracle.Cache(B, L // S, H, D, S, False, DEV)
+    fill(cache, [L], 1)
+    q, lens = randn((B, 1, heads, D), 2).to(DEV), i32([L])
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(spc.SpcError) as e:
+            spc.spc_kv_attend(q, *cache.args(lens), out=out)
+        assert e.value.status == -6
+        out.zero_()
+    want = spc.spc_kv_attend(q, *cache.args(lens))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        spc.spc_kv_attend(q, *cache.args(lens), out=out)
+    for _ in range(2):
+        out.fill_(1.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
 def test_attend_offsets_past_32_bits():
     """Pages whose byte offsets pass 2^32: the last of 600 000 pages of 8 KiB."""
     S, H, D, pages = 16, 2, 128, 600_000

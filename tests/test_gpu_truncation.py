@@ -210,6 +210,37 @@ def test_scalar_settings_and_strided_rows():
     check_sample(rows, u[:5], [(1.0, 9, 1.0, 0.0)] * 5)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [32768, 32769, 40001])
+def test_strided_long_rows(V, dtype):
+    """Positions of a [B, 3, V] tensor, and rows that start at odd elements."""
+    z = logits(5 * 3, V, dtype, 4).view(5, 3, V)
+    u = np.random.RandomState(7).random_sample(5).astype(np.float32)
+    settings = [SETTINGS[i] for i in (0, 1, 3, 5, 8)]
+    check_sample(z.to(DEV)[:, 1], u, settings)
+    flat = torch.zeros(5 * (V + 3) + 1, dtype=z.dtype, device=DEV)
+    rows = flat[1:].view(5, V + 3)[:, :V]
+    rows.copy_(z[:, 2])
+    check_sample(rows, u, settings)
+    check_truncate(z[:, 0].contiguous().view(5, 1, V), settings, 1)
+
+
+@pytest.mark.parametrize("V", [3001, 70001])
+def test_bins_that_hold_thousands(V):
+    """Cuts that end among many entries of nearly one probability, inside and
+    outside the bins near the maximum, more than are ranked or held."""
+    g = torch.Generator().manual_seed(V)
+    z = torch.stack([-1.0 + 1e-3 * torch.randn(V, generator=g), torch.randint(0, 2, (V,), generator=g) * 0.01,
+                     torch.cat([torch.full((1,), 30.0), -20.0 + 1e-4 * torch.randn(V - 1, generator=g)]),
+                     torch.full((V,), 2.5), torch.randn(V, generator=g) * 1e-6])
+    u = np.array([0.1, 0.5, 0.3, 0.77, 0.999], np.float32)
+    for s in ((1.0, 1500, 1.0, 0.0), (1.0, 0, 0.5, 0.0), (0.3, 2000, 0.25, 0.0), (1.0, V - 1, 0.75, 0.0)):
+        for dtype in ("f32", "bf16"):
+            zz = z.to(DT[dtype])
+            check_sample(zz, u, [s] * 5)
+            check_truncate(zz.view(5, 1, V), [s] * 5, 1)
+
+
 @pytest.mark.parametrize("V,B", [(1000, 4), (32128, 3), (100000, 5)])
 def test_graph_replays_and_streams(V, B):
     """Captured calls replay on new inputs as eager ones, with eager work between."""
