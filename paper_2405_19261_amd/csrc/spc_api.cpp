@@ -881,7 +881,20 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
                            int64_t tokens, bool f8) {
   AttendLayout L;
   const int64_t rows = n * (heads / H);
-  L.tile_rows = rows <= 16 ? 16 : rows <= 32 || (D > 128 && rows <= 64) ? 32 : rows <= 64 ? 64 : 128;
+  // Rows a workgroup takes.  More of them read the keys less often, from a die's
+  // cache; fewer leave registers for two wavefronts a SIMD, of which 8-bit keys,
+  // widened as they come, need more.  us of 32 sequences over 4096 tokens, 8
+  // key/value heads, by tiles of 16 / 32 / 128 rows:
+  //   bf16 heads of 128: 32 rows 157 / 116 / 155, 64: 250 / 164 / 165, 96: 369 /
+  //     227 / 171, 128: 482 / 255 / 183; of 64: 32 rows 80 / 72 / 106, 64: 125 / 109
+  //     / 116, 128: 239 / 160 / 128; of 256: 32 rows 310 / 278 / 485, 64: 525 / 429 /
+  //     483, 128: 1010 / 712 / 541
+  //   e4m3 heads of 128: 32 rows 93 / 104 / 162, 64: 126 / 157 / 174, 96: 181 / 221 /
+  //     183, 128: 236 / 233 / 189; of 256: 32 rows 183 / 246 / 402, 64: 285 / 378 /
+  //     415, 128: 533 / 594 / 441; of 64: 32 rows 62 / 51 / 132, 128: 127 / 107 / 152,
+  //     256: 228 / 198 / 277
+  if (f8 && D > 64) L.tile_rows = rows <= 64 ? 16 : 128;
+  else L.tile_rows = rows <= 16 ? 16 : rows <= (f8 ? 256 : 64) ? 32 : 128;
   const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
   // up to four workgroups to a compute unit
   const int64_t most = std::max<int64_t>(1, tokens / spc::kv_share_keys(L.tile_rows, f8));

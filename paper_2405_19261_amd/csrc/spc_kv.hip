@@ -252,7 +252,7 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b) {
 // 64 positions of a head by a workgroup, in groups of 16 (a group lies in one
 // page).  Keys go from 16-byte loads to 16-byte stores; values are turned around
 // in LDS, in 32 bits.  Bound by the bytes: 134M values of e4m3 to bfloat16 take
-// 85 us (4.8 TB/s); one wavefront a position, whose loads of a value's
+// 96 us (4.2 TB/s); one wavefront a position, whose loads of a value's
 // dimensions lie a page row apart, took 244.
 template <int DST, bool F8, int D>
 __global__ void __launch_bounds__(256) k_kv_read(KvParams P) {
@@ -366,7 +366,10 @@ __device__ __forceinline__ void first_of(u32x4& w, int n) {
 // are two steps of the products, so there T = 64, else 32.  Which dimension
 // stands where in Q K^T does not matter so long as Q is loaded alike.
 // Statistics and O are held in 32 bits; P is rounded to bfloat16 (by at most
-// 2^-8) for the matrix unit, its sum is of the values before that.
+// 2^-8) for the matrix unit, its sum is of the values before that.  Bound by the
+// bytes of the cache for few rows (32 sequences over 4096 bfloat16 tokens, 8
+// heads of 128: one row 103 us, 5.2 TB/s, 8 rows of 4 heads each 116), by the
+// vector instructions of the softmax and of widening 8 bits for more.
 constexpr int kAttendWaves = 4;
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512.  (One token
@@ -392,8 +395,15 @@ __device__ __forceinline__ Span span_of(const KvParams& P, int32_t len, int n, i
   return s;
 }
 
+// Wavefronts a SIMD that registers are kept free for: two where they then do not
+// spill.
+constexpr int attend_waves(int D, bool f8, int mt) {
+  return D <= 128 && mt * D <= (f8 ? 128 : 256) ? 2 : 1;
+}
+
 template <int D, bool F8, int MT>
-__global__ void __launch_bounds__(64 * kAttendWaves, MT * D <= (F8 ? 128 : 256) && D <= 128 ? 2 : 1) k_kv_attend(KvParams P) {
+__global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
+    k_kv_attend(KvParams P) {
   constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
   constexpr int kQuarters = T / 16, kG = T / 4;  // score tiles; a lane's keys
   constexpr int kL = D * EB / 64;                // 16-byte loads of a key row by four lanes
@@ -663,8 +673,9 @@ constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
 // double-buffered: the next tile's are written behind the products of this one
 // and the loads of the one after it are then under way.  What bounds it is the
 // LDS, whose reads of a tile take as long as the products of 32 rows with it,
-// and the softmax's vector instructions; with 64 rows a wavefront, whose O fills
-// the registers of a whole SIMD, nothing hides them.
+// and the softmax's vector instructions: 4 chunks of 1024 rows over 4096 tokens,
+// 32/8 heads of 128, take 406 us in bfloat16 (593 TFLOP/s; 515 with 32 keys a
+// tile, 653 with 64 rows a workgroup and its wavefronts apart over the keys).
 template <int D, bool F8>
 __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
   constexpr int MT = 2, kRows = 16 * MT * kAttendWaves;
@@ -689,8 +700,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * kRows;
   if (r0 >= rows) return;
   const int32_t len = max(P.len[b], 0), there = min(len, P.width * P.S), pos0 = len - ch.n;
-  const Span span = span_of<T, share_keys(kRows, F8)>(P, len, ch.n, (int)(r0 / G), (int)((min(r0 + kRows, rows) - 1) / G),
-                               P.splits);
+  const Span span =
+      span_of<T, share_keys(kRows, F8)>(P, len, ch.n, (int)(r0 / G),
+                                        (int)((min(r0 + kRows, rows) - 1) / G), P.splits);
   if (share >= span.shares) return;
   const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
 
@@ -908,7 +920,8 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
   if (r >= rows) return;
   const int64_t x = r / tile_rows, tiles_x = ((int64_t)P.n * G + tile_rows - 1) / tile_rows;
   const int64_t r0 = x * tile_rows;
-  const Span span = span_of<T, MIN>(P, max(P.len[b], 0), ch.n, (int)(r0 / G), (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
+  const Span span = span_of<T, MIN>(P, max(P.len[b], 0), ch.n, (int)(r0 / G),
+                                    (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
   if (span.shares == 1) return;
   const auto part = [&](int s) {
     return P.part + (((((int64_t)b * P.splits + s) * P.H + h) * tiles_x + x) * tile_rows + (r - r0)) *
@@ -956,9 +969,11 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows) {
 namespace {
 template <int SRC, bool F8>
 void write(const KvParams& P, hipStream_t stream) {
-  // rows by tiles where sequences bring 32 of them or more (16 and 17 rows a
-  // sequence: a wavefront a row and head is as fast)
-  if (P.rows >= 32 * (int64_t)P.B) {
+  // Rows by tiles where sequences bring many.  us by row / by tile, 8 heads of 128:
+  // into bfloat16, 32 sequences of 16 rows 8.8 / 9.3, of 24 9.2 / 9.2, of 32 11.0 /
+  // 9.2, 4 of 512 17.9 / 9.6; into e4m3, 32 of 32 11.7 / 17.4, of 64 17.4 / 18.7, of
+  // 128 28.4 / 22.1, 8 of 1000 51 / 30.
+  if (P.rows >= (F8 ? 128 : 32) * (int64_t)P.B) {
     const dim3 grid((uint32_t)((P.rows + 63) / 64), P.H), block(256);
     if (P.D == 64) k_kv_write_tile<SRC, F8, 64><<<grid, block, 0, stream>>>(P);
     else if (P.D == 128) k_kv_write_tile<SRC, F8, 128><<<grid, block, 0, stream>>>(P);
@@ -996,13 +1011,14 @@ void attend(const KvParams& P, hipStream_t stream) {
   const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups));
   const dim3 block(64 * kAttendWaves);
   if (P.tile_rows == 16) k_kv_attend<D, F8, 1><<<grid, block, 0, stream>>>(P);
-  else if (P.tile_rows == 32) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
   else if (P.tile_rows == 128) k_kv_attend_rows<D, F8><<<grid, block, 0, stream>>>(P);
-  else if constexpr (D <= 128) k_kv_attend<D, F8, 4><<<grid, block, 0, stream>>>(P);
+  else if constexpr (!F8 || D == 64) k_kv_attend<D, F8, 2><<<grid, block, 0, stream>>>(P);
   if (P.splits > 1) {
     const dim3 join((uint32_t)((rows + 3) / 4), P.H, P.B);
-    if (P.tile_rows == 128) k_kv_join<D, rows_tile(D, F8), share_keys(128, F8)><<<join, 256, 0, stream>>>(P, 128);
-    else k_kv_join<D, F8 ? 64 : 32, share_keys(64, F8)><<<join, 256, 0, stream>>>(P, P.tile_rows);
+    if (P.tile_rows == 128)
+      k_kv_join<D, rows_tile(D, F8), share_keys(128, F8)><<<join, 256, 0, stream>>>(P, 128);
+    else
+      k_kv_join<D, F8 ? 64 : 32, share_keys(64, F8)><<<join, 256, 0, stream>>>(P, P.tile_rows);
   }
 }
 }  // namespace

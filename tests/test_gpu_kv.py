@@ -112,6 +112,30 @@ def test_write_and_read(S, H, D, dtype, f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("S,lens", [(16, [131, 300, 129]), (48, [400, 7, 257]), (128, [129, 128, 255])])
+def test_long_chunks_written(S, lens, D, f8):
+    """Chunks long enough to be written in tiles, from any slot, sequence after
+    sequence inside a tile."""
+    B, H = len(lens), 2
+    cache = ops_oracle.Cache(B, (max(lens) + 5 + S - 1) // S, H, D, S, f8, DEV, seed=D)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    k, v = randn((int(start[-1]), H, D), 1, F32), randn((int(start[-1]), H, D), 2, F32)
+    at = np.array(lens) + [5, 0, 3]  # the chunks begin at slots 5, 0 and 3
+    spc.spc_kv_write(k.to(DEV), v.to(DEV), *cache.args(i32(at)), q_start=i32(start), **cache.scales())
+    for b in range(B):
+        kd, vd, _ = cache.dense(b, int(at[b]))
+        for got, x in ((kd, k), (vd, v)):
+            x = x[start[b]:start[b + 1]]
+            if f8:
+                codes, scale = ops_oracle.quantised(x.numpy())
+                want = codes * scale[..., None].astype(np.float64)
+            else:
+                want = x.to(BF16).double().numpy()
+            np.testing.assert_array_equal(got[at[b] - lens[b]:], want)
+
+
+@pytest.mark.parametrize("f8", [False, True])
 def test_write_a_chunk_behind_what_is_there(f8):
     """Uniform chunks at any offset into a page leave the tokens before them alone."""
     B, S, H, D, n = 5, 16, 2, 64, 9
