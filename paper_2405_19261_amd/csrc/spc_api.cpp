@@ -588,6 +588,7 @@ spc_status guarded(F&& body) noexcept {
   try {
     return body();
   } catch (...) {
+    g_err = "host exception";  // (short enough to need no allocation)
     return SPC_E_HIP;
   }
 }
