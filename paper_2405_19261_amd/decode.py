@@ -137,17 +137,21 @@ class GpuBackend:
     the rules they hold.
 
     ``truncate`` (called before ``prepare`` where the rounds are truncated)
-    takes top_k, top_p and min_p as [B] tensors."""
+    takes top_k, top_p and min_p as [B] tensors.  They hold for one run: the
+    next ``prepare`` without a ``truncate`` before it leaves distributions
+    whole again."""
 
     def __init__(self):
         self._scalar = None
         self._rules_present = 0
-        self._cut = None
+        self._cut = self._next_cut = None
 
     def truncate(self, top_k, top_p, min_p):
-        self._cut = dict(top_k_per_seq=top_k, top_p_per_seq=top_p, min_p_per_seq=min_p)
+        self._cut = self._next_cut = dict(top_k_per_seq=top_k, top_p_per_seq=top_p,
+                                          min_p_per_seq=min_p)
 
     def prepare(self, rule, alpha, temperature):
+        self._cut, self._next_cut = self._next_cut, None
         r, a, t = rule.cpu(), alpha.cpu(), temperature.cpu()
         self._rules_present = sum(1 << int(x) for x in set(r.tolist()) if 0 <= x < 31)
         same = bool((r == r[0]).all() and (a == a[0]).all() and (t == t[0]).all())
