@@ -464,8 +464,8 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
                          size_t workspace_bytes, hipStream_t stream);
 
 /* Bytes of device workspace one spc_kv_attend call of these sizes needs (its
- * contents need no preparation); max_rows as there, 0 without row_start.  Of
- * the cache only its sizes are read. */
+ * contents need no preparation; 0: none, or sizes that no call takes); max_rows
+ * as there, 0 without row_start.  Of the cache only its sizes and type are read. */
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
                               int32_t max_rows);
 

@@ -770,14 +770,8 @@ spc_status truncate_impl(const void* logits, int32_t dtype, int32_t B, int32_t r
   return truncated_impl(P, dtype, workspace, workspace_bytes, stream);
 }
 
-// The checks every cache call makes of the cache, and its parameters.
-spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
-  if (!c || !c->k_pages || !c->v_pages || !c->page_table || !c->kv_len)
-    return fail(SPC_E_NULL, "a required pointer is NULL");
-  if (c->dtype != SPC_BF16 && c->dtype != SPC_E4M3)
-    return fail(SPC_E_PARAM, "unknown cache dtype %d", c->dtype);
-  const bool f8 = c->dtype == SPC_E4M3;
-  if (f8 && (!c->k_scale || !c->v_scale)) return fail(SPC_E_NULL, "an e4m3 cache needs its scales");
+// The sizes of a cache.
+spc_status check_cache_sizes(const spc_kv_cache* c) {
   if (c->B < 1 || c->B > 65535 || c->num_pages < 1 || c->table_width < 1 || c->kv_heads < 1 ||
       c->kv_heads > 65535)
     return fail(SPC_E_SHAPE, "bad cache: B=%d num_pages=%d table_width=%d kv_heads=%d", c->B,
@@ -790,6 +784,19 @@ spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
                 c->table_width, c->page_size);
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
     return fail(SPC_E_SHAPE, "head_dim must be 64, 128 or 256 (got %d)", c->head_dim);
+  return SPC_OK;
+}
+
+// The checks every cache call makes of the cache, and its parameters.
+spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
+  if (!c || !c->k_pages || !c->v_pages || !c->page_table || !c->kv_len)
+    return fail(SPC_E_NULL, "a required pointer is NULL");
+  if (c->dtype != SPC_BF16 && c->dtype != SPC_E4M3)
+    return fail(SPC_E_PARAM, "unknown cache dtype %d", c->dtype);
+  const bool f8 = c->dtype == SPC_E4M3;
+  if (f8 && (!c->k_scale || !c->v_scale)) return fail(SPC_E_NULL, "an e4m3 cache needs its scales");
+  const spc_status st = check_cache_sizes(c);
+  if (st != SPC_OK) return st;
   if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages |
        (f8 ? (uintptr_t)c->k_scale | (uintptr_t)c->v_scale : 0)) % 16 != 0)
     return fail(SPC_E_ALIGN, "pages and scales must be 16-byte aligned");
@@ -814,9 +821,10 @@ spc_status kv_params(const spc_kv_cache* c, spc::KvParams& P) {
   return SPC_OK;
 }
 
-// The rows of a chunk of new tokens.
+// The rows of a chunk of new tokens, at most kKvRows.
+constexpr int64_t kKvRows = int64_t(1) << 24;
 spc_status kv_rows(int64_t rows, const int32_t* row_start, int32_t max_rows, spc::KvParams& P) {
-  if (rows < 1 || rows > (int64_t(1) << 24))
+  if (rows < 1 || rows > kKvRows)
     return fail(SPC_E_SHAPE, "rows must be from 1 to 2^24 (got %lld)", (long long)rows);
   if (!row_start && rows % P.B != 0)
     return fail(SPC_E_SHAPE, "%lld rows do not divide into %d sequences (no row_start)",
@@ -1008,9 +1016,10 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
 
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
                               int32_t max_rows) {
-  if (!cache || cache->B < 1 || cache->kv_heads < 1 || heads < 1 || rows < 1 ||
-      heads % cache->kv_heads != 0 || cache->table_width < 1 || cache->page_size < 1)
+  if (!cache || (cache->dtype != SPC_BF16 && cache->dtype != SPC_E4M3) ||
+      check_cache_sizes(cache) != SPC_OK || heads < 1 || heads % cache->kv_heads != 0)
     return 0;
+  if (rows < 1 || rows > kKvRows || max_rows < 0 || (max_rows == 0 && rows % cache->B != 0)) return 0;
   const int64_t n = max_rows > 0 ? std::min<int64_t>(max_rows, rows) : rows / cache->B;
   return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
                        (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
