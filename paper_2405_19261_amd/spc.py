@@ -529,10 +529,15 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
     return out
 
 
-def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=0, *,
-                           k_scale=None, v_scale=None):
-    """Bytes of workspace an spc_kv_attend call of this cache and chunk needs."""
+def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=None, *,
+                           k_scale=None, v_scale=None, q_start=None):
+    """Bytes of workspace an spc_kv_attend call of this cache and chunk needs:
+    ``rows`` rows in all, ``q_start`` and ``max_q`` as the call gets them (with
+    ``q_start``, ``max_q`` None: all rows may be one sequence's; a ``max_q`` alone
+    stands for a call with ``q_start``)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if max_q is None:
+        max_q = 0 if q_start is None else rows
     return lib().spc_kv_workspace_bytes(cache, heads, rows, max_q)
 
 

@@ -4,6 +4,7 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 from paper_2405_19261_amd import spc
 
@@ -57,3 +58,28 @@ def test_the_query_and_the_call_agree(rows, max_rows, dtype):
     status = spc.lib().spc_kv_attend(c, OK, spc.SPC_BF16, 512, 4, rows, OK if max_rows else None,
                                      max_rows, 0.1, 0, OK, 512, OK, n - 1, None)
     assert status == -6 and f"need {n}," in spc.spc_last_error()
+
+
+def test_the_binding_asks_for_what_its_call_needs(monkeypatch):
+    """With the same q_start and max_q (defaults too) the query gives the size
+    that spc_kv_attend lays out."""
+    B, H, S, D, width, heads = 4, 2, 16, 64, 1000, 8
+    k = torch.zeros((8, H, S, D), dtype=torch.bfloat16)
+    v = torch.zeros((8, H, D, S), dtype=torch.bfloat16)
+    args = (k, v, torch.zeros((B, width), dtype=torch.int32), torch.zeros(B, dtype=torch.int32))
+    short = torch.zeros(4096, dtype=torch.uint8)[:1]  # (no call gets past its check of the workspace)
+    start = torch.zeros(B + 1, dtype=torch.int32)
+    monkeypatch.setattr(spc, "_on_current_device", lambda t: None)
+    monkeypatch.setattr(spc, "_stream", lambda s: None)
+    for rows, q_start, max_q in ((8, None, None), (9, start, None), (9, start, 3), (3, start, 3),
+                                 (3, start, None), (400, start, None), (400, None, None)):
+        lead = (rows,) if q_start is not None else (B, rows // B)
+        q = torch.zeros(lead + (heads, D), dtype=torch.bfloat16)
+        n = spc.spc_kv_workspace_bytes(*args, heads, rows, max_q, q_start=q_start)
+        assert n > 0
+        with pytest.raises(spc.SpcError, match=f"need {n},"):
+            spc.spc_kv_attend(q, *args, q_start=q_start, max_q=max_q, workspace=short)
+    # a size alone is that of even rows, or with max_q of a call with q_start
+    assert spc.spc_kv_workspace_bytes(*args, heads, 3) == 0
+    assert (spc.spc_kv_workspace_bytes(*args, heads, 9, 3) ==
+            spc.spc_kv_workspace_bytes(*args, heads, 9, 3, q_start=start) > 0)
