@@ -378,6 +378,13 @@ constexpr int kAttendWaves = 4;
 
 constexpr int share_keys(int tile_rows, bool f8) { return tile_rows > 64 ? 512 : f8 ? 256 : 128; }
 
+// The first position that a row at position t sees (under 0: from 0).  A row
+// before position 0 sees nothing: it is taken as at 0, where no window of 32 bits
+// passes them.
+__device__ __forceinline__ int32_t first_seen(const KvParams& P, int32_t t) {
+  return P.window > 0 ? max(t, 0) - P.window + 1 : 0;
+}
+
 // The keys that rows of a chunk's tokens i0 .. i1 see: tiles of T from `begin`
 // (a multiple of T), cut into shares of `per` tiles.
 struct Span {
@@ -388,7 +395,7 @@ __device__ __forceinline__ Span span_of(const KvParams& P, int32_t len, int n, i
                                         int splits) {
   const int32_t end = min(min(len, P.width * P.S), len - n + i1 + 1);
   Span s;
-  s.begin = P.window > 0 ? max(len - n + i0 - P.window + 1, 0) & ~(T - 1) : 0;
+  s.begin = max(first_seen(P, len - n + i0), 0) & ~(T - 1);
   s.tiles = end > s.begin ? (end - s.begin + T - 1) / T : 0;
   s.shares = max(1, min(splits, s.tiles / (MIN / T)));
   s.per = (s.tiles + s.shares - 1) / s.shares;
@@ -447,10 +454,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
           bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
     }
     last[mt] = pos0 + i;
-    first[mt] = P.window > 0 ? last[mt] - P.window + 1 : 0;
+    first[mt] = first_seen(P, last[mt]);
   }
   // a tile within these is seen whole by every row
-  const int32_t all_from = P.window > 0 ? pos0 + i1 - P.window + 1 : 0;
+  const int32_t all_from = first_seen(P, pos0 + i1);
   const int32_t all_to = min(pos0 + i0 + 1, there);
 
   f32x4 o[MT][kM] = {};
@@ -722,10 +729,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
           bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
     }
     last[mt] = pos0 + i;
-    first[mt] = P.window > 0 ? last[mt] - P.window + 1 : 0;
+    first[mt] = first_seen(P, last[mt]);
   }
   const int i0 = (int)(min(w0, rows - 1) / G), i1 = (int)((min(w0 + 16 * MT, rows) - 1) / G);
-  const int32_t all_from = P.window > 0 ? pos0 + i1 - P.window + 1 : 0;
+  const int32_t all_from = first_seen(P, pos0 + i1);
   const int32_t all_to = min(pos0 + i0 + 1, there);
 
   f32x4 o[MT][kM] = {};
