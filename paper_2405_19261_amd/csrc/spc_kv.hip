@@ -131,7 +131,8 @@ __global__ void __launch_bounds__(256) k_kv_write_tile(KvParams P) {
   typedef typename std::conditional<F8, uint8_t, uint16_t>::type T;
   __shared__ T turned[D * kRow];
   __shared__ int32_t pages[64], slots[64], whole[9];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y;
+  const int lane = threadIdx.x & 63, h = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int64_t r0 = (int64_t)blockIdx.x * 64;
   const int n = (int)min(P.rows - r0, (int64_t)64);
   if (wave == 0) {
@@ -147,13 +148,17 @@ __global__ void __launch_bounds__(256) k_kv_write_tile(KvParams P) {
     slots[lane] = slot;
   }
   __syncthreads();
+  const uint64_t live = __ballot(pages[lane] >= 0);  // the rows that are written
+  if (!live) return;
+  const int some = __builtin_ctzll(live);
   // kAtOnce rows of a wavefront at a time: their loads are under way together
   constexpr int kAtOnce = 4;
   for (int i0 = wave * kAtOnce; i0 < n; i0 += 4 * kAtOnce) {
     float x[kAtOnce][2][E];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const int64_t r = r0 + min(i0 + k, n - 1);
+      const int i = min(i0 + k, n - 1);
+      const int64_t r = r0 + (live >> i & 1 ? i : some);  // (no other row is read)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         x[k][0][e] = source<SRC>(P.k_new, r * P.k_stride + (int64_t)h * D + e * 64 + lane);
