@@ -83,7 +83,9 @@ class ContextLM:
     at consecutive positions), writes their keys and values and attends from
     all of them.  A position that comes again overwrites what it held, and a
     call reads no further than its last position: rolling back needs no more
-    than going on from an earlier position."""
+    than going on from an earlier position.  A token at or past ``capacity``
+    (``max_len`` in whole pages) is not kept: ``spec_decode`` raises after rounds
+    that came that far; one's own calls stay below."""
 
     def __init__(self, base, B, max_len, heads=4, kv_heads=2, head_dim=64, page_size=16,
                  cache_dtype=torch.bfloat16, mix=1.0, seed=0):
@@ -99,6 +101,7 @@ class ContextLM:
         self.v_table = table(base.rows, kv_heads, head_dim)
         self.project = table(heads * head_dim, base.V, s=mix * (heads * head_dim) ** -0.5)
         width = (max_len + page_size - 1) // page_size
+        self.capacity = width * page_size
         # pages in a seeded order, as an allocator leaves them after a while
         self.page_table = torch.randperm(B * width, generator=g).view(B, width).to(
             self.device, torch.int32)
@@ -207,7 +210,9 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
     scattered into a device buffer (a round writes its gamma+1 candidates at
     the sequence's length and advances the length by j* + 1, so the
     candidates past j* are overwritten by the next round), and the host reads
-    the buffer and the accept lengths once, after the last round.
+    the buffer and the accept lengths once, after the last round.  A model with a
+    ``capacity`` (the tokens of a sequence that its cache holds) that they went
+    past is an error then.
 
     ``graph=True`` captures one round (the 2*gamma+1 model and sampling calls,
     the verification and the emission) into a HIP graph and replays it once
@@ -318,6 +323,13 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
     if bad.numel():
         raise RuntimeError(f"sequence {int(bad[0, 1])}: invalid parameters (accept_len -1)")
     buf_h, len_h = buf.cpu(), length.cpu()
+    if rounds:
+        # the last round's models were called up to gamma past where it began
+        reached = int((len_h - acc_h[-1]).max()) + gamma
+        for name, lm in (("drafter", drafter), ("verifier", verifier)):
+            if reached > getattr(lm, "capacity", reached):
+                raise RuntimeError(f"the rounds reached {reached} tokens of a sequence, the "
+                                   f"{name}'s cache holds {lm.capacity}")
     res = DecodeResult(tokens=[buf_h[b, :int(len_h[b])].tolist() for b in range(B)])
     res.accept_len = [a.to(torch.int32) for a in acc_h]
     return res

@@ -53,6 +53,43 @@ def test_truncation_holds_for_one_run(cut):
         assert all(c is None for c in backend.cuts)
 
 
+class Bounded:
+    """A model with a cache of `capacity` tokens a sequence, noting how far it was called."""
+
+    def __init__(self, capacity):
+        self.lm, self.device = decode.SyntheticLM(V, rows=4, device="cpu"), torch.device("cpu")
+        self.capacity, self.reached = capacity, 0
+
+    def __call__(self, last, positions):
+        self.reached = max(self.reached, int(positions.max()) + 1)
+        return self.lm(last, positions)
+
+
+class Keeper(Recorder):
+    """All drafts kept by sequence 0, none by the others."""
+
+    def verify(self, q, p, drafts, *rest):
+        acc = torch.zeros(len(q), dtype=torch.int32)
+        acc[0] = drafts.shape[1]
+        return acc, torch.zeros(len(q), dtype=torch.int32)
+
+
+@pytest.mark.parametrize("backend,reached", [(Recorder, 3 + 5), (Keeper, 4 * 5)])
+def test_rounds_past_a_cache_are_an_error(backend, reached):
+    """4 rounds of gamma = 4: one token a round, or five.  A cache that just holds
+    what the rounds reached is enough, whatever more they might have taken."""
+    def decode_with(*capacities):
+        lms = [Bounded(c) for c in capacities]
+        decode.spec_decode(*lms, torch.zeros(B, dtype=torch.long), rounds=4, gamma=4, rule=W.ALWAYS,
+                           alpha=0.0, temperature=1.0, backend=backend())
+        assert all(lm.reached == reached for lm in lms)
+
+    decode_with(reached, reached)
+    for name, c in (("drafter", (reached - 1, reached)), ("verifier", (reached, reached - 1))):
+        with pytest.raises(RuntimeError, match=f"{name}'s cache holds {reached - 1}"):
+            decode_with(*c)
+
+
 @pytest.mark.gpu
 def test_a_used_backend_decodes_as_a_new_one():
     p = decode.SyntheticLM(2000, rows=16, seed=1, device="cuda")
@@ -68,3 +105,23 @@ def test_a_used_backend_decodes_as_a_new_one():
     whole = run_on(used)
     assert whole == run_on(decode.GpuBackend()) and whole != cut
     assert run_on(used, top_k=3) == cut
+
+
+def test_a_context_model_holds_whole_pages():
+    lm = decode.ContextLM(decode.SyntheticLM(V, rows=4, device="cpu"), B, 33, page_size=16)
+    assert lm.capacity == 48
+
+
+@pytest.mark.gpu
+def test_rounds_past_a_context_models_cache_are_an_error():
+    p = decode.SyntheticLM(500, rows=16, seed=1, device="cuda")
+
+    def run_in(tokens, rounds, graph):
+        lms = [decode.ContextLM(p, 2, tokens, seed=3) for _ in range(2)]
+        return decode.spec_decode(*lms, torch.arange(2, device="cuda"), rounds, 3, W.ALWAYS, 0.0, 1.0,
+                                  graph=graph).tokens
+
+    for graph in (False, True):  # (every draft of an identical model is kept: 4 tokens a round)
+        assert run_in(16, 4, graph) == run_in(160, 4, graph)
+        with pytest.raises(RuntimeError, match="cache holds 16"):
+            run_in(16, 5, graph)
