@@ -140,7 +140,8 @@ class GpuBackend:
     the rules they hold.
 
     ``truncate`` (called before ``prepare`` where the rounds are truncated)
-    takes top_k, top_p and min_p as [B] tensors.  They hold for one run: the
+    takes top_k, top_p and min_p as [B] tensors and raises on values out of
+    range, whose sequences the library would leave without a token.  They hold for one run: the
     next ``prepare`` without a ``truncate`` before it leaves distributions
     whole again."""
 
@@ -150,6 +151,12 @@ class GpuBackend:
         self._cut = self._next_cut = None
 
     def truncate(self, top_k, top_p, min_p):
+        k, p, m = top_k.cpu(), top_p.cpu(), min_p.cpu()
+        bad = (~((k >= 0) & (p > 0) & (p <= 1) & (m >= 0) & (m <= 1))).nonzero()
+        if bad.numel():
+            b = int(bad[0])
+            raise ValueError(f"sequence {b}: top_k must be >= 0, top_p in (0, 1] and min_p in [0, 1] "
+                             f"(got {int(k[b])}, {float(p[b]):g} and {float(m[b]):g})")
         self._cut = self._next_cut = dict(top_k_per_seq=top_k, top_p_per_seq=top_p,
                                           min_p_per_seq=min_p)
 

@@ -53,6 +53,24 @@ def test_truncation_holds_for_one_run(cut):
         assert all(c is None for c in backend.cuts)
 
 
+NAN = float("nan")
+
+
+@pytest.mark.parametrize("cut,b", [
+    (dict(top_k=-1), 0), (dict(top_p=0.0), 0), (dict(top_p=1.5), 0), (dict(min_p=-0.1), 0),
+    (dict(min_p=1.1), 0), (dict(top_p=NAN), 0), (dict(min_p=NAN), 0),
+    (dict(top_k=torch.tensor([5, 0, -2])), 2), (dict(top_p=torch.tensor([1.0, 0.0, 0.5])), 1),
+    (dict(top_k=4, min_p=torch.tensor([0.0, 1.0, 2.0])), 2)])
+def test_settings_out_of_range_are_an_error(cut, b):
+    """Not rounds of rows without an entry; and the backend goes on without them."""
+    backend = Recorder()
+    with pytest.raises(ValueError, match=f"sequence {b}:"):
+        run(backend, **cut)
+    assert backend.cuts == []
+    run(backend)
+    assert all(c is None for c in backend.cuts)
+
+
 class Bounded:
     """A model with a cache of `capacity` tokens a sequence, noting how far it was called."""
 
