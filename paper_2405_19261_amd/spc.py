@@ -205,6 +205,14 @@ def _expect(name, t, dtype, like, shape):
         _check_arg(name, t, dtype, like.device, shape)
 
 
+def _int32(name, x):
+    """x as an integer argument of 32 bits (ctypes alone takes it modulo 2^32)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must be an integer of 32 bits, not {x}")
+    return x
+
+
 def _on_current_device(t):
     """Raise unless the kernels, which run on the current device, may read t."""
     d = t.get_device()
@@ -316,13 +324,14 @@ def spc_draft_sample(logits, temperature, uniforms=None, temp_per_seq=None, out=
 
 def _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq, top_p_per_seq,
                 min_p_per_seq, like, B):
+    top_k = _int32("top_k", top_k)
     if temp_per_seq is top_k_per_seq is top_p_per_seq is min_p_per_seq is None:
-        return Truncation(temperature, int(top_k), top_p, min_p)
+        return Truncation(temperature, top_k, top_p, min_p)
     _expect("temp_per_seq", temp_per_seq, torch.float32, like, (B,))
     _expect("top_k_per_seq", top_k_per_seq, torch.int32, like, (B,))
     _expect("top_p_per_seq", top_p_per_seq, torch.float32, like, (B,))
     _expect("min_p_per_seq", min_p_per_seq, torch.float32, like, (B,))
-    return Truncation(temperature, int(top_k), top_p, min_p, _ptr(temp_per_seq),
+    return Truncation(temperature, top_k, top_p, min_p, _ptr(temp_per_seq),
                       _ptr(top_k_per_seq), _ptr(top_p_per_seq), _ptr(min_p_per_seq))
 
 
@@ -347,6 +356,8 @@ def spc_sample(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.0, min_p
     if logits.dim() != 2:
         raise ValueError("logits must be a [B, V] tensor")
     B, V = logits.shape
+    _int32("the number of rows", B)
+    _int32("the length of a row", V)
     if logits.stride(1) != 1 or (B > 1 and logits.stride(0) < V):
         raise ValueError("the entries of a row of logits must be contiguous, rows not overlap")
     _expect("uniforms", uniforms, torch.float32, logits, (B,))
@@ -375,6 +386,9 @@ def spc_truncate(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, *, temp
     if logits.dim() not in (2, 3) or not logits.is_contiguous():
         raise ValueError("logits must be a contiguous [B, rows, V] or [B, V] tensor")
     B, V = logits.shape[0], logits.shape[-1]
+    rows = logits.shape[1] if logits.dim() == 3 else 1
+    for n in (B, rows, V):
+        _int32("a dimension of logits", n)
     cut = _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq,
                       top_p_per_seq, min_p_per_seq, logits, B)
     if out is None:
@@ -383,13 +397,13 @@ def spc_truncate(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, *, temp
     code = _dtype_code(logits)
     ws, nbytes = _workspace(workspace, logits)
     _on_current_device(logits)
-    _check(lib().spc_truncate(_ptr(logits), code, B, logits.shape[1] if logits.dim() == 3 else 1,
-                              V, cut, _ptr(out), ws, nbytes, _stream(stream)))
+    _check(lib().spc_truncate(_ptr(logits), code, B, rows, V, cut, _ptr(out), ws, nbytes,
+                              _stream(stream)))
     return out
 
 
 def spc_truncation_workspace_bytes(rows, V, dtype_code):
-    return lib().spc_truncation_workspace_bytes(rows, V, dtype_code)
+    return lib().spc_truncation_workspace_bytes(rows, _int32("V", V), dtype_code)
 
 
 def _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale):
@@ -481,6 +495,8 @@ def spc_kv_read(k_pages, v_pages, page_table, kv_len, length=None, *, k_scale=No
     ``out``: a pair to write instead; positions past ``kv_len`` keep what they
     hold (new tensors: zero)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if length is not None:
+        length = _int32("length", length)
     if out is None:
         if length is None:
             raise ValueError("length or out must be given")
@@ -488,7 +504,7 @@ def spc_kv_read(k_pages, v_pages, page_table, kv_len, length=None, *, k_scale=No
         out = tuple(torch.zeros(shape, dtype=dtype, device=k_pages.device) for _ in range(2))
     k, v = out
     if length is None:
-        length = k.shape[1]
+        length = _int32("length", k.shape[1])
     shape = (cache.B, length, cache.kv_heads, cache.head_dim)
     _expect("out", k, k.dtype, k_pages, shape)
     _expect("out", v, k.dtype, k_pages, shape)
@@ -519,13 +535,14 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
         raise ValueError("out must have the shape and type of q")
     os_ = _kv_rows("out", out, k_pages, cache.B, q_start, dim)[2]
     ws, nbytes = _workspace(workspace, k_pages)
+    window = _int32("window", window)
+    most = rows if max_q is None else _int32("max_q", max_q)
     if rows == 0:
         return out
     _on_current_device(k_pages)
     _check(lib().spc_kv_attend(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start),
-                               rows if max_q is None else max_q,
-                               dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                               os_, ws, nbytes, _stream(stream)))
+                               most, dim ** -0.5 if scale is None else scale, window,
+                               out.data_ptr(), os_, ws, nbytes, _stream(stream)))
     return out
 
 
@@ -538,7 +555,7 @@ def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, ma
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
     if max_q is None:
         max_q = 0 if q_start is None else rows
-    return lib().spc_kv_workspace_bytes(cache, heads, rows, max_q)
+    return lib().spc_kv_workspace_bytes(cache, _int32("heads", heads), rows, _int32("max_q", max_q))
 
 
 def spc_workspace_bytes(B, gamma, V, dtype_code):
