@@ -325,6 +325,7 @@ def spc_draft_sample(logits, temperature, uniforms=None, temp_per_seq=None, out=
 def _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq, top_p_per_seq,
                 min_p_per_seq, like, B):
     top_k = _int32("top_k", top_k)
+    temperature, top_p, min_p = float(temperature), float(top_p), float(min_p)
     if temp_per_seq is top_k_per_seq is top_p_per_seq is min_p_per_seq is None:
         return Truncation(temperature, top_k, top_p, min_p)
     _expect("temp_per_seq", temp_per_seq, torch.float32, like, (B,))
@@ -541,7 +542,7 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
         return out
     _on_current_device(k_pages)
     _check(lib().spc_kv_attend(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start),
-                               most, dim ** -0.5 if scale is None else scale, window,
+                               most, dim ** -0.5 if scale is None else float(scale), window,
                                out.data_ptr(), os_, ws, nbytes, _stream(stream)))
     return out
 

@@ -1,5 +1,6 @@
 """Numbers as arguments of the truncation and cache calls (CPU: every call here
 ends in the binding)."""
+import numpy as np
 import pytest
 import torch
 
@@ -45,3 +46,19 @@ def test_rows_that_do_not_fit_are_refused(shape):
     for call in (lambda: spc.spc_sample(z, temperature=0.0), lambda: spc.spc_truncate(z)):
         with pytest.raises(ValueError, match="32 bits"):
             call()
+
+
+@pytest.mark.parametrize("number", [np.float32, np.float64, torch.tensor, lambda x: np.array(x)])
+def test_settings_of_any_number_type(number):
+    """As the verify and drafter calls take theirs: these get as far as the tensors,
+    which are the host's."""
+    z, u, q = torch.zeros(3, 50), torch.zeros(3), torch.zeros((3, 2, 4, 64), dtype=torch.bfloat16)
+    kw = dict(temperature=number(0.5), top_p=number(0.75), min_p=number(0.25))
+    for call in (lambda: spc.spc_sample(z, u, **kw), lambda: spc.spc_truncate(z, **kw),
+                 lambda: spc.spc_sample(z, u, top_k_per_seq=torch.ones(3, dtype=torch.int32), **kw),
+                 lambda: spc.spc_kv_attend(q, *cache(), scale=number(0.5))):
+        with pytest.raises(ValueError, match="current HIP device"):
+            call()
+    cut = spc._truncation(kw["temperature"], np.int64(7), kw["top_p"], kw["min_p"], None, None, None,
+                          None, z, 3)
+    assert (cut.temperature, cut.top_k, cut.top_p, cut.min_p) == (0.5, 7, 0.75, 0.25)
