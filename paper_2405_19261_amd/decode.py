@@ -83,7 +83,7 @@ class ContextLM:
     at consecutive positions), writes their keys and values and attends from
     all of them.  A position that comes again overwrites what it held, and a
     call reads no further than its last position: rolling back needs no more
-    than going on from an earlier position.  A token at or past ``capacity``
+    than going on from an earlier position.  A token at or past ``cache_tokens``
     (``max_len`` in whole pages) is not kept: ``spec_decode`` raises after rounds
     that came that far; one's own calls stay below."""
 
@@ -101,7 +101,7 @@ class ContextLM:
         self.v_table = table(base.rows, kv_heads, head_dim)
         self.project = table(heads * head_dim, base.V, s=mix * (heads * head_dim) ** -0.5)
         width = (max_len + page_size - 1) // page_size
-        self.capacity = width * page_size
+        self.cache_tokens = width * page_size
         # pages in a seeded order, as an allocator leaves them after a while
         self.page_table = torch.randperm(B * width, generator=g).view(B, width).to(
             self.device, torch.int32)
@@ -218,7 +218,7 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
     the sequence's length and advances the length by j* + 1, so the
     candidates past j* are overwritten by the next round), and the host reads
     the buffer and the accept lengths once, after the last round.  A model with a
-    ``capacity`` (the tokens of a sequence that its cache holds) that they went
+    ``cache_tokens`` (the tokens of a sequence that its cache holds) that they went
     past is an error then.
 
     ``graph=True`` captures one round (the 2*gamma+1 model and sampling calls,
@@ -334,9 +334,9 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
         # the last round's models were called up to gamma past where it began
         reached = int((len_h - acc_h[-1]).max()) + gamma
         for name, lm in (("drafter", drafter), ("verifier", verifier)):
-            if reached > getattr(lm, "capacity", reached):
+            if reached > getattr(lm, "cache_tokens", reached):
                 raise RuntimeError(f"the rounds reached {reached} tokens of a sequence, the "
-                                   f"{name}'s cache holds {lm.capacity}")
+                                   f"{name}'s cache holds {lm.cache_tokens}")
     res = DecodeResult(tokens=[buf_h[b, :int(len_h[b])].tolist() for b in range(B)])
     res.accept_len = [a.to(torch.int32) for a in acc_h]
     return res

@@ -76,7 +76,7 @@ class Bounded:
 
     def __init__(self, capacity):
         self.lm, self.device = decode.SyntheticLM(V, rows=4, device="cpu"), torch.device("cpu")
-        self.capacity, self.reached = capacity, 0
+        self.cache_tokens, self.reached = capacity, 0
 
     def __call__(self, last, positions):
         self.reached = max(self.reached, int(positions.max()) + 1)
@@ -127,7 +127,7 @@ def test_a_used_backend_decodes_as_a_new_one():
 
 def test_a_context_model_holds_whole_pages():
     lm = decode.ContextLM(decode.SyntheticLM(V, rows=4, device="cpu"), B, 33, page_size=16)
-    assert lm.capacity == 48
+    assert lm.cache_tokens == 48
 
 
 @pytest.mark.gpu
