@@ -374,7 +374,8 @@ size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype);
  *   k_scale, v_scale  [num_pages][kv_heads][page_size] float32, for SPC_E4M3
  *             only: a value is its code times its token's and head's scale
  *   dtype     SPC_BF16 or SPC_E4M3
- *   page_size a multiple of 16 (16 .. 1024); head_dim 64, 128 or 256
+ *   page_size a multiple of 16 (16 .. 1024); head_dim 64, 128 or 256; kv_heads
+ *             and B at most 65535
  *   page_table [B][table_width] int32 device array; table_width * page_size
  *             is at most 2^30
  *   kv_len    [B] int32 device array: the tokens of a sequence, its new tokens
@@ -385,8 +386,9 @@ size_t spc_truncation_workspace_bytes(int64_t rows, int32_t V, int32_t dtype);
  * every sequence, sequence after sequence; with it (a [B+1] int32 device
  * array, not decreasing) sequence b has rows row_start[b] .. row_start[b+1]-1.
  * The last of a sequence's n new rows is at position kv_len[b] - 1, the first
- * at kv_len[b] - n.  A call takes at most 2^24 rows.  Rows before row_start[0] and from row_start[B] on belong
- * to no sequence: they are not read, and outputs for them are left as they are.
+ * at kv_len[b] - n.  A call takes at most 2^24 rows.  Rows before row_start[0]
+ * and from row_start[B] on belong to no sequence: they are not read, and outputs
+ * for them are left as they are.
  *
  * Rolling back is a smaller kv_len: nothing at or past it is read.  A token
  * whose page id lies outside [0, num_pages), or whose position lies outside
@@ -429,8 +431,8 @@ spc_status spc_kv_write(const spc_kv_cache* cache, const void* k, const void* v,
  * spc_kv_read -- positions 0 .. length - 1 of every sequence as dense rows.
  *
  *   out_k, out_v  [B][length][kv_heads][head_dim], `dtype` (SPC_F32 or
- *               SPC_BF16), 16-byte aligned.  Positions at or past kv_len, or
- *               not in the cache, are left as they are.
+ *               SPC_BF16), 16-byte aligned; length at most 2^26.  Positions at or
+ *               past kv_len, or not in the cache, are left as they are.
  */
 spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int32_t dtype,
                        int32_t length, hipStream_t stream);
@@ -440,7 +442,7 @@ spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int3
  * them already (spc_kv_write first):
  *   out = sum_t softmax_t(scale q.k_t) v_t,  t from max(0, s - window + 1) to s
  * for the new token at position s (window 0: from 0).  A row that sees no
- * cached token is zero.
+ * cached token is zero, as are rows before position 0 (a chunk longer than kv_len).
  *
  *   q           [rows][heads][head_dim] bfloat16, row r at element r * q_stride;
  *               heads a multiple of kv_heads, head i reading key/value head
@@ -448,7 +450,9 @@ spc_status spc_kv_read(const spc_kv_cache* cache, void* out_k, void* out_v, int3
  *   out         the same, row r at element r * out_stride, 8-byte aligned, the
  *               stride a multiple of 4
  *   max_rows    with row_start, the most rows of one sequence (rows of a
- *               longer one past it are left as they are); else ignored
+ *               longer one past it are left as they are); else ignored.  It
+ *               sizes the launch and the workspace for every sequence: where
+ *               they would be too large for one call, SPC_E_SHAPE
  * Scores, softmax statistics and sums are in 32 bits; probabilities enter the
  * second product in bfloat16.  Cached tokens below kv_len are finite (not
  * checked: a NaN in one makes the rows that see it NaN, and may make rows NaN

@@ -1,5 +1,6 @@
 // spc_internal.h -- structures shared by the C interface (spc_api.cpp) and the
-// gfx950 kernels (spc_kernels.hip, spc_sample.hip, spc_kv.hip).  Not part of the public interface.
+// gfx950 kernels (spc_kernels.hip, spc_sample.hip, spc_kv.hip).  Not part of the
+// public interface.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -240,7 +241,7 @@ struct KvParams {
   int64_t q_stride, out_stride;
   int32_t heads, window;
   float scale;              // of q.k, times log2(e)
-  int32_t tile_rows;        // rows (new token, query head) a workgroup takes: 16, 32 or 64
+  int32_t tile_rows;        // rows (new token, query head) a workgroup takes: 16, 32 or 128
   int32_t splits;           // most shares the keys are cut into
   float* part;              // [B * splits][H][row tiles][tile_rows][D + 2], splits > 1
 };

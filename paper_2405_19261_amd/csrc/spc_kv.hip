@@ -6,7 +6,8 @@
 // values as [H][D][S]: transposed, because the attention's second product
 // takes V^T as the left operand of a matrix instruction, whose lanes then load
 // eight consecutive tokens of one dimension with one instruction, as they load
-// eight dimensions of one key.  No operand passes through LDS.
+// eight dimensions of one key.  Chunks of few rows take their operands straight
+// from memory (k_kv_attend), chunks of many through LDS (k_kv_attend_rows).
 #include <math.h>
 
 #include <type_traits>
@@ -370,11 +371,14 @@ __device__ __forceinline__ void first_of(u32x4& w, int n) {
 // straight to registers, sixteen bytes a lane: with 8-bit values a lane's bytes
 // are two steps of the products, so there T = 64, else 32.  Which dimension
 // stands where in Q K^T does not matter so long as Q is loaded alike.
-// Statistics and O are held in 32 bits; P is rounded to bfloat16 (by at most
-// 2^-8) for the matrix unit, its sum is of the values before that.  Bound by the
-// bytes of the cache for few rows (32 sequences over 4096 bfloat16 tokens, 8
-// heads of 128: one row 103 us, 5.2 TB/s, 8 rows of 4 heads each 116), by the
-// vector instructions of the softmax and of widening 8 bits for more.
+// Statistics and O are held in 32 bits.  P (with 8-bit values times their scale)
+// is rounded to bfloat16, by at most 2^-8, because the matrix unit takes both
+// operands in one type; its sum is of the values before that.  (The error of
+// answers to random values: 2.0e-3 to 2.3e-3, with P in 32 bits 1.7e-3, which is
+// their own rounding to bfloat16.)  Bound by the bytes of the cache for few rows
+// (32 sequences over 4096 tokens, 8 heads of 128, one row: bfloat16 101 us, 5.3
+// TB/s, e4m3 52; 8 rows of 4 heads each, bfloat16, 114), by the vector
+// instructions of the softmax and of widening 8 bits for more.
 constexpr int kAttendWaves = 4;
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512.  (One token
@@ -686,8 +690,9 @@ constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
 // and the loads of the one after it are then under way.  What bounds it is the
 // LDS, whose reads of a tile take as long as the products of 32 rows with it,
 // and the softmax's vector instructions: 4 chunks of 1024 rows over 4096 tokens,
-// 32/8 heads of 128, take 406 us in bfloat16 (593 TFLOP/s; 515 with 32 keys a
-// tile, 653 with 64 rows a workgroup and its wavefronts apart over the keys).
+// 32/8 heads of 128, take 383 to 406 us in bfloat16 (593 to 629 TFLOP/s; by 406,
+// 515 us with 32 keys a tile, 653 with 64 rows a workgroup and its wavefronts apart
+// over the keys) and 437 in e4m3.
 template <int D, bool F8>
 __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
   constexpr int MT = 2, kRows = 16 * MT * kAttendWaves;

@@ -375,9 +375,7 @@ __device__ __forceinline__ uint32_t block_extreme(Shared& S, uint32_t x) {
   return MAX ? x : ~x;
 }
 
-// One value per wavefront, summed over the wavefronts before this one.  Every
-// wavefront scans the 16 sums in its first lanes; `slot` alternates between
-// calls, so that one barrier a call is enough.
+// A lane's value, in every lane (`lane` is uniform).
 template <class T>
 __device__ __forceinline__ T lane_value(T v, int lane) {
   if constexpr (sizeof(T) == 4) {
@@ -399,7 +397,8 @@ __device__ __forceinline__ T row_incl_scan(T v) {  // over 16 lanes
   return v;
 }
 
-// Counts c and masses m, one of each per thread, summed in thread order.
+// Counts c and masses m, one of each per thread, summed in thread order.  Every
+// wavefront scans the wavefronts' 16 sums in its first lanes.
 struct Sums {
   uint32_t c, upto_c;
   double m, upto_m, before_m;  // inclusive, exclusive

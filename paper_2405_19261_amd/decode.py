@@ -83,9 +83,9 @@ class ContextLM:
     at consecutive positions), writes their keys and values and attends from
     all of them.  A position that comes again overwrites what it held, and a
     call reads no further than its last position: rolling back needs no more
-    than going on from an earlier position.  A token at or past ``cache_tokens``
-    (``max_len`` in whole pages) is not kept: ``spec_decode`` raises after rounds
-    that came that far; one's own calls stay below."""
+    than going on from an earlier position.  A token at or past
+    ``cache_tokens`` (``max_len`` in whole pages) is not kept: ``spec_decode``
+    raises after rounds that came that far; one's own calls stay below."""
 
     def __init__(self, base, B, max_len, heads=4, kv_heads=2, head_dim=64, page_size=16,
                  cache_dtype=torch.bfloat16, mix=1.0, seed=0):
@@ -141,9 +141,9 @@ class GpuBackend:
 
     ``truncate`` (called before ``prepare`` where the rounds are truncated)
     takes top_k, top_p and min_p as [B] tensors and raises on values out of
-    range, whose sequences the library would leave without a token.  They hold for one run: the
-    next ``prepare`` without a ``truncate`` before it leaves distributions
-    whole again."""
+    range, whose sequences the library would leave without a token.  They hold
+    for one run: the next ``prepare`` without a ``truncate`` before it leaves
+    distributions whole again."""
 
     def __init__(self):
         self._scalar = None
@@ -217,9 +217,9 @@ def spec_decode(drafter, verifier, first_tokens, rounds, gamma, rule, alpha, tem
     scattered into a device buffer (a round writes its gamma+1 candidates at
     the sequence's length and advances the length by j* + 1, so the
     candidates past j* are overwritten by the next round), and the host reads
-    the buffer and the accept lengths once, after the last round.  A model with a
-    ``cache_tokens`` (the tokens of a sequence that its cache holds) that they went
-    past is an error then.
+    the buffer and the accept lengths once, after the last round.  Rounds that
+    went past a model's ``cache_tokens`` (an attribute it may have: the tokens
+    of a sequence that its cache holds) are an error then.
 
     ``graph=True`` captures one round (the 2*gamma+1 model and sampling calls,
     the verification and the emission) into a HIP graph and replays it once
