@@ -22,7 +22,8 @@
 //            (1024 a pass) to one value, and equal values by index.
 //   the draw Kept entries weigh 2^((t - t_max)/16) in fixed point: sums are
 //            exact, so the inverse CDF in vocabulary order is a function of
-//            the inputs alone.
+//            the inputs alone.  A uniform of less than a unit of them (0) is
+//            decided among the entries that weigh nothing, by their masses.
 //
 // All arithmetic on probabilities is in 64 bits (t, the weights and the sums):
 // a sampled token and the kept set are discrete, and 32-bit sums over 256 000
@@ -944,6 +945,45 @@ __device__ __forceinline__ int64_t draw_among(Shared& S, const Row& row, const C
   }
 }
 
+// A uniform of less than one unit of the weights (0, as a rule) falls on `token`
+// among the weights, the first that does not round to nothing.  The entries
+// before it have masses all the same: the first of them whose cumulative mass
+// exceeds x units (u times the total), in 64-bit floats, or `token`.  (A mass is
+// relative to the largest: one that is 0 there, past 2^-1074, is none.)
+template <int DT>
+__device__ __noinline__ int64_t draw_below_a_unit(Shared& S, const ScanRow<DT>& row, const Cut& cut,
+                                                  double c, double top, double scale, float zmax,
+                                                  int64_t token, double x) {
+  const double t_max = (double)zmax * c, most = exp2((t_max - top) * 0.0625) * scale;
+  int64_t lo = 0, n = token;
+  for (int slot = 1; n > 0; slot ^= 1) {
+    const int64_t q = (n + kNT - 1) / kNT, e0 = (int64_t)threadIdx.x * q;
+    uint32_t some = 0;
+    double m = 0.0;
+    for (int64_t e = lo + e0; e < lo + min(e0 + q, n); ++e) {
+      const float z = row.at(e);
+      const double w = kept(cut, z, e) ? exp2(((double)z * c - t_max) * 0.0625) * most : 0.0;
+      some += w > 0.0;
+      m += w;
+    }
+    const double past = __longlong_as_double(__double_as_longlong(x) + 1);  // the next float
+    const Reached f = reach(S, slot, sums_of(S, some, m), true, 0u, past);
+    if (f.at < 0 || (lo == 0 && n == token && !(f.above_mass + f.in_mass > x))) return token;
+    lo += (int64_t)f.at * q;
+    n = min(q, n - (int64_t)f.at * q);
+    x = fmax(x - f.above_mass, 0.0);
+    if (q == 1) return lo;
+  }
+  return token;
+}
+template <int DT>
+__device__ __forceinline__ int64_t draw_past_units(Shared& S, const ScanRow<DT>& row, const Cut& cut,
+                                                   double c, double top, double scale, float zmax,
+                                                   int64_t token, float u, uint64_t sum) {
+  const double x = u > 0.0f ? (double)u * (double)sum : 0.0;
+  return x < 1.0 ? draw_below_a_unit(S, row, cut, c, top, scale, zmax, token, x) : token;
+}
+
 // Entries kept, over the block.
 __device__ __forceinline__ uint32_t block_sum(Shared& S, uint32_t k) {
   k = wave_incl_scan(k);
@@ -1012,8 +1052,8 @@ __device__ __forceinline__ uint64_t held_weight(const Shared& S, const HeldRow<D
 // The draw of a row in one workgroup: held, or read from memory.
 template <int DT, int U>
 __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
-                                     const HeldRow<DT, U>& row, const Cut& cut, const Ask& a,
-                                     double top) {
+                                     const HeldRow<DT, U>& row, const ScanRow<DT>& mem,
+                                     const Cut& cut, const Ask& a, double top, float zmax) {
   constexpr int E = HeldRow<DT, U>::E;
   const double scale = pow2(sum_bits(row.V));
   uint32_t n;
@@ -1023,14 +1063,15 @@ __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
   int at;
   const uint64_t sum = find_sum(S, s, true, P.uniforms[r], thr, at);
   __syncthreads();
-  const int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * E,
-                                   min(E, row.V - at * E), thr);
+  int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * E,
+                             min(E, row.V - at * E), thr);
+  token = draw_past_units(S, mem, cut, a.c, top, scale, zmax, token, P.uniforms[r], sum);
   drawn_token(P, r, token, row.at(token), a, top, (double)sum / scale, n_kept);
 }
 template <int DT>
 __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
-                                     const ScanRow<DT>& row, const Cut& cut, const Ask& a,
-                                     double top) {
+                                     const ScanRow<DT>& row, const ScanRow<DT>&, const Cut& cut,
+                                     const Ask& a, double top, float zmax) {
   const double scale = pow2(sum_bits(row.V));
   const int64_t q = ((int64_t)row.V + kNT - 1) / kNT, e0 = (int64_t)threadIdx.x * q;
   uint32_t n = 0;
@@ -1047,8 +1088,9 @@ __device__ __forceinline__ void draw(Shared& S, const TruncParams& P, int64_t r,
   int at;
   const uint64_t sum = find_sum(S, s, true, P.uniforms[r], thr, at);
   __syncthreads();
-  const int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * q,
-                                   min(q, row.V - (int64_t)at * q), thr);
+  int64_t token = draw_among(S, row, cut, a.c, top, scale, (int64_t)at * q,
+                             min(q, row.V - (int64_t)at * q), thr);
+  token = draw_past_units(S, row, cut, a.c, top, scale, zmax, token, P.uniforms[r], sum);
   drawn_token(P, r, token, row.at(token), a, top, (double)sum / scale, n_kept);
 }
 
@@ -1123,7 +1165,7 @@ __device__ __forceinline__ void one_row(Shared& S, uint32_t* values, const Trunc
     greedy_token(P, r, block_extreme<false>(S, first));
   } else {
     const Cut cut = cut_of<PACK, DT>(S, values, row, mem, a, zmax, top);
-    draw(S, P, r, row, cut, a, top);
+    draw(S, P, r, row, mem, cut, a, top, zmax);
   }
 }
 
@@ -1425,8 +1467,8 @@ __global__ void __launch_bounds__(kNT) k_slice_end(TruncParams P, int sub) {
     const uint64_t sum = find_sum(S, S.mass[threadIdx.x], true, P.uniforms[r], thr, at);
     __syncthreads();
     const int64_t lo = (int64_t)at * G * sub;
-    const int64_t token =
-        draw_among(S, row, cut, a.c, R.top, scale, lo, min(G * sub, P.V - lo), thr);
+    int64_t token = draw_among(S, row, cut, a.c, R.top, scale, lo, min(G * sub, P.V - lo), thr);
+    token = draw_past_units(S, row, cut, a.c, R.top, scale, R.zmax, token, P.uniforms[r], sum);
     drawn_token(P, r, token, row.at(token), a, R.top, (double)sum / scale, n);
   }
 }
