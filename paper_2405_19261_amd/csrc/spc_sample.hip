@@ -697,6 +697,15 @@ __device__ __noinline__ Cut cut_in_bins(Shared& S, const Row& row, double c, dou
   return Cut{of_key(key), (int32_t)i.x};
 }
 
+// The mass that top-p asks for of bins plo and on, `whole` being that of the first
+// k.  Sums of up to V terms are rounded at 2^-53 here and there: what comes within
+// 2^-48 of the whole has reached it, so that entries of one mass are cut where
+// their number says (p = 1/2 of 262 142 equal ones: 131 071).  p has 24 bits: up to
+// 2^24 such entries p n is an integer or further from one than 2^-48 p n.
+__device__ __forceinline__ double wanted(const Ask& a, const Plan& p, double whole) {
+  return (double)a.p * whole * (1.0 - 0x1p-48) - p.p_above;
+}
+
 // The cut by top-k and top-p, from the entries of the bins in question (or all
 // entries of the row).
 template <class Row>
@@ -711,7 +720,7 @@ __device__ __forceinline__ Cut resolve(Shared& S, const Row& row, const Ask& a, 
   }
   if (p.plo >= 0) {
     double part;
-    const double want = ((double)a.p * whole - p.p_above) / S.edge[p.plo];
+    const double want = wanted(a, p, whole) / S.edge[p.plo];
     cut = tighter(cut, cut_in_bins(S, row, a.c, top, p.plo, p.phi, true, 0u, want, part));
   }
   return cut;
@@ -803,7 +812,7 @@ __device__ __forceinline__ Cut resolve_ranked(Shared& S, const Ask& a, double to
     }
     if (p.plo >= 0)
       cut = tighter(cut, cut_at(reach_place(p.plo, p.phi, true,
-                                            ((double)a.p * whole - p.p_above) / S.edge[p.plo])));
+                                            wanted(a, p, whole) / S.edge[p.plo])));
     if (lane == 0) S.cut = cut;
   }
   __syncthreads();
