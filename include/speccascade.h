@@ -473,6 +473,116 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
                               int32_t max_rows);
 
+/*
+ * spc_kv_attend_shared -- spc_kv_attend for a batch whose sequences begin with
+ * the same tokens, whose keys and values are read once for all of them.
+ *
+ *   shared       positions 0 .. shared - 1 of every sequence are the shared
+ *                tokens (0: none, and the call is spc_kv_attend; at most 2^30;
+ *                any number, whole pages or not)
+ *   shared_table int32 device array of the ceil(shared / page_size) pages that
+ *                hold them; a page id out of range is no page, as elsewhere
+ * Positions from `shared` on lie in the pages of page_table as always; its
+ * entries for positions before are not used.  kv_len counts the shared tokens.
+ * Everything else, and the answer, is as if every sequence's table held them.
+ *   workspace    of spc_kv_shared_workspace_bytes(...) bytes, or NULL, as there
+ */
+spc_status spc_kv_attend_shared(const spc_kv_cache* cache, int32_t shared,
+                                const int32_t* shared_table, const void* q, int32_t dtype,
+                                int64_t q_stride, int32_t heads, int64_t rows,
+                                const int32_t* row_start, int32_t max_rows, float scale,
+                                int32_t window, void* out, int64_t out_stride, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
+/* As spc_kv_workspace_bytes, for spc_kv_attend_shared. */
+size_t spc_kv_shared_workspace_bytes(const spc_kv_cache* cache, int32_t shared, int32_t heads,
+                                     int64_t rows, int32_t max_rows);
+
+/*
+ * spc_cross_attend -- attention of a decoder's rows to an encoder's states: the
+ * cache holds the keys and values of the encoder's kv_len[b] tokens (spc_kv_write
+ * them once), and every row of sequence b sees all of them but masked ones,
+ * whatever its own position:
+ *   out = sum_t softmax_t(scale q.k_t) v_t,  t < kv_len[b], key_mask[b][t] != 0
+ * A row that sees nothing is zero.  Several decoder sequences of one input may be
+ * rows of one sequence here.
+ *
+ *   key_mask     bytes, row b at key_mask + b * mask_stride (0: one row for all), of
+ *                mask_width tokens (those from there on are masked); NULL: nothing
+ *                is masked
+ * The keys and values of masked tokens may be anything.  Other arguments, types
+ * and the workspace (spc_kv_workspace_bytes) as for spc_kv_attend.
+ */
+spc_status spc_cross_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                            int64_t q_stride, int32_t heads, int64_t rows,
+                            const int32_t* row_start, int32_t max_rows, float scale,
+                            const uint8_t* key_mask, int64_t mask_stride, int32_t mask_width,
+                            void* out, int64_t out_stride, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * spc_kv_weigh -- the attention weight that cached tokens get from new ones, on
+ * top of what they had, for each key/value head:
+ *   out[b][h][t] = weights[b][h][t] + sum of softmax_t(scale q.k_t)
+ * over the new tokens of sequence b and the query heads that read head h.  Rows,
+ * positions, scale and window as for spc_kv_attend (only keys are read); a row's
+ * weights sum to 1, or to 0 where it sees nothing.  The chunk's own tokens
+ * (positions from kv_len - n on) begin at 0 whatever `weights` holds there.
+ *
+ *   weights      [B][kv_heads] rows of `length` float32, row (b, h) at element
+ *                (b * kv_heads + h) * weights_stride (at least length), or NULL:
+ *                all begin at 0.  length is at most 2^26
+ *   out          the same; may be `weights` itself, but not overlap it otherwise.
+ *                Positions at or past length get none; those at or past kv_len
+ *                (or the table's last slot) are left as they are
+ *   max_rows     as for spc_kv_attend; rows past it are not counted
+ * Scores, statistics and sums are in 32 bits, and sums over rows always in one
+ * order.  Cached keys below kv_len are finite (not checked).
+ *   workspace    of spc_kv_weigh_workspace_bytes(...) bytes, or NULL, as there
+ */
+spc_status spc_kv_weigh(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,
+                        int32_t heads, int64_t rows, const int32_t* row_start, int32_t max_rows,
+                        float scale, int32_t window, const float* weights, float* out,
+                        int64_t weights_stride, int32_t length, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/* As spc_kv_workspace_bytes, for spc_kv_weigh. */
+size_t spc_kv_weigh_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                                    int32_t max_rows);
+
+/*
+ * spc_kv_evict -- a bounded cache: of every sequence and key/value head at most
+ * `keep` tokens, in the order of their positions, into other pages.  Kept are the
+ * first `first` and the last `recent` tokens, and of the others those of the
+ * largest weights (the lowest position on a tie; a NaN is the smallest).
+ *
+ *   weights      as spc_kv_weigh leaves them (positions at or past length: 0)
+ *   keep         at most 2^26; first + recent at most keep
+ *   out_table    [B][out_width] int32 device array: the pages of the same pools
+ *                that receive the tokens of sequence b, at positions 0, 1, ...;
+ *                out_width * page_size at least keep.  They are pages that no
+ *                sequence of the call holds tokens in, but that a token which
+ *                comes to lie where it was is not moved: a sequence of at most
+ *                `keep` tokens may be given its own pages.  A page id out of
+ *                range takes nothing
+ *   out_len      [B] int32: the tokens kept, min(keep, those in the cache), the
+ *                same for every head (may be kv_len of a later call, but not
+ *                this one's)
+ *   out_index    [B][kv_heads][keep] int32: the positions they had, ascending, -1
+ *                behind the last
+ *   out_weights  [B][kv_heads] rows of keep float32, out_stride apart (at least
+ *                keep), or NULL: their weights, entries behind the last one left
+ *                as they are.  Not `weights` itself, nor overlapping it
+ * The pages they came from, and page_table, are left as they are.  Positions are
+ * the caller's to follow (out_index): queries and keys that encode them stay as
+ * they were written, and the next new token is at out_len.  No workspace.
+ */
+spc_status spc_kv_evict(const spc_kv_cache* cache, const float* weights, int64_t weights_stride,
+                        int32_t length, int32_t keep, int32_t first, int32_t recent,
+                        const int32_t* out_table, int32_t out_width, int32_t* out_len,
+                        int32_t* out_index, float* out_weights, int64_t out_stride,
+                        hipStream_t stream);
+
 /* Bytes of device workspace one call of this shape needs. */
 size_t spc_workspace_bytes(int32_t B, int32_t gamma, int32_t V, int32_t dtype);
 

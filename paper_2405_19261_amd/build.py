@@ -6,13 +6,15 @@ interface into ``paper_2405_19261_amd/libspeccascade.so``.
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libspeccascade.so")
-SOURCES = ["spc_kernels.hip", "spc_sample.hip", "spc_kv.hip", "spc_api.cpp"]
+SOURCES = ["spc_kernels.hip", "spc_sample.hip", "spc_kv.hip", "spc_kv_shared.hip",
+           "spc_kv_evict.hip", "spc_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -24,16 +26,18 @@ FLAGS = [
 
 
 def build(out=LIB, extra=(), verbose=False):
-    objs = []
-    for src in SOURCES:
-        obj = os.path.join(CSRC, src + ".o")
+    objs = [os.path.join(CSRC, src + ".o") for src in SOURCES]
+
+    def compile_one(src, obj):
         lang = ["-x", "hip"] if src.endswith(".cpp") else []
         cmd = [HIPCC, *FLAGS, *extra, "-I", INCLUDE, "-I", CSRC, *lang, "-c",
                os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd))
         subprocess.run(cmd, check=True)
-        objs.append(obj)
+
+    with ThreadPoolExecutor(max_workers=6) as pool:
+        list(pool.map(compile_one, SOURCES, objs))
     tmp = out + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp]
     subprocess.run(cmd, check=True)

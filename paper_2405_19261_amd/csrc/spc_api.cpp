@@ -913,13 +913,10 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   return L;
 }
 
-spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtype,
-                          int64_t q_stride, int32_t heads, int64_t rows,
-                          const int32_t* row_start, int32_t max_rows, float scale, int32_t window,
-                          void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
-                          hipStream_t stream) {
-  g_err.clear();
-  spc::KvParams P{};
+// The queries of an attention and the chunk they come in.
+spc_status kv_queries(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,
+                      int32_t heads, int64_t rows, const int32_t* row_start, int32_t max_rows,
+                      float scale, int32_t window, const void* out, spc::KvParams& P) {
   spc_status st = kv_params(cache, P);
   if (st == SPC_OK && (!q || !out)) st = fail(SPC_E_NULL, "a required pointer is NULL");
   if (st == SPC_OK) st = kv_rows(rows, row_start, max_rows, P);
@@ -927,36 +924,276 @@ spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtyp
   if (dtype != SPC_BF16) return fail(SPC_E_PARAM, "queries must be bfloat16 (dtype %d)", dtype);
   if (heads < 1 || heads % P.H != 0)
     return fail(SPC_E_SHAPE, "heads=%d is no multiple of kv_heads=%d", heads, P.H);
-  if (q_stride < (int64_t)heads * P.D || out_stride < (int64_t)heads * P.D)
+  if (q_stride < (int64_t)heads * P.D)
     return fail(SPC_E_SHAPE, "row strides must be at least heads * head_dim");
   if (!isfinite(scale)) return fail(SPC_E_PARAM, "scale is not finite");
   if (window < 0) return fail(SPC_E_PARAM, "window must be >= 0 (got %d)", window);
-  if ((uintptr_t)q % 2 != 0 || (uintptr_t)out % 8 != 0 || out_stride % 4 != 0)
-    return fail(SPC_E_ALIGN, "q must be element-aligned, out and its rows 8-byte aligned");
+  if ((uintptr_t)q % 2 != 0) return fail(SPC_E_ALIGN, "q must be element-aligned");
   P.q = q;
   P.q_stride = q_stride;
   P.heads = heads;
   P.scale = (float)((double)scale * 1.4426950408889634074);
   P.window = window;
+  return SPC_OK;
+}
+
+spc_status kv_answers(void* out, int64_t out_stride, spc::KvParams& P) {
+  if (out_stride < (int64_t)P.heads * P.D)
+    return fail(SPC_E_SHAPE, "row strides must be at least heads * head_dim");
+  if ((uintptr_t)out % 8 != 0 || out_stride % 4 != 0)
+    return fail(SPC_E_ALIGN, "out and its rows must be 8-byte aligned");
   P.out = out;
   P.out_stride = out_stride;
+  return SPC_OK;
+}
+
+// A launch of B sequences of n rows, cut by L, has few enough workgroups.
+spc_status kv_launch_size(int64_t B, int64_t H, int64_t rows, const AttendLayout& L,
+                          const int32_t* row_start) {
+  const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows;
+  if (tiles * ((H * B * L.splits + 7) / 8 * 8) >= (int64_t(1) << 24))
+    return fail(SPC_E_SHAPE, "%lld rows of each of %lld sequences are too many for one call%s",
+                (long long)rows, (long long)B, row_start ? ": pass max_rows" : "");
+  return SPC_OK;
+}
+
+// cross: to all tokens of a sequence (P.mask and its sizes are set), else up to each row's own.
+spc_status attend_impl(spc::KvParams& P, bool cross, void* workspace, size_t workspace_bytes,
+                       hipStream_t stream) {
   const AttendLayout L =
-      attend_layout(P.B, P.H, heads, P.n, P.D, (int64_t)P.width * P.S, P.f8);
+      attend_layout(P.B, P.H, P.heads, P.n, P.D, (int64_t)P.width * P.S, P.f8);
   P.tile_rows = L.tile_rows;
   P.splits = L.splits;
-  const int64_t tiles = ((int64_t)P.n * (heads / P.H) + L.tile_rows - 1) / L.tile_rows;
-  if (tiles * (((int64_t)P.H * P.B * L.splits + 7) / 8 * 8) >= (int64_t(1) << 24))
-    return fail(SPC_E_SHAPE, "%d rows of each of %d sequences are too many for one call%s", P.n,
-                P.B, row_start ? ": pass max_rows" : "");
+  spc_status st = kv_launch_size(P.B, P.H, (int64_t)P.n * (P.heads / P.H), L, P.start);
+  if (st != SPC_OK) return st;
   if (L.bytes) {
     char* ws = nullptr;
     st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
     if (st != SPC_OK) return st;
     P.part = reinterpret_cast<float*>(ws);
   }
-  const hipError_t e = spc::launch_kv_attend(P, stream);
+  const hipError_t e =
+      cross ? spc::launch_cross_attend(P, stream) : spc::launch_kv_attend(P, stream);
   if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
   return SPC_OK;
+}
+
+spc_status kv_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                          int64_t q_stride, int32_t heads, int64_t rows,
+                          const int32_t* row_start, int32_t max_rows, float scale, int32_t window,
+                          void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_queries(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                             window, out, P);
+  if (st == SPC_OK) st = kv_answers(out, out_stride, P);
+  if (st != SPC_OK) return st;
+  return attend_impl(P, false, workspace, workspace_bytes, stream);
+}
+
+spc_status cross_attend_impl(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                             int64_t q_stride, int32_t heads, int64_t rows,
+                             const int32_t* row_start, int32_t max_rows, float scale,
+                             const uint8_t* key_mask, int64_t mask_stride, int32_t mask_width,
+                             void* out, int64_t out_stride, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_queries(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale, 0,
+                             out, P);
+  if (st == SPC_OK) st = kv_answers(out, out_stride, P);
+  if (st != SPC_OK) return st;
+  if (key_mask) {
+    if (mask_width < 1 || mask_stride < 0)
+      return fail(SPC_E_SHAPE, "bad mask: mask_width=%d mask_stride=%lld", mask_width,
+                  (long long)mask_stride);
+    P.mask = key_mask;
+    P.mask_stride = mask_stride;
+    P.mask_width = mask_width;
+  }
+  return attend_impl(P, true, workspace, workspace_bytes, stream);
+}
+
+// How the attention behind a shared prefix is cut: the prefix, with the rows of
+// all sequences as one's, and the tokens of their own (splits = 0: none).
+struct SharedLayout {
+  AttendLayout pre, own;
+  size_t own_at, bytes;
+};
+// Every row leaves its sums, also where one share is all of a row's keys.
+size_t part_bytes(const AttendLayout& L, int64_t B, int64_t H, int64_t rows, int64_t D) {
+  const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows;
+  return align_up((size_t)(B * H * L.splits * tiles * L.tile_rows) * (size_t)(D + 2) * 4, 256);
+}
+SharedLayout shared_layout(int64_t B, int64_t H, int64_t heads, int64_t rows, int64_t n, int64_t D,
+                           int64_t shared, int64_t tokens, bool f8) {
+  SharedLayout L;
+  L.pre = attend_layout(1, H, heads, rows, D, shared, f8);
+  L.own = attend_layout(B, H, heads, n, D, std::max<int64_t>(1, tokens - shared), f8);
+  if (tokens <= shared) L.own.splits = 0;
+  const int64_t G = heads / H;
+  L.own_at = part_bytes(L.pre, 1, H, rows * G, D);
+  L.bytes = L.own_at + part_bytes(L.own, B, H, n * G, D);
+  return L;
+}
+
+spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
+                                 const int32_t* shared_table, const void* q, int32_t dtype,
+                                 int64_t q_stride, int32_t heads, int64_t rows,
+                                 const int32_t* row_start, int32_t max_rows, float scale,
+                                 int32_t window, void* out, int64_t out_stride, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_queries(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                             window, out, P);
+  if (st == SPC_OK) st = kv_answers(out, out_stride, P);
+  if (st != SPC_OK) return st;
+  if (shared < 0 || shared > (1 << 30))
+    return fail(SPC_E_SHAPE, "shared must be from 0 to 2^30 (got %d)", shared);
+  if (shared == 0) return attend_impl(P, false, workspace, workspace_bytes, stream);
+  if (!shared_table) return fail(SPC_E_NULL, "a required pointer is NULL");
+  if ((uintptr_t)shared_table % 4 != 0)
+    return fail(SPC_E_ALIGN, "shared_table must be 4-byte aligned");
+  const int64_t G = heads / P.H;
+  const SharedLayout L = shared_layout(P.B, P.H, heads, rows, P.n, P.D, shared,
+                                       (int64_t)P.width * P.S, P.f8);
+  st = kv_launch_size(P.B, P.H, P.n * G, L.own, row_start);
+  if (st == SPC_OK) st = kv_launch_size(1, P.H, rows * G, L.pre, nullptr);
+  char* ws = nullptr;
+  if (st == SPC_OK) st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
+  if (st != SPC_OK) return st;
+  spc::KvParams pre = P;
+  pre.shared = shared;
+  pre.table = shared_table;
+  pre.width = (shared + P.S - 1) / P.S;
+  pre.tile_rows = L.pre.tile_rows;
+  pre.splits = L.pre.splits;
+  pre.part = reinterpret_cast<float*>(ws);
+  P.from = shared;
+  P.partial = 1;
+  P.tile_rows = L.own.tile_rows;
+  P.splits = L.own.splits;
+  P.part = reinterpret_cast<float*>(ws + L.own_at);
+  const hipError_t e = spc::launch_kv_attend_shared(P, pre, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
+// How weighing is cut, and its workspace: the scores of few rows are kept where
+// they take at most kScoreBytes (the on-chip cache of the memory side).
+constexpr double kScoreBytes = 256.0 * (1 << 20);
+struct WeighLayout {
+  AttendLayout cut;
+  bool scores;
+  size_t kept_at, bytes;
+};
+WeighLayout weigh_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t tokens, bool f8) {
+  WeighLayout L;
+  const int64_t rows = n * (heads / H);
+  L.scores = rows <= spc::kWeighRows && 4.0 * B * H * rows * tokens <= kScoreBytes;
+  L.cut.tile_rows = L.scores && rows <= 16 ? 16 : 32;
+  const int64_t tiles = (rows + L.cut.tile_rows - 1) / L.cut.tile_rows, groups = B * H * tiles;
+  const int64_t most = std::max<int64_t>(1, tokens / spc::kv_share_keys(L.cut.tile_rows, f8));
+  L.cut.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
+                                                         (int64_t)spc::kKvShares, 65535 / B}));
+  L.cut.bytes = (size_t)(groups * L.cut.splits * L.cut.tile_rows) * 8;
+  L.kept_at = align_up(L.cut.bytes, 256);
+  L.bytes = L.kept_at + (size_t)(B * H * rows) * (L.scores ? (size_t)tokens * 4 : 8);
+  return L;
+}
+
+// Weights: [B * kv_heads] rows of `length`, a stride apart.
+spc_status weight_rows(const void* weights, int64_t stride, int32_t length) {
+  if (length < 1 || length > (1 << 26))
+    return fail(SPC_E_SHAPE, "length must be from 1 to 2^26 (got %d)", length);
+  if (stride < length)
+    return fail(SPC_E_SHAPE, "weights_stride must be at least length (got %lld)", (long long)stride);
+  if ((uintptr_t)weights % 4 != 0) return fail(SPC_E_ALIGN, "weights must be 4-byte aligned");
+  return SPC_OK;
+}
+
+spc_status kv_weigh_impl(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,
+                         int32_t heads, int64_t rows, const int32_t* row_start, int32_t max_rows,
+                         float scale, int32_t window, const float* weights, float* out,
+                         int64_t weights_stride, int32_t length, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  g_err.clear();
+  spc::KvParams P{};
+  spc_status st = kv_queries(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                             window, out, P);
+  if (st == SPC_OK) st = weight_rows(out, weights_stride, length);
+  if (st != SPC_OK) return st;
+  if ((uintptr_t)weights % 4 != 0) return fail(SPC_E_ALIGN, "weights must be 4-byte aligned");
+  const WeighLayout L =
+      weigh_layout(P.B, P.H, heads, P.n, (int64_t)P.width * P.S, P.f8);
+  st = kv_launch_size(P.B, P.H, (int64_t)P.n * (heads / P.H), L.cut, row_start);
+  char* ws = nullptr;
+  if (st == SPC_OK) st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
+  if (st != SPC_OK) return st;
+  P.tile_rows = L.cut.tile_rows;
+  P.splits = L.cut.splits;
+  P.part = reinterpret_cast<float*>(ws);
+  (L.scores ? P.scores : P.stats) = reinterpret_cast<float*>(ws + L.kept_at);
+  P.weights = weights;
+  P.out_weights = out;
+  P.weights_stride = weights_stride;
+  P.L = length;
+  const hipError_t e = spc::launch_kv_weigh(P, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
+spc_status kv_evict_impl(const spc_kv_cache* cache, const float* weights, int64_t weights_stride,
+                         int32_t length, int32_t keep, int32_t first, int32_t recent,
+                         const int32_t* out_table, int32_t out_width, int32_t* out_len,
+                         int32_t* out_index, float* out_weights, int64_t out_stride,
+                         hipStream_t stream) {
+  g_err.clear();
+  spc::EvictParams P{};
+  spc_status st = kv_params(cache, P.cache);
+  if (st == SPC_OK && (!weights || !out_table || !out_len || !out_index))
+    st = fail(SPC_E_NULL, "a required pointer is NULL");
+  if (st == SPC_OK) st = weight_rows(weights, weights_stride, length);
+  if (st != SPC_OK) return st;
+  if (keep < 1 || keep > (1 << 26))
+    return fail(SPC_E_SHAPE, "keep must be from 1 to 2^26 (got %d)", keep);
+  if (first < 0 || recent < 0 || (int64_t)first + recent > keep)
+    return fail(SPC_E_PARAM, "first=%d and recent=%d must be >= 0 and at most keep=%d together",
+                first, recent, keep);
+  if (out_width < 1 || (int64_t)out_width * P.cache.S < keep)
+    return fail(SPC_E_SHAPE, "out_width=%d pages of %d do not hold keep=%d tokens", out_width,
+                P.cache.S, keep);
+  if (out_weights && out_stride < keep)
+    return fail(SPC_E_SHAPE, "out_stride must be at least keep (got %lld)", (long long)out_stride);
+  if (((uintptr_t)out_table | (uintptr_t)out_len | (uintptr_t)out_index | (uintptr_t)out_weights) % 4)
+    return fail(SPC_E_ALIGN, "arrays must be 4-byte aligned");
+  P.weights = weights;
+  P.weights_stride = weights_stride;
+  P.out_stride = out_stride;
+  P.length = length;
+  P.keep = keep;
+  P.first = first;
+  P.recent = recent;
+  P.out_table = out_table;
+  P.out_width = out_width;
+  P.out_len = out_len;
+  P.out_index = out_index;
+  P.out_weights = out_weights;
+  const hipError_t e = spc::launch_kv_evict(P, stream);
+  if (e != hipSuccess) return fail(SPC_E_HIP, "kernel launch: %s", hipGetErrorString(e));
+  return SPC_OK;
+}
+
+// The rows a sequence of a call has at most (the workspace queries), or 0: sizes
+// that no call takes.
+int64_t query_rows(const spc_kv_cache* cache, int32_t heads, int64_t rows, int32_t max_rows) {
+  if (!cache || (cache->dtype != SPC_BF16 && cache->dtype != SPC_E4M3) ||
+      check_cache_sizes(cache) != SPC_OK || heads < 1 || heads % cache->kv_heads != 0)
+    return 0;
+  if (rows < 1 || rows > kKvRows || max_rows < 0 || (max_rows == 0 && rows % cache->B != 0)) return 0;
+  return max_rows > 0 ? std::min<int64_t>(max_rows, rows) : rows / cache->B;
 }
 
 }  // namespace
@@ -1016,14 +1253,78 @@ spc_status spc_kv_attend(const spc_kv_cache* cache, const void* q, int32_t dtype
 
 size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
                               int32_t max_rows) {
-  if (!cache || (cache->dtype != SPC_BF16 && cache->dtype != SPC_E4M3) ||
-      check_cache_sizes(cache) != SPC_OK || heads < 1 || heads % cache->kv_heads != 0)
-    return 0;
-  if (rows < 1 || rows > kKvRows || max_rows < 0 || (max_rows == 0 && rows % cache->B != 0)) return 0;
-  const int64_t n = max_rows > 0 ? std::min<int64_t>(max_rows, rows) : rows / cache->B;
+  const int64_t n = query_rows(cache, heads, rows, max_rows);
+  if (n == 0) return 0;
   return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
                        (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
       .bytes;
+}
+
+spc_status spc_kv_attend_shared(const spc_kv_cache* cache, int32_t shared,
+                                const int32_t* shared_table, const void* q, int32_t dtype,
+                                int64_t q_stride, int32_t heads, int64_t rows,
+                                const int32_t* row_start, int32_t max_rows, float scale,
+                                int32_t window, void* out, int64_t out_stride, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&] {
+    return kv_attend_shared_impl(cache, shared, shared_table, q, dtype, q_stride, heads, rows,
+                                 row_start, max_rows, scale, window, out, out_stride, workspace,
+                                 workspace_bytes, stream);
+  });
+}
+
+size_t spc_kv_shared_workspace_bytes(const spc_kv_cache* cache, int32_t shared, int32_t heads,
+                                     int64_t rows, int32_t max_rows) {
+  const int64_t n = query_rows(cache, heads, rows, max_rows);
+  if (n == 0 || shared < 0 || shared > (1 << 30)) return 0;
+  if (shared == 0) return spc_kv_workspace_bytes(cache, heads, rows, max_rows);
+  return shared_layout(cache->B, cache->kv_heads, heads, rows, n, cache->head_dim, shared,
+                       (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
+      .bytes;
+}
+
+spc_status spc_cross_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
+                            int64_t q_stride, int32_t heads, int64_t rows,
+                            const int32_t* row_start, int32_t max_rows, float scale,
+                            const uint8_t* key_mask, int64_t mask_stride, int32_t mask_width,
+                            void* out, int64_t out_stride, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&] {
+    return cross_attend_impl(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale,
+                             key_mask, mask_stride, mask_width, out, out_stride, workspace,
+                             workspace_bytes, stream);
+  });
+}
+
+spc_status spc_kv_weigh(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,
+                        int32_t heads, int64_t rows, const int32_t* row_start, int32_t max_rows,
+                        float scale, int32_t window, const float* weights, float* out,
+                        int64_t weights_stride, int32_t length, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&] {
+    return kv_weigh_impl(cache, q, dtype, q_stride, heads, rows, row_start, max_rows, scale, window,
+                         weights, out, weights_stride, length, workspace, workspace_bytes, stream);
+  });
+}
+
+size_t spc_kv_weigh_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                                    int32_t max_rows) {
+  const int64_t n = query_rows(cache, heads, rows, max_rows);
+  if (n == 0) return 0;
+  return weigh_layout(cache->B, cache->kv_heads, heads, n,
+                      (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
+      .bytes;
+}
+
+spc_status spc_kv_evict(const spc_kv_cache* cache, const float* weights, int64_t weights_stride,
+                        int32_t length, int32_t keep, int32_t first, int32_t recent,
+                        const int32_t* out_table, int32_t out_width, int32_t* out_len,
+                        int32_t* out_index, float* out_weights, int64_t out_stride,
+                        hipStream_t stream) {
+  return guarded([&] {
+    return kv_evict_impl(cache, weights, weights_stride, length, keep, first, recent, out_table,
+                         out_width, out_len, out_index, out_weights, out_stride, stream);
+  });
 }
 
 spc_status spc_verify(const void* q_logits, const void* p_logits, int32_t dtype,

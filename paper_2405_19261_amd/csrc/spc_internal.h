@@ -241,15 +241,48 @@ struct KvParams {
   int64_t q_stride, out_stride;
   int32_t heads, window;
   float scale;              // of q.k, times log2(e)
+  int32_t from;             // positions before it are left out (another launch takes them)
+  int32_t partial;          // rows leave their sums in part, also where one share is all
+  const uint8_t* mask;      // spc_cross_attend: [B] rows of mask_width, mask_stride apart, or NULL
+  int64_t mask_stride;
+  int32_t mask_width;
+  int32_t shared;           // spc_kv_attend_shared: tokens that table's only row holds for all
   int32_t tile_rows;        // rows (new token, query head) a workgroup takes: 16, 32 or 128
   int32_t splits;           // most shares the keys are cut into
   float* part;              // [B * splits][H][row tiles][tile_rows][D + 2], splits > 1
+  // spc_kv_weigh (length: L): part is [B * splits][H][row tiles][tile_rows][2]
+  const float* weights;     // [B * H] rows, weights_stride apart, or NULL
+  float* out_weights;
+  int64_t weights_stride;
+  float* scores;            // [B][H][n heads / H][width * S], or NULL
+  float* stats;             // [B][H][n heads / H][2]
 };
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
 constexpr int kKvShares = 128;                // shares the keys of a row are cut into, at most
 int kv_share_keys(int tile_rows, bool f8);  // keys that a share of them has at least
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream);
+hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
+// own: every sequence's tokens from pre.shared on (splits = 0: none has any); pre:
+// the shared ones, with table their pages alone and the rows of all sequences as
+// one's (tile_rows, splits, part of its own).
+hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream);
+constexpr int kWeighRows = 64;  // rows of a key/value head whose scores a call may keep
+hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream);
+
+// spc_kv_evict: of every sequence and head the tokens of the largest weights.
+struct EvictParams {
+  KvParams cache;
+  const float* weights;     // [B * H] rows, weights_stride apart, of `length`
+  int64_t weights_stride, out_stride;
+  int32_t length, keep, first, recent;
+  const int32_t* out_table;  // [B][out_width]
+  int32_t out_width;
+  int32_t* out_len;         // [B]
+  int32_t* out_index;       // [B][H][keep]
+  float* out_weights;       // rows of keep, out_stride apart, or NULL
+};
+hipError_t launch_kv_evict(const EvictParams& P, hipStream_t stream);
 
 // Enqueue a kernel writing `bytes` zero bytes at `ptr` (a multiple of 4, ptr
 // 4-byte aligned): a fill a graph capture may record.

@@ -1,0 +1,684 @@
+// spc_kv_evict.hip -- gfx950 kernels that keep a paged cache bounded: the attention
+// weight that cached tokens get from new ones, and the tokens of the largest
+// weights into other pages.
+#include "spc_kv_attend.h"
+
+namespace spc {
+namespace {
+
+// ------------------------------------------------------------------ weights
+// A[t] += sum over the rows (new token, query head) of a key/value head of
+// softmax_t(scale q.k_t), in two steps: every row's largest score and its sum of
+// 2^(score - largest), over shares of the keys (k_weigh_rows), then the sums over
+// rows.  Where rows are few, the first step leaves the scores in the workspace
+// (4 bytes a row and key, against 2 D of the key) and the second reads these
+// (k_weigh_sum); where they are many, it takes the products again with a tile of
+// keys in registers (k_weigh_keys), and scores are never stored.  Each weight is
+// one workgroup's, its rows always added in one order: no atomics.
+
+// The first step: as k_kv_attend, without values.
+template <int D, bool F8, int MT, bool STORE>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_rows(KvParams P) {
+  constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
+  constexpr int kQuarters = T / 16, kG = T / 4;
+  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
+  __shared__ float m_lds[kAttendWaves][16 * MT], l_lds[kAttendWaves][16 * MT];
+  const uint32_t tiles_x = (uint32_t)(((int64_t)P.n * (P.heads / P.H) + 16 * MT - 1) / (16 * MT));
+  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
+  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  if (group >= (uint32_t)(P.H * P.B * P.splits)) return;
+  const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Chunk ch = chunk_of(P, b);
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * (16 * MT);
+  if (r0 >= rows) return;
+  const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
+  const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
+  const Span span = span_of<kOwn>(P, T, share_keys(16 * MT, F8), len, ch.n, i0, i1, P.splits);
+  if (share >= span.shares) return;
+  const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
+
+  bf16x8 q[MT][kC];
+  int32_t last[MT], first[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int64_t r = min(r0 + 16 * mt + c16, rows - 1);
+    const int i = (int)(r / G), g = (int)(r % G);
+    const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
+      q[mt][c] = __builtin_bit_cast(
+          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+    }
+    const Limits seen = limits_of<kOwn>(P, ch, len, there, i);
+    last[mt] = seen.last;
+    first[mt] = seen.first;
+  }
+  const int32_t all_from = limits_of<kOwn>(P, ch, len, there, i1).first;
+  const int32_t all_to = min(limits_of<kOwn>(P, ch, len, there, i0).last + 1, there);
+
+  float m[MT], l[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = kNegInf;
+    l[mt] = 0.0f;
+  }
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  const auto index_of = [&](uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  };
+  const auto page_at = [&](int32_t t) {
+    const int p = table[index_of((uint32_t)min(t, there - 1))];
+    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
+  };
+  const int key = kG * (c16 >> 2);
+  u32x4 kf[kQuarters][kL];
+  f32x4 ks[kQuarters];
+  int any = 0, own_page = -1;  // some lane's page is none; the page of this lane's own keys
+  const auto load = [&](int32_t t0, int pk, int ps) {
+    const uint32_t tk = (uint32_t)(t0 + key), ts = (uint32_t)(t0 + kG * j);
+    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
+    const int64_t at = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D * EB + 16 * j;
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd)
+#pragma unroll
+      for (int c = 0; c < kL; ++c) kf[qd][c] = load16(P.k, at + 4 * qd * D * EB + 64 * c);
+    if constexpr (F8) {
+      const int slot = (int)(ts - index_of(ts) * (uint32_t)P.S);
+      const int64_t line = ((int64_t)max(ps, 0) * P.H + h) * P.S + slot;
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd)
+        ks[qd] = *reinterpret_cast<const f32x4*>(P.k_scale + line + 4 * qd);
+    }
+    any = __any((pk | ps) < 0);
+    own_page = ps;
+  };
+  const int64_t held = (int64_t)P.width * P.S;
+  int tile = tile0 + wave;
+  if (tile < tile1) {
+    const int32_t t0 = span.begin + T * tile;
+    load(t0, page_at(t0 + key), page_at(t0 + kG * j));
+  }
+  for (; tile < tile1; tile += kAttendWaves) {
+    const int32_t t0 = span.begin + T * tile, ts = t0 + kG * j;
+    const int32_t tn = t0 + T * kAttendWaves;
+    const bool more = tile + kAttendWaves < tile1;
+    int pk = -1, ps = -1;
+    if (more) {
+      pk = page_at(tn + key);
+      ps = page_at(tn + kG * j);
+    }
+    f32x4 s[MT][kQuarters];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) {
+        const bf16x8 k8 = widen<F8>(kf[qd][c / kSteps], c % kSteps);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
+      }
+    const bool whole = t0 >= all_from && t0 + T <= all_to && !any;
+    const bool page = own_page >= 0;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) {
+        s[mt][qd] *= P.scale;
+        if constexpr (F8) s[mt][qd] *= ks[qd];
+      }
+    if (more) load(tn, pk, ps);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float x[kG];
+#pragma unroll
+      for (int e = 0; e < kG; ++e) x[e] = s[mt][e >> 2][e & 3];
+      if (!whole) {  // uniform
+        const int32_t hi = page ? min(there - 1, last[mt]) : -1;
+#pragma unroll
+        for (int e = 0; e < kG; ++e)
+          x[e] = ((ts + e <= hi) & (ts + e >= first[mt])) ? x[e] : kNegInf;
+      }
+      if constexpr (STORE) {
+        const int64_t r = r0 + 16 * mt + c16;
+        // (a tile may reach past the table's last slot)
+        if (r < rows && ts < held) {
+          float* to = P.scores + ((b * (int64_t)P.H + h) * P.n * G + r) * held + ts;
+#pragma unroll
+          for (int e = 0; e < kG; e += 4)
+            *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        }
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int e = 1; e < kG; ++e) mx = fmaxf(mx, x[e]);
+      if (__any(mx > m[mt])) {  // some lane's maximum grows (each lane keeps its own)
+        const float m_new = fmaxf(m[mt], mx);
+        l[mt] *= m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[mt] - m_new);
+        m[mt] = m_new;
+      }
+      const float base = m[mt] == kNegInf ? 0.0f : m[mt];
+#pragma unroll
+      for (int e = 0; e < kG; ++e) l[mt] += __builtin_amdgcn_exp2f(x[e] - base);
+    }
+  }
+  // join the lanes and wavefronts of a row
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float top = fmaxf(m[mt], __shfl_xor(m[mt], 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    float sum = m[mt] == kNegInf ? l[mt] : l[mt] * __builtin_amdgcn_exp2f(m[mt] - top);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (j == 0) {
+      m_lds[wave][16 * mt + c16] = top;
+      l_lds[wave][16 * mt + c16] = sum;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 16 * MT) {
+    float top = m_lds[0][threadIdx.x], sum = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w) top = fmaxf(top, m_lds[w][threadIdx.x]);
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) {
+      const float mw = m_lds[w][threadIdx.x], lw = l_lds[w][threadIdx.x];
+      sum += mw == kNegInf ? lw : lw * __builtin_amdgcn_exp2f(mw - top);
+    }
+    float* to = P.part + 2 * ((((int64_t)z * P.H + h) * tiles_x + tile_x) * (16 * MT) + threadIdx.x);
+    to[0] = top;
+    to[1] = sum;
+  }
+}
+
+// A row's largest score and one over its sum, from its shares.
+struct RowStat {
+  float m, inv;
+};
+__device__ __forceinline__ RowStat row_stat(const KvParams& P, int T, int least, int b, int h,
+                                            const Chunk& ch, int64_t rows, int64_t r) {
+  const int G = P.heads / P.H;
+  const int64_t x = r / P.tile_rows, r0 = x * P.tile_rows;
+  const int64_t tiles_x = ((int64_t)P.n * G + P.tile_rows - 1) / P.tile_rows;
+  const Span span =
+      span_of<kOwn>(P, T, least, max(P.len[b], 0), ch.n, (int)(r0 / G),
+                    (int)((min(r0 + P.tile_rows, rows) - 1) / G), P.splits);
+  const float* part = P.part + 2 * ((((int64_t)b * P.splits * P.H + h) * tiles_x) * P.tile_rows + r);
+  const int64_t step = 2 * (int64_t)P.H * tiles_x * P.tile_rows;
+  float top = kNegInf, sum = 0.0f;
+  for (int s0 = 0; s0 < span.shares; s0 += 8) {  // eight shares under way together
+    float m[8], l[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t at = min(s0 + k, span.shares - 1) * step;
+      m[k] = part[at];
+      l[k] = part[at + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (s0 + k >= span.shares) break;
+      const float m_new = fmaxf(top, m[k]);
+      if (m_new == kNegInf) sum += l[k];  // (nothing seen: 0, or NaN)
+      else sum = sum * (top == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(top - m_new)) +
+                 l[k] * (m[k] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[k] - m_new));
+      top = m_new;
+    }
+  }
+  return RowStat{top == kNegInf ? 0.0f : top, sum == 0.0f ? 0.0f : 1.0f / sum};
+}
+
+// The weight position t had: new tokens begin at zero.
+__device__ __forceinline__ float weight_before(const KvParams& P, int b, int h, int64_t t,
+                                               int64_t pos0) {
+  return P.weights && t < pos0 ? P.weights[((int64_t)b * P.H + h) * P.weights_stride + t] : 0.0f;
+}
+
+// The second step of few rows: 1024 positions a workgroup.
+__global__ void __launch_bounds__(256) k_weigh_sum(KvParams P, int T, int least) {
+  __shared__ float m_lds[kWeighRows], inv_lds[kWeighRows];
+  const int h = blockIdx.y, b = blockIdx.z;
+  const Chunk ch = chunk_of(P, b);
+  const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
+  const int64_t end = min((int64_t)min(there, P.L), (int64_t)1 << 30);
+  const int64_t t0 = (int64_t)blockIdx.x * 1024;
+  if (t0 >= end) return;
+  const int G = P.heads / P.H, n = min(ch.n, P.n);
+  const int rows = n * G;
+  if ((int)threadIdx.x < rows) {
+    const RowStat s = row_stat(P, T, least, b, h, ch, rows, threadIdx.x);
+    m_lds[threadIdx.x] = s.m;
+    inv_lds[threadIdx.x] = s.inv;
+  }
+  __syncthreads();
+  const int64_t pos0 = (int64_t)len - ch.n, held = (int64_t)P.width * P.S;
+  const float* scores = P.scores + (b * (int64_t)P.H + h) * P.n * G * held;
+  float sum[4];
+  int32_t t[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    t[k] = (int32_t)t0 + 256 * k + (int)threadIdx.x;
+    sum[k] = 0.0f;
+  }
+  for (int i = 0; i < n; ++i) {
+    const Limits seen = limits_of<kOwn>(P, ch, len, there, i);
+    for (int g = 0; g < G; ++g) {
+      const int r = i * G + g;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (t[k] < end && t[k] >= seen.first && t[k] <= seen.last)
+          sum[k] += __builtin_amdgcn_exp2f(scores[r * held + t[k]] - m_lds[r]) * inv_lds[r];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (t[k] < end)
+      P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t[k]] =
+          weight_before(P, b, h, t[k], pos0) + sum[k];
+}
+
+// Statistics of all rows, for k_weigh_keys: [B][H][n G] pairs.
+__global__ void __launch_bounds__(256) k_weigh_stats(KvParams P, int T, int least) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  const Chunk ch = chunk_of(P, b);
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows) return;
+  const RowStat s = row_stat(P, T, least, b, h, ch, rows, r);
+  float* to = P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G + r);
+  to[0] = s.m;
+  to[1] = s.inv;
+}
+
+// The second step of many rows: a workgroup holds 64 keys, its wavefronts take
+// every fourth 16 rows.
+template <int D, bool F8>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
+  constexpr int EB = F8 ? 1 : 2, T = 64, kQuarters = 4, kG = 16;
+  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
+  __shared__ float sums[kAttendWaves][T];
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Chunk ch = chunk_of(P, b);
+  const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
+  const int32_t end = min(there, P.L);
+  if ((int64_t)blockIdx.x * T >= end) return;
+  const int32_t t0 = (int32_t)blockIdx.x * T, ts = t0 + kG * j;
+  const int G = P.heads / P.H, n = min(ch.n, P.n);
+  const int64_t rows = (int64_t)n * G, pos0 = (int64_t)len - ch.n;
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  const auto index_of = [&](uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  };
+  const auto page_at = [&](int32_t t) {
+    const int p = table[index_of((uint32_t)min(t, there - 1))];
+    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
+  };
+  const int key = kG * (c16 >> 2);
+  const int pk = page_at(t0 + key), ps = page_at(ts);
+  bf16x8 k8[kQuarters][kC];
+  f32x4 ks[kQuarters];
+  {
+    const uint32_t tk = (uint32_t)(t0 + key);
+    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
+    const int64_t at = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D * EB + 16 * j;
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd)
+#pragma unroll
+      for (int c = 0; c < kL; ++c) {
+        const u32x4 w = load16(P.k, at + 4 * qd * D * EB + 64 * c);
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) k8[qd][c * kSteps + step] = widen<F8>(w, step);
+      }
+    const int slot = (int)((uint32_t)ts - index_of((uint32_t)ts) * (uint32_t)P.S);
+    const int64_t line = ((int64_t)max(ps, 0) * P.H + h) * P.S + slot;
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd) {
+      ks[qd] = f32x4{P.scale, P.scale, P.scale, P.scale};
+      if constexpr (F8) ks[qd] *= *reinterpret_cast<const f32x4*>(P.k_scale + line + 4 * qd);
+    }
+  }
+  float acc[kG] = {};
+  // the first row that sees t0, and with a window the last that sees the tile's last key
+  const int64_t from = max((int64_t)t0 - pos0, (int64_t)0) * G / 16;
+  const int64_t to = P.window > 0 ? min(rows, ((int64_t)t0 + T - 1 + P.window - pos0) * G) : rows;
+  const int64_t tiles = (to + 15) / 16;
+  const float* stats = P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G);
+  bf16x8 q[kC];
+  float m = 0.0f, inv = 0.0f;
+  const auto load = [&](int64_t tile) {
+    const int64_t r = min(16 * tile + c16, rows - 1);
+    const int i = (int)(r / G), g = (int)(r % G);
+    const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
+      q[c] = __builtin_bit_cast(
+          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+    }
+    m = stats[2 * r];
+    inv = stats[2 * r + 1];
+  };
+  const int live = ps >= 0 ? min(there - ts, kG) : 0;
+  if (from + wave < tiles) load(from + wave);
+  for (int64_t tile = from + wave; tile < tiles; tile += kAttendWaves) {
+    f32x4 s[kQuarters];
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd)
+        s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
+    const float m_now = m, inv_now = inv;
+    const int64_t r = 16 * tile + c16;
+    const Limits seen = limits_of<kOwn>(P, ch, len, there, (int)(min(r, rows - 1) / G));
+    if (tile + kAttendWaves < tiles) load(tile + kAttendWaves);
+    // this lane's keys that the row sees: lo <= e < hi
+    const int lo = max(seen.first - ts, 0), hi = r < rows ? min(live, seen.last + 1 - ts) : 0;
+    if (__any(lo > 0 || hi < kG)) {
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        const float w = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] * ks[e >> 2][e & 3] - m_now) * inv_now;
+        acc[e] += (e >= lo && e < hi) ? w : 0.0f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kG; ++e)
+        acc[e] += __builtin_amdgcn_exp2f(s[e >> 2][e & 3] * ks[e >> 2][e & 3] - m_now) * inv_now;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kG; ++e) {
+#pragma unroll
+    for (int d = 8; d; d >>= 1) acc[e] += __shfl_xor(acc[e], d);
+    if (c16 == e) sums[wave][kG * j + e] = acc[e];
+  }
+  __syncthreads();
+  if (threadIdx.x < T) {
+    const int32_t t = t0 + (int)threadIdx.x;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) sum += sums[w][threadIdx.x];
+    if (t < end)
+      P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t] =
+          weight_before(P, b, h, t, pos0) + sum;
+  }
+}
+
+template <int D, bool F8>
+void weigh(const KvParams& P, hipStream_t stream) {
+  constexpr int T = F8 ? 64 : 32;
+  const int64_t rows = (int64_t)P.n * (P.heads / P.H), held = (int64_t)P.width * P.S;
+  const int64_t groups = ((int64_t)P.H * P.B * P.splits + 7) / 8 * 8;
+  const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups));
+  const dim3 block(64 * kAttendWaves);
+  const int least = share_keys(P.tile_rows, F8);
+  const int64_t end = held < P.L ? held : P.L;  // positions that get a weight
+  if (P.scores) {
+    if (P.tile_rows == 16) k_weigh_rows<D, F8, 1, true><<<grid, block, 0, stream>>>(P);
+    else k_weigh_rows<D, F8, 2, true><<<grid, block, 0, stream>>>(P);
+    k_weigh_sum<<<dim3((uint32_t)((end + 1023) / 1024), P.H, P.B), 256, 0, stream>>>(P, T, least);
+  } else {
+    k_weigh_rows<D, F8, 2, false><<<grid, block, 0, stream>>>(P);
+    k_weigh_stats<<<dim3((uint32_t)((rows + 255) / 256), P.H, P.B), 256, 0, stream>>>(P, T, least);
+    k_weigh_keys<D, F8>
+        <<<dim3((uint32_t)((end + 63) / 64), P.H, P.B), block, 0, stream>>>(P);
+  }
+}
+
+// ------------------------------------------------------------------ eviction
+// Which tokens of a sequence and head stay: one workgroup finds the weight of the
+// last one kept by counting, 8 bits of it a pass, the highest first, among those
+// that agree in the bits before, and then writes the positions of what is above
+// it, and of the first ones equal to it, in their order.  Weights are compared as
+// 32-bit words of their order: 0 for a position that is in no page (never kept),
+// 1 for a NaN, the largest for tokens that stay whatever they weigh.
+constexpr int kSelect = 1024, kSelectKeys = 32;  // threads; keys of one, held at a time
+__device__ __forceinline__ uint32_t order_of(float w) {
+  if (w != w) return 1u;
+  const uint32_t u = __float_as_uint(w + 0.0f);  // (-0 as 0)
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
+  constexpr int kCopies = 16;  // of a count: lanes that add to one bin do not wait for each other
+  __shared__ uint32_t bins[256 * kCopies];
+  __shared__ uint32_t more[kSelectKeys][kSelect / 64], same[kSelectKeys][kSelect / 64];
+  __shared__ uint32_t pick[4], valid;
+  const int h = blockIdx.x, b = blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const KvParams& C = P.cache;
+  const int32_t len = min(max(C.len[b], 0), C.width * C.S);
+  const float* weights = P.weights + ((int64_t)b * C.H + h) * P.weights_stride;
+  const int64_t recent = (int64_t)max(C.len[b], 0) - P.recent;  // tokens from here on stay
+  const auto key_at = [&](int64_t t) -> uint32_t {
+    if (t >= len || page_of(C, b, t) < 0) return 0u;
+    if (t < P.first || t >= recent) return 0xffffffffu;
+    return order_of(t < P.length ? weights[t] : 0.0f);
+  };
+  uint32_t key[kSelectKeys];
+  const auto fill = [&](int64_t base) {
+#pragma unroll
+    for (int i = 0; i < kSelectKeys; ++i) {
+      const int64_t t = base + (int64_t)i * kSelect + tid;
+      key[i] = base + (int64_t)i * kSelect < len ? key_at(t) : 0u;
+    }
+  };
+  constexpr int64_t kStep = (int64_t)kSelect * kSelectKeys;
+  const bool held = len <= kStep;
+  if (tid == 0) valid = 0;
+  __syncthreads();
+  // how many there are
+  uint32_t mine = 0;
+  for (int64_t base = 0; base < len; base += kStep) {
+    fill(base);
+#pragma unroll
+    for (int i = 0; i < kSelectKeys; ++i) mine += key[i] != 0u;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mine += __shfl_xor(mine, d);
+  if (lane == 0) atomicAdd(&valid, mine);
+  __syncthreads();
+  const uint32_t kept = min((uint32_t)P.keep, valid);
+  // the kept-th largest key, and how many of that value are kept
+  uint32_t border = 1u, need = kept;
+  if (kept < valid) {
+    border = 0u;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int i = tid; i < 256 * kCopies; i += kSelect) bins[i] = 0u;
+      __syncthreads();
+      for (int64_t base = 0; base < len; base += kStep) {
+        if (!held) fill(base);
+#pragma unroll
+        for (int i = 0; i < kSelectKeys; ++i)
+          if (key[i] && (shift == 24 || key[i] >> (shift + 8) == border))
+            atomicAdd(&bins[(key[i] >> shift & 255u) * kCopies + (lane & (kCopies - 1))], 1u);
+      }
+      __syncthreads();
+      if (wave == 0) {  // bins from the largest down, four a lane
+        uint32_t n[4], sum = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          n[k] = 0;
+#pragma unroll
+          for (int c = 0; c < kCopies; ++c) n[k] += bins[(255 - 4 * lane - k) * kCopies + c];
+          sum += n[k];
+        }
+        uint32_t before = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const uint32_t y = __shfl_up(before, d);
+          if (lane >= d) before += y;
+        }
+        before -= sum;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (before < need && before + n[k] >= need) {
+            pick[0] = 255 - 4 * lane - k;
+            pick[1] = before;
+          }
+          before += n[k];
+        }
+      }
+      __syncthreads();
+      border = border << 8 | pick[0];
+      need -= pick[1];
+      __syncthreads();
+    }
+  } else {
+    need = 0;  // all: what is above 0, of which none is left out
+    border = 0u;
+  }
+  // positions in their order
+  uint32_t above = 0, equal = 0;  // before the present ones
+  int32_t* index = P.out_index + ((int64_t)b * C.H + h) * P.keep;
+  float* out_w = P.out_weights ? P.out_weights + ((int64_t)b * C.H + h) * P.out_stride : nullptr;
+  for (int64_t base = 0; base < len; base += kStep) {
+    if (!held) fill(base);
+#pragma unroll
+    for (int i = 0; i < kSelectKeys; ++i) {
+      const uint32_t a = __popcll(__ballot(key[i] > border));
+      const uint32_t e = __popcll(__ballot(key[i] && key[i] == border));
+      if (lane == 0) {
+        more[i][wave] = a;
+        same[i][wave] = e;
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {  // counts before each wavefront's: 8 a lane, in order
+      constexpr int kEach = kSelectKeys * (kSelect / 64) / 64;
+      uint32_t* flat_a = &more[0][0];
+      uint32_t* flat_e = &same[0][0];
+      uint32_t a[kEach], e[kEach], sa = 0, se = 0;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        a[k] = flat_a[lane * kEach + k];
+        e[k] = flat_e[lane * kEach + k];
+        sa += a[k];
+        se += e[k];
+      }
+      uint32_t ba = sa, be = se;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t ya = __shfl_up(ba, d), ye = __shfl_up(be, d);
+        if (lane >= d) {
+          ba += ya;
+          be += ye;
+        }
+      }
+      if (lane == 63) {
+        pick[2] = ba;
+        pick[3] = be;
+      }
+      ba -= sa;
+      be -= se;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        flat_a[lane * kEach + k] = ba;
+        flat_e[lane * kEach + k] = be;
+        ba += a[k];
+        be += e[k];
+      }
+    }
+    __syncthreads();
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kSelectKeys; ++i) {
+      const uint64_t in_a = __ballot(key[i] > border), in_e = __ballot(key[i] && key[i] == border);
+      const uint32_t ra = above + more[i][wave] + (uint32_t)__popcll(in_a & below);
+      const uint32_t re = equal + same[i][wave] + (uint32_t)__popcll(in_e & below);
+      const bool stays = key[i] > border || (key[i] && key[i] == border && re < need);
+      if (stays) {
+        const uint32_t at = ra + min(re, need);
+        const int64_t t = base + (int64_t)i * kSelect + tid;
+        index[at] = (int32_t)t;
+        if (out_w) out_w[at] = t < P.length ? weights[t] : 0.0f;
+      }
+    }
+    above += pick[2];
+    equal += pick[3];
+    __syncthreads();
+  }
+  for (int64_t i = (int64_t)kept + tid; i < P.keep; i += kSelect) index[i] = -1;
+  if (h == 0 && tid == 0) P.out_len[b] = (int32_t)kept;
+}
+
+// The kept tokens of a head to their new places, 64 a workgroup.
+template <int D, bool F8>
+__global__ void __launch_bounds__(256) k_evict_move(EvictParams P) {
+  constexpr int EB = F8 ? 1 : 2, kLoads = D * EB / 16;
+  typedef typename std::conditional<F8, uint8_t, uint16_t>::type E;
+  __shared__ int32_t from_page[64], from_slot[64], to_page[64], to_slot[64];
+  const int h = blockIdx.y, b = blockIdx.z;
+  const KvParams& C = P.cache;
+  const int kept = P.out_len[b];
+  const int64_t j0 = (int64_t)blockIdx.x * 64;
+  if (j0 >= kept) return;
+  const int n = (int)min((int64_t)64, kept - j0);
+  if (threadIdx.x < 64) {
+    const int i = min((int)threadIdx.x, n - 1);
+    const int32_t t = P.out_index[((int64_t)b * C.H + h) * P.keep + j0 + i];
+    const int32_t j = (int32_t)j0 + i;
+    const int p = P.out_table[(int64_t)b * P.out_width + j / C.S];
+    const int from = page_of(C, b, t), slot = t % C.S;
+    int to = p >= 0 && p < C.pages ? p : -1;
+    if (from < 0 || (int)threadIdx.x >= n || (to == from && slot == j % C.S)) to = -1;  // (in place)
+    from_page[threadIdx.x] = max(from, 0);
+    from_slot[threadIdx.x] = max(slot, 0);
+    to_page[threadIdx.x] = to;
+    to_slot[threadIdx.x] = j % C.S;
+  }
+  __syncthreads();
+  for (int k = (int)threadIdx.x; k < 64 * kLoads; k += 256) {
+    const int i = k / kLoads, d = k % kLoads * 16;
+    if (to_page[i] < 0) continue;
+    const int64_t src = (((int64_t)from_page[i] * C.H + h) * C.S + from_slot[i]) * D * EB + d;
+    const int64_t dst = (((int64_t)to_page[i] * C.H + h) * C.S + to_slot[i]) * D * EB + d;
+    *reinterpret_cast<u32x4*>(static_cast<char*>(C.k) + dst) = load16(C.k, src);
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (to_page[lane] < 0) return;
+  const int64_t src_head = (int64_t)from_page[lane] * C.H + h, dst_head = (int64_t)to_page[lane] * C.H + h;
+  const E* src = static_cast<const E*>(C.v) + src_head * D * C.S + from_slot[lane];
+  E* dst = static_cast<E*>(C.v) + dst_head * D * C.S + to_slot[lane];
+#pragma unroll 8
+  for (int d = wave; d < D; d += 4) dst[(int64_t)d * C.S] = src[(int64_t)d * C.S];
+  if constexpr (F8) {
+    if (wave == 0) C.k_scale[dst_head * C.S + to_slot[lane]] = C.k_scale[src_head * C.S + from_slot[lane]];
+    if (wave == 1) C.v_scale[dst_head * C.S + to_slot[lane]] = C.v_scale[src_head * C.S + from_slot[lane]];
+  }
+}
+
+template <int D, bool F8>
+void move(const EvictParams& P, hipStream_t stream) {
+  k_evict_move<D, F8><<<dim3((uint32_t)((P.keep + 63) / 64), P.cache.H, P.cache.B), 256, 0, stream>>>(P);
+}
+
+}  // namespace
+
+hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream) {
+  if (P.D == 64) P.f8 ? weigh<64, true>(P, stream) : weigh<64, false>(P, stream);
+  else if (P.D == 128) P.f8 ? weigh<128, true>(P, stream) : weigh<128, false>(P, stream);
+  else P.f8 ? weigh<256, true>(P, stream) : weigh<256, false>(P, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_evict(const EvictParams& P, hipStream_t stream) {
+  const KvParams& C = P.cache;
+  k_evict_select<<<dim3(C.H, C.B), kSelect, 0, stream>>>(P);
+  if (C.D == 64) C.f8 ? move<64, true>(P, stream) : move<64, false>(P, stream);
+  else if (C.D == 128) C.f8 ? move<128, true>(P, stream) : move<128, false>(P, stream);
+  else C.f8 ? move<256, true>(P, stream) : move<256, false>(P, stream);
+  return hipGetLastError();
+}
+
+}  // namespace spc

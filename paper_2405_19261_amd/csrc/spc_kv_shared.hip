@@ -1,0 +1,109 @@
+// spc_kv_shared.hip -- gfx950 kernels of the attentions whose rows share keys: to
+// an encoder's states, and of a batch behind one prefix.
+#include "spc_kv_attend.h"
+
+namespace spc {
+namespace {
+
+// The shares of a row of a batch behind a prefix: the prefix's (taken for the
+// rows of all sequences together), then those of its own tokens, joined in
+// that order by a wavefront.  own.splits = 0: no sequence has tokens of its own.
+template <int D>
+__global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre, int own_T,
+                                                     int own_least, int pre_T, int pre_least) {
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63;
+  const Chunk ch = chunk_of(own, b);
+  const int G = own.heads / own.H;
+  const int64_t rows = (int64_t)min(ch.n, own.n) * G;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  const int shares_pre = span_of<kShared>(pre, pre_T, pre_least, 0, 0, 0, 0, pre.splits).shares;
+  int shares_own = 0;
+  const int64_t x = r / own.tile_rows, r0 = x * own.tile_rows;
+  if (own.splits)
+    shares_own = span_of<kOwn>(own, own_T, own_least, max(own.len[b], 0), ch.n, (int)(r0 / G),
+                               (int)((min(r0 + own.tile_rows, rows) - 1) / G), own.splits)
+                     .shares;
+  const int shares = shares_pre + shares_own;
+  // shares lie `step` floats apart, from the row's first one
+  const int64_t tiles_own = ((int64_t)own.n * G + own.tile_rows - 1) / own.tile_rows;
+  const int64_t tiles_pre = (pre.rows * G + pre.tile_rows - 1) / pre.tile_rows;
+  const int64_t row_pre = ch.first * G + r;
+  const float* of_pre = pre.part + (h * tiles_pre * pre.tile_rows + row_pre) * (D + 2);
+  const int64_t step_pre = (int64_t)own.H * tiles_pre * pre.tile_rows * (D + 2);
+  const float* of_own =
+      own.part + (((int64_t)b * own.splits * own.H + h) * tiles_own * own.tile_rows + r) * (D + 2);
+  const int64_t step_own = (int64_t)own.H * tiles_own * own.tile_rows * (D + 2);
+  const auto part = [&](int s) {
+    return s < shares_pre ? of_pre + s * step_pre : of_own + (s - shares_pre) * step_own;
+  };
+  // the shares' maxima and sums, four a lane
+  static_assert(kKvShares == 128, "both together at most four a lane");
+  float f[4], sum = 0.0f, top = kNegInf;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    f[k] = lane + 64 * k < shares ? part(lane + 64 * k)[0] : kNegInf;
+    top = fmaxf(top, f[k]);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    f[k] = f[k] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(f[k] - top);
+    if (lane + 64 * k < shares) sum += part(lane + 64 * k)[1] * f[k];
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  constexpr int E = D / 64;
+  float y[E] = {};
+  for (int s0 = 0; s0 < shares; s0 += 8) {  // eight shares' values under way together
+    float v[8][E];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = part(min(s0 + k, shares - 1))[2 + lane * E + e];
+    const float of_lane = s0 < 64 ? f[0] : s0 < 128 ? f[1] : s0 < 192 ? f[2] : f[3];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float fade = s0 + k < shares ? __shfl(of_lane, (s0 + k) & 63) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] += v[k][e] * fade;
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int i = (int)(r / G), g = (int)(r % G);
+  __bf16* out =
+      static_cast<__bf16*>(own.out) + (ch.first + i) * own.out_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[lane * E + e] = (__bf16)(y[e] * inv);
+}
+
+template <int D, bool F8>
+void shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
+  attend_shares<D, F8, kShared>(pre, stream);
+  if (own.splits) attend_shares<D, F8, kOwn>(own, stream);
+  const int64_t rows = (int64_t)own.n * (own.heads / own.H);
+  k_shared_join<D><<<dim3((uint32_t)((rows + 3) / 4), own.H, own.B), 256, 0, stream>>>(
+      own, pre, tile_keys(D, F8, own.tile_rows), share_keys(own.tile_rows, F8),
+      tile_keys(D, F8, pre.tile_rows), share_keys(pre.tile_rows, F8));
+}
+
+}  // namespace
+
+hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
+  if (own.D == 64) own.f8 ? shared<64, true>(own, pre, stream) : shared<64, false>(own, pre, stream);
+  else if (own.D == 128)
+    own.f8 ? shared<128, true>(own, pre, stream) : shared<128, false>(own, pre, stream);
+  else own.f8 ? shared<256, true>(own, pre, stream) : shared<256, false>(own, pre, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream) {
+  if (P.D == 64) P.f8 ? attend<64, true, kCross>(P, stream) : attend<64, false, kCross>(P, stream);
+  else if (P.D == 128)
+    P.f8 ? attend<128, true, kCross>(P, stream) : attend<128, false, kCross>(P, stream);
+  else P.f8 ? attend<256, true, kCross>(P, stream) : attend<256, false, kCross>(P, stream);
+  return hipGetLastError();
+}
+
+}  // namespace spc

@@ -108,6 +108,23 @@ def lib():
         L.spc_kv_attend.restype = ctypes.c_int
         L.spc_kv_workspace_bytes.argtypes = [cache, _I32, i64, _I32]
         L.spc_kv_workspace_bytes.restype = ctypes.c_size_t
+        queries = [_P, _I32, i64, _I32, i64, _P, _I32, ctypes.c_float]  # q .. scale
+        L.spc_kv_attend_shared.argtypes = [cache, _I32, _P, *queries, _I32, _P, i64, _P,
+                                           ctypes.c_size_t, _P]
+        L.spc_kv_attend_shared.restype = ctypes.c_int
+        L.spc_kv_shared_workspace_bytes.argtypes = [cache, _I32, _I32, i64, _I32]
+        L.spc_kv_shared_workspace_bytes.restype = ctypes.c_size_t
+        L.spc_cross_attend.argtypes = [cache, *queries, _P, i64, _I32, _P, i64, _P,
+                                       ctypes.c_size_t, _P]
+        L.spc_cross_attend.restype = ctypes.c_int
+        L.spc_kv_weigh.argtypes = [cache, *queries, _I32, _P, _P, i64, _I32, _P, ctypes.c_size_t,
+                                   _P]
+        L.spc_kv_weigh.restype = ctypes.c_int
+        L.spc_kv_weigh_workspace_bytes.argtypes = [cache, _I32, i64, _I32]
+        L.spc_kv_weigh_workspace_bytes.restype = ctypes.c_size_t
+        L.spc_kv_evict.argtypes = [cache, _P, i64, _I32, _I32, _I32, _I32, _P, _I32, _P, _P, _P,
+                                   i64, _P]
+        L.spc_kv_evict.restype = ctypes.c_int
         L.spc_workspace_bytes.argtypes = [_I32, _I32, _I32, ctypes.c_int]
         L.spc_workspace_bytes.restype = ctypes.c_size_t
         L.spc_workspace_zero_bytes.argtypes = [_I32, _I32, _I32, ctypes.c_int]
@@ -517,6 +534,25 @@ def spc_kv_read(k_pages, v_pages, page_table, kv_len, length=None, *, k_scale=No
     return k, v
 
 
+def _queries(q, cache, k_pages, q_start, scale):
+    """(rows, heads, row stride, scale) of an attention's queries."""
+    dim = cache.head_dim
+    rows, heads, stride = _kv_rows("q", q, k_pages, cache.B, q_start, dim)
+    if q.dtype is not torch.bfloat16:
+        raise TypeError(f"q must be bfloat16, not {q.dtype}")
+    return rows, heads, stride, dim ** -0.5 if scale is None else float(scale)
+
+
+def _answers(out, q, cache, k_pages, q_start):
+    """(out, its row stride) of an attention."""
+    if out is None:  # (rows of no sequence stay zero)
+        out = (torch.empty if q_start is None else torch.zeros)(q.shape, dtype=q.dtype,
+                                                                device=q.device)
+    if out.shape != q.shape or out.dtype is not q.dtype:
+        raise ValueError("out must have the shape and type of q")
+    return out, _kv_rows("out", out, k_pages, cache.B, q_start, cache.head_dim)[2]
+
+
 def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window=0, k_scale=None,
                   v_scale=None, q_start=None, max_q=None, out=None, workspace=None, stream=None):
     """Attention of new tokens, whose keys and values the cache holds
@@ -525,16 +561,8 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
     sequence; None: all rows).  ``scale`` None: 1 / sqrt(dim).  ``window`` > 0:
     only the last ``window`` tokens.  Returns ``out`` (as ``q``)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
-    dim = cache.head_dim
-    rows, heads, qs = _kv_rows("q", q, k_pages, cache.B, q_start, dim)
-    if q.dtype is not torch.bfloat16:
-        raise TypeError(f"q must be bfloat16, not {q.dtype}")
-    if out is None:  # (rows of no sequence stay zero)
-        out = (torch.empty if q_start is None else torch.zeros)(q.shape, dtype=q.dtype,
-                                                                device=q.device)
-    if out.shape != q.shape or out.dtype is not q.dtype:
-        raise ValueError("out must have the shape and type of q")
-    os_ = _kv_rows("out", out, k_pages, cache.B, q_start, dim)[2]
+    rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
+    out, os_ = _answers(out, q, cache, k_pages, q_start)
     ws, nbytes = _workspace(workspace, k_pages)
     window = _int32("window", window)
     most = rows if max_q is None else _int32("max_q", max_q)
@@ -542,9 +570,155 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
         return out
     _on_current_device(k_pages)
     _check(lib().spc_kv_attend(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start),
-                               most, dim ** -0.5 if scale is None else float(scale), window,
-                               out.data_ptr(), os_, ws, nbytes, _stream(stream)))
+                               most, scale, window, out.data_ptr(), os_, ws, nbytes,
+                               _stream(stream)))
     return out
+
+
+def spc_kv_attend_shared(q, k_pages, v_pages, page_table, kv_len, shared, *, shared_table=None,
+                         scale=None, window=0, k_scale=None, v_scale=None, q_start=None,
+                         max_q=None, out=None, workspace=None, stream=None):
+    """``spc_kv_attend`` for a batch whose sequences begin with the same
+    ``shared`` tokens, which are read once for all of them: from the pages of
+    ``shared_table`` (int32, of whole pages or more; None: the first row of
+    ``page_table``).  ``page_table`` says where the positions from ``shared`` on
+    are; ``kv_len`` counts the shared tokens.  Returns ``out`` (as ``q``)."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
+    out, os_ = _answers(out, q, cache, k_pages, q_start)
+    ws, nbytes = _workspace(workspace, k_pages)
+    window, shared = _int32("window", window), _int32("shared", shared)
+    most = rows if max_q is None else _int32("max_q", max_q)
+    if shared_table is None:
+        shared_table = page_table[0]
+    if shared_table.dim() != 1 or shared_table.shape[0] * cache.page_size < shared:
+        raise ValueError(f"shared_table must be a row of pages that hold {shared} tokens")
+    _expect("shared_table", shared_table, torch.int32, k_pages, shared_table.shape)
+    if rows == 0:
+        return out
+    _on_current_device(k_pages)
+    _check(lib().spc_kv_attend_shared(cache, shared, shared_table.data_ptr(), q.data_ptr(),
+                                      SPC_BF16, qs, heads, rows, _ptr(q_start), most, scale, window,
+                                      out.data_ptr(), os_, ws, nbytes, _stream(stream)))
+    return out
+
+
+def spc_cross_attend(q, k_pages, v_pages, page_table, kv_len, *, key_mask=None, scale=None,
+                     k_scale=None, v_scale=None, q_start=None, max_q=None, out=None,
+                     workspace=None, stream=None):
+    """Attention of a decoder's rows to the ``kv_len`` tokens of an encoder
+    whose keys and values the cache holds: every row of a sequence sees all of
+    them but those where ``key_mask`` (bool or uint8 [B, width]; tokens past its
+    width are masked) is 0.  Rows as for ``spc_kv_attend``; several decoder
+    sequences of one input may be rows of one sequence.  Returns ``out`` (as
+    ``q``); a row that sees nothing is zero."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
+    out, os_ = _answers(out, q, cache, k_pages, q_start)
+    ws, nbytes = _workspace(workspace, k_pages)
+    most = rows if max_q is None else _int32("max_q", max_q)
+    mask, mask_stride, mask_width = None, 0, 0
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"key_mask must be bool or uint8, not {key_mask.dtype}")
+        if key_mask.dim() != 2 or key_mask.shape[0] != cache.B or key_mask.stride(1) != 1:
+            raise ValueError("key_mask must be [B, width], the bytes of a row contiguous")
+        if key_mask.get_device() != k_pages.get_device():
+            raise ValueError(f"key_mask must be on {k_pages.device}, not {key_mask.device}")
+        mask, mask_stride = key_mask.data_ptr(), key_mask.stride(0)
+        mask_width = _int32("the width of key_mask", key_mask.shape[1])
+    if rows == 0:
+        return out
+    _on_current_device(k_pages)
+    _check(lib().spc_cross_attend(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start),
+                                  most, scale, mask, mask_stride, mask_width, out.data_ptr(), os_,
+                                  ws, nbytes, _stream(stream)))
+    return out
+
+
+def _weight_rows(name, t, cache, like, length=None):
+    """The stride between the rows [B, kv_heads, length] of weights."""
+    if t.dtype is not torch.float32:
+        raise TypeError(f"{name} must be {torch.float32}, not {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be on {like.device}, not {t.device}")
+    B, H = cache.B, cache.kv_heads
+    if t.dim() != 3 or t.shape[:2] != (B, H) or length not in (None, t.shape[2]):
+        raise ValueError(f"{name} must have shape {(B, H, length or 'length')}, not {tuple(t.shape)}")
+    n = _int32(f"the length of {name}", t.shape[2])
+    stride = t.stride(1) if H > 1 else t.stride(0) if B > 1 else n
+    if t.stride(2) != 1 and n > 1 or stride < n or (H > 1 and B > 1 and t.stride(0) != H * stride):
+        raise ValueError(f"the rows of {name} must be contiguous and evenly spaced")
+    return stride
+
+
+def spc_kv_weigh(q, k_pages, v_pages, page_table, kv_len, weights=None, *, scale=None, window=0,
+                 k_scale=None, v_scale=None, q_start=None, max_q=None, out=None, workspace=None,
+                 stream=None):
+    """The attention weight that every cached token gets from new ones, on top
+    of ``weights`` (float32 [B, kv_heads, length]; None: nothing), summed over
+    the new tokens and the query heads of a key/value head; the chunk's own
+    tokens begin at zero.  Rows and positions as for ``spc_kv_attend``.
+    Returns ``out``, which may be ``weights`` (None: a new tensor, zero from
+    ``kv_len`` on, of ``length`` or, without weights, of the table's tokens)."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
+    ws, nbytes = _workspace(workspace, k_pages)
+    window = _int32("window", window)
+    most = rows if max_q is None else _int32("max_q", max_q)
+    shape = (cache.B, cache.kv_heads, cache.table_width * cache.page_size)
+    if weights is not None:
+        shape = weights.shape
+    if out is None:
+        out = torch.zeros(shape, dtype=torch.float32, device=k_pages.device)
+    stride = _weight_rows("out", out, cache, k_pages)
+    if weights is not None and weights is not out:
+        if _weight_rows("weights", weights, cache, k_pages, out.shape[2]) != stride:
+            raise ValueError("weights and out must have rows at one stride")
+    if rows == 0:
+        raise ValueError("there must be a new token")
+    _on_current_device(k_pages)
+    _check(lib().spc_kv_weigh(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start), most,
+                              scale, window, _ptr(weights), out.data_ptr(), stride, out.shape[2],
+                              ws, nbytes, _stream(stream)))
+    return out
+
+
+def spc_kv_evict(k_pages, v_pages, page_table, kv_len, weights, keep, out_table, *, first=0,
+                 recent=0, k_scale=None, v_scale=None, out_len=None, out_index=None,
+                 out_weights=None, stream=None):
+    """At most ``keep`` tokens of every sequence and key/value head, in their
+    order, into the pages of ``out_table`` (int32 [B, pages], of the same
+    pools): the first ``first``, the last ``recent`` and, of the others, those
+    of the largest ``weights`` (float32 [B, kv_heads, length], as
+    ``spc_kv_weigh`` leaves them).  Returns (the tokens kept [B] int32, the
+    positions they had [B, kv_heads, keep] int32, -1 behind the last, their
+    weights [B, kv_heads, keep], new ones zero behind the last)."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    B, H, dev = cache.B, cache.kv_heads, k_pages.device
+    keep, first, recent = _int32("keep", keep), _int32("first", first), _int32("recent", recent)
+    stride = _weight_rows("weights", weights, cache, k_pages)
+    if out_table.dim() != 2:
+        raise ValueError("out_table must be [B, pages of a sequence]")
+    width = _int32("the width of out_table", out_table.shape[1])
+    _expect("out_table", out_table, torch.int32, k_pages, (B, width))
+    if keep < 1:
+        raise ValueError(f"keep must be at least 1, not {keep}")
+    if out_len is None:
+        out_len = torch.empty(B, dtype=torch.int32, device=dev)
+    if out_index is None:
+        out_index = torch.empty((B, H, keep), dtype=torch.int32, device=dev)
+    if out_weights is None:
+        out_weights = torch.zeros((B, H, keep), device=dev)
+    _expect("out_len", out_len, torch.int32, k_pages, (B,))
+    _expect("out_index", out_index, torch.int32, k_pages, (B, H, keep))
+    out_stride = _weight_rows("out_weights", out_weights, cache, k_pages, keep)
+    _on_current_device(k_pages)
+    _check(lib().spc_kv_evict(cache, weights.data_ptr(), stride, weights.shape[2], keep, first,
+                              recent, out_table.data_ptr(), width, out_len.data_ptr(),
+                              out_index.data_ptr(), out_weights.data_ptr(), out_stride,
+                              _stream(stream)))
+    return out_len, out_index, out_weights
 
 
 def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=None, *,
@@ -557,6 +731,26 @@ def spc_kv_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, ma
     if max_q is None:
         max_q = 0 if q_start is None else rows
     return lib().spc_kv_workspace_bytes(cache, _int32("heads", heads), rows, _int32("max_q", max_q))
+
+
+def spc_kv_shared_workspace_bytes(k_pages, v_pages, page_table, kv_len, shared, heads, rows,
+                                  max_q=None, *, k_scale=None, v_scale=None, q_start=None):
+    """As ``spc_kv_workspace_bytes``, for ``spc_kv_attend_shared``."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if max_q is None:
+        max_q = 0 if q_start is None else rows
+    return lib().spc_kv_shared_workspace_bytes(cache, _int32("shared", shared),
+                                               _int32("heads", heads), rows, _int32("max_q", max_q))
+
+
+def spc_kv_weigh_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=None, *,
+                                 k_scale=None, v_scale=None, q_start=None):
+    """As ``spc_kv_workspace_bytes``, for ``spc_kv_weigh``."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if max_q is None:
+        max_q = 0 if q_start is None else rows
+    return lib().spc_kv_weigh_workspace_bytes(cache, _int32("heads", heads), rows,
+                                              _int32("max_q", max_q))
 
 
 def spc_workspace_bytes(B, gamma, V, dtype_code):

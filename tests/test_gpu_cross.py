@@ -1,0 +1,177 @@
+"""Cross attention to an encoder's states (spc_cross_attend) against the 64-bit definition
+(tolerances: ops_oracle.attend)."""
+import numpy as np
+import pytest
+import torch
+
+import ops_oracle
+from cache_oracle import BF16, check_rows, fill, i32, randn
+from paper_2405_19261_amd import spc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    yield
+    torch.cuda.synchronize()
+
+
+def check(cache, q, lens, starts=None, mask=None, scale=None, **kw):
+    D = q.shape[-1]
+    out = spc.spc_cross_attend(q, *cache.args(i32(lens)), key_mask=mask, scale=scale,
+                               q_start=None if starts is None else i32(starts), **cache.scales(), **kw)
+    m = None if mask is None else mask.cpu().numpy() != 0
+
+    def sees(b, at):
+        s = np.ones(max(int(lens[b]), 0), bool)
+        if m is not None:
+            s[:m.shape[1]] &= m[b, :len(s)]
+            s[m.shape[1]:] = False
+        return s
+
+    worst = check_rows(out, q, lens, starts, lambda b: cache.dense(b, max(int(lens[b]), 0)), sees,
+                       D ** -0.5 if scale is None else scale)
+    return out, worst
+
+
+def encoder(lens, H, D, S, f8, seed=0):
+    cache = ops_oracle.Cache(len(lens), (max(max(lens), 1) + S - 1) // S, H, D, S, f8, DEV, seed=seed)
+    fill(cache, lens, seed + 50)
+    return cache
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L", [(1, 1), (1, 33), (7, 3), (9, 100), (17, 64), (1, 700), (33, 513), (70, 31),
+                                 (150, 90)])
+def test_lengths(n, L, D, f8):
+    """Rows before, at and past the encoder's length alike."""
+    lens = [L, max(L - 5, 0)]
+    check(encoder(lens, 2, D, 16, f8, seed=n), randn((2, n, 4, D), 3).to(DEV), lens)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("H,heads,S,n", [(1, 1, 32, 1), (1, 3, 48, 4), (4, 4, 128, 3), (1, 16, 16, 2),
+                                         (3, 15, 16, 9), (2, 64, 32, 4)])
+def test_heads_and_pages(H, heads, S, n, f8):
+    lens = [3 * S // 2 + 1, 4 * S, 1]
+    check(encoder(lens, H, 64, S, f8), randn((3, n, heads, 64), heads).to(DEV), lens)
+
+
+def masks(B, width, seed):
+    g = torch.Generator().manual_seed(seed)
+    m = torch.rand((B, width), generator=g) < 0.6
+    m[:, :40] = False  # a tile of which nothing is seen
+    return m
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L,width", [(1, 300, 300), (8, 300, 299), (3, 77, 130), (40, 333, 320),
+                                       (140, 150, 150), (1, 45, 41)])
+def test_masks(n, L, width, D, f8):
+    """Masks with holes, of widths that divide by nothing, narrower and wider than the sequence; NaN
+    and infinities in keys, values and scales that are masked."""
+    lens = [L, L - 9]
+    cache = encoder(lens, 2, D, 16, f8, seed=L)
+    mask = masks(2, width, n).to(DEV)
+    for b in range(2):
+        for t in range(lens[b]):
+            if t >= width or not bool(mask[b, t]):
+                p, s = int(cache.table[b, t // 16]), t % 16
+                if f8:
+                    cache.k.view(torch.uint8)[p, :, s] = 0x7f
+                    cache.v.view(torch.uint8)[p, :, :, s] = 0x7f
+                    cache.ks[p, :, s] = float("inf")
+                    cache.vs[p, :, s] = float("nan")
+                else:
+                    cache.k[p, :, s] = float("nan")
+                    cache.v[p, :, :, s] = float("inf") if t % 2 else float("nan")
+    q = randn((2, n, 4, D), 3).to(DEV)
+    out, _ = check(cache, q, lens, mask=mask)
+    # bytes that are not 0 or 1, a row stride, an odd address
+    wide = torch.full((2, width + 13), 77, dtype=torch.uint8, device=DEV)
+    wide[:, 3:3 + width] = mask.to(torch.uint8) * i32([1, 128, 255, 64])[torch.arange(width) % 4].to(torch.uint8)
+    again = spc.spc_cross_attend(q, *cache.args(i32(lens)), key_mask=wide[:, 3:3 + width], **cache.scales())
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n", [1, 5, 90])
+def test_rows_that_see_nothing(n, f8):
+    """Empty encoders and masks that leave nothing: zeros, whatever the cache holds."""
+    lens = [0, 200, 200, 50]
+    cache = encoder(lens, 1, 128, 16, f8)
+    mask = torch.zeros((4, 200), dtype=torch.bool, device=DEV)
+    mask[2] = True
+    out, _ = check(cache, randn((4, n, 4, 128), 2).to(DEV), lens, mask=mask)
+    assert bool((out[[0, 1, 3]] == 0).all()) and bool((out[2] != 0).any())
+    # one mask for all, as an expanded row
+    one = torch.ones((1, 200), dtype=torch.bool, device=DEV)
+    one[:, 20:60] = False
+    check(cache, randn((4, n, 4, 128), 2).to(DEV), lens, mask=one.expand(4, 200))
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_ragged(f8):
+    """Targets of their own lengths, rows of no sequence, chunks past max_q, pages that are none."""
+    ns, lens = [0, 1, 40, 7, 3], [40, 130, 64, 0, 90]
+    cache = encoder(lens, 2, 128, 32, f8)
+    cache.table[1, 1] = -1
+    cache.table[4, 0] = cache.pages + 5
+    starts = (np.concatenate([[0], np.cumsum(ns)]) + 2).tolist()
+    q = randn((starts[-1] + 3, 6, 128), 8).to(DEV)
+    out = torch.full_like(q, 3.0)
+    check(cache, q, lens, starts, max_q=40, out=out)
+    assert bool((out[:2] == 3.0).all()) and bool((out[-3:] == 3.0).all())
+    assert bool((out[starts[3]:starts[4]] == 0).all())
+    part = torch.full_like(q, 5.0)
+    spc.spc_cross_attend(q, *cache.args(i32(lens)), q_start=i32(starts), max_q=8, out=part,
+                         **cache.scales())
+    assert bool((part[starts[2] + 8:starts[3]] == 5.0).all())
+    assert bool((part[starts[2]:starts[2] + 8] != 5.0).any())
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("s,scale", [(12.0, None), (1.0, 0.0), (1.0, -0.3), (0.3, 1.0)])
+def test_scales_and_peaked_scores(s, scale, f8):
+    lens = [500, 77]
+    cache = encoder(lens, 1, 128, 64, f8)
+    fill(cache, lens, 3, s)
+    check(cache, randn((2, 3, 4, 128), 1, BF16, s).to(DEV), lens, scale=scale)
+
+
+@pytest.mark.parametrize("n,L", [(1, 40), (3, 700), (140, 300)])
+def test_a_nan_that_a_row_sees_is_its_answer(n, L):
+    cache = encoder([L, L], 1, 128, 16, False)
+    cache.v[int(cache.table[1, 1]), 0, 7, 4] = float("nan")
+    cache.k[int(cache.table[0, 1]), 0, 4, 9] = float("nan")
+    out = spc.spc_cross_attend(randn((2, n, 4, 128), 4).to(DEV), *cache.args(i32([L, L]))).float()
+    assert bool(out[0].isnan().all()) and bool(out[1, ..., 7].isnan().all())
+    assert not bool(torch.cat([out[1, ..., :7], out[1, ..., 8:]], -1).isnan().any())
+
+
+def test_captured_and_replayed():
+    cache = encoder([900, 650], 2, 64, 16, True)
+    q, lens = randn((2, 6, 8, 64), 2).to(DEV), i32([900, 650])
+    mask = masks(2, 900, 1).to(DEV)
+    out = torch.empty_like(q)
+
+    def call(**kw):
+        return spc.spc_cross_attend(q, *cache.args(lens), key_mask=mask, **cache.scales(), **kw)
+
+    call(out=out)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(out=out)
+    for k in range(4):
+        q.copy_(randn(q.shape, 20 + k))
+        lens.copy_(i32([900 - 31 * k, 17 * k]))
+        mask.copy_(masks(2, 900, 7 + k))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call())
