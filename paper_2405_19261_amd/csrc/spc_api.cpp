@@ -934,6 +934,10 @@ spc_status kv_queries(const spc_kv_cache* cache, const void* q, int32_t dtype, i
   P.heads = heads;
   P.scale = (float)((double)scale * 1.4426950408889634074);
   P.window = window;
+  // ceil(2^32 / G): with r < 2^32 / G the product is r / G and less than 1 / G more
+  const uint64_t G = (uint64_t)(heads / P.H);
+  if (G > 1 && (uint64_t)rows * G < ((uint64_t(1) << 32) / G))
+    P.g_magic = (uint32_t)(((uint64_t(1) << 32) + G - 1) / G);
   return SPC_OK;
 }
 
@@ -1086,21 +1090,23 @@ spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
 constexpr double kScoreBytes = 256.0 * (1 << 20);
 struct WeighLayout {
   AttendLayout cut;
-  bool scores;
+  bool scores, stats;
   size_t kept_at, bytes;
 };
 WeighLayout weigh_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t tokens, bool f8) {
   WeighLayout L;
   const int64_t rows = n * (heads / H);
   L.scores = rows <= spc::kWeighRows && 4.0 * B * H * rows * tokens <= kScoreBytes;
-  L.cut.tile_rows = L.scores && rows <= 16 ? 16 : 32;
+  L.stats = !L.scores && rows > spc::kWeighStats;
+  L.cut.tile_rows = !L.scores ? 128 : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + L.cut.tile_rows - 1) / L.cut.tile_rows, groups = B * H * tiles;
-  const int64_t most = std::max<int64_t>(1, tokens / spc::kv_share_keys(L.cut.tile_rows, f8));
+  const int64_t least = L.scores ? spc::kv_share_keys(L.cut.tile_rows, f8) : spc::kWeighShare;
+  const int64_t most = std::max<int64_t>(1, tokens / least);
   L.cut.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
                                                          (int64_t)spc::kKvShares, 65535 / B}));
   L.cut.bytes = (size_t)(groups * L.cut.splits * L.cut.tile_rows) * 8;
   L.kept_at = align_up(L.cut.bytes, 256);
-  L.bytes = L.kept_at + (size_t)(B * H * rows) * (L.scores ? (size_t)tokens * 4 : 8);
+  L.bytes = L.kept_at + (size_t)(B * H * rows) * (L.scores ? (size_t)tokens * 4 : L.stats ? 8 : 0);
   return L;
 }
 
@@ -1135,7 +1141,8 @@ spc_status kv_weigh_impl(const spc_kv_cache* cache, const void* q, int32_t dtype
   P.tile_rows = L.cut.tile_rows;
   P.splits = L.cut.splits;
   P.part = reinterpret_cast<float*>(ws);
-  (L.scores ? P.scores : P.stats) = reinterpret_cast<float*>(ws + L.kept_at);
+  if (L.scores) P.scores = reinterpret_cast<float*>(ws + L.kept_at);
+  if (L.stats) P.stats = reinterpret_cast<float*>(ws + L.kept_at);
   P.weights = weights;
   P.out_weights = out;
   P.weights_stride = weights_stride;

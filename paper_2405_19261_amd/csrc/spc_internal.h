@@ -240,6 +240,7 @@ struct KvParams {
   void* out;
   int64_t q_stride, out_stride;
   int32_t heads, window;
+  uint32_t g_magic;         // r / (heads / H) = r g_magic / 2^32 for every row r (0: not so)
   float scale;              // of q.k, times log2(e)
   int32_t from;             // positions before it are left out (another launch takes them)
   int32_t partial;          // rows leave their sums in part, also where one share is all
@@ -255,7 +256,7 @@ struct KvParams {
   float* out_weights;
   int64_t weights_stride;
   float* scores;            // [B][H][n heads / H][width * S], or NULL
-  float* stats;             // [B][H][n heads / H][2]
+  float* stats;             // [B][H][n heads / H][2], or NULL
 };
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
@@ -267,7 +268,9 @@ hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
 // the shared ones, with table their pages alone and the rows of all sequences as
 // one's (tile_rows, splits, part of its own).
 hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream);
-constexpr int kWeighRows = 64;  // rows of a key/value head whose scores a call may keep
+constexpr int kWeighRows = 64;     // rows of a key/value head whose scores a call may keep
+constexpr int kWeighShare = 512;   // keys that a share of more rows has at least
+constexpr int kWeighStats = 2048;  // rows whose statistics the second step takes itself
 hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream);
 
 // spc_kv_evict: of every sequence and head the tokens of the largest weights.

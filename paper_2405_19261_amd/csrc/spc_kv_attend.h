@@ -65,6 +65,12 @@ __device__ __forceinline__ int32_t tokens_there(const KvParams& P, int32_t len) 
   if (MODE == kCross && P.mask) return min(min(len, held), P.mask_width);
   return min(len, held);
 }
+// The new token of row r of a key/value head, G rows a token.
+__device__ __forceinline__ int token_of(const KvParams& P, int G, int64_t r) {
+  const uint32_t x = (uint32_t)r;  // (under 2^31: a launch has fewer than 2^24 tiles of rows)
+  if (P.g_magic) return (int)__umulhi(x, P.g_magic);
+  return (int)(G == 1 ? x : x / (uint32_t)G);
+}
 // The positions that row i of ch sees.
 struct Limits {
   int32_t first, last;
@@ -205,7 +211,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
   const int64_t rows = (int64_t)min(ch.n, tokens_of<MODE>(P)) * G, r0 = (int64_t)tile_x * (16 * MT);
   if (r0 >= rows) return;
   const int32_t len = MODE == kShared ? 0 : max(P.len[b], 0), there = tokens_there<MODE>(P, len);
-  const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
+  const int i0 = token_of(P, G, r0), i1 = token_of(P, G, min(r0 + 16 * MT, rows) - 1);
   const Span span =
       span_of<MODE>(P, T, share_keys(16 * MT, F8), len, ch.n, i0, i1, P.splits);
   if (share >= span.shares) return;
@@ -216,7 +222,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int64_t r = min(r0 + 16 * mt + c16, rows - 1);
-    const int i = (int)(r / G), g = (int)(r % G);
+    const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
@@ -453,7 +459,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
       }
       if (alone) {
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int i = (int)(r / G), g = (int)(r % G);
+        const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
         bf16x4 z;
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
@@ -471,6 +477,58 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
     }
   }
 }
+
+// Where a tile of keys lies: its four lane groups' kG consecutive keys, each in one
+// page.  All of it is the same for a wavefront, so pages are read and offsets are
+// computed by the scalar unit, a tile ahead of the loads that need them, and a lane
+// selects its group's.
+template <int D, int EB, int kG>
+struct TilePages {
+  int32_t p[4];
+  int64_t head[4];  // where the group's page holds the head, in bytes
+  int32_t slot[4];  // of the group's first key
+  uint32_t valid;   // a bit a group
+
+  __device__ __forceinline__ static uint32_t index_of(const KvParams& P, uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  }
+  __device__ __forceinline__ void fetch(const KvParams& P, const int32_t* table, int32_t there,
+                                        int32_t t0) {
+    typedef const __attribute__((address_space(4))) int32_t* Constant;
+    const Constant of = (Constant)table;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) p[g] = of[index_of(P, (uint32_t)min(t0 + kG * g, there - 1))];
+  }
+  // Waits for the pages here rather than at a read of LDS.
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) asm volatile("" : "+s"(p[g]));
+  }
+  __device__ __forceinline__ void place(const KvParams& P, int h, int32_t there, int32_t t0) {
+    valid = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const uint32_t t = (uint32_t)(t0 + kG * g);
+      const bool ok = (int32_t)t < there && (uint32_t)p[g] < (uint32_t)P.pages;
+      valid |= (uint32_t)ok << g;
+      slot[g] = (int32_t)(t - index_of(P, t) * (uint32_t)P.S);
+      // (a cache has fewer than 2^32 pages of a head: one is 1 KiB at least)
+      head[g] = (int64_t)((uint64_t)((ok ? (uint32_t)p[g] : 0u) * (uint32_t)P.H + (uint32_t)h) *
+                          (uint32_t)(P.S * D * EB));
+    }
+  }
+  template <class X>
+  __device__ __forceinline__ static X select(X a, X b, X c, X d, int g) {
+    const X lo = g & 1 ? b : a, hi = g & 1 ? d : c;
+    return g & 2 ? hi : lo;
+  }
+  __device__ __forceinline__ int64_t head_of(int g) const {
+    return select(head[0], head[1], head[2], head[3], g);
+  }
+  __device__ __forceinline__ int32_t slot_of(int g) const {
+    return select(slot[0], slot[1], slot[2], slot[3], g);
+  }
+};
 
 // Keys in a tile of k_kv_attend_rows.
 constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
@@ -495,6 +553,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   constexpr int kVL = T * EB / 64;                   // 16-byte loads of a lane's keys of V
   constexpr int kFrags = kQuarters * kL + kM * kVL;  // of 1 KiB: K's, then V's
   constexpr int kMine = kFrags / kAttendWaves;       // that a wavefront brings
+  constexpr int kAhead = 4;                          // reads of LDS under way
   static_assert(kQuarters * kL % kAttendWaves == 0 && kM * kVL % kAttendWaves == 0, "whole shares");
   __shared__ u32x4 frags[2][kFrags][64];
   __shared__ float scales[2][2][F8 ? T : 1];         // of keys, of values
@@ -512,8 +571,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   if (r0 >= rows) return;
   const int32_t len = MODE == kShared ? 0 : max(P.len[b], 0), there = tokens_there<MODE>(P, len);
   const Span span =
-      span_of<MODE>(P, T, share_keys(kRows, F8), len, ch.n, (int)(r0 / G),
-                    (int)((min(r0 + kRows, rows) - 1) / G), P.splits);
+      span_of<MODE>(P, T, share_keys(kRows, F8), len, ch.n, token_of(P, G, r0),
+                    token_of(P, G, min(r0 + kRows, rows) - 1), P.splits);
   if (share >= span.shares) return;
   int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
 
@@ -524,7 +583,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int64_t r = min(w0 + 16 * mt + c16, rows - 1);
-    const int i = (int)(r / G), g = (int)(r % G);
+    const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
@@ -556,7 +615,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     tile0 = max(tile0, __builtin_amdgcn_readfirstlane(from) / T);  // (no other is seen by any)
     tile1 = min(tile1, (__builtin_amdgcn_readfirstlane(to) + T - 1) / T);
   } else {
-    const int i0 = (int)(min(w0, rows - 1) / G), i1 = (int)((min(w0 + 16 * MT, rows) - 1) / G);
+    const int i0 = token_of(P, G, min(w0, rows - 1));
+    const int i1 = token_of(P, G, min(w0 + 16 * MT, rows) - 1);
     all_from = limits_of<MODE>(P, ch, len, there, i1).first;
     all_to = min(limits_of<MODE>(P, ch, len, there, i0).last + 1, there);
   }
@@ -564,60 +624,69 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   f32x4 o[MT][kM] = {};
   float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};
   const int32_t* table = P.table + (int64_t)b * P.width;
-  const auto index_of = [&](uint32_t t) {
-    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
-  };
-  const auto page_at = [&](int32_t t) {
-    const int p = table[index_of((uint32_t)min(t, there - 1))];
-    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
-  };
-  const int key = kG * (c16 >> 2);
   // the fragments this wavefront brings of a tile at t0, and a lane's scale
   u32x4 mine[kMine];
   float my_scale = 0.0f;
-  int page_next = -1, page_now = -1;  // the page of this lane's own keys
-  MaskBytes<kG> mask_next{}, mask_now{};
+  TilePages<D, EB, kG> pages;
+  uint32_t valid_next = 0, valid_now = 0;  // groups of keys that are in a page
+  int32_t ts_next = 0;                     // the first of this lane's own keys
+  MaskBytes<kG> mask_next{};
+  uint32_t see = 0;                        // of this tile: this lane's keys that are there
+  const int lane_k = (c16 & 3) * D * EB + 16 * j + wave / kL * 4 * D * EB + wave % kL * 64;
+  const int lane_v = (c16 + wave / kVL * 16) * P.S * EB + wave % kVL * 16;
+  const int step_v = kAttendWaves / kVL * 16 * P.S * EB;
   const auto bring = [&](int32_t t0) {
-    const int pk = page_at(t0 + key), ps = page_at(t0 + kG * j);
-    const uint32_t tk = (uint32_t)(t0 + key), ts = (uint32_t)(t0 + kG * j);
-    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
-    const int slot = (int)(ts - index_of(ts) * (uint32_t)P.S);
-    const int64_t hk = (int64_t)max(pk, 0) * P.H + h, hs = (int64_t)max(ps, 0) * P.H + h;
-    const int64_t at_k = (hk * P.S + slot_k) * D * EB + 16 * j;
-    const int64_t at_v = ((hs * D + c16) * P.S + slot) * EB;
-    page_next = ps;
+    pages.place(P, h, there, t0);
+    valid_next = pages.valid;
+    ts_next = t0 + kG * j;
     if constexpr (MODE == kCross)
-      if (P.mask)
-        mask_next = mask_bytes<kG>(P.mask + b * P.mask_stride + (int32_t)ts, there - (int32_t)ts);
+      if (P.mask) mask_next = mask_bytes<kG>(P.mask + b * P.mask_stride + ts_next, there - ts_next);
+    const int gk = c16 >> 2;
+    const char* k = static_cast<const char*>(P.k) + pages.head_of(gk) +
+                    (pages.slot_of(gk) * (D * EB) + lane_k);
+    const char* v = static_cast<const char*>(P.v) + pages.head_of(j) + (pages.slot_of(j) * EB + lane_v);
+    constexpr int kKeys = kQuarters * kL / kAttendWaves;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int f = wave + i * kAttendWaves;
-      if (i < kQuarters * kL / kAttendWaves)
-        mine[i] = load16(P.k, at_k + (f / kL) * 4 * D * EB + f % kL * 64);
-      else
-        mine[i] = load16(P.v, at_v + (int64_t)(16 * ((f - kQuarters * kL) / kVL)) * P.S * EB +
-                                  (f - kQuarters * kL) % kVL * 16);
+    for (int i = 0; i < kMine; ++i) {  // fragments wave, wave + 4, ...
+      if (i < kKeys)
+        mine[i] = load16(k, kAttendWaves * i / kL * 4 * D * EB + kAttendWaves * i % kL * 64);
+      else mine[i] = load16(v, (int64_t)((i - kKeys) * step_v));
     }
     if constexpr (F8) {
       if (threadIdx.x < 2 * T) {  // a thread a key and kind
-        const uint32_t t = (uint32_t)t0 + threadIdx.x % T;
-        const int p = page_at((int32_t)t);
-        const int64_t at = ((int64_t)max(p, 0) * P.H + h) * P.S + (t - index_of(t) * (uint32_t)P.S);
-        my_scale = p < 0 ? 0.0f : threadIdx.x < T ? P.k_scale[at] * P.scale : P.v_scale[at];
+        const bool ok = t0 + lane < there && (pages.valid >> j & 1u);
+        const int64_t at = pages.head_of(j) / D + pages.slot_of(j) + c16;
+        my_scale = !ok ? 0.0f : threadIdx.x < T ? P.k_scale[at] * P.scale : P.v_scale[at];
       }
     }
   };
   const auto put = [&](int buf) {
+    // values outside the keys (or masked) may be anything, NaN too: zeros instead
+    constexpr uint32_t kAll = (1u << kG) - 1u;
+    const int live = valid_next >> j & 1u ? there - ts_next : 0;
+    see = live <= 0 ? 0u : live >= kG ? kAll : (1u << live) - 1u;
+    if (MODE == kOwn && P.from > ts_next) see &= kAll << min(P.from - ts_next, kG);
+    if constexpr (MODE == kCross)
+      if (P.mask) see &= mask_bits(mask_next);
+    if (__any(see != kAll)) {
+#pragma unroll
+      for (int i = kQuarters * kL / kAttendWaves; i < kMine; ++i) {
+        const int part = (wave + i * kAttendWaves - kQuarters * kL) % kVL;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mine[i][w] &= word_mask<F8>(see >> (8 * part), w);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kMine; ++i) frags[buf][wave + i * kAttendWaves][lane] = mine[i];
     if constexpr (F8)
       if (threadIdx.x < 2 * T) scales[buf][threadIdx.x / T][threadIdx.x % T] = my_scale;
   };
   if (tile0 < tile1) {
+    pages.fetch(P, table, there, span.begin + T * tile0);
     bring(span.begin + T * tile0);
+    if (tile0 + 1 < tile1) pages.fetch(P, table, there, span.begin + T * (tile0 + 1));
     put(0);
-    page_now = page_next;
-    mask_now = mask_next;
+    valid_now = valid_next;
     if (tile0 + 1 < tile1) bring(span.begin + T * (tile0 + 1));
   }
   __syncthreads();
@@ -629,23 +698,35 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    {
+      u32x4 ring[kAhead];
 #pragma unroll
-    for (int qd = 0; qd < kQuarters; ++qd)
+      for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][f][lane];
 #pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        const bf16x8 k8 = widen<F8>(frags[buf][qd * kL + c / kSteps][lane], c % kSteps);
+      for (int f = 0; f < kQuarters * kL; ++f) {
+        const int qd = f / kL;
+        const u32x4 k = ring[f % kAhead];
+        if (f + kAhead < kQuarters * kL) ring[f % kAhead] = frags[buf][f + kAhead][lane];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
+        for (int step = 0; step < kSteps; ++step) {
+          const bf16x8 k8 = widen<F8>(k, step);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                k8, q[mt][f % kL * kSteps + step], s[mt][qd], 0, 0, 0);
+        }
       }
-    bool whole = t0 >= all_from && t0 + T <= all_to && !__any(page_now < 0);
-    uint32_t see = 0xffffffffu;  // of kCross: this lane's keys that are seen
-    if constexpr (MODE == kCross) {
-      const int live = page_now >= 0 ? there - ts : 0;
-      see = live <= 0 ? 0u : live >= kG ? (1u << kG) - 1u : (1u << live) - 1u;
-      if (P.mask) see &= mask_bits(mask_now);
-      whole = !__any(see != (1u << kG) - 1u);
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+      for (int f = 0; f < kQuarters * kL; ++f) {
+        if (F8) __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, MT * kSteps, 0);
+        if (f + kAhead < kQuarters * kL) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
     }
+    if (tile + 2 < tile1) pages.fetch(P, table, there, t0 + 2 * T);
+    const bool whole = MODE == kCross ? !__any(see != (1u << kG) - 1u)
+                                      : t0 >= all_from && t0 + T <= all_to && valid_now == 15u;
     bf16x8 p[MT][kG / 8];
     float x[MT][kG], mx[MT];
     bool grows = false;
@@ -657,7 +738,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
         else x[mt][e] = s[mt][e >> 2][e & 3] * P.scale;
       }
       if (!whole) {  // uniform
-        const int32_t hi = page_now >= 0 ? min(there - 1, last[mt]) : -1;
+        const int32_t hi = valid_now >> j & 1u ? min(there - 1, last[mt]) : -1;
 #pragma unroll
         for (int e = 0; e < kG; ++e) {
           if constexpr (MODE == kCross) x[mt][e] = see >> e & 1u ? x[mt][e] : kNegInf;
@@ -696,36 +777,37 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
         p[mt][e >> 3][e & 7] = (__bf16)w;
       }
     }
-    const int live = page_now >= 0 ? there - ts : 0;
+    if (tile + 2 < tile1) pages.arrive();
+    // (V's fragments: those of the next products are under way)
+    constexpr int kValues = kM * kVL;
+    u32x4 ring[kAhead];
 #pragma unroll
-    for (int d = 0; d < kM; ++d)
+    for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][kQuarters * kL + f][lane];
 #pragma unroll
-      for (int part = 0; part < kVL; ++part) {
-        u32x4 v = frags[buf][kQuarters * kL + d * kVL + part][lane];
-        // what lies outside the keys (or is masked) may be anything, NaN too
-        if (!whole) {
-          if constexpr (MODE == kCross) {
+    for (int f = 0; f < kValues; ++f) {
+      const int d = f / kVL, part = f % kVL;
+      const u32x4 v = ring[f % kAhead];
+      if (f + kAhead < kValues) ring[f % kAhead] = frags[buf][kQuarters * kL + f + kAhead][lane];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] &= word_mask<F8>(see >> (part * 8), i);
-          } else {
-            first_of<F8>(v, live - part * 8);
-            if (MODE == kOwn && P.from > ts) without_first<F8>(v, P.from - ts - part * 8);
-          }
-        }
+      for (int step = 0; step < kSteps; ++step) {
+        const bf16x8 v8 = widen<F8>(v, step);
 #pragma unroll
-        for (int step = 0; step < kSteps; ++step) {
-          const bf16x8 v8 = widen<F8>(v, step);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-            o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][part * kSteps + step],
-                                                               o[mt][d], 0, 0, 0);
-        }
+        for (int mt = 0; mt < MT; ++mt)
+          o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][part * kSteps + step],
+                                                             o[mt][d], 0, 0, 0);
       }
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+    for (int f = 0; f < kValues; ++f) {
+      if (F8) __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, MT * kSteps, 0);
+      if (f + kAhead < kValues) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
     // (the buffer written here was last read before the last barrier)
     if (tile + 1 < tile1) {
       put(buf ^ 1);
-      page_now = page_next;
-      mask_now = mask_next;
+      valid_now = valid_next;
       if (tile + 2 < tile1) bring(t0 + 2 * T);
     }
     __syncthreads();
@@ -740,7 +822,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     if (r >= rows) continue;
     if (alone) {
       const float inv = l[mt] == 0.0f ? 0.0f : 1.0f / l[mt];
-      const int i = (int)(r / G), g = (int)(r % G);
+      const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
       uint16_t* out = static_cast<uint16_t*>(P.out) + (ch.first + i) * P.out_stride +
                       (int64_t)(h * G + g) * D + 4 * j;
 #pragma unroll
@@ -776,8 +858,8 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows, int 
   if (r >= rows) return;
   const int64_t x = r / tile_rows, tiles_x = ((int64_t)P.n * G + tile_rows - 1) / tile_rows;
   const int64_t r0 = x * tile_rows;
-  const Span span = span_of<MODE>(P, T, least, max(P.len[b], 0), ch.n, (int)(r0 / G),
-                                  (int)((min(r0 + tile_rows, rows) - 1) / G), P.splits);
+  const Span span = span_of<MODE>(P, T, least, max(P.len[b], 0), ch.n, token_of(P, G, r0),
+                                  token_of(P, G, min(r0 + tile_rows, rows) - 1), P.splits);
   if (span.shares == 1) return;
   const auto part = [&](int s) {
     return P.part + (((((int64_t)b * P.splits + s) * P.H + h) * tiles_x + x) * tile_rows + (r - r0)) *
@@ -814,7 +896,7 @@ __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows, int 
     }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int i = (int)(r / G), g = (int)(r % G);
+  const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
   __bf16* out = static_cast<__bf16*>(P.out) + (ch.first + i) * P.out_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
   for (int e = 0; e < E; ++e) out[lane * E + e] = (__bf16)(y[e] * inv);

@@ -9,16 +9,17 @@ namespace {
 // ------------------------------------------------------------------ weights
 // A[t] += sum over the rows (new token, query head) of a key/value head of
 // softmax_t(scale q.k_t), in two steps: every row's largest score and its sum of
-// 2^(score - largest), over shares of the keys (k_weigh_rows), then the sums over
-// rows.  Where rows are few, the first step leaves the scores in the workspace
-// (4 bytes a row and key, against 2 D of the key) and the second reads these
-// (k_weigh_sum); where they are many, it takes the products again with a tile of
-// keys in registers (k_weigh_keys), and scores are never stored.  Each weight is
-// one workgroup's, its rows always added in one order: no atomics.
+// 2^(score - largest), over shares of the keys, then the sums over rows.  Where
+// rows are few, the first step leaves the scores in the workspace (4 bytes a row
+// and key, against 2 D of the key) and the second reads these (k_weigh_rows,
+// k_weigh_sum); where they are many, it takes the products again with a tile of
+// keys in registers (k_weigh_tile, k_weigh_keys), and scores are never stored.
+// Each weight is one workgroup's, its rows always added in one order: no atomics.
 
 // The first step: as k_kv_attend, without values.
-template <int D, bool F8, int MT, bool STORE>
-__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_rows(KvParams P) {
+template <int D, bool F8, int MT>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 && MT * (F8 ? 2 : 1) < 4 ? 4 : 2)
+    k_weigh_rows(KvParams P) {
   constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
   constexpr int kQuarters = T / 16, kG = T / 4;
   constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
@@ -35,7 +36,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_r
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * (16 * MT);
   if (r0 >= rows) return;
   const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
-  const int i0 = (int)(r0 / G), i1 = (int)((min(r0 + 16 * MT, rows) - 1) / G);
+  const int i0 = token_of(P, G, r0), i1 = token_of(P, G, min(r0 + 16 * MT, rows) - 1);
   const Span span = span_of<kOwn>(P, T, share_keys(16 * MT, F8), len, ch.n, i0, i1, P.splits);
   if (share >= span.shares) return;
   const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_r
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int64_t r = min(r0 + 16 * mt + c16, rows - 1);
-    const int i = (int)(r / G), g = (int)(r % G);
+    const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
@@ -146,15 +147,12 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_r
         for (int e = 0; e < kG; ++e)
           x[e] = ((ts + e <= hi) & (ts + e >= first[mt])) ? x[e] : kNegInf;
       }
-      if constexpr (STORE) {
-        const int64_t r = r0 + 16 * mt + c16;
-        // (a tile may reach past the table's last slot)
-        if (r < rows && ts < held) {
-          float* to = P.scores + ((b * (int64_t)P.H + h) * P.n * G + r) * held + ts;
+      const int64_t r = r0 + 16 * mt + c16;
+      if (r < rows && ts < held) {  // (a tile may reach past the table's last slot)
+        float* to = P.scores + ((b * (int64_t)P.H + h) * P.n * G + r) * held + ts;
 #pragma unroll
-          for (int e = 0; e < kG; e += 4)
-            *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-        }
+        for (int e = 0; e < kG; e += 4)
+          *reinterpret_cast<f32x4*>(to + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
       }
       float mx = x[0];
 #pragma unroll
@@ -198,6 +196,187 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 4 : 2) k_weigh_r
   }
 }
 
+// The first step of many rows: 128 of them a workgroup, 32 a wavefront, over every
+// tile of 64 keys of the share.  The keys pass through LDS in the order of the
+// products' lanes, double-buffered, 8-bit ones widened once as they are written.
+// Every lane keeps a maximum and a sum of its own keys until the end.
+template <int D, bool F8>
+__global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 128 ? 3 : 4) k_weigh_tile(KvParams P) {
+  constexpr int MT = 2, kRows = 16 * MT * kAttendWaves, T = 64;
+  constexpr int EB = F8 ? 1 : 2, kQuarters = T / 16, kG = T / 4;
+  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
+  constexpr int kMine = kQuarters * kL / kAttendWaves;  // 16-byte loads of a lane
+  __shared__ u32x4 frags[2][kQuarters * kC][64];
+  __shared__ float scales[2][F8 ? T : 1];
+  const uint32_t tiles_x = (uint32_t)(((int64_t)P.n * (P.heads / P.H) + kRows - 1) / kRows);
+  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
+  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  if (group >= (uint32_t)(P.H * P.B * P.splits)) return;
+  const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Chunk ch = chunk_of(P, b);
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r0 = (int64_t)tile_x * kRows;
+  if (r0 >= rows) return;
+  const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
+  const Span span = span_of<kOwn>(P, T, kWeighShare, len, ch.n, token_of(P, G, r0),
+                                  token_of(P, G, min(r0 + kRows, rows) - 1), P.splits);
+  if (share >= span.shares) return;
+  const int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
+  // this wavefront's rows (the last row again behind the end); a negative scale is
+  // taken as a positive one of negated queries, so that maxima need no scaling
+  const int64_t w0 = r0 + 16 * MT * wave;
+  const uint32_t sign = P.scale < 0.0f ? 0x80008000u : 0u;
+  const float scale = fabsf(P.scale);
+  bf16x8 q[MT][kC];
+  int32_t last[MT], first[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int64_t r = min(w0 + 16 * mt + c16, rows - 1);
+    const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
+    const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
+      u32x4 w = *reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d);
+      w ^= sign;
+      q[mt][c] = __builtin_bit_cast(bf16x8, w);
+    }
+    const Limits seen = limits_of<kOwn>(P, ch, len, there, i);
+    last[mt] = seen.last;
+    first[mt] = seen.first;
+  }
+  const int i0 = token_of(P, G, min(w0, rows - 1));
+  const int i1 = token_of(P, G, min(w0 + 16 * MT, rows) - 1);
+  const int32_t all_from = limits_of<kOwn>(P, ch, len, there, i1).first;
+  const int32_t all_to = min(limits_of<kOwn>(P, ch, len, there, i0).last + 1, there);
+
+  float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};  // m of unscaled scores
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  const auto index_of = [&](uint32_t t) {
+    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
+  };
+  const auto page_at = [&](int32_t t) {
+    const int p = table[index_of((uint32_t)min(t, there - 1))];
+    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
+  };
+  const int key = kG * (c16 >> 2);
+  u32x4 mine[kMine];
+  float my_scale = 0.0f;
+  int page_next = -1, page_now = -1;  // the page of this lane's own keys
+  const auto bring = [&](int32_t t0) {
+    const int pk = page_at(t0 + key);
+    const uint32_t tk = (uint32_t)(t0 + key);
+    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
+    const int64_t at = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D * EB + 16 * j;
+    page_next = page_at(t0 + kG * j);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int f = wave + i * kAttendWaves;
+      mine[i] = load16(P.k, at + (f / kL) * 4 * D * EB + f % kL * 64);
+    }
+    if constexpr (F8) {
+      if (threadIdx.x < T) {
+        const uint32_t t = (uint32_t)t0 + threadIdx.x;
+        const int p = page_at((int32_t)t);
+        my_scale = p < 0 ? 0.0f
+                         : P.k_scale[((int64_t)p * P.H + h) * P.S + (t - index_of(t) * (uint32_t)P.S)];
+      }
+    }
+  };
+  const auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int f = wave + i * kAttendWaves;
+#pragma unroll
+      for (int step = 0; step < kSteps; ++step)
+        frags[buf][f * kSteps + step][lane] = __builtin_bit_cast(u32x4, widen<F8>(mine[i], step));
+    }
+    if constexpr (F8)
+      if (threadIdx.x < T) scales[buf][threadIdx.x] = my_scale;
+  };
+  if (tile0 < tile1) {
+    bring(span.begin + T * tile0);
+    put(0);
+    page_now = page_next;
+    if (tile0 + 1 < tile1) bring(span.begin + T * (tile0 + 1));
+  }
+  __syncthreads();
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int buf = (tile - tile0) & 1;
+    const int32_t t0 = span.begin + T * tile, ts = t0 + kG * j;
+    f32x4 s[MT][kQuarters];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int qd = 0; qd < kQuarters; ++qd)
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const bf16x8 k8 = __builtin_bit_cast(bf16x8, frags[buf][qd * kC + c][lane]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
+      }
+    const bool whole = t0 >= all_from && t0 + T <= all_to && !__any(page_now < 0);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float x[kG];
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        x[e] = s[mt][e >> 2][e & 3];
+        if constexpr (F8) x[e] *= scales[buf][kG * j + e];
+      }
+      const int32_t hi = page_now >= 0 ? min(there - 1, last[mt]) : -1;
+      const int lo_e = first[mt] - ts, hi_e = hi - ts;  // this lane's keys that the row sees
+      if (!whole) {  // uniform
+#pragma unroll
+        for (int e = 0; e < kG; ++e) x[e] = (e <= hi_e && e >= lo_e) ? x[e] : kNegInf;
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int e = 1; e < kG; ++e) mx = fmaxf(mx, x[e]);
+      if (__any(mx > m[mt])) {  // some lane's maximum grows
+        const float m_new = fmaxf(m[mt], mx);
+        l[mt] *= m[mt] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m[mt] - m_new) * scale);
+        m[mt] = m_new;
+      }
+      const float base = m[mt] == kNegInf ? 0.0f : m[mt] * scale;
+      if (whole) {
+#pragma unroll
+        for (int e = 0; e < kG; ++e) l[mt] += __builtin_amdgcn_exp2f(fmaf(x[e], scale, -base));
+      } else {
+#pragma unroll
+        for (int e = 0; e < kG; ++e)
+          l[mt] += (e <= hi_e && e >= lo_e) ? __builtin_amdgcn_exp2f(fmaf(x[e], scale, -base)) : 0.0f;
+      }
+    }
+    // (the buffer written here was last read before the last barrier)
+    if (tile + 1 < tile1) {
+      put(buf ^ 1);
+      page_now = page_next;
+      if (tile + 2 < tile1) bring(t0 + 2 * T);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float top = fmaxf(m[mt], __shfl_xor(m[mt], 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    float sum = m[mt] == kNegInf ? 0.0f : l[mt] * __builtin_amdgcn_exp2f((m[mt] - top) * scale);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const int64_t r = w0 + 16 * mt + c16;
+    if (r < rows && j == 0) {
+      float* to = P.part + 2 * ((((int64_t)z * P.H + h) * tiles_x + tile_x) * kRows + (r - r0));
+      to[0] = top == kNegInf ? kNegInf : top * scale;
+      to[1] = sum;
+    }
+  }
+}
+
 // A row's largest score and one over its sum, from its shares.
 struct RowStat {
   float m, inv;
@@ -208,8 +387,8 @@ __device__ __forceinline__ RowStat row_stat(const KvParams& P, int T, int least,
   const int64_t x = r / P.tile_rows, r0 = x * P.tile_rows;
   const int64_t tiles_x = ((int64_t)P.n * G + P.tile_rows - 1) / P.tile_rows;
   const Span span =
-      span_of<kOwn>(P, T, least, max(P.len[b], 0), ch.n, (int)(r0 / G),
-                    (int)((min(r0 + P.tile_rows, rows) - 1) / G), P.splits);
+      span_of<kOwn>(P, T, least, max(P.len[b], 0), ch.n, token_of(P, G, r0),
+                    token_of(P, G, min(r0 + P.tile_rows, rows) - 1), P.splits);
   const float* part = P.part + 2 * ((((int64_t)b * P.splits * P.H + h) * tiles_x) * P.tile_rows + r);
   const int64_t step = 2 * (int64_t)P.H * tiles_x * P.tile_rows;
   float top = kNegInf, sum = 0.0f;
@@ -240,51 +419,58 @@ __device__ __forceinline__ float weight_before(const KvParams& P, int b, int h, 
   return P.weights && t < pos0 ? P.weights[((int64_t)b * P.H + h) * P.weights_stride + t] : 0.0f;
 }
 
-// The second step of few rows: 1024 positions a workgroup.
+// The second step of few rows: 1024 positions a workgroup, four rows of a thread's
+// four positions under way together, the first of them before the statistics.
 __global__ void __launch_bounds__(256) k_weigh_sum(KvParams P, int T, int least) {
   __shared__ float m_lds[kWeighRows], inv_lds[kWeighRows];
   const int h = blockIdx.y, b = blockIdx.z;
   const Chunk ch = chunk_of(P, b);
   const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
-  const int64_t end = min((int64_t)min(there, P.L), (int64_t)1 << 30);
-  const int64_t t0 = (int64_t)blockIdx.x * 1024;
+  const int32_t end = min(there, P.L), t0 = (int32_t)blockIdx.x * 1024;
   if (t0 >= end) return;
   const int G = P.heads / P.H, n = min(ch.n, P.n);
   const int rows = n * G;
+  const int64_t pos0 = (int64_t)len - ch.n, held = (int64_t)P.width * P.S;
+  const float* scores = P.scores + (b * (int64_t)P.H + h) * P.n * G * held + t0 + threadIdx.x;
+  const auto at = [&](int k) { return t0 + 256 * k + (int)threadIdx.x; };
+  float s[4][4], sum[4] = {};
+  const auto load = [&](int r0) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (r0 + r < rows && at(k) < end) s[r][k] = scores[(r0 + r) * held + 256 * k];
+  };
+  load(0);
+  float before[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) before[k] = at(k) < end ? weight_before(P, b, h, at(k), pos0) : 0.0f;
   if ((int)threadIdx.x < rows) {
-    const RowStat s = row_stat(P, T, least, b, h, ch, rows, threadIdx.x);
-    m_lds[threadIdx.x] = s.m;
-    inv_lds[threadIdx.x] = s.inv;
+    const RowStat x = row_stat(P, T, least, b, h, ch, rows, threadIdx.x);
+    m_lds[threadIdx.x] = x.m;
+    inv_lds[threadIdx.x] = x.inv;
   }
   __syncthreads();
-  const int64_t pos0 = (int64_t)len - ch.n, held = (int64_t)P.width * P.S;
-  const float* scores = P.scores + (b * (int64_t)P.H + h) * P.n * G * held;
-  float sum[4];
-  int32_t t[4];
+  for (int r0 = 0; r0 < rows; r0 += 4) {
+    if (r0) load(r0);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    t[k] = (int32_t)t0 + 256 * k + (int)threadIdx.x;
-    sum[k] = 0.0f;
-  }
-  for (int i = 0; i < n; ++i) {
-    const Limits seen = limits_of<kOwn>(P, ch, len, there, i);
-    for (int g = 0; g < G; ++g) {
-      const int r = i * G + g;
+    for (int r = 0; r < 4; ++r) {
+      if (r0 + r >= rows) break;
+      const Limits seen = limits_of<kOwn>(P, ch, len, there, (r0 + r) / G);
+      const float m = m_lds[r0 + r], inv = inv_lds[r0 + r];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (t[k] < end && t[k] >= seen.first && t[k] <= seen.last)
-          sum[k] += __builtin_amdgcn_exp2f(scores[r * held + t[k]] - m_lds[r]) * inv_lds[r];
-      }
+      for (int k = 0; k < 4; ++k)
+        if (at(k) >= seen.first && at(k) <= min(seen.last, end - 1))
+          sum[k] += __builtin_amdgcn_exp2f(s[r][k] - m) * inv;
     }
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k)
-    if (t[k] < end)
-      P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t[k]] =
-          weight_before(P, b, h, t[k], pos0) + sum[k];
+    if (at(k) < end)
+      P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + at(k)] = before[k] + sum[k];
 }
 
-// Statistics of all rows, for k_weigh_keys: [B][H][n G] pairs.
+// Statistics of more rows than k_weigh_keys takes itself: [B][H][n G] pairs.
 __global__ void __launch_bounds__(256) k_weigh_stats(KvParams P, int T, int least) {
   const int h = blockIdx.y, b = blockIdx.z;
   const Chunk ch = chunk_of(P, b);
@@ -297,23 +483,27 @@ __global__ void __launch_bounds__(256) k_weigh_stats(KvParams P, int T, int leas
   to[1] = s.inv;
 }
 
-// The second step of many rows: a workgroup holds 64 keys, its wavefronts take
-// every fourth 16 rows.
-template <int D, bool F8>
-__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
+// The second step of many rows: a wavefront holds 64 keys and takes 16 rows at a
+// time.  KEYS: the wavefronts of a workgroup have keys of their own and take the
+// same rows; else they share 64 keys and take every kWaves-th 16 rows, and their
+// sums are added in LDS.
+template <int D, bool F8, bool KEYS>
+__global__ void __launch_bounds__(KEYS ? 256 : 512, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
+  constexpr int kWaves = KEYS ? 4 : 8;
   constexpr int EB = F8 ? 1 : 2, T = 64, kQuarters = 4, kG = 16;
   constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
-  __shared__ float sums[kAttendWaves][T];
+  __shared__ float sums[KEYS ? 1 : kWaves][T];
+  __shared__ float stats[2 * kWeighStats];
   const int h = blockIdx.y, b = blockIdx.z;
   const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Chunk ch = chunk_of(P, b);
   const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
   const int32_t end = min(there, P.L);
-  if ((int64_t)blockIdx.x * T >= end) return;
-  const int32_t t0 = (int32_t)blockIdx.x * T, ts = t0 + kG * j;
-  const int G = P.heads / P.H, n = min(ch.n, P.n);
-  const int64_t rows = (int64_t)n * G, pos0 = (int64_t)len - ch.n;
+  if ((int64_t)blockIdx.x * (KEYS ? T * kWaves : T) >= end) return;
+  const int32_t t0 = (int32_t)(KEYS ? blockIdx.x * kWaves + wave : blockIdx.x) * T, ts = t0 + kG * j;
+  const int G = P.heads / P.H;
+  const int64_t rows = (int64_t)min(ch.n, P.n) * G, pos0 = (int64_t)len - ch.n;
   const int32_t* table = P.table + (int64_t)b * P.width;
   const auto index_of = [&](uint32_t t) {
     return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
@@ -346,17 +536,34 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_k
       if constexpr (F8) ks[qd] *= *reinterpret_cast<const f32x4*>(P.k_scale + line + 4 * qd);
     }
   }
+  // the rows that see some of the keys, and those of them that see all
+  const auto row_at = [&](int64_t position) { return (position - pos0) * G; };
+  const int64_t r_first = max(row_at(t0), (int64_t)0), r_all = row_at((int64_t)t0 + T - 1);
+  int64_t r_end = rows, r_all_end = rows;
+  if (P.window > 0) {
+    r_end = min(rows, row_at((int64_t)t0 + T - 1 + P.window));
+    r_all_end = min(rows, row_at((int64_t)t0 + P.window));
+  }
+  const int64_t tile0 = r_first / 16, tiles = t0 < end ? (r_end + 15) / 16 : 0;
+  const int live = ps >= 0 ? min(there - ts, kG) : 0;
+  const bool all_live = !__any(live < kG);
+  // their statistics
+  if (!P.stats) {
+    for (int r = (int)threadIdx.x; r < (int)rows; r += 64 * kWaves) {
+      const RowStat x = row_stat(P, T, kWeighShare, b, h, ch, rows, r);
+      stats[2 * r] = x.m;
+      stats[2 * r + 1] = x.inv;
+    }
+    __syncthreads();
+  }
+  const float* all_stats = P.stats ? P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G) : stats;
+
   float acc[kG] = {};
-  // the first row that sees t0, and with a window the last that sees the tile's last key
-  const int64_t from = max((int64_t)t0 - pos0, (int64_t)0) * G / 16;
-  const int64_t to = P.window > 0 ? min(rows, ((int64_t)t0 + T - 1 + P.window - pos0) * G) : rows;
-  const int64_t tiles = (to + 15) / 16;
-  const float* stats = P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G);
   bf16x8 q[kC];
   float m = 0.0f, inv = 0.0f;
   const auto load = [&](int64_t tile) {
     const int64_t r = min(16 * tile + c16, rows - 1);
-    const int i = (int)(r / G), g = (int)(r % G);
+    const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
@@ -364,12 +571,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_k
       q[c] = __builtin_bit_cast(
           bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
     }
-    m = stats[2 * r];
-    inv = stats[2 * r + 1];
+    m = all_stats[2 * r];
+    inv = all_stats[2 * r + 1];
   };
-  const int live = ps >= 0 ? min(there - ts, kG) : 0;
-  if (from + wave < tiles) load(from + wave);
-  for (int64_t tile = from + wave; tile < tiles; tile += kAttendWaves) {
+  constexpr int kStride = KEYS ? 1 : kWaves;
+  int64_t tile = tile0 + (KEYS ? 0 : wave);
+  if (tile < tiles) load(tile);
+  for (; tile < tiles; tile += kStride) {
     f32x4 s[kQuarters];
 #pragma unroll
     for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -379,60 +587,71 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_k
       for (int qd = 0; qd < kQuarters; ++qd)
         s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
     const float m_now = m, inv_now = inv;
-    const int64_t r = 16 * tile + c16;
-    const Limits seen = limits_of<kOwn>(P, ch, len, there, (int)(min(r, rows - 1) / G));
-    if (tile + kAttendWaves < tiles) load(tile + kAttendWaves);
-    // this lane's keys that the row sees: lo <= e < hi
-    const int lo = max(seen.first - ts, 0), hi = r < rows ? min(live, seen.last + 1 - ts) : 0;
-    if (__any(lo > 0 || hi < kG)) {
-#pragma unroll
-      for (int e = 0; e < kG; ++e) {
-        const float w = __builtin_amdgcn_exp2f(s[e >> 2][e & 3] * ks[e >> 2][e & 3] - m_now) * inv_now;
-        acc[e] += (e >= lo && e < hi) ? w : 0.0f;
-      }
-    } else {
+    if (tile + kStride < tiles) load(tile + kStride);
+    if (all_live && 16 * tile >= r_all && 16 * tile + 16 <= r_all_end) {  // uniform
 #pragma unroll
       for (int e = 0; e < kG; ++e)
-        acc[e] += __builtin_amdgcn_exp2f(s[e >> 2][e & 3] * ks[e >> 2][e & 3] - m_now) * inv_now;
+        acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], ks[e >> 2][e & 3], -m_now)),
+                      inv_now, acc[e]);
+    } else {
+      const int64_t r = 16 * tile + c16;
+      const Limits seen = limits_of<kOwn>(P, ch, len, there, token_of(P, G, min(r, rows - 1)));
+      // this lane's keys that the row sees: lo <= e < hi
+      const int lo = max(seen.first - ts, 0), hi = r < rows ? min(live, seen.last + 1 - ts) : 0;
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        const float w =
+            __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], ks[e >> 2][e & 3], -m_now)) * inv_now;
+        acc[e] += (e >= lo && e < hi) ? w : 0.0f;
+      }
     }
   }
 #pragma unroll
   for (int e = 0; e < kG; ++e) {
 #pragma unroll
     for (int d = 8; d; d >>= 1) acc[e] += __shfl_xor(acc[e], d);
-    if (c16 == e) sums[wave][kG * j + e] = acc[e];
   }
-  __syncthreads();
-  if (threadIdx.x < T) {
-    const int32_t t = t0 + (int)threadIdx.x;
-    float sum = 0.0f;
+  float sum = 0.0f;  // of key t0 + lane
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) sum += sums[w][threadIdx.x];
-    if (t < end)
-      P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t] =
-          weight_before(P, b, h, t, pos0) + sum;
+  for (int e = 0; e < kG; ++e)
+    if (c16 == e) sum = acc[e];
+  const int t = kG * j + c16;
+  if constexpr (!KEYS) {
+    sums[wave][t] = sum;
+    __syncthreads();
+    if (wave) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += sums[w][t];
   }
+  if (t0 + t < end)
+    P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t0 + t] =
+        weight_before(P, b, h, t0 + t, pos0) + sum;
 }
 
 template <int D, bool F8>
 void weigh(const KvParams& P, hipStream_t stream) {
-  constexpr int T = F8 ? 64 : 32;
   const int64_t rows = (int64_t)P.n * (P.heads / P.H), held = (int64_t)P.width * P.S;
   const int64_t groups = ((int64_t)P.H * P.B * P.splits + 7) / 8 * 8;
   const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups));
-  const dim3 block(64 * kAttendWaves);
-  const int least = share_keys(P.tile_rows, F8);
   const int64_t end = held < P.L ? held : P.L;  // positions that get a weight
   if (P.scores) {
-    if (P.tile_rows == 16) k_weigh_rows<D, F8, 1, true><<<grid, block, 0, stream>>>(P);
-    else k_weigh_rows<D, F8, 2, true><<<grid, block, 0, stream>>>(P);
-    k_weigh_sum<<<dim3((uint32_t)((end + 1023) / 1024), P.H, P.B), 256, 0, stream>>>(P, T, least);
-  } else {
-    k_weigh_rows<D, F8, 2, false><<<grid, block, 0, stream>>>(P);
-    k_weigh_stats<<<dim3((uint32_t)((rows + 255) / 256), P.H, P.B), 256, 0, stream>>>(P, T, least);
-    k_weigh_keys<D, F8>
-        <<<dim3((uint32_t)((end + 63) / 64), P.H, P.B), block, 0, stream>>>(P);
+    if (P.tile_rows == 16) k_weigh_rows<D, F8, 1><<<grid, 64 * kAttendWaves, 0, stream>>>(P);
+    else k_weigh_rows<D, F8, 2><<<grid, 64 * kAttendWaves, 0, stream>>>(P);
+    k_weigh_sum<<<dim3((uint32_t)((end + 1023) / 1024), P.H, P.B), 256, 0, stream>>>(
+        P, F8 ? 64 : 32, share_keys(P.tile_rows, F8));
+    return;
   }
+  k_weigh_tile<D, F8><<<grid, 64 * kAttendWaves, 0, stream>>>(P);
+  if (P.stats)
+    k_weigh_stats<<<dim3((uint32_t)((rows + 255) / 256), P.H, P.B), 256, 0, stream>>>(P, 64,
+                                                                                    kWeighShare);
+  if ((int64_t)P.B * P.H * ((end + 255) / 256) >= 512)
+    k_weigh_keys<D, F8, true>
+        <<<dim3((uint32_t)((end + 255) / 256), P.H, P.B), 256, 0, stream>>>(P);
+  else
+    k_weigh_keys<D, F8, false>
+        <<<dim3((uint32_t)((end + 63) / 64), P.H, P.B), 512, 0, stream>>>(P);
 }
 
 // ------------------------------------------------------------------ eviction

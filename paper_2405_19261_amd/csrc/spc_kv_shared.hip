@@ -21,8 +21,8 @@ __global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre,
   int shares_own = 0;
   const int64_t x = r / own.tile_rows, r0 = x * own.tile_rows;
   if (own.splits)
-    shares_own = span_of<kOwn>(own, own_T, own_least, max(own.len[b], 0), ch.n, (int)(r0 / G),
-                               (int)((min(r0 + own.tile_rows, rows) - 1) / G), own.splits)
+    shares_own = span_of<kOwn>(own, own_T, own_least, max(own.len[b], 0), ch.n, token_of(own, G, r0),
+                               token_of(own, G, min(r0 + own.tile_rows, rows) - 1), own.splits)
                      .shares;
   const int shares = shares_pre + shares_own;
   // shares lie `step` floats apart, from the row's first one
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre,
     }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int i = (int)(r / G), g = (int)(r % G);
+  const int i = token_of(own, G, r), g = (int)(r - (int64_t)i * G);
   __bf16* out =
       static_cast<__bf16*>(own.out) + (ch.first + i) * own.out_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
