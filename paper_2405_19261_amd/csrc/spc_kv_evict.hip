@@ -660,78 +660,95 @@ void weigh(const KvParams& P, hipStream_t stream) {
 // that agree in the bits before, and then writes the positions of what is above
 // it, and of the first ones equal to it, in their order.  Weights are compared as
 // 32-bit words of their order: 0 for a position that is in no page (never kept),
-// 1 for a NaN, the largest for tokens that stay whatever they weigh.
-constexpr int kSelect = 1024, kSelectKeys = 32;  // threads; keys of one, held at a time
+// 1 for a NaN, the largest for tokens that stay whatever they weigh.  THREADS
+// times KEYS positions are held in registers; of longer rows the keys are taken
+// again from memory every pass.
 __device__ __forceinline__ uint32_t order_of(float w) {
   if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.0f);  // (-0 as 0)
   return u >> 31 ? ~u : u | 0x80000000u;
 }
+// t / S of positions under 2^30.
+__device__ __forceinline__ uint32_t page_index(const KvParams& C, uint32_t t) {
+  return C.s16_magic ? __umulhi(t >> 4, C.s16_magic) : t >> 4;
+}
 
-__global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
-  constexpr int kCopies = 16;  // of a count: lanes that add to one bin do not wait for each other
-  __shared__ uint32_t bins[256 * kCopies];
-  __shared__ uint32_t more[kSelectKeys][kSelect / 64], same[kSelectKeys][kSelect / 64];
-  __shared__ uint32_t pick[4], valid;
+template <int THREADS, int KEYS>
+__global__ void __launch_bounds__(THREADS) k_evict_select(EvictParams P) {
+  // copies of a count: lanes that add to one bin do not wait for each other, and a
+  // bin's copies lie in different banks
+  constexpr int kCopies = 16, kCopy = 257, kWaves = THREADS / 64;
+  __shared__ uint32_t bins[kCopies * kCopy];
+  __shared__ __align__(16) uint32_t total[256];
+  __shared__ uint32_t more[KEYS * kWaves], same[KEYS * kWaves];
+  __shared__ uint32_t pick[4], valid[kWaves];
   const int h = blockIdx.x, b = blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const KvParams& C = P.cache;
-  const int32_t len = min(max(C.len[b], 0), C.width * C.S);
+  const int32_t whole_len = max(C.len[b], 0), len = min(whole_len, C.width * C.S);
   const float* weights = P.weights + ((int64_t)b * C.H + h) * P.weights_stride;
-  const int64_t recent = (int64_t)max(C.len[b], 0) - P.recent;  // tokens from here on stay
-  const auto key_at = [&](int64_t t) -> uint32_t {
-    if (t >= len || page_of(C, b, t) < 0) return 0u;
-    if (t < P.first || t >= recent) return 0xffffffffu;
-    return order_of(t < P.length ? weights[t] : 0.0f);
-  };
-  uint32_t key[kSelectKeys];
+  const int32_t* table = C.table + (int64_t)b * C.width;
+  const int64_t recent = (int64_t)whole_len - P.recent;  // tokens from here on stay
+  uint32_t key[KEYS];
   const auto fill = [&](int64_t base) {
+    float w[KEYS];
+    int32_t page[KEYS];
 #pragma unroll
-    for (int i = 0; i < kSelectKeys; ++i) {
-      const int64_t t = base + (int64_t)i * kSelect + tid;
-      key[i] = base + (int64_t)i * kSelect < len ? key_at(t) : 0u;
+    for (int i = 0; i < KEYS; ++i) {
+      const int64_t t = base + (int64_t)i * THREADS + tid;
+      w[i] = t < min(len, P.length) ? weights[t] : 0.0f;
+      page[i] = t < len ? table[page_index(C, (uint32_t)t)] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+      const int64_t t = base + (int64_t)i * THREADS + tid;
+      key[i] = t < P.first || t >= recent ? 0xffffffffu : order_of(w[i]);
+      if ((uint32_t)page[i] >= (uint32_t)C.pages) key[i] = 0u;
     }
   };
-  constexpr int64_t kStep = (int64_t)kSelect * kSelectKeys;
+  constexpr int64_t kStep = (int64_t)THREADS * KEYS;
   const bool held = len <= kStep;
-  if (tid == 0) valid = 0;
-  __syncthreads();
   // how many there are
   uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) key[i] = 0u;
   for (int64_t base = 0; base < len; base += kStep) {
     fill(base);
 #pragma unroll
-    for (int i = 0; i < kSelectKeys; ++i) mine += key[i] != 0u;
+    for (int i = 0; i < KEYS; ++i) mine += (uint32_t)__popcll(__ballot(key[i] != 0u));
   }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) mine += __shfl_xor(mine, d);
-  if (lane == 0) atomicAdd(&valid, mine);
+  if (lane == 0) valid[wave] = mine;
+  for (int i = tid; i < kCopies * kCopy; i += THREADS) bins[i] = 0u;
   __syncthreads();
-  const uint32_t kept = min((uint32_t)P.keep, valid);
-  // the kept-th largest key, and how many of that value are kept
-  uint32_t border = 1u, need = kept;
-  if (kept < valid) {
-    border = 0u;
+  uint32_t there = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) there += valid[w];
+  const uint32_t kept = min((uint32_t)P.keep, there);
+  // the kept-th largest key, and how many of that value are kept (all: what is above 0)
+  uint32_t border = 0u, need = kept < there ? kept : 0u;
+  if (kept < there) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256 * kCopies; i += kSelect) bins[i] = 0u;
-      __syncthreads();
       for (int64_t base = 0; base < len; base += kStep) {
         if (!held) fill(base);
 #pragma unroll
-        for (int i = 0; i < kSelectKeys; ++i)
+        for (int i = 0; i < KEYS; ++i)
           if (key[i] && (shift == 24 || key[i] >> (shift + 8) == border))
-            atomicAdd(&bins[(key[i] >> shift & 255u) * kCopies + (lane & (kCopies - 1))], 1u);
+            atomicAdd(&bins[(lane & (kCopies - 1)) * kCopy + (key[i] >> shift & 255u)], 1u);
+      }
+      __syncthreads();
+      if (tid < 256) {  // (and the counts are zero again)
+        uint32_t n = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) {
+          n += bins[c * kCopy + tid];
+          bins[c * kCopy + tid] = 0u;
+        }
+        total[255 - tid] = n;
       }
       __syncthreads();
       if (wave == 0) {  // bins from the largest down, four a lane
-        uint32_t n[4], sum = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          n[k] = 0;
-#pragma unroll
-          for (int c = 0; c < kCopies; ++c) n[k] += bins[(255 - 4 * lane - k) * kCopies + c];
-          sum += n[k];
-        }
+        const u32x4 n = *reinterpret_cast<const u32x4*>(&total[4 * lane]);
+        const uint32_t sum = n[0] + n[1] + n[2] + n[3];
         uint32_t before = sum;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -751,11 +768,7 @@ __global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
       __syncthreads();
       border = border << 8 | pick[0];
       need -= pick[1];
-      __syncthreads();
     }
-  } else {
-    need = 0;  // all: what is above 0, of which none is left out
-    border = 0u;
   }
   // positions in their order
   uint32_t above = 0, equal = 0;  // before the present ones
@@ -764,24 +777,22 @@ __global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
   for (int64_t base = 0; base < len; base += kStep) {
     if (!held) fill(base);
 #pragma unroll
-    for (int i = 0; i < kSelectKeys; ++i) {
-      const uint32_t a = __popcll(__ballot(key[i] > border));
-      const uint32_t e = __popcll(__ballot(key[i] && key[i] == border));
+    for (int i = 0; i < KEYS; ++i) {
+      const uint64_t a = __ballot(key[i] > border), e = __ballot(key[i] && key[i] == border);
       if (lane == 0) {
-        more[i][wave] = a;
-        same[i][wave] = e;
+        more[i * kWaves + wave] = (uint32_t)__popcll(a);
+        same[i * kWaves + wave] = (uint32_t)__popcll(e);
       }
     }
     __syncthreads();
-    if (wave == 0) {  // counts before each wavefront's: 8 a lane, in order
-      constexpr int kEach = kSelectKeys * (kSelect / 64) / 64;
-      uint32_t* flat_a = &more[0][0];
-      uint32_t* flat_e = &same[0][0];
+    if (wave == 0) {  // counts before each wavefront's, some a lane, in order
+      constexpr int kEach = (KEYS * kWaves + 63) / 64;
       uint32_t a[kEach], e[kEach], sa = 0, se = 0;
 #pragma unroll
       for (int k = 0; k < kEach; ++k) {
-        a[k] = flat_a[lane * kEach + k];
-        e[k] = flat_e[lane * kEach + k];
+        const int at = lane * kEach + k;
+        a[k] = at < KEYS * kWaves ? more[at] : 0u;
+        e[k] = at < KEYS * kWaves ? same[at] : 0u;
         sa += a[k];
         se += e[k];
       }
@@ -802,8 +813,11 @@ __global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
       be -= se;
 #pragma unroll
       for (int k = 0; k < kEach; ++k) {
-        flat_a[lane * kEach + k] = ba;
-        flat_e[lane * kEach + k] = be;
+        const int at = lane * kEach + k;
+        if (at < KEYS * kWaves) {
+          more[at] = ba;
+          same[at] = be;
+        }
         ba += a[k];
         be += e[k];
       }
@@ -811,14 +825,13 @@ __global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
     __syncthreads();
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int i = 0; i < kSelectKeys; ++i) {
+    for (int i = 0; i < KEYS; ++i) {
       const uint64_t in_a = __ballot(key[i] > border), in_e = __ballot(key[i] && key[i] == border);
-      const uint32_t ra = above + more[i][wave] + (uint32_t)__popcll(in_a & below);
-      const uint32_t re = equal + same[i][wave] + (uint32_t)__popcll(in_e & below);
-      const bool stays = key[i] > border || (key[i] && key[i] == border && re < need);
-      if (stays) {
+      const uint32_t ra = above + more[i * kWaves + wave] + (uint32_t)__popcll(in_a & below);
+      const uint32_t re = equal + same[i * kWaves + wave] + (uint32_t)__popcll(in_e & below);
+      if (key[i] > border || (key[i] && key[i] == border && re < need)) {
         const uint32_t at = ra + min(re, need);
-        const int64_t t = base + (int64_t)i * kSelect + tid;
+        const int64_t t = base + (int64_t)i * THREADS + tid;
         index[at] = (int32_t)t;
         if (out_w) out_w[at] = t < P.length ? weights[t] : 0.0f;
       }
@@ -827,53 +840,127 @@ __global__ void __launch_bounds__(kSelect) k_evict_select(EvictParams P) {
     equal += pick[3];
     __syncthreads();
   }
-  for (int64_t i = (int64_t)kept + tid; i < P.keep; i += kSelect) index[i] = -1;
+  for (int64_t i = (int64_t)kept + tid; i < P.keep; i += THREADS) index[i] = -1;
   if (h == 0 && tid == 0) P.out_len[b] = (int32_t)kept;
 }
 
-// The kept tokens of a head to their new places, 64 a workgroup.
+// The kept tokens of a head to their new places, 64 a workgroup.  Keys go as rows.
+// Values are gathered in LDS from the sixteen-byte pieces (N tokens of a dimension)
+// that hold a kept token, each loaded once, as many dimensions at a time as fit, and
+// stored as whole pieces.
 template <int D, bool F8>
 __global__ void __launch_bounds__(256) k_evict_move(EvictParams P) {
-  constexpr int EB = F8 ? 1 : 2, kLoads = D * EB / 16;
+  constexpr int EB = F8 ? 1 : 2, kLoads = D * EB / 16, N = 16 / EB, kPieces = 64 / N;
+  constexpr int kHeld = 2048;  // pieces of a dimension that LDS holds
   typedef typename std::conditional<F8, uint8_t, uint16_t>::type E;
-  __shared__ int32_t from_page[64], from_slot[64], to_page[64], to_slot[64];
-  const int h = blockIdx.y, b = blockIdx.z;
+  __shared__ u32x4 held[kHeld];
+  __shared__ int64_t from_key[64], to_key[64];  // lines of the key pages; to: -1, none
+  __shared__ int64_t piece_at[64];              // of values: bytes, dimension 0
+  __shared__ int64_t to_value[kPieces];         // of a whole piece, -1: element by element
+  __shared__ uint16_t place[64];                // a token's piece and place in it
+  __shared__ int32_t pieces;
+  const int h = blockIdx.y, b = blockIdx.z, tid = (int)threadIdx.x;
   const KvParams& C = P.cache;
   const int kept = P.out_len[b];
   const int64_t j0 = (int64_t)blockIdx.x * 64;
   if (j0 >= kept) return;
   const int n = (int)min((int64_t)64, kept - j0);
-  if (threadIdx.x < 64) {
-    const int i = min((int)threadIdx.x, n - 1);
-    const int32_t t = P.out_index[((int64_t)b * C.H + h) * P.keep + j0 + i];
+  if (tid < 64) {
+    const int i = min(tid, n - 1);
+    const int32_t t = max(P.out_index[((int64_t)b * C.H + h) * P.keep + j0 + i], 0);
     const int32_t j = (int32_t)j0 + i;
-    const int p = P.out_table[(int64_t)b * P.out_width + j / C.S];
-    const int from = page_of(C, b, t), slot = t % C.S;
-    int to = p >= 0 && p < C.pages ? p : -1;
-    if (from < 0 || (int)threadIdx.x >= n || (to == from && slot == j % C.S)) to = -1;  // (in place)
-    from_page[threadIdx.x] = max(from, 0);
-    from_slot[threadIdx.x] = max(slot, 0);
-    to_page[threadIdx.x] = to;
-    to_slot[threadIdx.x] = j % C.S;
+    const uint32_t ij = page_index(C, (uint32_t)j), it = page_index(C, (uint32_t)t);
+    const int p = P.out_table[(int64_t)b * P.out_width + ij];
+    const int from = C.table[(int64_t)b * C.width + it];
+    const int sf = t - (int)it * C.S, st = j - (int)ij * C.S;
+    const bool ok = tid < n && (uint32_t)p < (uint32_t)C.pages && (uint32_t)from < (uint32_t)C.pages &&
+                    !(p == from && sf == st);  // (in place: not moved)
+    const int64_t hf = (int64_t)(ok ? from : 0) * C.H + h, ht = (int64_t)(ok ? p : 0) * C.H + h;
+    from_key[tid] = hf * C.S + sf;
+    to_key[tid] = ok ? ht * C.S + st : -1;
+    // the pieces, numbered where they begin (tokens ascend)
+    const int id = ok ? t / N : -1;
+    const int id_before = __shfl_up(id, 1);
+    const bool first = ok && (tid == 0 || id_before != id);
+    const uint64_t firsts = __ballot(first);
+    const int piece = (int)__popcll(firsts & (((uint64_t)2 << tid) - 1)) - 1;
+    if (first) piece_at[piece] = (hf * D * C.S + (sf & ~(N - 1))) * EB;
+    place[tid] = (uint16_t)(max(piece, 0) * N + (sf & (N - 1)));
+    const uint64_t all = __ballot(ok);
+    if (tid % N == 0) {
+      const uint64_t mask = ((uint64_t)1 << N) - 1;
+      to_value[tid / N] = (all >> tid & mask) == mask ? (ht * D * C.S + st) * EB : -1;
+    }
+    if (tid == 0) pieces = (int)__popcll(firsts);
   }
   __syncthreads();
-  for (int k = (int)threadIdx.x; k < 64 * kLoads; k += 256) {
-    const int i = k / kLoads, d = k % kLoads * 16;
-    if (to_page[i] < 0) continue;
-    const int64_t src = (((int64_t)from_page[i] * C.H + h) * C.S + from_slot[i]) * D * EB + d;
-    const int64_t dst = (((int64_t)to_page[i] * C.H + h) * C.S + to_slot[i]) * D * EB + d;
-    *reinterpret_cast<u32x4*>(static_cast<char*>(C.k) + dst) = load16(C.k, src);
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (to_page[lane] < 0) return;
-  const int64_t src_head = (int64_t)from_page[lane] * C.H + h, dst_head = (int64_t)to_page[lane] * C.H + h;
-  const E* src = static_cast<const E*>(C.v) + src_head * D * C.S + from_slot[lane];
-  E* dst = static_cast<E*>(C.v) + dst_head * D * C.S + to_slot[lane];
-#pragma unroll 8
-  for (int d = wave; d < D; d += 4) dst[(int64_t)d * C.S] = src[(int64_t)d * C.S];
-  if constexpr (F8) {
-    if (wave == 0) C.k_scale[dst_head * C.S + to_slot[lane]] = C.k_scale[src_head * C.S + from_slot[lane]];
-    if (wave == 1) C.v_scale[dst_head * C.S + to_slot[lane]] = C.v_scale[src_head * C.S + from_slot[lane]];
+  const int count = pieces;
+  if (count == 0) return;  // (all in place)
+  // dimensions at a time: a power of two, so that the pieces fit
+  int dims = D;
+  while (dims * count > kHeld) dims >>= 1;
+  const int shift = 31 - __clz(dims);
+  const int64_t stride = (int64_t)C.S * EB;  // between dimensions
+  for (int d0 = 0; d0 < D; d0 += dims) {
+    constexpr int kAtOnce = kHeld / 256;
+    u32x4 v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = k * 256 + tid;
+      if (i < count << shift)
+        v[k] = load16(C.v, piece_at[i >> shift] + (d0 + (i & (dims - 1))) * stride);
+    }
+    if (d0 == 0) {  // keys, under the first loads
+      for (int k = tid; k < 64 * kLoads; k += 256) {
+        const int i = k / kLoads, d = k % kLoads * 16;
+        if (to_key[i] < 0) continue;
+        *reinterpret_cast<u32x4*>(static_cast<char*>(C.k) + to_key[i] * (D * EB) + d) =
+            load16(C.k, from_key[i] * (D * EB) + d);
+      }
+      if constexpr (F8) {
+        if (tid < 128 && to_key[tid & 63] >= 0) {
+          float* scale = tid < 64 ? C.k_scale : C.v_scale;
+          scale[to_key[tid & 63]] = scale[from_key[tid & 63]];
+        }
+      }
+    }
+    if (d0) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = k * 256 + tid;
+      if (i < count << shift) held[i] = v[k];
+    }
+    __syncthreads();
+    const E* lds = reinterpret_cast<const E*>(held);
+    for (int k = tid; k < kPieces << shift; k += 256) {
+      const int d = k & (dims - 1), q = k >> shift;
+      E x[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int at = place[q * N + e];
+        x[e] = lds[(((at / N) << shift) + d) * N + at % N];
+      }
+      const int64_t to = to_value[q];
+      if (to >= 0) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (F8)
+            w[i] = (uint32_t)x[4 * i] | (uint32_t)x[4 * i + 1] << 8 | (uint32_t)x[4 * i + 2] << 16 |
+                   (uint32_t)x[4 * i + 3] << 24;
+          else w[i] = (uint32_t)x[2 * i] | (uint32_t)x[2 * i + 1] << 16;
+        }
+        *reinterpret_cast<u32x4*>(static_cast<char*>(C.v) + to + (d0 + d) * stride) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int64_t line = to_key[q * N + e];
+          if (line < 0) continue;
+          const int64_t page_head = line / C.S;
+          static_cast<E*>(C.v)[(page_head * D + d0 + d) * C.S + (line - page_head * C.S)] = x[e];
+        }
+      }
+    }
   }
 }
 
@@ -893,7 +980,11 @@ hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream) {
 
 hipError_t launch_kv_evict(const EvictParams& P, hipStream_t stream) {
   const KvParams& C = P.cache;
-  k_evict_select<<<dim3(C.H, C.B), kSelect, 0, stream>>>(P);
+  const int64_t tokens = (int64_t)C.width * C.S;
+  const dim3 heads(C.H, C.B);
+  if (tokens <= 2048) k_evict_select<256, 8><<<heads, 256, 0, stream>>>(P);
+  else if (tokens <= 8192) k_evict_select<1024, 8><<<heads, 1024, 0, stream>>>(P);
+  else k_evict_select<1024, 32><<<heads, 1024, 0, stream>>>(P);
   if (C.D == 64) C.f8 ? move<64, true>(P, stream) : move<64, false>(P, stream);
   else if (C.D == 128) C.f8 ? move<128, true>(P, stream) : move<128, false>(P, stream);
   else C.f8 ? move<256, true>(P, stream) : move<256, false>(P, stream);
