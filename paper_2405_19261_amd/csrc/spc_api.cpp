@@ -1090,23 +1090,30 @@ spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
 constexpr double kScoreBytes = 256.0 * (1 << 20);
 struct WeighLayout {
   AttendLayout cut;
-  bool scores, stats;
+  bool scores;
+  int32_t parts;
   size_t kept_at, bytes;
 };
 WeighLayout weigh_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t tokens, bool f8) {
   WeighLayout L;
   const int64_t rows = n * (heads / H);
   L.scores = rows <= spc::kWeighRows && 4.0 * B * H * rows * tokens <= kScoreBytes;
-  L.stats = !L.scores && rows > spc::kWeighStats;
   L.cut.tile_rows = !L.scores ? 128 : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + L.cut.tile_rows - 1) / L.cut.tile_rows, groups = B * H * tiles;
   const int64_t least = L.scores ? spc::kv_share_keys(L.cut.tile_rows, f8) : spc::kWeighShare;
-  const int64_t most = std::max<int64_t>(1, tokens / least);
-  L.cut.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
+  const int64_t most = std::max<int64_t>(1, tokens / least), target = L.scores ? 1024 : 512;
+  L.cut.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                          (int64_t)spc::kKvShares, 65535 / B}));
   L.cut.bytes = (size_t)(groups * L.cut.splits * L.cut.tile_rows) * 8;
   L.kept_at = align_up(L.cut.bytes, 256);
-  L.bytes = L.kept_at + (size_t)(B * H * rows) * (L.scores ? (size_t)tokens * 4 : L.stats ? 8 : 0);
+  // the second step takes 256 keys and all rows a workgroup, or parts of them (of 64
+  // rows at least) until there are two workgroups a compute unit
+  const int64_t key_groups = B * H * ((tokens + 255) / 256);
+  L.parts = L.scores ? 1 : (int32_t)std::max<int64_t>(
+                               1, std::min({(rows + 63) / 64, (512 + key_groups - 1) / key_groups,
+                                            65535 / B}));
+  L.bytes = L.kept_at + (size_t)(B * H * tokens) * 4 *
+                            (L.scores ? (size_t)rows : L.parts > 1 ? (size_t)L.parts : 0);
   return L;
 }
 
@@ -1142,7 +1149,8 @@ spc_status kv_weigh_impl(const spc_kv_cache* cache, const void* q, int32_t dtype
   P.splits = L.cut.splits;
   P.part = reinterpret_cast<float*>(ws);
   if (L.scores) P.scores = reinterpret_cast<float*>(ws + L.kept_at);
-  if (L.stats) P.stats = reinterpret_cast<float*>(ws + L.kept_at);
+  P.parts = L.parts;
+  P.sums = reinterpret_cast<float*>(ws + L.kept_at);
   P.weights = weights;
   P.out_weights = out;
   P.weights_stride = weights_stride;

@@ -256,7 +256,8 @@ struct KvParams {
   float* out_weights;
   int64_t weights_stride;
   float* scores;            // [B][H][n heads / H][width * S], or NULL
-  float* stats;             // [B][H][n heads / H][2], or NULL
+  int32_t parts;            // that the rows are cut into for their sums
+  float* sums;              // [parts][B][H][min(width * S, L)], parts > 1
 };
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
@@ -270,7 +271,7 @@ hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
 hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream);
 constexpr int kWeighRows = 64;     // rows of a key/value head whose scores a call may keep
 constexpr int kWeighShare = 512;   // keys that a share of more rows has at least
-constexpr int kWeighStats = 2048;  // rows whose statistics the second step takes itself
+constexpr int kWeighStats = 1024;  // rows whose statistics the second step holds
 hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream);
 
 // spc_kv_evict: of every sequence and head the tokens of the largest weights.

@@ -254,34 +254,24 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
 
   float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};  // m of unscaled scores
   const int32_t* table = P.table + (int64_t)b * P.width;
-  const auto index_of = [&](uint32_t t) {
-    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
-  };
-  const auto page_at = [&](int32_t t) {
-    const int p = table[index_of((uint32_t)min(t, there - 1))];
-    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
-  };
-  const int key = kG * (c16 >> 2);
   u32x4 mine[kMine];
   float my_scale = 0.0f;
-  int page_next = -1, page_now = -1;  // the page of this lane's own keys
+  TilePages<D, EB, kG> pages;
+  uint32_t valid_next = 0, valid_now = 0;  // groups of keys that are in a page
+  const int lane_k = (c16 & 3) * D * EB + 16 * j + wave / kL * 4 * D * EB + wave % kL * 64;
   const auto bring = [&](int32_t t0) {
-    const int pk = page_at(t0 + key);
-    const uint32_t tk = (uint32_t)(t0 + key);
-    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
-    const int64_t at = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D * EB + 16 * j;
-    page_next = page_at(t0 + kG * j);
+    pages.place(P, h, there, t0);
+    valid_next = pages.valid;
+    const int gk = c16 >> 2;
+    const char* k = static_cast<const char*>(P.k) + pages.head_of(gk) +
+                    (pages.slot_of(gk) * (D * EB) + lane_k);
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int f = wave + i * kAttendWaves;
-      mine[i] = load16(P.k, at + (f / kL) * 4 * D * EB + f % kL * 64);
-    }
+    for (int i = 0; i < kMine; ++i)  // fragments wave, wave + 4, ...
+      mine[i] = load16(k, kAttendWaves * i / kL * 4 * D * EB + kAttendWaves * i % kL * 64);
     if constexpr (F8) {
-      if (threadIdx.x < T) {
-        const uint32_t t = (uint32_t)t0 + threadIdx.x;
-        const int p = page_at((int32_t)t);
-        my_scale = p < 0 ? 0.0f
-                         : P.k_scale[((int64_t)p * P.H + h) * P.S + (t - index_of(t) * (uint32_t)P.S)];
+      if (wave == 0) {
+        const bool ok = t0 + lane < there && (pages.valid >> j & 1u);
+        my_scale = ok ? P.k_scale[pages.head_of(j) / D + pages.slot_of(j) + c16] : 0.0f;
       }
     }
   };
@@ -294,12 +284,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
         frags[buf][f * kSteps + step][lane] = __builtin_bit_cast(u32x4, widen<F8>(mine[i], step));
     }
     if constexpr (F8)
-      if (threadIdx.x < T) scales[buf][threadIdx.x] = my_scale;
+      if (wave == 0) scales[buf][lane] = my_scale;
   };
   if (tile0 < tile1) {
+    pages.fetch(P, table, there, span.begin + T * tile0);
     bring(span.begin + T * tile0);
+    if (tile0 + 1 < tile1) pages.fetch(P, table, there, span.begin + T * (tile0 + 1));
     put(0);
-    page_now = page_next;
+    valid_now = valid_next;
     if (tile0 + 1 < tile1) bring(span.begin + T * (tile0 + 1));
   }
   __syncthreads();
@@ -311,16 +303,29 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    {
+      constexpr int kAhead = 4, kKeys = kQuarters * kC;
+      u32x4 ring[kAhead];
 #pragma unroll
-    for (int qd = 0; qd < kQuarters; ++qd)
+      for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][f][lane];
 #pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        const bf16x8 k8 = __builtin_bit_cast(bf16x8, frags[buf][qd * kC + c][lane]);
+      for (int f = 0; f < kKeys; ++f) {
+        const bf16x8 k8 = __builtin_bit_cast(bf16x8, ring[f % kAhead]);
+        if (f + kAhead < kKeys) ring[f % kAhead] = frags[buf][f + kAhead][lane];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][c], s[mt][qd], 0, 0, 0);
+          s[mt][f / kC] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][f % kC], s[mt][f / kC], 0, 0, 0);
       }
-    const bool whole = t0 >= all_from && t0 + T <= all_to && !__any(page_now < 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+      for (int f = 0; f < kKeys; ++f) {
+        __builtin_amdgcn_sched_group_barrier(0x8, MT, 0);
+        if (f + kAhead < kKeys) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    if (tile + 2 < tile1) pages.fetch(P, table, there, t0 + 2 * T);
+    const bool whole = t0 >= all_from && t0 + T <= all_to && valid_now == 15u;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float x[kG];
@@ -329,7 +334,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
         x[e] = s[mt][e >> 2][e & 3];
         if constexpr (F8) x[e] *= scales[buf][kG * j + e];
       }
-      const int32_t hi = page_now >= 0 ? min(there - 1, last[mt]) : -1;
+      const int32_t hi = valid_now >> j & 1u ? min(there - 1, last[mt]) : -1;
       const int lo_e = first[mt] - ts, hi_e = hi - ts;  // this lane's keys that the row sees
       if (!whole) {  // uniform
 #pragma unroll
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
     // (the buffer written here was last read before the last barrier)
     if (tile + 1 < tile1) {
       put(buf ^ 1);
-      page_now = page_next;
+      valid_now = valid_next;
       if (tile + 2 < tile1) bring(t0 + 2 * T);
     }
     __syncthreads();
@@ -470,140 +475,142 @@ __global__ void __launch_bounds__(256) k_weigh_sum(KvParams P, int T, int least)
       P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + at(k)] = before[k] + sum[k];
 }
 
-// Statistics of more rows than k_weigh_keys takes itself: [B][H][n G] pairs.
-__global__ void __launch_bounds__(256) k_weigh_stats(KvParams P, int T, int least) {
-  const int h = blockIdx.y, b = blockIdx.z;
-  const Chunk ch = chunk_of(P, b);
-  const int G = P.heads / P.H;
-  const int64_t rows = (int64_t)min(ch.n, P.n) * G, r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r >= rows) return;
-  const RowStat s = row_stat(P, T, least, b, h, ch, rows, r);
-  float* to = P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G + r);
-  to[0] = s.m;
-  to[1] = s.inv;
-}
-
-// The second step of many rows: a wavefront holds 64 keys and takes 16 rows at a
-// time.  KEYS: the wavefronts of a workgroup have keys of their own and take the
-// same rows; else they share 64 keys and take every kWaves-th 16 rows, and their
-// sums are added in LDS.
-template <int D, bool F8, bool KEYS>
-__global__ void __launch_bounds__(KEYS ? 256 : 512, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
-  constexpr int kWaves = KEYS ? 4 : 8;
-  constexpr int EB = F8 ? 1 : 2, T = 64, kQuarters = 4, kG = 16;
-  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32;
-  __shared__ float sums[KEYS ? 1 : kWaves][T];
+// The second step of many rows: each of four wavefronts holds 64 keys, all take the
+// same rows, 64 at a time through LDS, whose statistics the workgroup has put there
+// (kWeighStats rows at a time).  Rows that see some of the keys are cut into P.parts,
+// whose sums k_weigh_add adds, where there are too few keys to fill the card.
+template <int D, bool F8>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
+  constexpr int EB = F8 ? 1 : 2, T = 64, kQuarters = 4, kG = 16, kBlock = 64;
+  constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32, kTiles = kBlock / 16;
+  static_assert(kTiles == kAttendWaves, "a wavefront brings 16 rows");
+  __shared__ u32x4 rows_lds[2][kTiles][kC][64];
   __shared__ float stats[2 * kWeighStats];
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.y, z = blockIdx.z, b = z / P.parts, part = z % P.parts;
   const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Chunk ch = chunk_of(P, b);
   const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
   const int32_t end = min(there, P.L);
-  if ((int64_t)blockIdx.x * (KEYS ? T * kWaves : T) >= end) return;
-  const int32_t t0 = (int32_t)(KEYS ? blockIdx.x * kWaves + wave : blockIdx.x) * T, ts = t0 + kG * j;
+  const int32_t wg0 = (int32_t)blockIdx.x * (T * kAttendWaves);
+  if (wg0 >= end) return;
+  const int32_t t0 = wg0 + T * wave, ts = t0 + kG * j;
   const int G = P.heads / P.H;
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, pos0 = (int64_t)len - ch.n;
-  const int32_t* table = P.table + (int64_t)b * P.width;
-  const auto index_of = [&](uint32_t t) {
-    return P.s16_magic ? __umulhi(t >> 4, P.s16_magic) : t >> 4;
-  };
-  const auto page_at = [&](int32_t t) {
-    const int p = table[index_of((uint32_t)min(t, there - 1))];
-    return t < there && (uint32_t)p < (uint32_t)P.pages ? p : -1;
-  };
-  const int key = kG * (c16 >> 2);
-  const int pk = page_at(t0 + key), ps = page_at(ts);
+  TilePages<D, EB, kG> pages;
+  pages.fetch(P, P.table + (int64_t)b * P.width, there, t0);
+  pages.place(P, h, there, t0);
   bf16x8 k8[kQuarters][kC];
-  f32x4 ks[kQuarters];
+  f32x4 ks[F8 ? kQuarters : 1];
   {
-    const uint32_t tk = (uint32_t)(t0 + key);
-    const int slot_k = (int)(tk - index_of(tk) * (uint32_t)P.S) + (c16 & 3);
-    const int64_t at = (((int64_t)max(pk, 0) * P.H + h) * P.S + slot_k) * D * EB + 16 * j;
+    const int gk = c16 >> 2;
+    const char* k = static_cast<const char*>(P.k) + pages.head_of(gk) +
+                    ((pages.slot_of(gk) + (c16 & 3)) * (D * EB) + 16 * j);
 #pragma unroll
     for (int qd = 0; qd < kQuarters; ++qd)
 #pragma unroll
       for (int c = 0; c < kL; ++c) {
-        const u32x4 w = load16(P.k, at + 4 * qd * D * EB + 64 * c);
+        const u32x4 w = load16(k, 4 * qd * D * EB + 64 * c);
 #pragma unroll
         for (int step = 0; step < kSteps; ++step) k8[qd][c * kSteps + step] = widen<F8>(w, step);
       }
-    const int slot = (int)((uint32_t)ts - index_of((uint32_t)ts) * (uint32_t)P.S);
-    const int64_t line = ((int64_t)max(ps, 0) * P.H + h) * P.S + slot;
+    if constexpr (F8) {
+      const float* scale = P.k_scale + (pages.head_of(j) / D + pages.slot_of(j));
 #pragma unroll
-    for (int qd = 0; qd < kQuarters; ++qd) {
-      ks[qd] = f32x4{P.scale, P.scale, P.scale, P.scale};
-      if constexpr (F8) ks[qd] *= *reinterpret_cast<const f32x4*>(P.k_scale + line + 4 * qd);
+      for (int qd = 0; qd < kQuarters; ++qd)
+        ks[qd] = *reinterpret_cast<const f32x4*>(scale + 4 * qd) * P.scale;
     }
   }
-  // the rows that see some of the keys, and those of them that see all
+  const auto factor = [&](int e) { return F8 ? ks[F8 ? e >> 2 : 0][e & 3] : P.scale; };
+  // rows that see some of the workgroup's keys, and those that see all of the wavefront's
   const auto row_at = [&](int64_t position) { return (position - pos0) * G; };
-  const int64_t r_first = max(row_at(t0), (int64_t)0), r_all = row_at((int64_t)t0 + T - 1);
   int64_t r_end = rows, r_all_end = rows;
   if (P.window > 0) {
-    r_end = min(rows, row_at((int64_t)t0 + T - 1 + P.window));
+    r_end = min(rows, row_at((int64_t)wg0 + T * kAttendWaves - 1 + P.window));
     r_all_end = min(rows, row_at((int64_t)t0 + P.window));
   }
-  const int64_t tile0 = r_first / 16, tiles = t0 < end ? (r_end + 15) / 16 : 0;
-  const int live = ps >= 0 ? min(there - ts, kG) : 0;
+  const int64_t r_all = row_at((int64_t)t0 + T - 1);
+  const int block0 = (int)(max(row_at(wg0), (int64_t)0) / kBlock);
+  const int blocks = max((int)((max(r_end, (int64_t)0) + kBlock - 1) / kBlock) - block0, 0);
+  const int per = (blocks + P.parts - 1) / P.parts;
+  const int first = block0 + min(part * per, blocks), last = block0 + min((part + 1) * per, blocks);
+  const int live = pages.valid >> j & 1u ? min(there - ts, kG) : 0;
   const bool all_live = !__any(live < kG);
-  // their statistics
-  if (!P.stats) {
-    for (int r = (int)threadIdx.x; r < (int)rows; r += 64 * kWaves) {
-      const RowStat x = row_stat(P, T, kWeighShare, b, h, ch, rows, r);
-      stats[2 * r] = x.m;
-      stats[2 * r + 1] = x.inv;
-    }
-    __syncthreads();
-  }
-  const float* all_stats = P.stats ? P.stats + 2 * (((int64_t)b * P.H + h) * P.n * G) : stats;
 
-  float acc[kG] = {};
-  bf16x8 q[kC];
-  float m = 0.0f, inv = 0.0f;
-  const auto load = [&](int64_t tile) {
-    const int64_t r = min(16 * tile + c16, rows - 1);
+  u32x4 mine[kC];
+  const auto bring = [&](int block) {
+    const int64_t r = min((int64_t)block * kBlock + 16 * wave + c16, rows - 1);
     const int i = token_of(P, G, r), g = (int)(r - (int64_t)i * G);
     const int64_t q_at = (ch.first + i) * P.q_stride + (int64_t)(h * G + g) * D;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
       const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
-      q[c] = __builtin_bit_cast(
-          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+      mine[c] = *reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d);
     }
-    m = all_stats[2 * r];
-    inv = all_stats[2 * r + 1];
   };
-  constexpr int kStride = KEYS ? 1 : kWaves;
-  int64_t tile = tile0 + (KEYS ? 0 : wave);
-  if (tile < tiles) load(tile);
-  for (; tile < tiles; tile += kStride) {
-    f32x4 s[kQuarters];
+  const auto put = [&](int buf) {
 #pragma unroll
-    for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < kC; ++c) rows_lds[buf][wave][c][lane] = mine[c];
+  };
+  float acc[kG] = {};
+  if (first < last) bring(first);
+  constexpr int kChunk = kWeighStats / kBlock;
+  for (int chunk = first; chunk < last; chunk += kChunk) {
+    const int chunk_end = min(chunk + kChunk, last);
+    const int64_t s0 = (int64_t)chunk * kBlock;
+    // (the last reads of the chunk before are behind its last barrier)
+    for (int64_t r = s0 + threadIdx.x; r < min((int64_t)chunk_end * kBlock, rows);
+         r += 64 * kAttendWaves) {
+      const RowStat x = row_stat(P, T, kWeighShare, b, h, ch, rows, r);
+      stats[2 * (r - s0)] = x.m;
+      stats[2 * (r - s0) + 1] = x.inv;
+    }
+    if (chunk == first) {
+      put(0);
+      if (first + 1 < last) bring(first + 1);
+    }
+    __syncthreads();
+    for (int block = chunk; block < chunk_end; ++block) {
+      const int buf = (block - first) & 1;
 #pragma unroll
-    for (int c = 0; c < kC; ++c)
+      for (int tile = 0; tile < kTiles; ++tile) {
+        const int64_t r0 = (int64_t)block * kBlock + 16 * tile;
+        if (r0 >= rows) break;  // uniform
+        bf16x8 q[kC];
 #pragma unroll
-      for (int qd = 0; qd < kQuarters; ++qd)
-        s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
-    const float m_now = m, inv_now = inv;
-    if (tile + kStride < tiles) load(tile + kStride);
-    if (all_live && 16 * tile >= r_all && 16 * tile + 16 <= r_all_end) {  // uniform
+        for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(bf16x8, rows_lds[buf][tile][c][lane]);
+        const int64_t r = min(r0 + c16, rows - 1);
+        const float m = stats[2 * (r - s0)], inv = stats[2 * (r - s0) + 1];
+        f32x4 s[kQuarters];
 #pragma unroll
-      for (int e = 0; e < kG; ++e)
-        acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], ks[e >> 2][e & 3], -m_now)),
-                      inv_now, acc[e]);
-    } else {
-      const int64_t r = 16 * tile + c16;
-      const Limits seen = limits_of<kOwn>(P, ch, len, there, token_of(P, G, min(r, rows - 1)));
-      // this lane's keys that the row sees: lo <= e < hi
-      const int lo = max(seen.first - ts, 0), hi = r < rows ? min(live, seen.last + 1 - ts) : 0;
+        for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int e = 0; e < kG; ++e) {
-        const float w =
-            __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], ks[e >> 2][e & 3], -m_now)) * inv_now;
-        acc[e] += (e >= lo && e < hi) ? w : 0.0f;
+        for (int c = 0; c < kC; ++c)
+#pragma unroll
+          for (int qd = 0; qd < kQuarters; ++qd)
+            s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
+        if (all_live && r0 >= r_all && r0 + 16 <= r_all_end) {  // uniform
+#pragma unroll
+          for (int e = 0; e < kG; ++e)
+            acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], factor(e), -m)), inv, acc[e]);
+        } else {
+          const Limits seen = limits_of<kOwn>(P, ch, len, there, token_of(P, G, r));
+          // this lane's keys that the row sees: lo <= e < hi
+          const int lo = max(seen.first - ts, 0);
+          const int hi = r0 + c16 < rows ? min(live, seen.last + 1 - ts) : 0;
+#pragma unroll
+          for (int e = 0; e < kG; ++e) {
+            const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], factor(e), -m)) * inv;
+            acc[e] += (e >= lo && e < hi) ? w : 0.0f;
+          }
+        }
       }
+      // (the buffer written here was last read before the last barrier)
+      if (block + 1 < last) {
+        put(buf ^ 1);
+        if (block + 2 < last) bring(block + 2);
+      }
+      __syncthreads();
     }
   }
 #pragma unroll
@@ -611,22 +618,31 @@ __global__ void __launch_bounds__(KEYS ? 256 : 512, D <= 128 ? 2 : 1) k_weigh_ke
 #pragma unroll
     for (int d = 8; d; d >>= 1) acc[e] += __shfl_xor(acc[e], d);
   }
-  float sum = 0.0f;  // of key t0 + lane
+  float sum = 0.0f;  // of this lane's key
 #pragma unroll
   for (int e = 0; e < kG; ++e)
     if (c16 == e) sum = acc[e];
-  const int t = kG * j + c16;
-  if constexpr (!KEYS) {
-    sums[wave][t] = sum;
-    __syncthreads();
-    if (wave) return;
-    sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += sums[w][t];
-  }
-  if (t0 + t < end)
-    P.out_weights[((int64_t)b * P.H + h) * P.weights_stride + t0 + t] =
-        weight_before(P, b, h, t0 + t, pos0) + sum;
+  const int32_t t = ts + c16;
+  if (t >= end) return;
+  const int64_t row = (int64_t)b * P.H + h;
+  if (P.parts > 1)
+    P.sums[((int64_t)part * P.B * P.H + row) * min((int64_t)P.width * P.S, (int64_t)P.L) + t] = sum;
+  else P.out_weights[row * P.weights_stride + t] = weight_before(P, b, h, t, pos0) + sum;
+}
+
+// The sums of k_weigh_keys' parts of the rows, in their order.
+__global__ void __launch_bounds__(256) k_weigh_add(KvParams P) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  const Chunk ch = chunk_of(P, b);
+  const int32_t len = max(P.len[b], 0), end = min(tokens_there<kOwn>(P, len), P.L);
+  const int32_t t = (int32_t)(blockIdx.x * 256 + threadIdx.x);
+  if (t >= end) return;
+  const int64_t row = (int64_t)b * P.H + h, n = min((int64_t)P.width * P.S, (int64_t)P.L);
+  float sum = 0.0f;
+  for (int part = 0; part < P.parts; ++part)
+    sum += P.sums[((int64_t)part * P.B * P.H + row) * n + t];
+  P.out_weights[row * P.weights_stride + t] =
+      weight_before(P, b, h, t, (int64_t)len - ch.n) + sum;
 }
 
 template <int D, bool F8>
@@ -643,15 +659,10 @@ void weigh(const KvParams& P, hipStream_t stream) {
     return;
   }
   k_weigh_tile<D, F8><<<grid, 64 * kAttendWaves, 0, stream>>>(P);
-  if (P.stats)
-    k_weigh_stats<<<dim3((uint32_t)((rows + 255) / 256), P.H, P.B), 256, 0, stream>>>(P, 64,
-                                                                                    kWeighShare);
-  if ((int64_t)P.B * P.H * ((end + 255) / 256) >= 512)
-    k_weigh_keys<D, F8, true>
-        <<<dim3((uint32_t)((end + 255) / 256), P.H, P.B), 256, 0, stream>>>(P);
-  else
-    k_weigh_keys<D, F8, false>
-        <<<dim3((uint32_t)((end + 63) / 64), P.H, P.B), 512, 0, stream>>>(P);
+  k_weigh_keys<D, F8><<<dim3((uint32_t)((end + 255) / 256), P.H, P.B * P.parts), 64 * kAttendWaves,
+                        0, stream>>>(P);
+  if (P.parts > 1)
+    k_weigh_add<<<dim3((uint32_t)((end + 255) / 256), P.H, P.B), 256, 0, stream>>>(P);
 }
 
 // ------------------------------------------------------------------ eviction

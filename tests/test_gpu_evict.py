@@ -74,6 +74,18 @@ def test_weigh_windows(n, L, window, f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("window", [0, 333])
+@pytest.mark.parametrize("width,n,heads", [(128, 700, 8), (2048, 560, 8), (40, 37, 8), (2048, 90, 8)])
+def test_weigh_many_rows(width, n, heads, window, f8):
+    """Rows in parts and in several pieces, tables much longer than the sequences."""
+    B, H, D, S = 2, 4, 64, 16
+    cache = ops_oracle.Cache(B, width, H, D, S, f8, DEV, seed=n)
+    lens = [min(n + 50, width * S), n + 1]
+    fill(cache, lens, 5)
+    check_weigh(cache, randn((B, n, heads, D), 3).to(DEV), lens, window=window, length=lens[0] + 3)
+
+
+@pytest.mark.parametrize("f8", [False, True])
 def test_weigh_ragged(f8):
     """Chunks of 0 to many rows, empty caches, rows before position 0, pages that are none, rows of no
     sequence, rows past max_q, weights narrower and wider than the sequences."""
