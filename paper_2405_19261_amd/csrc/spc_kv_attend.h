@@ -554,6 +554,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   constexpr int kFrags = kQuarters * kL + kM * kVL;  // of 1 KiB: K's, then V's
   constexpr int kMine = kFrags / kAttendWaves;       // that a wavefront brings
   constexpr int kAhead = 4;                          // reads of LDS under way
+  // The reference of a row's powers follows its maximum when that is more than
+  // kSlack above (powers up to 2^8 are as exact): O is then multiplied rarely.  A
+  // bfloat16 cache's scores are scaled within the power's argument, a negative scale
+  // is taken as a positive one of negated queries.  (kOwn keeps the sums it always had.)
+  constexpr float kSlack = MODE == kOwn ? 0.0f : 8.0f;
+  constexpr bool kFused = MODE != kOwn && !F8;
+  const uint32_t sign = kFused && P.scale < 0.0f ? 0x80008000u : 0u;
+  const float scale = fmaxf(fabsf(P.scale), 1e-37f);  // (not 0, for minus infinity times it)
   static_assert(kQuarters * kL % kAttendWaves == 0 && kM * kVL % kAttendWaves == 0, "whole shares");
   __shared__ u32x4 frags[2][kFrags][64];
   __shared__ float scales[2][2][F8 ? T : 1];         // of keys, of values
@@ -588,8 +596,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
       const int d = c / kSteps * (32 * kSteps) + j * (8 * kSteps) + c % kSteps * 8;
-      q[mt][c] = __builtin_bit_cast(
-          bf16x8, u32x4(*reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d)));
+      u32x4 w = *reinterpret_cast<const u32x4a2*>(static_cast<const uint16_t*>(P.q) + q_at + d);
+      w ^= sign;
+      q[mt][c] = __builtin_bit_cast(bf16x8, w);
     }
     const Limits seen = limits_of<MODE>(P, ch, len, there, i);
     last[mt] = seen.last;
@@ -698,6 +707,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int qd = 0; qd < kQuarters; ++qd) s[mt][qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    __builtin_amdgcn_s_setprio(1);
     {
       u32x4 ring[kAhead];
 #pragma unroll
@@ -724,6 +734,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
         if (f + kAhead < kQuarters * kL) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (tile + 2 < tile1) pages.fetch(P, table, there, t0 + 2 * T);
     const bool whole = MODE == kCross ? !__any(see != (1u << kG) - 1u)
                                       : t0 >= all_from && t0 + T <= all_to && valid_now == 15u;
@@ -731,13 +742,16 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
     float x[MT][kG], mx[MT];
     bool grows = false;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < kG; ++e) {
-        if constexpr (F8) x[mt][e] = s[mt][e >> 2][e & 3] * scales[buf][0][kG * j + e];
-        else x[mt][e] = s[mt][e >> 2][e & 3] * P.scale;
+        x[mt][e] = s[mt][e >> 2][e & 3];
+        if constexpr (F8) x[mt][e] *= scales[buf][0][kG * j + e];
+        else if constexpr (!kFused) x[mt][e] *= P.scale;
       }
-      if (!whole) {  // uniform
+    if (!whole) {  // uniform
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
         const int32_t hi = valid_now >> j & 1u ? min(there - 1, last[mt]) : -1;
 #pragma unroll
         for (int e = 0; e < kG; ++e) {
@@ -745,10 +759,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
           else x[mt][e] = ((ts + e <= hi) & (ts + e >= first[mt])) ? x[mt][e] : kNegInf;
         }
       }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
       mx[mt] = x[mt][0];
 #pragma unroll
       for (int e = 1; e < kG; ++e) mx[mt] = fmaxf(mx[mt], x[mt][e]);
-      grows |= mx[mt] > m[mt];
+      if constexpr (kFused) mx[mt] *= scale;
+      grows |= mx[mt] > m[mt] + kSlack;
     }
     if (__any(grows)) {  // some row's maximum grows
 #pragma unroll
@@ -768,7 +786,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
       const float base = m[mt] == kNegInf ? 0.0f : m[mt];  // (nothing seen yet)
 #pragma unroll
       for (int e = 0; e < kG; ++e) {
-        float w = __builtin_amdgcn_exp2f(x[mt][e] - base);
+        float w = __builtin_amdgcn_exp2f(kFused ? fmaf(x[mt][e], scale, -base) : x[mt][e] - base);
         l[mt] += w;
         if constexpr (F8) {
           w *= scales[buf][1][kG * j + e];
@@ -778,6 +796,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
       }
     }
     if (tile + 2 < tile1) pages.arrive();
+    __builtin_amdgcn_s_setprio(1);
     // (V's fragments: those of the next products are under way)
     constexpr int kValues = kM * kVL;
     u32x4 ring[kAhead];
@@ -804,6 +823,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
       __builtin_amdgcn_sched_group_barrier(0x8, MT * kSteps, 0);
       if (f + kAhead < kValues) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
     // (the buffer written here was last read before the last barrier)
     if (tile + 1 < tile1) {
       put(buf ^ 1);
