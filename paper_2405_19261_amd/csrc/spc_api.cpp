@@ -887,7 +887,7 @@ struct AttendLayout {
   size_t bytes;
 };
 AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t D,
-                           int64_t tokens, bool f8) {
+                           int64_t tokens, bool f8, spc::AttendKind kind) {
   AttendLayout L;
   const int64_t rows = n * (heads / H);
   // Rows a workgroup takes.  More of them read the keys less often, from a die's
@@ -905,9 +905,14 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   if (f8 && D > 64) L.tile_rows = rows <= 64 ? 16 : 128;
   else L.tile_rows = rows <= 16 ? 16 : rows <= (f8 ? 256 : 64) ? 32 : 128;
   const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
-  // up to four workgroups to a compute unit
-  const int64_t most = std::max<int64_t>(1, tokens / spc::kv_share_keys(L.tile_rows, f8));
-  L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (1024 + groups - 1) / groups,
+  // Workgroups: up to four to a compute unit, or two, as many as are there at once.
+  // (us by four / two: cross attention of 32 x 6 rows to up to 1024 tokens, 16 heads
+  // of 64, 23.9 / 19.7, of 16 x 8 rows to 4096 in e4m3, 8 heads of 128, 50.2 / 45.8;
+  // 8 rows of 32 sequences behind 8192 in e4m3 107 / 97.)
+  const int64_t most = std::max<int64_t>(
+      1, tokens / spc::kv_share_keys(L.tile_rows, f8, kind == spc::AttendKind::kPrefix));
+  const int64_t target = kind == spc::AttendKind::kOwnTokens ? 1024 : 512;
+  L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                      (int64_t)spc::kKvShares, 65535 / B}));
   L.bytes = L.splits > 1 ? (size_t)(groups * L.splits * L.tile_rows) * (size_t)(D + 2) * 4 : 0;
   return L;
@@ -965,7 +970,8 @@ spc_status kv_launch_size(int64_t B, int64_t H, int64_t rows, const AttendLayout
 spc_status attend_impl(spc::KvParams& P, bool cross, void* workspace, size_t workspace_bytes,
                        hipStream_t stream) {
   const AttendLayout L =
-      attend_layout(P.B, P.H, P.heads, P.n, P.D, (int64_t)P.width * P.S, P.f8);
+      attend_layout(P.B, P.H, P.heads, P.n, P.D, (int64_t)P.width * P.S, P.f8,
+                    cross ? spc::AttendKind::kCrossTokens : spc::AttendKind::kOwnTokens);
   P.tile_rows = L.tile_rows;
   P.splits = L.splits;
   spc_status st = kv_launch_size(P.B, P.H, (int64_t)P.n * (P.heads / P.H), L, P.start);
@@ -1033,8 +1039,9 @@ size_t part_bytes(const AttendLayout& L, int64_t B, int64_t H, int64_t rows, int
 SharedLayout shared_layout(int64_t B, int64_t H, int64_t heads, int64_t rows, int64_t n, int64_t D,
                            int64_t shared, int64_t tokens, bool f8) {
   SharedLayout L;
-  L.pre = attend_layout(1, H, heads, rows, D, shared, f8);
-  L.own = attend_layout(B, H, heads, n, D, std::max<int64_t>(1, tokens - shared), f8);
+  L.pre = attend_layout(1, H, heads, rows, D, shared, f8, spc::AttendKind::kPrefix);
+  L.own = attend_layout(B, H, heads, n, D, std::max<int64_t>(1, tokens - shared), f8,
+                        spc::AttendKind::kBehindPrefix);
   if (tokens <= shared) L.own.splits = 0;
   const int64_t G = heads / H;
   L.own_at = part_bytes(L.pre, 1, H, rows * G, D);
@@ -1100,7 +1107,7 @@ WeighLayout weigh_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64_t
   L.scores = rows <= spc::kWeighRows && 4.0 * B * H * rows * tokens <= kScoreBytes;
   L.cut.tile_rows = !L.scores ? 128 : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + L.cut.tile_rows - 1) / L.cut.tile_rows, groups = B * H * tiles;
-  const int64_t least = L.scores ? spc::kv_share_keys(L.cut.tile_rows, f8) : spc::kWeighShare;
+  const int64_t least = L.scores ? spc::kv_share_keys(L.cut.tile_rows, f8, false) : spc::kWeighShare;
   const int64_t most = std::max<int64_t>(1, tokens / least), target = L.scores ? 1024 : 512;
   L.cut.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                          (int64_t)spc::kKvShares, 65535 / B}));
@@ -1271,7 +1278,8 @@ size_t spc_kv_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t 
   const int64_t n = query_rows(cache, heads, rows, max_rows);
   if (n == 0) return 0;
   return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
-                       (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3)
+                       (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3,
+                       spc::AttendKind::kOwnTokens)
       .bytes;
 }
 

@@ -262,8 +262,11 @@ struct KvParams {
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
 constexpr int kKvShares = 128;                // shares the keys of a row are cut into, at most
-int kv_share_keys(int tile_rows, bool f8);  // keys that a share of them has at least
+// Keys that a share of them has at least (shared: of a prefix).
+int kv_share_keys(int tile_rows, bool f8, bool shared);
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream);
+// What an attention's workgroups take, for how it is cut.
+enum class AttendKind { kOwnTokens, kCrossTokens, kPrefix, kBehindPrefix };
 hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
 // own: every sequence's tokens from pre.shared on (splits = 0: none has any); pre:
 // the shared ones, with table their pages alone and the rows of all sequences as

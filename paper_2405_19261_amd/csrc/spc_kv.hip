@@ -324,7 +324,9 @@ hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream) {
   return hipGetLastError();
 }
 
-int kv_share_keys(int tile_rows, bool f8) { return share_keys(tile_rows, f8); }
+int kv_share_keys(int tile_rows, bool f8, bool shared) {
+  return share_keys(tile_rows, f8, shared ? kShared : kOwn);
+}
 
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream) {
   if (P.D == 64) P.f8 ? attend<64, true, kOwn>(P, stream) : attend<64, false, kOwn>(P, stream);

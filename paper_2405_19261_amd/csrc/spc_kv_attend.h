@@ -27,12 +27,7 @@ namespace {
 // TB/s, e4m3 52; 8 rows of 4 heads each, bfloat16, 114), by the vector
 // instructions of the softmax and of widening 8 bits for more.
 constexpr int kAttendWaves = 4;
-// A share of the keys has at least as many: a tile for each wavefront, or in
-// k_kv_attend_rows, whose wavefronts take every tile together, 512.  (One token
-// over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of 512, 6.9 in shares
-// of 128, and the join 4.4.)
 
-constexpr int share_keys(int tile_rows, bool f8) { return tile_rows > 64 ? 512 : f8 ? 256 : 128; }
 
 // The first position that a row at position t sees (under 0: from 0).  A row
 // before position 0 sees nothing: it is taken as at 0, where no window of 32 bits
@@ -47,6 +42,14 @@ __device__ __forceinline__ int32_t first_seen(const KvParams& P, int32_t t) {
 //   kShared  the first P.shared tokens (of P.table's only row) up to themselves;
 //            the rows of all sequences are taken as those of one
 enum AttendMode { kOwn, kCross, kShared };
+
+// A share of the keys has at least as many: a tile for each wavefront, or in
+// k_kv_attend_rows, whose wavefronts take every tile together, 512 (of a shared
+// prefix, which few workgroups take, 256).  (One token over 1500 bfloat16 tokens of
+// 8 heads: 13.9 us in shares of 512, 6.9 in shares of 128, and the join 4.4.)
+constexpr int share_keys(int tile_rows, bool f8, int mode = kOwn) {
+  return tile_rows > 64 ? (mode == kShared ? 256 : 512) : f8 ? 256 : 128;
+}
 
 // The tokens whose rows a launch is sized for, a sequence.
 template <int MODE>
@@ -184,24 +187,29 @@ __device__ __forceinline__ Seen seen_by(const int32_t (&first)[MT], const int32_
   return s;
 }
 
+template <int D>
+struct AttendLds {
+  float o[kAttendWaves][16][D + 4];
+  float m[kAttendWaves][16], l[kAttendWaves][16];
+};
+
 template <int D, bool F8, int MT, int MODE>
-__global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
-    k_kv_attend(KvParams P) {
+__device__ __forceinline__ void attend_few(const KvParams& P, uint32_t block, AttendLds<D>& lds) {
   constexpr int EB = F8 ? 1 : 2, T = F8 ? 64 : 32;
   constexpr int kQuarters = T / 16, kG = T / 4;  // score tiles; a lane's keys
   constexpr int kL = D * EB / 64;                // 16-byte loads of a key row by four lanes
   constexpr int kSteps = 2 / EB;                 // matrix steps in 16 bytes
   constexpr int kC = D / 32, kM = D / 16;
-  constexpr int kPad = 4;
-  __shared__ float o_lds[kAttendWaves][16][D + kPad];
-  __shared__ float m_lds[kAttendWaves][16], l_lds[kAttendWaves][16];
+  auto& o_lds = lds.o;
+  auto& m_lds = lds.m;
+  auto& l_lds = lds.l;
   // Workgroups are dealt to the 8 dies in turn: those of one sequence and head
   // (and share of its keys) go to one die, whose cache then holds their keys, the
   // row tiles that see most keys first.
   const uint32_t tiles_x =
       (uint32_t)(((int64_t)tokens_of<MODE>(P) * (P.heads / P.H) + 16 * MT - 1) / (16 * MT));
-  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
-  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  const uint32_t group = block / 8 / tiles_x * 8 + block % 8;
+  const uint32_t tile_x = tiles_x - 1 - block / 8 % tiles_x;
   if (group >= (uint32_t)(P.H * (MODE == kShared ? 1 : P.B) * P.splits)) return;
   const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
   const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
   const int32_t len = MODE == kShared ? 0 : max(P.len[b], 0), there = tokens_there<MODE>(P, len);
   const int i0 = token_of(P, G, r0), i1 = token_of(P, G, min(r0 + 16 * MT, rows) - 1);
   const Span span =
-      span_of<MODE>(P, T, share_keys(16 * MT, F8), len, ch.n, i0, i1, P.splits);
+      span_of<MODE>(P, T, share_keys(16 * MT, F8, MODE), len, ch.n, i0, i1, P.splits);
   if (share >= span.shares) return;
   int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
 
@@ -478,6 +486,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
   }
 }
 
+template <int D, bool F8, int MT, int MODE>
+__global__ void __launch_bounds__(64 * kAttendWaves, attend_waves(D, F8, MT))
+    k_kv_attend(KvParams P) {
+  __shared__ AttendLds<D> lds;
+  attend_few<D, F8, MT, MODE>(P, blockIdx.x, lds);
+}
+
 // Where a tile of keys lies: its four lane groups' kG consecutive keys, each in one
 // page.  All of it is the same for a wavefront, so pages are read and offsets are
 // computed by the scalar unit, a tile ahead of the loads that need them, and a lane
@@ -544,8 +559,16 @@ constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
 // 32/8 heads of 128, take 383 to 406 us in bfloat16 (593 to 629 TFLOP/s; by 406,
 // 515 us with 32 keys a tile, 653 with 64 rows a workgroup and its wavefronts apart
 // over the keys) and 437 in e4m3.
+template <int D, bool F8>
+struct RowsLds {
+  // 1 KiB fragments of keys, then of values, of two tiles; scales of keys, of values
+  u32x4 frags[2][rows_tile(D, F8) * D * (F8 ? 2 : 4) / 1024][64];
+  float scales[2][2][F8 ? rows_tile(D, F8) : 1];
+  int32_t seen_from[kAttendWaves], seen_to[kAttendWaves];
+};
+
 template <int D, bool F8, int MODE>
-__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
+__device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, RowsLds<D, F8>& lds) {
   constexpr int MT = 2, kRows = 16 * MT * kAttendWaves;
   constexpr int EB = F8 ? 1 : 2, T = rows_tile(D, F8);
   constexpr int kQuarters = T / 16, kG = T / 4;
@@ -563,12 +586,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   const uint32_t sign = kFused && P.scale < 0.0f ? 0x80008000u : 0u;
   const float scale = fmaxf(fabsf(P.scale), 1e-37f);  // (not 0, for minus infinity times it)
   static_assert(kQuarters * kL % kAttendWaves == 0 && kM * kVL % kAttendWaves == 0, "whole shares");
-  __shared__ u32x4 frags[2][kFrags][64];
-  __shared__ float scales[2][2][F8 ? T : 1];         // of keys, of values
+  static_assert(sizeof(lds.frags) == 2 * kFrags * 1024, "two tiles");
+  auto& frags = lds.frags;
+  auto& scales = lds.scales;
   const uint32_t tiles_x =
       (uint32_t)(((int64_t)tokens_of<MODE>(P) * (P.heads / P.H) + kRows - 1) / kRows);
-  const uint32_t group = blockIdx.x / 8 / tiles_x * 8 + blockIdx.x % 8;
-  const uint32_t tile_x = tiles_x - 1 - blockIdx.x / 8 % tiles_x;
+  const uint32_t group = block / 8 / tiles_x * 8 + block % 8;
+  const uint32_t tile_x = tiles_x - 1 - block / 8 % tiles_x;
   if (group >= (uint32_t)(P.H * (MODE == kShared ? 1 : P.B) * P.splits)) return;
   const int h = (int)(group % P.H), z = (int)(group / P.H), share = z % P.splits, b = z / P.splits;
   const int lane = threadIdx.x & 63, c16 = lane & 15, j = lane >> 4;
@@ -579,7 +603,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   if (r0 >= rows) return;
   const int32_t len = MODE == kShared ? 0 : max(P.len[b], 0), there = tokens_there<MODE>(P, len);
   const Span span =
-      span_of<MODE>(P, T, share_keys(kRows, F8), len, ch.n, token_of(P, G, r0),
+      span_of<MODE>(P, T, share_keys(kRows, F8, MODE), len, ch.n, token_of(P, G, r0),
                     token_of(P, G, min(r0 + kRows, rows) - 1), P.splits);
   if (share >= span.shares) return;
   int tile0 = share * span.per, tile1 = min(span.tiles, tile0 + span.per);
@@ -606,7 +630,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   }
   int32_t all_from, all_to;
   if constexpr (MODE == kShared) {
-    __shared__ int32_t seen_from[kAttendWaves], seen_to[kAttendWaves];
+    auto& seen_from = lds.seen_from;
+    auto& seen_to = lds.seen_to;
     const Seen seen = seen_by<MT>(first, last);
     all_from = seen.all_from;
     all_to = seen.all_to;
@@ -867,6 +892,12 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_atte
   }
 }
 
+template <int D, bool F8, int MODE>
+__global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_kv_attend_rows(KvParams P) {
+  __shared__ RowsLds<D, F8> lds;
+  attend_many<D, F8, MODE>(P, blockIdx.x, lds);
+}
+
 // The shares of a row joined, in their order: a wavefront a row.
 template <int D, int MODE>
 __global__ void __launch_bounds__(256) k_kv_join(KvParams P, int tile_rows, int T, int least) {
@@ -927,15 +958,23 @@ constexpr int tile_keys(int D, bool f8, int tile_rows) {
   return tile_rows > 64 ? rows_tile(D, f8) : f8 ? 64 : 32;
 }
 
-template <int D, bool F8, int MODE>
-void attend_shares(const KvParams& P, hipStream_t stream) {
+// Workgroups of a launch: a multiple of the 8 dies.
+template <int MODE>
+uint32_t attend_blocks(const KvParams& P) {
   const int64_t rows = (int64_t)(MODE == kShared ? P.rows : P.n) * (P.heads / P.H);
   const int64_t groups = ((int64_t)P.H * (MODE == kShared ? 1 : P.B) * P.splits + 7) / 8 * 8;
-  const dim3 grid((uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups));
+  return (uint32_t)((rows + P.tile_rows - 1) / P.tile_rows * groups);
+}
+
+template <int D, bool F8, int MODE>
+void attend_shares(const KvParams& P, hipStream_t stream) {
+  const dim3 grid(attend_blocks<MODE>(P));
   const dim3 block(64 * kAttendWaves);
-  if (P.tile_rows == 16) k_kv_attend<D, F8, 1, MODE><<<grid, block, 0, stream>>>(P);
-  else if (P.tile_rows == 128) k_kv_attend_rows<D, F8, MODE><<<grid, block, 0, stream>>>(P);
-  else if constexpr (!F8 || D == 64) k_kv_attend<D, F8, 2, MODE><<<grid, block, 0, stream>>>(P);
+  if (P.tile_rows == 128) k_kv_attend_rows<D, F8, MODE><<<grid, block, 0, stream>>>(P);
+  else if constexpr (MODE != kShared) {  // (few rows behind a prefix: k_shared_both)
+    if (P.tile_rows == 16) k_kv_attend<D, F8, 1, MODE><<<grid, block, 0, stream>>>(P);
+    else if constexpr (!F8 || D == 64) k_kv_attend<D, F8, 2, MODE><<<grid, block, 0, stream>>>(P);
+  }
 }
 
 template <int D, bool F8, int MODE>
