@@ -1,6 +1,8 @@
 // spc_kv_evict.hip -- gfx950 kernels that keep a paged cache bounded: the attention
 // weight that cached tokens get from new ones, and the tokens of the largest
 // weights into other pages.
+#include <algorithm>
+
 #include "spc_kv_attend.h"
 
 namespace spc {
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
   // taken as a positive one of negated queries, so that maxima need no scaling
   const int64_t w0 = r0 + 16 * MT * wave;
   const uint32_t sign = P.scale < 0.0f ? 0x80008000u : 0u;
-  const float scale = fabsf(P.scale);
+  const float scale = fmaxf(fabsf(P.scale), 1e-37f);  // (not 0, for minus infinity times it)
   bf16x8 q[MT][kC];
   int32_t last[MT], first[MT];
 #pragma unroll
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
   const int32_t all_from = limits_of<kOwn>(P, ch, len, there, i1).first;
   const int32_t all_to = min(limits_of<kOwn>(P, ch, len, there, i0).last + 1, there);
 
-  float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};  // m of unscaled scores
+  float m[MT] = {kNegInf, kNegInf}, l[MT] = {0.0f, 0.0f};
   const int32_t* table = P.table + (int64_t)b * P.width;
   u32x4 mine[kMine];
   float my_scale = 0.0f;
@@ -326,37 +328,45 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
     }
     if (tile + 2 < tile1) pages.fetch(P, table, there, t0 + 2 * T);
     const bool whole = t0 >= all_from && t0 + T <= all_to && valid_now == 15u;
+    float x[MT][kG], mx[MT];
+    bool grows = false;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float x[kG];
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < kG; ++e) {
-        x[e] = s[mt][e >> 2][e & 3];
-        if constexpr (F8) x[e] *= scales[buf][kG * j + e];
+        x[mt][e] = s[mt][e >> 2][e & 3];
+        if constexpr (F8) x[mt][e] *= scales[buf][kG * j + e];
       }
-      const int32_t hi = valid_now >> j & 1u ? min(there - 1, last[mt]) : -1;
-      const int lo_e = first[mt] - ts, hi_e = hi - ts;  // this lane's keys that the row sees
-      if (!whole) {  // uniform
+    if (!whole) {  // uniform
 #pragma unroll
-        for (int e = 0; e < kG; ++e) x[e] = (e <= hi_e && e >= lo_e) ? x[e] : kNegInf;
+      for (int mt = 0; mt < MT; ++mt) {
+        const int32_t hi = valid_now >> j & 1u ? min(there - 1, last[mt]) : -1;
+        const int lo_e = first[mt] - ts, hi_e = hi - ts;  // this lane's keys that the row sees
+#pragma unroll
+        for (int e = 0; e < kG; ++e) x[mt][e] = (e <= hi_e && e >= lo_e) ? x[mt][e] : kNegInf;
       }
-      float mx = x[0];
+    }
 #pragma unroll
-      for (int e = 1; e < kG; ++e) mx = fmaxf(mx, x[e]);
-      if (__any(mx > m[mt])) {  // some lane's maximum grows
-        const float m_new = fmaxf(m[mt], mx);
-        l[mt] *= m[mt] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f((m[mt] - m_new) * scale);
+    for (int mt = 0; mt < MT; ++mt) {
+      mx[mt] = x[mt][0];
+#pragma unroll
+      for (int e = 1; e < kG; ++e) mx[mt] = fmaxf(mx[mt], x[mt][e]);
+      mx[mt] *= scale;
+      grows |= mx[mt] > m[mt] + 8.0f;  // (powers up to 2^8 are as exact)
+    }
+    if (__any(grows)) {  // some lane's maximum grows
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const float m_new = fmaxf(m[mt], mx[mt]);
+        l[mt] *= m[mt] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[mt] - m_new);
         m[mt] = m_new;
       }
-      const float base = m[mt] == kNegInf ? 0.0f : m[mt] * scale;
-      if (whole) {
+    }
 #pragma unroll
-        for (int e = 0; e < kG; ++e) l[mt] += __builtin_amdgcn_exp2f(fmaf(x[e], scale, -base));
-      } else {
+    for (int mt = 0; mt < MT; ++mt) {
+      const float base = m[mt] == kNegInf ? 0.0f : m[mt];
 #pragma unroll
-        for (int e = 0; e < kG; ++e)
-          l[mt] += (e <= hi_e && e >= lo_e) ? __builtin_amdgcn_exp2f(fmaf(x[e], scale, -base)) : 0.0f;
-      }
+      for (int e = 0; e < kG; ++e) l[mt] += __builtin_amdgcn_exp2f(fmaf(x[mt][e], scale, -base));
     }
     // (the buffer written here was last read before the last barrier)
     if (tile + 1 < tile1) {
@@ -370,13 +380,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D > 128 ? 2 : F8 && D == 12
   for (int mt = 0; mt < MT; ++mt) {
     float top = fmaxf(m[mt], __shfl_xor(m[mt], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    float sum = m[mt] == kNegInf ? 0.0f : l[mt] * __builtin_amdgcn_exp2f((m[mt] - top) * scale);
+    float sum = m[mt] == kNegInf ? 0.0f : l[mt] * __builtin_amdgcn_exp2f(m[mt] - top);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     const int64_t r = w0 + 16 * mt + c16;
     if (r < rows && j == 0) {
       float* to = P.part + 2 * ((((int64_t)z * P.H + h) * tiles_x + tile_x) * kRows + (r - r0));
-      to[0] = top == kNegInf ? kNegInf : top * scale;
+      to[0] = top;
       to[1] = sum;
     }
   }
@@ -477,8 +487,10 @@ __global__ void __launch_bounds__(256) k_weigh_sum(KvParams P, int T, int least)
 
 // The second step of many rows: each of four wavefronts holds 64 keys, all take the
 // same rows, 64 at a time through LDS, whose statistics the workgroup has put there
-// (kWeighStats rows at a time).  Rows that see some of the keys are cut into P.parts,
-// whose sums k_weigh_add adds, where there are too few keys to fill the card.
+// (kWeighStats rows at a time).  Where all rows are at most two such pieces, which
+// then stay in LDS, a workgroup goes on to further keys.  Rows that see some of the
+// keys are cut into P.parts, whose sums k_weigh_add adds, where there are too few
+// keys to fill the card.
 template <int D, bool F8>
 __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_keys(KvParams P) {
   constexpr int EB = F8 ? 1 : 2, T = 64, kQuarters = 4, kG = 16, kBlock = 64;
@@ -492,51 +504,35 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_k
   const Chunk ch = chunk_of(P, b);
   const int32_t len = max(P.len[b], 0), there = tokens_there<kOwn>(P, len);
   const int32_t end = min(there, P.L);
-  const int32_t wg0 = (int32_t)blockIdx.x * (T * kAttendWaves);
+  constexpr int kKeys = T * kAttendWaves;  // of a workgroup at a time
+  int32_t wg0 = (int32_t)blockIdx.x * kKeys;
   if (wg0 >= end) return;
-  const int32_t t0 = wg0 + T * wave, ts = t0 + kG * j;
   const int G = P.heads / P.H;
   const int64_t rows = (int64_t)min(ch.n, P.n) * G, pos0 = (int64_t)len - ch.n;
+  const int32_t* table = P.table + (int64_t)b * P.width;
+  const int64_t row = (int64_t)b * P.H + h;
+  const bool stay = rows <= 2 * kBlock;  // all rows are in LDS
   TilePages<D, EB, kG> pages;
-  pages.fetch(P, P.table + (int64_t)b * P.width, there, t0);
-  pages.place(P, h, there, t0);
-  bf16x8 k8[kQuarters][kC];
+  uint32_t valid = 0;
+  u32x4 raw[kQuarters][kL];
   f32x4 ks[F8 ? kQuarters : 1];
-  {
+  const auto bring_keys = [&](int32_t t0) {
+    pages.place(P, h, there, t0);
+    valid = pages.valid;
     const int gk = c16 >> 2;
     const char* k = static_cast<const char*>(P.k) + pages.head_of(gk) +
                     ((pages.slot_of(gk) + (c16 & 3)) * (D * EB) + 16 * j);
 #pragma unroll
     for (int qd = 0; qd < kQuarters; ++qd)
 #pragma unroll
-      for (int c = 0; c < kL; ++c) {
-        const u32x4 w = load16(k, 4 * qd * D * EB + 64 * c);
-#pragma unroll
-        for (int step = 0; step < kSteps; ++step) k8[qd][c * kSteps + step] = widen<F8>(w, step);
-      }
+      for (int c = 0; c < kL; ++c) raw[qd][c] = load16(k, 4 * qd * D * EB + 64 * c);
     if constexpr (F8) {
       const float* scale = P.k_scale + (pages.head_of(j) / D + pages.slot_of(j));
 #pragma unroll
-      for (int qd = 0; qd < kQuarters; ++qd)
-        ks[qd] = *reinterpret_cast<const f32x4*>(scale + 4 * qd) * P.scale;
+      for (int qd = 0; qd < kQuarters; ++qd) ks[qd] = *reinterpret_cast<const f32x4*>(scale + 4 * qd);
     }
-  }
-  const auto factor = [&](int e) { return F8 ? ks[F8 ? e >> 2 : 0][e & 3] : P.scale; };
-  // rows that see some of the workgroup's keys, and those that see all of the wavefront's
+  };
   const auto row_at = [&](int64_t position) { return (position - pos0) * G; };
-  int64_t r_end = rows, r_all_end = rows;
-  if (P.window > 0) {
-    r_end = min(rows, row_at((int64_t)wg0 + T * kAttendWaves - 1 + P.window));
-    r_all_end = min(rows, row_at((int64_t)t0 + P.window));
-  }
-  const int64_t r_all = row_at((int64_t)t0 + T - 1);
-  const int block0 = (int)(max(row_at(wg0), (int64_t)0) / kBlock);
-  const int blocks = max((int)((max(r_end, (int64_t)0) + kBlock - 1) / kBlock) - block0, 0);
-  const int per = (blocks + P.parts - 1) / P.parts;
-  const int first = block0 + min(part * per, blocks), last = block0 + min((part + 1) * per, blocks);
-  const int live = pages.valid >> j & 1u ? min(there - ts, kG) : 0;
-  const bool all_live = !__any(live < kG);
-
   u32x4 mine[kC];
   const auto bring = [&](int block) {
     const int64_t r = min((int64_t)block * kBlock + 16 * wave + c16, rows - 1);
@@ -552,82 +548,150 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1) k_weigh_k
 #pragma unroll
     for (int c = 0; c < kC; ++c) rows_lds[buf][wave][c][lane] = mine[c];
   };
-  float acc[kG] = {};
-  if (first < last) bring(first);
   constexpr int kChunk = kWeighStats / kBlock;
-  for (int chunk = first; chunk < last; chunk += kChunk) {
-    const int chunk_end = min(chunk + kChunk, last);
-    const int64_t s0 = (int64_t)chunk * kBlock;
-    // (the last reads of the chunk before are behind its last barrier)
-    for (int64_t r = s0 + threadIdx.x; r < min((int64_t)chunk_end * kBlock, rows);
-         r += 64 * kAttendWaves) {
+  const auto statistics = [&](int64_t s0, int64_t s1) {
+    for (int64_t r = s0 + threadIdx.x; r < min(s1, rows); r += 64 * kAttendWaves) {
       const RowStat x = row_stat(P, T, kWeighShare, b, h, ch, rows, r);
       stats[2 * (r - s0)] = x.m;
       stats[2 * (r - s0) + 1] = x.inv;
     }
-    if (chunk == first) {
-      put(0);
-      if (first + 1 < last) bring(first + 1);
+  };
+  // (the next keys' loads are under way with the products where registers allow)
+  constexpr bool kEarly = D * EB <= 128;
+  const int32_t hop = (int32_t)gridDim.x * kKeys;
+  pages.fetch(P, table, there, wg0 + T * wave);
+  bring_keys(wg0 + T * wave);
+  if (wg0 + hop < end) pages.fetch(P, table, there, wg0 + hop + T * wave);
+  if (stay) {
+    for (int block = 0; block * kBlock < rows; ++block) {
+      bring(block);
+      put(block);
     }
+    statistics(0, 2 * kBlock);
     __syncthreads();
-    for (int block = chunk; block < chunk_end; ++block) {
-      const int buf = (block - first) & 1;
+  }
+  for (; wg0 < end; wg0 += hop) {
+    const int32_t t0 = wg0 + T * wave, ts = t0 + kG * j, next = wg0 + hop;
+    const int32_t t = ts + c16;  // this lane's key in the end
+    const float before = P.parts == 1 && t < end ? weight_before(P, b, h, t, pos0) : 0.0f;
+    // rows that see some of the workgroup's keys, and those that see all of the wavefront's
+    int64_t r_end = rows, r_all_end = rows;
+    if (P.window > 0) {
+      r_end = min(rows, row_at((int64_t)wg0 + kKeys - 1 + P.window));
+      r_all_end = min(rows, row_at((int64_t)t0 + P.window));
+    }
+    const int64_t r_all = row_at((int64_t)t0 + T - 1);
+    const int block0 = (int)(max(row_at(wg0), (int64_t)0) / kBlock);
+    const int blocks = max((int)((max(r_end, (int64_t)0) + kBlock - 1) / kBlock) - block0, 0);
+    const int per = (blocks + P.parts - 1) / P.parts;
+    const int first = block0 + min(part * per, blocks), last = block0 + min((part + 1) * per, blocks);
+    const int live = valid >> j & 1u ? min(there - ts, kG) : 0;
+    const bool all_live = !__any(live < kG);
+    bf16x8 k8[kQuarters][kC];
+    float factor[F8 ? kG : 1];
 #pragma unroll
-      for (int tile = 0; tile < kTiles; ++tile) {
-        const int64_t r0 = (int64_t)block * kBlock + 16 * tile;
-        if (r0 >= rows) break;  // uniform
-        bf16x8 q[kC];
+    for (int qd = 0; qd < kQuarters; ++qd)
 #pragma unroll
-        for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(bf16x8, rows_lds[buf][tile][c][lane]);
-        const int64_t r = min(r0 + c16, rows - 1);
-        const float m = stats[2 * (r - s0)], inv = stats[2 * (r - s0) + 1];
-        f32x4 s[kQuarters];
+      for (int c = 0; c < kC; ++c) k8[qd][c] = widen<F8>(raw[qd][c / kSteps], c % kSteps);
+    if constexpr (F8) {
 #pragma unroll
-        for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int e = 0; e < kG; ++e) factor[e] = ks[e >> 2][e & 3] * P.scale;
+    }
+    const auto bring_next = [&] {
+      if (next >= end) return;
+      bring_keys(next + T * wave);
+      if (next + hop < end) pages.fetch(P, table, there, next + hop + T * wave);
+    };
+    if constexpr (kEarly) bring_next();
+    float acc[kG] = {};
+    // a tile of 16 rows from r0, of which buf holds tile; stats begin at row s0
+    const auto take = [&](auto all, int64_t r0, int buf, int tile, int64_t s0) {
+      bf16x8 q[kC];
 #pragma unroll
-        for (int c = 0; c < kC; ++c)
+      for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(bf16x8, rows_lds[buf][tile][c][lane]);
+      const int64_t r = min(r0 + c16, rows - 1);
+      const float m = stats[2 * (r - s0)], inv = stats[2 * (r - s0) + 1];
+      f32x4 s[kQuarters];
 #pragma unroll
-          for (int qd = 0; qd < kQuarters; ++qd)
-            s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
-        if (all_live && r0 >= r_all && r0 + 16 <= r_all_end) {  // uniform
+      for (int qd = 0; qd < kQuarters; ++qd) s[qd] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int e = 0; e < kG; ++e)
-            acc[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], factor(e), -m)), inv, acc[e]);
-        } else {
-          const Limits seen = limits_of<kOwn>(P, ch, len, there, token_of(P, G, r));
-          // this lane's keys that the row sees: lo <= e < hi
-          const int lo = max(seen.first - ts, 0);
-          const int hi = r0 + c16 < rows ? min(live, seen.last + 1 - ts) : 0;
+      for (int c = 0; c < kC; ++c)
 #pragma unroll
-          for (int e = 0; e < kG; ++e) {
-            const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3], factor(e), -m)) * inv;
-            acc[e] += (e >= lo && e < hi) ? w : 0.0f;
-          }
+        for (int qd = 0; qd < kQuarters; ++qd)
+          s[qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8[qd][c], q[c], s[qd], 0, 0, 0);
+      if constexpr (decltype(all)::value) {
+#pragma unroll
+        for (int e = 0; e < kG; ++e)
+          acc[e] = fmaf(__builtin_amdgcn_exp2f(
+                            fmaf(s[e >> 2][e & 3], F8 ? factor[F8 ? e : 0] : P.scale, -m)),
+                        inv, acc[e]);
+      } else {
+        const Limits seen = limits_of<kOwn>(P, ch, len, there, token_of(P, G, r));
+        // this lane's keys that the row sees: lo <= e < hi
+        const int lo = max(seen.first - ts, 0);
+        const int hi = r0 + c16 < rows ? min(live, seen.last + 1 - ts) : 0;
+#pragma unroll
+        for (int e = 0; e < kG; ++e) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[e >> 2][e & 3],
+                                                      F8 ? factor[F8 ? e : 0] : P.scale, -m)) * inv;
+          acc[e] += (e >= lo && e < hi) ? w : 0.0f;
         }
       }
-      // (the buffer written here was last read before the last barrier)
-      if (block + 1 < last) {
-        put(buf ^ 1);
-        if (block + 2 < last) bring(block + 2);
+    };
+    const auto take_block = [&](int block, int buf, int64_t s0) {
+      const int64_t r0 = (int64_t)block * kBlock;
+      if (all_live && r0 >= r_all && r0 + kBlock <= r_all_end) {  // uniform
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile) take(std::true_type(), r0 + 16 * tile, buf, tile, s0);
+      } else {
+#pragma unroll 1
+        for (int tile = 0; tile < kTiles; ++tile)
+          if (r0 + 16 * tile < rows) take(std::false_type(), r0 + 16 * tile, buf, tile, s0);
       }
-      __syncthreads();
+    };
+    if (stay) {
+      for (int block = first; block < last; ++block) take_block(block, block, 0);
+    } else {
+      if (first < last) bring(first);
+      for (int chunk = first; chunk < last; chunk += kChunk) {
+        const int chunk_end = min(chunk + kChunk, last);
+        const int64_t s0 = (int64_t)chunk * kBlock;
+        // (the last reads of the chunk before are behind its last barrier)
+        statistics(s0, (int64_t)chunk_end * kBlock);
+        if (chunk == first) {
+          put(0);
+          if (first + 1 < last) bring(first + 1);
+        }
+        __syncthreads();
+        for (int block = chunk; block < chunk_end; ++block) {
+          const int buf = (block - first) & 1;
+          take_block(block, buf, s0);
+          // (the buffer written here was last read before the last barrier)
+          if (block + 1 < last) {
+            put(buf ^ 1);
+            if (block + 2 < last) bring(block + 2);
+          }
+          __syncthreads();
+        }
+      }
+    }
+    if constexpr (!kEarly) bring_next();
+    // over the 16 lanes that hold rows of the same keys: a lane keeps half of the sums
+    // and gives the other half, until it has those of its own key
+#pragma unroll
+    for (int d = 8; d; d >>= 1)
+#pragma unroll
+      for (int e = 0; e < d; ++e) {
+        const float keep = c16 & d ? acc[e + d] : acc[e], give = c16 & d ? acc[e] : acc[e + d];
+        acc[e] = keep + __shfl_xor(give, d);
+      }
+    if (t < end) {
+      if (P.parts > 1)
+        P.sums[((int64_t)part * P.B * P.H + row) * min((int64_t)P.width * P.S, (int64_t)P.L) + t] =
+            acc[0];
+      else P.out_weights[row * P.weights_stride + t] = before + acc[0];
     }
   }
-#pragma unroll
-  for (int e = 0; e < kG; ++e) {
-#pragma unroll
-    for (int d = 8; d; d >>= 1) acc[e] += __shfl_xor(acc[e], d);
-  }
-  float sum = 0.0f;  // of this lane's key
-#pragma unroll
-  for (int e = 0; e < kG; ++e)
-    if (c16 == e) sum = acc[e];
-  const int32_t t = ts + c16;
-  if (t >= end) return;
-  const int64_t row = (int64_t)b * P.H + h;
-  if (P.parts > 1)
-    P.sums[((int64_t)part * P.B * P.H + row) * min((int64_t)P.width * P.S, (int64_t)P.L) + t] = sum;
-  else P.out_weights[row * P.weights_stride + t] = weight_before(P, b, h, t, pos0) + sum;
 }
 
 // The sums of k_weigh_keys' parts of the rows, in their order.
@@ -659,8 +723,11 @@ void weigh(const KvParams& P, hipStream_t stream) {
     return;
   }
   k_weigh_tile<D, F8><<<grid, 64 * kAttendWaves, 0, stream>>>(P);
-  k_weigh_keys<D, F8><<<dim3((uint32_t)((end + 255) / 256), P.H, P.B * P.parts), 64 * kAttendWaves,
-                        0, stream>>>(P);
+  // (where rows stay in LDS, two workgroups a compute unit take all keys in turn)
+  int64_t key_groups = (end + 255) / 256;
+  if (rows <= 128) key_groups = std::min<int64_t>(key_groups, (511 + P.B * P.H) / (P.B * P.H));
+  k_weigh_keys<D, F8><<<dim3((uint32_t)key_groups, P.H, P.B * P.parts), 64 * kAttendWaves, 0,
+                        stream>>>(P);
   if (P.parts > 1)
     k_weigh_add<<<dim3((uint32_t)((end + 255) / 256), P.H, P.B), 256, 0, stream>>>(P);
 }
