@@ -1083,7 +1083,6 @@ spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
   pre.splits = L.pre.splits;
   pre.part = reinterpret_cast<float*>(ws);
   P.from = shared;
-  P.partial = 1;
   P.tile_rows = L.own.tile_rows;
   P.splits = L.own.splits;
   P.part = reinterpret_cast<float*>(ws + L.own_at);

@@ -243,7 +243,6 @@ struct KvParams {
   uint32_t g_magic;         // r / (heads / H) = r g_magic / 2^32 for every row r (0: not so)
   float scale;              // of q.k, times log2(e)
   int32_t from;             // positions before it are left out (another launch takes them)
-  int32_t partial;          // rows leave their sums in part, also where one share is all
   const uint8_t* mask;      // spc_cross_attend: [B] rows of mask_width, mask_stride apart, or NULL
   int64_t mask_stride;
   int32_t mask_width;

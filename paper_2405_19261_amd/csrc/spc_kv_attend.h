@@ -37,11 +37,12 @@ __device__ __forceinline__ int32_t first_seen(const KvParams& P, int32_t t) {
 }
 
 // What rows attend to:
-//   kOwn     the tokens of their sequence up to themselves, from P.from on
+//   kOwn     the tokens of their sequence up to themselves
+//   kBehind  those of them from P.from on
 //   kCross   all tokens of their sequence whose mask byte is not 0
 //   kShared  the first P.shared tokens (of P.table's only row) up to themselves;
 //            the rows of all sequences are taken as those of one
-enum AttendMode { kOwn, kCross, kShared };
+enum AttendMode { kOwn, kBehind, kCross, kShared };
 
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512 (of a shared
@@ -90,7 +91,7 @@ __device__ __forceinline__ Limits limits_of(const KvParams& P, const Chunk& ch, 
     return Limits{first_seen(P, t), min(t, there - 1)};
   }
   const int32_t t = len - ch.n + i;
-  return Limits{max(first_seen(P, t), P.from), t};
+  return Limits{MODE == kBehind ? max(first_seen(P, t), P.from) : first_seen(P, t), t};
 }
 
 // The keys that rows of a chunk's tokens i0 .. i1 see: tiles of T from `begin`
@@ -103,9 +104,11 @@ template <int MODE>
 __device__ __forceinline__ Span span_of(const KvParams& P, int T, int least, int32_t len, int n,
                                         int i0, int i1, int splits) {
   const int32_t there = tokens_there<MODE>(P, len);
-  const int32_t end = MODE == kOwn ? min(there, len - n + i1 + 1) : there;
+  const int32_t end = MODE <= kBehind ? min(there, len - n + i1 + 1) : there;
   Span s;
-  s.begin = MODE == kOwn ? max(first_seen(P, len - n + i0), P.from) & ~(T - 1) : 0;
+  s.begin = MODE <= kBehind
+                ? max(first_seen(P, len - n + i0), MODE == kBehind ? P.from : 0) & ~(T - 1)
+                : 0;
   s.tiles = end > s.begin ? (end - s.begin + T - 1) / T : 0;
   s.shares = max(1, min(splits, s.tiles / (least / T)));
   s.per = (s.tiles + s.shares - 1) / s.shares;
@@ -412,7 +415,7 @@ __device__ __forceinline__ void attend_few(const KvParams& P, uint32_t block, At
           for (int i = 0; i < 4; ++i) vf[d][i] &= word_mask<F8>(see, i);
         } else {
           first_of<F8>(vf[d], live);
-          if (MODE == kOwn && P.from > ts) without_first<F8>(vf[d], P.from - ts);
+          if (MODE == kBehind && P.from > ts) without_first<F8>(vf[d], P.from - ts);
         }
       }
     }
@@ -429,7 +432,7 @@ __device__ __forceinline__ void attend_few(const KvParams& P, uint32_t block, At
 
   // join the wavefronts, 16 rows at a time; a share that is all of its keys ends
   // here, others leave O, the maximum and the sum to k_kv_join
-  const bool alone = MODE != kShared && span.shares == 1 && !P.partial;
+  const bool alone = MODE != kShared && MODE != kBehind && span.shares == 1;
   float* part = P.part + ((((int64_t)z * P.H + h) * tiles_x + tile_x) * (16 * MT)) *
                              (int64_t)(D + 2);
 #pragma unroll
@@ -561,8 +564,9 @@ constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
 // over the keys) and 437 in e4m3.
 template <int D, bool F8>
 struct RowsLds {
-  // 1 KiB fragments of keys, then of values, of two tiles; scales of keys, of values
-  u32x4 frags[2][rows_tile(D, F8) * D * (F8 ? 2 : 4) / 1024][64];
+  // 1 KiB fragments of keys, then of values, of two tiles, in bfloat16; scales of keys,
+  // of values
+  u32x4 frags[2][rows_tile(D, F8) * D * 4 / 1024][64];
   float scales[2][2][F8 ? rows_tile(D, F8) : 1];
   int32_t seen_from[kAttendWaves], seen_to[kAttendWaves];
 };
@@ -574,8 +578,9 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
   constexpr int kQuarters = T / 16, kG = T / 4;
   constexpr int kL = D * EB / 64, kSteps = 2 / EB, kC = D / 32, kM = D / 16;
   constexpr int kVL = T * EB / 64;                   // 16-byte loads of a lane's keys of V
-  constexpr int kFrags = kQuarters * kL + kM * kVL;  // of 1 KiB: K's, then V's
-  constexpr int kMine = kFrags / kAttendWaves;       // that a wavefront brings
+  constexpr int kLoads = kQuarters * kL + kM * kVL;  // of 1 KiB: K's, then V's
+  constexpr int kMine = kLoads / kAttendWaves;       // that a wavefront brings
+  constexpr int kKeyFrags = kQuarters * kC, kFrags = kKeyFrags + kM * (T / 32);
   constexpr int kAhead = 4;                          // reads of LDS under way
   // The reference of a row's powers follows its maximum when that is more than
   // kSlack above (powers up to 2^8 are as exact): O is then multiplied rarely.  A
@@ -699,7 +704,7 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
     constexpr uint32_t kAll = (1u << kG) - 1u;
     const int live = valid_next >> j & 1u ? there - ts_next : 0;
     see = live <= 0 ? 0u : live >= kG ? kAll : (1u << live) - 1u;
-    if (MODE == kOwn && P.from > ts_next) see &= kAll << min(P.from - ts_next, kG);
+    if (MODE == kBehind && P.from > ts_next) see &= kAll << min(P.from - ts_next, kG);
     if constexpr (MODE == kCross)
       if (P.mask) see &= mask_bits(mask_next);
     if (__any(see != kAll)) {
@@ -711,7 +716,11 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
       }
     }
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) frags[buf][wave + i * kAttendWaves][lane] = mine[i];
+    for (int i = 0; i < kMine; ++i)
+#pragma unroll
+      for (int step = 0; step < kSteps; ++step)
+        frags[buf][(wave + i * kAttendWaves) * kSteps + step][lane] =
+            __builtin_bit_cast(u32x4, widen<F8>(mine[i], step));
     if constexpr (F8)
       if (threadIdx.x < 2 * T) scales[buf][threadIdx.x / T][threadIdx.x % T] = my_scale;
   };
@@ -738,25 +747,19 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
 #pragma unroll
       for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][f][lane];
 #pragma unroll
-      for (int f = 0; f < kQuarters * kL; ++f) {
-        const int qd = f / kL;
-        const u32x4 k = ring[f % kAhead];
-        if (f + kAhead < kQuarters * kL) ring[f % kAhead] = frags[buf][f + kAhead][lane];
+      for (int f = 0; f < kKeyFrags; ++f) {
+        const bf16x8 k8 = __builtin_bit_cast(bf16x8, ring[f % kAhead]);
+        if (f + kAhead < kKeyFrags) ring[f % kAhead] = frags[buf][f + kAhead][lane];
 #pragma unroll
-        for (int step = 0; step < kSteps; ++step) {
-          const bf16x8 k8 = widen<F8>(k, step);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-            s[mt][qd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                k8, q[mt][f % kL * kSteps + step], s[mt][qd], 0, 0, 0);
-        }
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][f / kC] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, q[mt][f % kC], s[mt][f / kC], 0, 0, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-      for (int f = 0; f < kQuarters * kL; ++f) {
-        if (F8) __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
-        __builtin_amdgcn_sched_group_barrier(0x8, MT * kSteps, 0);
-        if (f + kAhead < kQuarters * kL) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      for (int f = 0; f < kKeyFrags; ++f) {
+        __builtin_amdgcn_sched_group_barrier(0x8, MT, 0);
+        if (f + kAhead < kKeyFrags) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
     }
     __builtin_amdgcn_s_setprio(0);
@@ -823,29 +826,23 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
     if (tile + 2 < tile1) pages.arrive();
     __builtin_amdgcn_s_setprio(1);
     // (V's fragments: those of the next products are under way)
-    constexpr int kValues = kM * kVL;
+    constexpr int kValues = kM * (T / 32);
     u32x4 ring[kAhead];
 #pragma unroll
-    for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][kQuarters * kL + f][lane];
+    for (int f = 0; f < kAhead; ++f) ring[f] = frags[buf][kKeyFrags + f][lane];
 #pragma unroll
     for (int f = 0; f < kValues; ++f) {
-      const int d = f / kVL, part = f % kVL;
-      const u32x4 v = ring[f % kAhead];
-      if (f + kAhead < kValues) ring[f % kAhead] = frags[buf][kQuarters * kL + f + kAhead][lane];
+      const int d = f / (T / 32), part = f % (T / 32);
+      const bf16x8 v8 = __builtin_bit_cast(bf16x8, ring[f % kAhead]);
+      if (f + kAhead < kValues) ring[f % kAhead] = frags[buf][kKeyFrags + f + kAhead][lane];
 #pragma unroll
-      for (int step = 0; step < kSteps; ++step) {
-        const bf16x8 v8 = widen<F8>(v, step);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][part * kSteps + step],
-                                                             o[mt][d], 0, 0, 0);
-      }
+      for (int mt = 0; mt < MT; ++mt)
+        o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[mt][part], o[mt][d], 0, 0, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
     for (int f = 0; f < kValues; ++f) {
-      if (F8) __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
-      __builtin_amdgcn_sched_group_barrier(0x8, MT * kSteps, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, MT, 0);
       if (f + kAhead < kValues) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -858,7 +855,7 @@ __device__ __forceinline__ void attend_many(const KvParams& P, uint32_t block, R
     __syncthreads();
   }
 
-  const bool alone = MODE != kShared && span.shares == 1 && !P.partial;
+  const bool alone = MODE != kShared && MODE != kBehind && span.shares == 1;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     l[mt] += __shfl_xor(l[mt], 16);

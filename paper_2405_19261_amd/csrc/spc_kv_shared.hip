@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre,
   int shares_own = 0;
   const int64_t x = r / own.tile_rows, r0 = x * own.tile_rows;
   if (own.splits)
-    shares_own = span_of<kOwn>(own, own_T, own_least, max(own.len[b], 0), ch.n, token_of(own, G, r0),
+    shares_own = span_of<kBehind>(own, own_T, own_least, max(own.len[b], 0), ch.n, token_of(own, G, r0),
                                token_of(own, G, min(r0 + own.tile_rows, rows) - 1), own.splits)
                      .shares;
   const int shares = shares_pre + shares_own;
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1)
     else
       attend_few<D, F8, PRE, kShared>(pre, blockIdx.x, *reinterpret_cast<AttendLds<D>*>(lds));
   } else {
-    attend_few<D, F8, OWN, kOwn>(own, blockIdx.x - pre_blocks,
+    attend_few<D, F8, OWN, kBehind>(own, blockIdx.x - pre_blocks,
                                  *reinterpret_cast<AttendLds<D>*>(lds));
   }
 }
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1)
 template <int D, bool F8, int PRE, int OWN>
 void both(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   const uint32_t pre_blocks = attend_blocks<kShared>(pre);
-  const uint32_t own_blocks = own.splits ? attend_blocks<kOwn>(own) : 0;
+  const uint32_t own_blocks = own.splits ? attend_blocks<kBehind>(own) : 0;
   k_shared_both<D, F8, PRE, OWN>
       <<<pre_blocks + own_blocks, 64 * kAttendWaves, 0, stream>>>(own, pre, pre_blocks);
 }
@@ -111,7 +111,7 @@ template <int D, bool F8>
 void shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   if (own.tile_rows == 128) {  // (many rows a sequence: each fills the card)
     attend_shares<D, F8, kShared>(pre, stream);
-    if (own.splits) attend_shares<D, F8, kOwn>(own, stream);
+    if (own.splits) attend_shares<D, F8, kBehind>(own, stream);
   } else if (pre.tile_rows == 128) {
     if (own.tile_rows == 16) both<D, F8, 8, 1>(own, pre, stream);
     else if constexpr (!F8 || D == 64) both<D, F8, 8, 2>(own, pre, stream);
