@@ -37,35 +37,45 @@ __global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre,
   const auto part = [&](int s) {
     return s < shares_pre ? of_pre + s * step_pre : of_own + (s - shares_pre) * step_own;
   };
+  // sixteen shares' values under way together, the first of them with the statistics
+  constexpr int E = D / 64, kAtOnce = 16;
+  float v[kAtOnce][E];
+  const auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (s0 + k < shares)  // uniform
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = part(s0 + k)[2 + lane * E + e];
+  };
   // the shares' maxima and sums, four a lane
   static_assert(kKvShares == 128, "both together at most four a lane");
-  float f[4], sum = 0.0f, top = kNegInf;
+  float f[4], l[4], sum = 0.0f, top = kNegInf;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    f[k] = lane + 64 * k < shares ? part(lane + 64 * k)[0] : kNegInf;
-    top = fmaxf(top, f[k]);
+    const bool there = lane + 64 * k < shares;
+    f[k] = there ? part(lane + 64 * k)[0] : kNegInf;
+    l[k] = there ? part(lane + 64 * k)[1] : 0.0f;
   }
+  load(0);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) top = fmaxf(top, f[k]);
 #pragma unroll
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     f[k] = f[k] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(f[k] - top);
-    if (lane + 64 * k < shares) sum += part(lane + 64 * k)[1] * f[k];
+    sum += l[k] * f[k];
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  constexpr int E = D / 64;
   float y[E] = {};
-  for (int s0 = 0; s0 < shares; s0 += 8) {  // eight shares' values under way together
-    float v[8][E];
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = part(min(s0 + k, shares - 1))[2 + lane * E + e];
+  for (int s0 = 0; s0 < shares; s0 += kAtOnce) {
+    if (s0) load(s0);
     const float of_lane = s0 < 64 ? f[0] : s0 < 128 ? f[1] : s0 < 192 ? f[2] : f[3];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float fade = s0 + k < shares ? __shfl(of_lane, (s0 + k) & 63) : 0.0f;
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (s0 + k >= shares) break;  // uniform
+      const float fade = __shfl(of_lane, (s0 + k) & 63);
 #pragma unroll
       for (int e = 0; e < E; ++e) y[e] += v[k][e] * fade;
     }
