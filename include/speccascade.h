@@ -566,13 +566,13 @@ size_t spc_kv_weigh_workspace_bytes(const spc_kv_cache* cache, int32_t heads, in
  *                `keep` tokens may be given its own pages.  A page id out of
  *                range takes nothing
  *   out_len      [B] int32: the tokens kept, min(keep, those in the cache), the
- *                same for every head (may be kv_len of a later call, but not
- *                this one's)
+ *                same for every head (kv_len of later calls; not this call's:
+ *                SPC_E_PARAM)
  *   out_index    [B][kv_heads][keep] int32: the positions they had, ascending, -1
  *                behind the last
  *   out_weights  [B][kv_heads] rows of keep float32, out_stride apart (at least
  *                keep), or NULL: their weights, entries behind the last one left
- *                as they are.  Not `weights` itself, nor overlapping it
+ *                as they are.  Not `weights` itself (SPC_E_PARAM), nor overlapping it
  * The pages they came from, and page_table, are left as they are.  Positions are
  * the caller's to follow (out_index): queries and keys that encode them stay as
  * they were written, and the next new token is at out_len.  No workspace.

@@ -1190,6 +1190,8 @@ spc_status kv_evict_impl(const spc_kv_cache* cache, const float* weights, int64_
     return fail(SPC_E_SHAPE, "out_stride must be at least keep (got %lld)", (long long)out_stride);
   if (((uintptr_t)out_table | (uintptr_t)out_len | (uintptr_t)out_index | (uintptr_t)out_weights) % 4)
     return fail(SPC_E_ALIGN, "arrays must be 4-byte aligned");
+  if (out_len == cache->kv_len || out_weights == weights)
+    return fail(SPC_E_PARAM, "outputs must not be inputs of the call");
   P.weights = weights;
   P.weights_stride = weights_stride;
   P.out_stride = out_stride;

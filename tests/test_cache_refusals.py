@@ -35,8 +35,8 @@ def weigh(c, **kw):
 
 
 def evict(c, **kw):
-    a = dict(w=OK, ld=64, length=64, keep=32, first=4, recent=8, table=OK, width=2, n=OK, index=OK,
-             out_w=OK, out_ld=32)
+    a = dict(w=OK, ld=64, length=64, keep=32, first=4, recent=8, table=OK, width=2, n=OK + 4096, index=OK,
+             out_w=OK + 8192, out_ld=32)
     a.update(kw)
     return spc.lib().spc_kv_evict(c, a["w"], a["ld"], a["length"], a["keep"], a["first"], a["recent"],
                                   a["table"], a["width"], a["n"], a["index"], a["out_w"], a["out_ld"],
@@ -82,7 +82,7 @@ def test_query_refusals(kw, status):
     (evict, dict(first=-1), -4), (evict, dict(recent=-1), -4), (evict, dict(first=25), -4),
     (evict, dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), -4), (evict, dict(w=OK + 2), -5),
     (evict, dict(table=OK + 1), -5), (evict, dict(index=OK + 2), -5), (evict, dict(n=OK + 1), -5),
-    (evict, dict(out_w=OK + 3), -5),
+    (evict, dict(out_w=OK + 3), -5), (evict, dict(n=OK), -4), (evict, dict(out_w=OK), -4),
 ])
 def test_refusals(call, kw, status):
     assert call(cache(), **kw) == status

@@ -137,12 +137,14 @@ def test_ragged(f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n", [3, 70])
 @pytest.mark.parametrize("s,scale", [(12.0, None), (1.0, 0.0), (1.0, -0.3), (0.3, 1.0)])
-def test_scales_and_peaked_scores(s, scale, f8):
+def test_scales_and_peaked_scores(s, scale, n, f8):
     lens = [500, 77]
     cache = encoder(lens, 1, 128, 64, f8)
     fill(cache, lens, 3, s)
-    check(cache, randn((2, 3, 4, 128), 1, BF16, s).to(DEV), lens, scale=scale)
+    check(cache, randn((2, n, 4, 128), 1, BF16, s).to(DEV), lens, scale=scale)
+    check(cache, randn((2, n, 4, 128), 1, BF16, s).to(DEV), lens, scale=scale, mask=masks(2, 500, 3).to(DEV))
 
 
 @pytest.mark.parametrize("n,L", [(1, 40), (3, 700), (140, 300)])

@@ -194,11 +194,12 @@ def test_strides_workspaces_and_streams(f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n", [3, 30])
 @pytest.mark.parametrize("s,scale", [(12.0, None), (1.0, 0.0), (1.0, -0.3)])
-def test_scales_and_peaked_scores(s, scale, f8):
-    x = Batch(2, 500, [3, 77], 1, 128, 64, f8)
+def test_scales_and_peaked_scores(s, scale, n, f8):
+    x = Batch(2, 500, [n, 77], 1, 128, 64, f8)
     fill(x.all, x.lens + [500], 9, s)
-    check(x, randn((2, 3, 4, 128), 1, BF16, s).to(DEV), scale=scale)
+    check(x, randn((2, n, 4, 128), 1, BF16, s).to(DEV), scale=scale)
 
 
 def test_captured_and_replayed():
