@@ -85,10 +85,16 @@ class ContextLM:
     call reads no further than its last position: rolling back needs no more
     than going on from an earlier position.  A token at or past
     ``cache_tokens`` (``max_len`` in whole pages) is not kept: ``spec_decode``
-    raises after rounds that came that far; one's own calls stay below."""
+    raises after rounds that came that far; one's own calls stay below.
+
+    ``prompt`` tokens that all sequences begin with (seeded keys and values) stand
+    in pages of their own, before position 0, and every call reads them once for
+    the whole batch (``spc_kv_attend_shared``).  ``encoder_lens`` (B lengths) makes
+    the model a decoder with an encoder's states of its own for each sequence, to
+    which a second layer attends (``spc_cross_attend``)."""
 
     def __init__(self, base, B, max_len, heads=4, kv_heads=2, head_dim=64, page_size=16,
-                 cache_dtype=torch.bfloat16, mix=1.0, seed=0):
+                 cache_dtype=torch.bfloat16, mix=1.0, seed=0, prompt=0, encoder_lens=None):
         self.base, self.B, self.V, self.device = base, B, base.V, base.device
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         g = torch.Generator(device="cpu").manual_seed(seed)
@@ -100,19 +106,49 @@ class ContextLM:
         self.k_table = table(base.rows, kv_heads, head_dim)
         self.v_table = table(base.rows, kv_heads, head_dim)
         self.project = table(heads * head_dim, base.V, s=mix * (heads * head_dim) ** -0.5)
-        width = (max_len + page_size - 1) // page_size
-        self.cache_tokens = width * page_size
+        # pages of a sequence of its own, from the one that the prompt ends in
+        begin = prompt // page_size
+        width = (prompt + max_len + page_size - 1) // page_size - begin
+        self.prompt, self.cache_tokens = prompt, (begin + width) * page_size - prompt
+        shared = (prompt + page_size - 1) // page_size
         # pages in a seeded order, as an allocator leaves them after a while
-        self.page_table = torch.randperm(B * width, generator=g).view(B, width).to(
-            self.device, torch.int32)
-        shape = (B * width, kv_heads, page_size, head_dim)
-        self.k_pages = torch.zeros(shape, device=self.device, dtype=cache_dtype)
-        self.v_pages = torch.zeros((B * width, kv_heads, head_dim, page_size), device=self.device,
-                                   dtype=cache_dtype)
-        self.scales = {}
-        if cache_dtype == torch.float8_e4m3fn:
-            self.scales = {k: torch.zeros(shape[:3], device=self.device)
-                           for k in ("k_scale", "v_scale")}
+        order = torch.randperm(B * width + shared, generator=g).to(self.device, torch.int32)
+        self.shared_table = order[B * width:].contiguous()
+        self.page_table = torch.cat([self.shared_table[:begin].expand(B, begin),
+                                     order[:B * width].view(B, width)], dim=1).contiguous()
+        self.k_pages, self.v_pages, self.scales = self._pages(order.numel(), page_size, cache_dtype)
+        if prompt:
+            self._write(g, self.k_pages, self.v_pages, self.shared_table[None], [prompt], self.scales)
+        self.encoder = None
+        if encoder_lens is not None:
+            lens = [int(x) for x in encoder_lens]
+            w = (max(lens) + page_size - 1) // page_size
+            pages = torch.randperm(B * w, generator=g).view(B, w).to(self.device, torch.int32)
+            k, v, scales = self._pages(B * w, page_size, cache_dtype)
+            self._write(g, k, v, pages, lens, scales)
+            self.encoder = (k, v, pages, torch.tensor(lens, dtype=torch.int32, device=self.device))
+            self.encoder_scales = scales
+            self.cross_table = table(base.rows, heads, head_dim)
+            self.cross_project = table(heads * head_dim, base.V, s=mix * (heads * head_dim) ** -0.5)
+
+    def _pages(self, n, page_size, dtype):
+        """Zeroed pages for keys and for values, and their scales (of 8 bits)."""
+        shape = (n, self.kv_heads, page_size, self.head_dim)
+        k = torch.zeros(shape, device=self.device, dtype=dtype)
+        v = torch.zeros((n, self.kv_heads, self.head_dim, page_size), device=self.device, dtype=dtype)
+        scales = {}
+        if dtype == torch.float8_e4m3fn:
+            scales = {name: torch.zeros(shape[:3], device=self.device)
+                      for name in ("k_scale", "v_scale")}
+        return k, v, scales
+
+    def _write(self, g, k_pages, v_pages, table, lens, scales):
+        """Seeded tokens 0 .. lens[b] - 1 of every sequence into their pages."""
+        k, v = (torch.randn(sum(lens), self.kv_heads, self.head_dim, generator=g).to(
+            self.device, torch.bfloat16) for _ in range(2))
+        start = torch.tensor([sum(lens[:b]) for b in range(len(lens) + 1)], dtype=torch.int32)
+        spc.spc_kv_write(k, v, k_pages, v_pages, table.contiguous(), start.diff().to(self.device),
+                         q_start=start.to(self.device), **scales)
 
     def __call__(self, last_tokens, positions):
         B, n = self.B, last_tokens.numel() // self.B
@@ -121,11 +157,18 @@ class ContextLM:
         def of(t):
             return t.index_select(0, row).view(B, n, t.shape[1], t.shape[2])
 
-        kv_len = (positions.view(B, n)[:, -1] + 1).to(torch.int32)
+        kv_len = (positions.view(B, n)[:, -1] + (self.prompt + 1)).to(torch.int32)
         cache = (self.k_pages, self.v_pages, self.page_table, kv_len)
         spc.spc_kv_write(of(self.k_table), of(self.v_table), *cache, **self.scales)
-        o = spc.spc_kv_attend(of(self.q_table), *cache, **self.scales)
+        if self.prompt:
+            o = spc.spc_kv_attend_shared(of(self.q_table), *cache, self.prompt,
+                                         shared_table=self.shared_table, **self.scales)
+        else:
+            o = spc.spc_kv_attend(of(self.q_table), *cache, **self.scales)
         z = torch.matmul(o.view(B * n, -1), self.project)
+        if self.encoder is not None:
+            c = spc.spc_cross_attend(of(self.cross_table), *self.encoder, **self.encoder_scales)
+            z = z + torch.matmul(c.view(B * n, -1), self.cross_project)
         return self.base.logits_table.index_select(0, row) + z.to(self.base.dtype)
 
 
