@@ -904,6 +904,16 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   //     256: 228 / 198 / 277
   if (f8 && D > 64) L.tile_rows = rows <= 64 ? 16 : 128;
   else L.tile_rows = rows <= 16 ? 16 : rows <= (f8 ? 256 : 64) ? 32 : 128;
+  // Rows of shared keys gain more by 128.  us by 16 / 32 / 128 rows, cross attention
+  // of 32 sequences to 4096 tokens, 8 heads of 128, bfloat16: 32 rows 142 / 111 / 115,
+  // 64: 251 / 145 / 122; 16 sequences, 4 heads of 256: 32 rows 82 / 72 / 85, 64: 140 /
+  // 106 / 90.  A prefix is read at the rate that few workgroups reach, by 16 rows
+  // each sooner: of 8192 tokens, bfloat16, heads of 128, 32 rows 25 / 30 / 24, 64: 30 /
+  // 30 / 26 (of 1000: 32 rows 12 / 15 / 21), heads of 64, 64 rows 19 / 20 / 21, of 256
+  // 41 / 50 / 33.
+  if (kind == spc::AttendKind::kCrossTokens && !f8 && D > 64 && rows > 32) L.tile_rows = 128;
+  if (kind == spc::AttendKind::kPrefix)
+    L.tile_rows = rows <= 32 || (rows <= 64 && D <= 128) ? 16 : 128;
   const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows, groups = B * H * tiles;
   // Workgroups: up to four to a compute unit, or two, as many as are there at once.
   // (us by four / two: cross attention of 32 x 6 rows to up to 1024 tokens, 16 heads
@@ -914,6 +924,9 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   const int64_t target = kind == spc::AttendKind::kOwnTokens ? 1024 : 512;
   L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                      (int64_t)spc::kKvShares, 65535 / B}));
+  // A second launch costs more than it gains where a head's keys are few (one row of 8
+  // heads: 512 tokens of 128 10.2 us in one share, 11.9 in four, 1024 15.7 and 11.8).
+  if (kind == spc::AttendKind::kCrossTokens && tokens * D * (f8 ? 1 : 2) <= (128 << 10)) L.splits = 1;
   L.bytes = L.splits > 1 ? (size_t)(groups * L.splits * L.tile_rows) * (size_t)(D + 2) * 4 : 0;
   return L;
 }
@@ -1092,7 +1105,10 @@ spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
 }
 
 // How weighing is cut, and its workspace: the scores of few rows are kept where
-// they take at most kScoreBytes (the on-chip cache of the memory side).
+// they take at most kScoreBytes (the on-chip cache of the memory side).  us of 8
+// sequences over 8192 tokens, 8 heads of 128, with scores kept / products taken
+// again: 16 rows bfloat16 42 / 63, e4m3 35 / 58, 32: 53 / 63 and 53 / 59, 64: 96 / 65
+// and 84 / 60.
 constexpr double kScoreBytes = 256.0 * (1 << 20);
 struct WeighLayout {
   AttendLayout cut;

@@ -271,7 +271,7 @@ hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
 // the shared ones, with table their pages alone and the rows of all sequences as
 // one's (tile_rows, splits, part of its own).
 hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream);
-constexpr int kWeighRows = 64;     // rows of a key/value head whose scores a call may keep
+constexpr int kWeighRows = 32;     // rows of a key/value head whose scores a call may keep
 constexpr int kWeighShare = 512;   // keys that a share of more rows has at least
 constexpr int kWeighStats = 1024;  // rows whose statistics the second step holds
 hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream);

@@ -104,11 +104,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1)
       attend_few<D, F8, PRE, kShared>(pre, blockIdx.x, *reinterpret_cast<AttendLds<D>*>(lds));
   } else {
     attend_few<D, F8, OWN, kBehind>(own, blockIdx.x - pre_blocks,
-                                 *reinterpret_cast<AttendLds<D>*>(lds));
+                                    *reinterpret_cast<AttendLds<D>*>(lds));
   }
 }
 
-// Rows of a workgroup in sixteens: 1, 2, or 8.
+// Rows of a workgroup in sixteens: 1 or 8 of the prefix, 1 or 2 of the others.
 template <int D, bool F8, int PRE, int OWN>
 void both(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   const uint32_t pre_blocks = attend_blocks<kShared>(pre);
@@ -125,13 +125,10 @@ void shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   } else if (pre.tile_rows == 128) {
     if (own.tile_rows == 16) both<D, F8, 8, 1>(own, pre, stream);
     else if constexpr (!F8 || D == 64) both<D, F8, 8, 2>(own, pre, stream);
-  } else if (pre.tile_rows == 32) {
-    if constexpr (!F8 || D == 64) {
-      if (own.tile_rows == 16) both<D, F8, 2, 1>(own, pre, stream);
-      else both<D, F8, 2, 2>(own, pre, stream);
-    }
-  } else {
+  } else if (own.tile_rows == 16) {
     both<D, F8, 1, 1>(own, pre, stream);
+  } else if constexpr (!F8 || D == 64) {
+    both<D, F8, 1, 2>(own, pre, stream);
   }
   const int64_t rows = (int64_t)own.n * (own.heads / own.H);
   k_shared_join<D><<<dim3((uint32_t)((rows + 3) / 4), own.H, own.B), 256, 0, stream>>>(
