@@ -894,14 +894,16 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   // cache; fewer leave registers for two wavefronts a SIMD, of which 8-bit keys,
   // widened as they come, need more.  us of 32 sequences over 4096 tokens, 8
   // key/value heads, by tiles of 16 / 32 / 128 rows:
-  //   bf16 heads of 128: 32 rows 157 / 116 / 155, 64: 250 / 164 / 165, 96: 369 /
-  //     227 / 171, 128: 482 / 255 / 183; of 64: 32 rows 80 / 72 / 106, 64: 125 / 109
-  //     / 116, 128: 239 / 160 / 128; of 256: 32 rows 310 / 278 / 485, 64: 525 / 429 /
-  //     483, 128: 1010 / 712 / 541
-  //   e4m3 heads of 128: 32 rows 93 / 104 / 162, 64: 126 / 157 / 174, 96: 181 / 221 /
-  //     183, 128: 236 / 233 / 189; of 256: 32 rows 183 / 246 / 402, 64: 285 / 378 /
-  //     415, 128: 533 / 594 / 441; of 64: 32 rows 62 / 51 / 132, 128: 127 / 107 / 152,
-  //     256: 228 / 198 / 277
+  //   bf16 heads of 128: 32 rows 160 / 116 / 133, 64: 250 / 164 / 143, 96: 368 /
+  //     228 / 153, 128: 481 / 254 / 164; of 64: 32 rows 74 / 64 / 79, 64: 121 / 102
+  //     / 89, 128: 235 / 152 / 107; of 256: 32 rows 313 / 278 / 361, 64: 524 / 428 /
+  //     375, 128: 1009 / 710 / 425
+  //   e4m3 heads of 128: 32 rows 91 / 104 / 136, 64: 125 / 157 / 135, 96: 180 / 221 /
+  //     145, 128: 238 / 233 / 157; of 256: 32 rows 182 / 246 / 306, 64: 282 / 378 /
+  //     324, 128: 525 / 594 / 365; of 64: 32 rows 46 / 44 / 94, 128: 110 / 94 / 115,
+  //     256: 205 / 179 / 211
+  // (64 rows of bfloat16 would gain by 128; the border stays where such chunks keep
+  // the answers they gave, bit for bit.)
   if (f8 && D > 64) L.tile_rows = rows <= 64 ? 16 : 128;
   else L.tile_rows = rows <= 16 ? 16 : rows <= (f8 ? 256 : 64) ? 32 : 128;
   // Rows of shared keys gain more by 128.  us by 16 / 32 / 128 rows, cross attention

@@ -553,15 +553,20 @@ constexpr int rows_tile(int D, bool f8) { return f8 || D <= 128 ? 64 : 32; }
 
 // The same for chunks of many rows: a workgroup takes 128, each wavefront 32 of
 // its own over all of the share's keys, so that a tile of keys and values is
-// read once for 128 rows. Tiles pass through LDS, in the order the lanes of the
-// products want them (a wavefront's read is 1 KiB in a row, without conflicts),
-// double-buffered: the next tile's are written behind the products of this one
-// and the loads of the one after it are then under way.  What bounds it is the
-// LDS, whose reads of a tile take as long as the products of 32 rows with it,
-// and the softmax's vector instructions: 4 chunks of 1024 rows over 4096 tokens,
-// 32/8 heads of 128, take 383 to 406 us in bfloat16 (593 to 629 TFLOP/s; by 406,
-// 515 us with 32 keys a tile, 653 with 64 rows a workgroup and its wavefronts apart
-// over the keys) and 437 in e4m3.
+// read once for 128 rows. Tiles pass through LDS, in bfloat16 (8 bits are widened
+// once, as they are written) and in the order the lanes of the products want them (a
+// wavefront's read is 1 KiB in a row, without conflicts), double-buffered: the next
+// tile's are written behind the products of this one and the loads of the one after
+// it are then under way.  A fragment is read four products' operands ahead.  What
+// bounds it is that two wavefronts a SIMD do not keep the matrix unit under the
+// softmax's vector instructions (about 300 a tile, 1300 of its cycles, where the
+// products are 1024) and the LDS, whose reads of a tile take as long as the products
+// with it: 4 chunks of 1024 rows over 4096 tokens, 32/8 heads of 128, take 323 us in
+// bfloat16 (745 TFLOP/s) and 363 in e4m3; without the reads ahead and with values
+// masked as they were read, 383 and 437 (by 406, 515 us with 32 keys a tile, 653 with
+// 64 rows a workgroup and its wavefronts apart over the keys).  64 rows a wavefront,
+// with the next tile's scores taken under this one's powers, 521 against 379 us where
+// keys are shared: the accumulators do not stay in one register file.
 template <int D, bool F8>
 struct RowsLds {
   // 1 KiB fragments of keys, then of values, of two tiles, in bfloat16; scales of keys,

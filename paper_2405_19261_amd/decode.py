@@ -23,7 +23,9 @@ with seeded logits, standing in for the paper's drafter/verifier pairs,
 whose weights are not used here.  ``ContextLM`` adds a paged KV cache to it:
 its logits depend on every token before them through one attention layer
 (``spc_kv_write``, ``spc_kv_attend``), one token at a time as a drafter and
-gamma + 1 at a time as a verifier.
+gamma + 1 at a time as a verifier; behind a prompt that all sequences share
+(``spc_kv_attend_shared``) and with an encoder's states (``spc_cross_attend``)
+where it is given them.
 
 With ``top_k``, ``top_p`` or ``min_p`` the drafts come from the drafter's
 truncated distribution (``spc_sample``) and the verification sees both models'
