@@ -510,8 +510,9 @@ size_t spc_kv_shared_workspace_bytes(const spc_kv_cache* cache, int32_t shared, 
  *   key_mask     bytes, row b at key_mask + b * mask_stride (0: one row for all), of
  *                mask_width tokens (those from there on are masked); NULL: nothing
  *                is masked
- * The keys and values of masked tokens may be anything.  Other arguments, types
- * and the workspace (spc_kv_workspace_bytes) as for spc_kv_attend.
+ * The keys and values of masked tokens may be anything.  Other arguments and types
+ * as for spc_kv_attend.
+ *   workspace    of spc_cross_workspace_bytes(...) bytes, or NULL, as there
  */
 spc_status spc_cross_attend(const spc_kv_cache* cache, const void* q, int32_t dtype,
                             int64_t q_stride, int32_t heads, int64_t rows,
@@ -519,6 +520,10 @@ spc_status spc_cross_attend(const spc_kv_cache* cache, const void* q, int32_t dt
                             const uint8_t* key_mask, int64_t mask_stride, int32_t mask_width,
                             void* out, int64_t out_stride, void* workspace,
                             size_t workspace_bytes, hipStream_t stream);
+
+/* As spc_kv_workspace_bytes, for spc_cross_attend. */
+size_t spc_cross_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                                 int32_t max_rows);
 
 /*
  * spc_kv_weigh -- the attention weight that cached tokens get from new ones, on

@@ -971,11 +971,15 @@ spc_status kv_answers(void* out, int64_t out_stride, spc::KvParams& P) {
   return SPC_OK;
 }
 
-// A launch of B sequences of n rows, cut by L, has few enough workgroups.
+// Workgroups of B sequences of `rows` rows (of a key/value head), cut by L.
+int64_t kv_groups(int64_t B, int64_t H, int64_t rows, const AttendLayout& L) {
+  return (rows + L.tile_rows - 1) / L.tile_rows * ((H * B * L.splits + 7) / 8 * 8);
+}
+
+// A launch of them and of `others` has few enough.
 spc_status kv_launch_size(int64_t B, int64_t H, int64_t rows, const AttendLayout& L,
-                          const int32_t* row_start) {
-  const int64_t tiles = (rows + L.tile_rows - 1) / L.tile_rows;
-  if (tiles * ((H * B * L.splits + 7) / 8 * 8) >= (int64_t(1) << 24))
+                          const int32_t* row_start, int64_t others = 0) {
+  if (kv_groups(B, H, rows, L) + others >= (int64_t(1) << 24))
     return fail(SPC_E_SHAPE, "%lld rows of each of %lld sequences are too many for one call%s",
                 (long long)rows, (long long)B, row_start ? ": pass max_rows" : "");
   return SPC_OK;
@@ -1086,7 +1090,8 @@ spc_status kv_attend_shared_impl(const spc_kv_cache* cache, int32_t shared,
   const SharedLayout L = shared_layout(P.B, P.H, heads, rows, P.n, P.D, shared,
                                        (int64_t)P.width * P.S, P.f8);
   st = kv_launch_size(P.B, P.H, P.n * G, L.own, row_start);
-  if (st == SPC_OK) st = kv_launch_size(1, P.H, rows * G, L.pre, nullptr);
+  if (st == SPC_OK)
+    st = kv_launch_size(1, P.H, rows * G, L.pre, nullptr, kv_groups(P.B, P.H, P.n * G, L.own));
   char* ws = nullptr;
   if (st == SPC_OK) st = plain_workspace(workspace, workspace_bytes, L.bytes, stream, &ws);
   if (st != SPC_OK) return st;
@@ -1336,6 +1341,16 @@ spc_status spc_cross_attend(const spc_kv_cache* cache, const void* q, int32_t dt
                              key_mask, mask_stride, mask_width, out, out_stride, workspace,
                              workspace_bytes, stream);
   });
+}
+
+size_t spc_cross_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64_t rows,
+                                 int32_t max_rows) {
+  const int64_t n = query_rows(cache, heads, rows, max_rows);
+  if (n == 0) return 0;
+  return attend_layout(cache->B, cache->kv_heads, heads, n, cache->head_dim,
+                       (int64_t)cache->table_width * cache->page_size, cache->dtype == SPC_E4M3,
+                       spc::AttendKind::kCrossTokens)
+      .bytes;
 }
 
 spc_status spc_kv_weigh(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,

@@ -117,6 +117,8 @@ def lib():
         L.spc_cross_attend.argtypes = [cache, *queries, _P, i64, _I32, _P, i64, _P,
                                        ctypes.c_size_t, _P]
         L.spc_cross_attend.restype = ctypes.c_int
+        L.spc_cross_workspace_bytes.argtypes = [cache, _I32, i64, _I32]
+        L.spc_cross_workspace_bytes.restype = ctypes.c_size_t
         L.spc_kv_weigh.argtypes = [cache, *queries, _I32, _P, _P, i64, _I32, _P, ctypes.c_size_t,
                                    _P]
         L.spc_kv_weigh.restype = ctypes.c_int
@@ -741,6 +743,16 @@ def spc_kv_shared_workspace_bytes(k_pages, v_pages, page_table, kv_len, shared, 
         max_q = 0 if q_start is None else rows
     return lib().spc_kv_shared_workspace_bytes(cache, _int32("shared", shared),
                                                _int32("heads", heads), rows, _int32("max_q", max_q))
+
+
+def spc_cross_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=None, *,
+                              k_scale=None, v_scale=None, q_start=None):
+    """As ``spc_kv_workspace_bytes``, for ``spc_cross_attend``."""
+    cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if max_q is None:
+        max_q = 0 if q_start is None else rows
+    return lib().spc_cross_workspace_bytes(cache, _int32("heads", heads), rows,
+                                           _int32("max_q", max_q))
 
 
 def spc_kv_weigh_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, rows, max_q=None, *,

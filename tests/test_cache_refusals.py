@@ -71,6 +71,8 @@ def test_query_refusals(kw, status):
     (shared, dict(shared=(1 << 30) + 1), -2), (shared, dict(window=-1), -4), (shared, dict(os=1023), -2),
     (shared, dict(out=OK + 4), -5), (shared, dict(os=1026), -5),
     (shared, dict(rows=1 << 24, start=OK, most=1, heads=4096, qs=1 << 20, os=1 << 20), -2),
+    # (two parts that one launch could not hold, each of which alone it could)
+    (shared, dict(rows=2620000, start=OK, most=2620000, heads=128, qs=1 << 14, os=1 << 14), -2),
     (cross, dict(mw=0), -2), (cross, dict(ms=-1), -2), (cross, dict(os=1023), -2),
     (cross, dict(out=OK + 4), -5),
     (weigh, dict(window=-1), -4), (weigh, dict(length=0), -2), (weigh, dict(length=(1 << 26) + 1, ld=1 << 27), -2),
@@ -93,8 +95,8 @@ def test_workspace_queries():
     """Sizes that no call takes give 0; others what a call of them asks for."""
     L = spc.lib()
     for f in (lambda c, h, r, m: L.spc_kv_shared_workspace_bytes(c, 100, h, r, m),
-              L.spc_kv_weigh_workspace_bytes):
-        assert f(cache(), 8, 6, 0) > 0
+              L.spc_kv_weigh_workspace_bytes, L.spc_cross_workspace_bytes):
+        assert f(cache(table_width=64), 8, 6, 0) > 0
         for bad in (dict(B=0), dict(page_size=8), dict(head_dim=96), dict(dtype=0), dict(kv_heads=0)):
             assert f(cache(**bad), 8, 6, 0) == 0
         for h, r, m in ((7, 6, 0), (0, 6, 0), (8, 0, 0), (8, 7, 0), (8, 6, -1), (8, (1 << 24) + 1, 2)):
@@ -109,6 +111,8 @@ def test_workspace_queries():
     assert weigh(c, ws=OK, n=need - 1) == -6
     need = L.spc_kv_shared_workspace_bytes(c, 20, 8, 6, 0)
     assert shared(c, ws=OK, n=need - 1) == -6
+    need = L.spc_cross_workspace_bytes(c, 8, 6, 0)
+    assert cross(c, ws=OK, n=need - 1) == -6
 
 
 def tensors(B=2, H=2, S=16, D=64, width=4, pages=12):

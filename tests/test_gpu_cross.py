@@ -157,6 +157,23 @@ def test_a_nan_that_a_row_sees_is_its_answer(n, L):
     assert not bool(torch.cat([out[1, ..., :7], out[1, ..., 8:]], -1).isnan().any())
 
 
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("heads,n", [(1, 1), (4, 10), (8, 8), (16, 30)])
+def test_workspaces(heads, n, f8):
+    """A workspace of the size that the query gives is enough, and is not written past."""
+    lens = [3000]
+    cache = encoder(lens, 1, 128, 64, f8)
+    q = randn((1, n, heads, 128), 3).to(DEV)
+    need = spc.spc_cross_workspace_bytes(*cache.args(i32(lens)), heads, n, **cache.scales())
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device=DEV)
+    out, _ = check(cache, q, lens, workspace=ws[:need])
+    assert bool((ws[need:] == 255).all())
+    assert torch.equal(out, spc.spc_cross_attend(q, *cache.args(i32(lens)), **cache.scales()))
+    if need:
+        with pytest.raises(spc.SpcError):
+            spc.spc_cross_attend(q, *cache.args(i32(lens)), workspace=ws[:need - 256], **cache.scales())
+
+
 def test_captured_and_replayed():
     cache = encoder([900, 650], 2, 64, 16, True)
     q, lens = randn((2, 6, 8, 64), 2).to(DEV), i32([900, 650])
