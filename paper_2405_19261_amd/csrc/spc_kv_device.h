@@ -18,6 +18,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4a2 __attribute__((aligned(2)));
+typedef u32x4 u32x4a4 __attribute__((aligned(4)));
 typedef u32x2 u32x2a2 __attribute__((aligned(2)));
 
 constexpr float kNegInf = -__builtin_huge_valf();

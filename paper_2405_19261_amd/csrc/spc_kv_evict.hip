@@ -740,22 +740,45 @@ void weigh(const KvParams& P, hipStream_t stream) {
 // ------------------------------------------------------------------ eviction
 // Which tokens of a sequence and head stay: one workgroup finds the weight of the
 // last one kept by counting, 8 bits of it a pass, the highest first, among those
-// that agree in the bits before, and then writes the positions of what is above
-// it, and of the first ones equal to it, in their order.  Weights are compared as
-// 32-bit words of their order: 0 for a position that is in no page (never kept),
-// 1 for a NaN, the largest for tokens that stay whatever they weigh.  THREADS
-// times KEYS positions are held in registers; of longer rows the keys are taken
-// again from memory every pass.  Bound by its chain of some 20 barriers: 8192
-// positions 16 us (33 with 32 registers of keys and bins whose copies shared banks),
-// 1200 10.
-__device__ __forceinline__ uint32_t order_of(float w) {
-  if (w != w) return 1u;
-  const uint32_t u = __float_as_uint(w + 0.0f);  // (-0 as 0)
+// that agree in the bits before, until all or few of them are left, which it ranks;
+// then it writes the positions of what is above that weight, and of the first ones
+// equal to it, in their order.  Weights are compared as 32-bit words of their order:
+// 0 for a position that is in no page (never kept), 1 for a NaN, the largest for
+// tokens that stay whatever they weigh.  A lane takes four positions in a row (of one
+// page), KEYS in all, in registers; of rows longer than THREADS times KEYS they are
+// taken again from memory every pass.  Bound by its chain of barriers, in long rows by
+// what one compute unit's LDS counts: 1200 positions 7.5 us, 8192 11, 28385 27 (11,
+// 17 and 36 with a position a lane, all passes to the last, a kept token's weight
+// loaded where it is written).
+__device__ __forceinline__ uint32_t order_of(uint32_t u) {
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 1u;
+  if (u == 0x80000000u) u = 0u;  // (-0 as 0)
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 // t / S of positions under 2^30.
 __device__ __forceinline__ uint32_t page_index(const KvParams& C, uint32_t t) {
   return C.s16_magic ? __umulhi(t >> 4, C.s16_magic) : t >> 4;
+}
+// Sums over the lanes up to each: inside rows of 16, then of the rows before.
+template <int N>
+__device__ __forceinline__ uint32_t lanes_up(uint32_t v) {  // row_shr: 0 where there is none
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x110 + N, 0xf, 0xf, false);
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+__device__ __forceinline__ uint32_t sums_upto(uint32_t v) {
+  v += lanes_up<1>(v);
+  v += lanes_up<2>(v);
+  v += lanes_up<4>(v);
+  v += lanes_up<8>(v);
+  const uint32_t a = lane_of(v, 15), b = a + lane_of(v, 31), c = b + lane_of(v, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return v + (row == 0 ? 0u : row == 1 ? a : row == 2 ? b : c);
+}
+// Lanes below this one in the mask, and n.
+__device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t n) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, n));
 }
 
 template <int THREADS, int KEYS>
@@ -763,167 +786,206 @@ __global__ void __launch_bounds__(THREADS) k_evict_select(EvictParams P) {
   // copies of a count: lanes that add to one bin do not wait for each other, and a
   // bin's copies lie in different banks
   constexpr int kCopies = 16, kCopy = 257, kWaves = THREADS / 64;
+  constexpr int kRuns = KEYS / 4, kCounts = kRuns * kWaves, kFew = 64;
   __shared__ uint32_t bins[kCopies * kCopy];
   __shared__ __align__(16) uint32_t total[256];
-  __shared__ uint32_t more[KEYS * kWaves], same[KEYS * kWaves];
-  __shared__ uint32_t pick[4], valid[kWaves];
+  __shared__ uint32_t counts[kCounts], few[kFew], few_count;
   const int h = blockIdx.x, b = blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const KvParams& C = P.cache;
-  const int32_t whole_len = max(C.len[b], 0), len = min(whole_len, C.width * C.S);
+  const int32_t whole_len = max(C.len[b], 0);
+  const int32_t len = (int32_t)min((int64_t)whole_len, (int64_t)C.width * C.S);
+  const int32_t weighed = min(len, P.length);  // positions that have a weight
   const float* weights = P.weights + ((int64_t)b * C.H + h) * P.weights_stride;
   const int32_t* table = C.table + (int64_t)b * C.width;
-  const int64_t recent = (int64_t)whole_len - P.recent;  // tokens from here on stay
+  const int32_t recent = max(whole_len - P.recent, 0);  // tokens from here on stay
   uint32_t key[KEYS];
-  const auto fill = [&](int64_t base) {
-    float w[KEYS];
-    int32_t page[KEYS];
+  const auto fill = [&](int32_t base) {  // (len > 0)
+    u32x4 w[kRuns];
+    int32_t page[kRuns];
+    const auto at = [&](int i) { return base + 4 * (i * THREADS + tid); };
+    if (weighed >= 4) {  // uniform; at the end, the last four
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) {
-      const int64_t t = base + (int64_t)i * THREADS + tid;
-      w[i] = t < min(len, P.length) ? weights[t] : 0.0f;
-      page[i] = t < len ? table[page_index(C, (uint32_t)t)] : -1;
+      for (int i = 0; i < kRuns; ++i)
+        w[i] = *reinterpret_cast<const u32x4a4*>(weights + min(at(i), weighed - 4));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+      if (at(0) == 0)
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (k < weighed) w[0][k] = __float_as_uint(weights[k]);
     }
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) {
-      const int64_t t = base + (int64_t)i * THREADS + tid;
-      key[i] = t < P.first || t >= recent ? 0xffffffffu : order_of(w[i]);
-      if ((uint32_t)page[i] >= (uint32_t)C.pages) key[i] = 0u;
+    for (int i = 0; i < kRuns; ++i) page[i] = table[page_index(C, (uint32_t)min(at(i), len - 1))];
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const int32_t t = at(i), past = weighed >= 4 ? min(max(t - (weighed - 4), 0), 4) : 0;
+      u32x4 x = w[i];
+      if (past & 1) x = u32x4{x[1], x[2], x[3], 0u};
+      if (past & 2) x = u32x4{x[2], x[3], 0u, 0u};
+      if (past & 4) x = u32x4{0u, 0u, 0u, 0u};
+      const bool there = (uint32_t)page[i] < (uint32_t)C.pages;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t o = t + k < P.first || t + k >= recent ? 0xffffffffu : order_of(x[k]);
+        key[4 * i + k] = there && t + k < len ? o : 0u;
+      }
     }
   };
-  constexpr int64_t kStep = (int64_t)THREADS * KEYS;
+  constexpr int32_t kStep = THREADS * KEYS;
   const bool held = len <= kStep;
-  // how many there are
-  uint32_t mine = 0;
 #pragma unroll
   for (int i = 0; i < KEYS; ++i) key[i] = 0u;
-  for (int64_t base = 0; base < len; base += kStep) {
-    fill(base);
-#pragma unroll
-    for (int i = 0; i < KEYS; ++i) mine += (uint32_t)__popcll(__ballot(key[i] != 0u));
-  }
-  if (lane == 0) valid[wave] = mine;
   for (int i = tid; i < kCopies * kCopy; i += THREADS) bins[i] = 0u;
+  if (tid == 0) few_count = 0u;
+  if (held && len) fill(0);
   __syncthreads();
-  uint32_t there = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) there += valid[w];
-  const uint32_t kept = min((uint32_t)P.keep, there);
   // the kept-th largest key, and how many of that value are kept (all: what is above 0)
-  uint32_t border = 0u, need = kept < there ? kept : 0u;
-  if (kept < there) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int64_t base = 0; base < len; base += kStep) {
+  uint32_t border = 0u, need = 0u, kept = 0u;
+  for (int shift = 24;; shift -= 8) {
+    for (int32_t base = 0; base < len; base += kStep) {
+      if (!held) fill(base);
+#pragma unroll
+      for (int i = 0; i < KEYS; ++i)
+        if (key[i] && (shift == 24 || key[i] >> (shift + 8) == border))
+          atomicAdd(&bins[(lane & (kCopies - 1)) * kCopy + (key[i] >> shift & 255u)], 1u);
+    }
+    __syncthreads();
+    if (tid < 256) {  // (and the counts are zero again)
+      uint32_t n = 0;
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) {
+        n += bins[c * kCopy + tid];
+        bins[c * kCopy + tid] = 0u;
+      }
+      total[255 - tid] = n;
+    }
+    __syncthreads();
+    // every wavefront for itself: bins from the largest down, four a lane
+    const u32x4 n = *reinterpret_cast<const u32x4*>(&total[4 * lane]);
+    const uint32_t sum = n[0] + n[1] + n[2] + n[3], upto = sums_upto(sum);
+    if (shift == 24) {
+      const uint32_t there = lane_of(upto, 63);
+      kept = min((uint32_t)P.keep, there);
+      if (kept == there) break;
+      need = kept;
+    }
+    uint32_t before = upto - sum, digit = 0u, ahead = 0u, left = 0u;
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (before < need && before + n[k] >= need) {
+        found = true;
+        digit = (uint32_t)(255 - 4 * lane - k);
+        ahead = before;
+        left = n[k];
+      }
+      before += n[k];
+    }
+    const int at = __ffsll((unsigned long long)__ballot(found)) - 1;
+    border = border << 8 | lane_of(digit, at);
+    need -= lane_of(ahead, at);
+    left = lane_of(left, at);  // that begin with these bits, of which `need` stay
+    if (shift == 0) break;
+    if (left == need) {
+      border = max(border << shift, 1u) - 1u;
+      need = 0u;
+      break;
+    }
+    if (left <= kFew) {
+      for (int32_t base = 0; base < len; base += kStep) {
         if (!held) fill(base);
 #pragma unroll
         for (int i = 0; i < KEYS; ++i)
-          if (key[i] && (shift == 24 || key[i] >> (shift + 8) == border))
-            atomicAdd(&bins[(lane & (kCopies - 1)) * kCopy + (key[i] >> shift & 255u)], 1u);
-      }
-      __syncthreads();
-      if (tid < 256) {  // (and the counts are zero again)
-        uint32_t n = 0;
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) {
-          n += bins[c * kCopy + tid];
-          bins[c * kCopy + tid] = 0u;
-        }
-        total[255 - tid] = n;
-      }
-      __syncthreads();
-      if (wave == 0) {  // bins from the largest down, four a lane
-        const u32x4 n = *reinterpret_cast<const u32x4*>(&total[4 * lane]);
-        const uint32_t sum = n[0] + n[1] + n[2] + n[3];
-        uint32_t before = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const uint32_t y = __shfl_up(before, d);
-          if (lane >= d) before += y;
-        }
-        before -= sum;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (before < need && before + n[k] >= need) {
-            pick[0] = 255 - 4 * lane - k;
-            pick[1] = before;
+          if (key[i] && key[i] >> shift == border) {
+            const uint32_t at_few = atomicAdd(&few_count, 1u);
+            if (at_few < kFew) few[at_few] = key[i];
           }
-          before += n[k];
-        }
       }
       __syncthreads();
-      border = border << 8 | pick[0];
-      need -= pick[1];
+      const uint32_t x = lane < (int)left ? few[lane] : 0u;
+      uint32_t larger = 0u, same = 0u;
+      for (int j = 0; j < (int)left; ++j) {
+        const uint32_t y = lane_of(x, j);
+        larger += y > x;
+        same += y == x;
+      }
+      const int last = __ffsll((unsigned long long)__ballot(lane < (int)left && larger < need &&
+                                                           larger + same >= need)) - 1;
+      border = lane_of(x, last);
+      need -= lane_of(larger, last);
+      break;
     }
   }
   // positions in their order
   uint32_t above = 0, equal = 0;  // before the present ones
   int32_t* index = P.out_index + ((int64_t)b * C.H + h) * P.keep;
   float* out_w = P.out_weights ? P.out_weights + ((int64_t)b * C.H + h) * P.out_stride : nullptr;
-  for (int64_t base = 0; base < len; base += kStep) {
+  for (int32_t base = 0; base < len; base += kStep) {
     if (!held) fill(base);
+    // what is above (the lower half of a word) and equal, by runs of the wavefronts
+    uint32_t mine = 0u;
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) {
-      const uint64_t a = __ballot(key[i] > border), e = __ballot(key[i] && key[i] == border);
-      if (lane == 0) {
-        more[i * kWaves + wave] = (uint32_t)__popcll(a);
-        same[i * kWaves + wave] = (uint32_t)__popcll(e);
+    for (int i = 0; i < kRuns; ++i) {
+      uint32_t n = 0u;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = key[4 * i + k];
+        n += (uint32_t)__popcll(__ballot(x > border)) +
+             ((uint32_t)__popcll(__ballot(x && x == border)) << 16);
       }
+      mine = lane == i ? n : mine;
     }
+    if (lane < kRuns) counts[lane * kWaves + wave] = mine;
     __syncthreads();
-    if (wave == 0) {  // counts before each wavefront's, some a lane, in order
-      constexpr int kEach = (KEYS * kWaves + 63) / 64;
-      uint32_t a[kEach], e[kEach], sa = 0, se = 0;
+    // (the masks are taken again: hundreds of them spill from the scalar registers)
 #pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int at = lane * kEach + k;
-        a[k] = at < KEYS * kWaves ? more[at] : 0u;
-        e[k] = at < KEYS * kWaves ? same[at] : 0u;
-        sa += a[k];
-        se += e[k];
+    for (int i = 0; i < KEYS; ++i) asm("" : "+v"(key[i]));
+    static_assert(THREADS * KEYS < 65536, "two counts a word");
+    constexpr int kEach = (kCounts + 63) / 64;
+    static_assert(kEach == 1 || (kEach == 2 && kWaves % 2 == 0), "by the wavefront's parity");
+    uint32_t part[kEach], sum = 0u;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int at = lane * kEach + k;
+      part[k] = at < kCounts ? counts[at] : 0u;
+      sum += part[k];
+    }
+    const uint32_t upto = sums_upto(sum);
+    const uint32_t of_mine = upto - sum + (kEach == 2 && (wave & 1) ? part[0] : 0u);
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const uint32_t pre = lane_of(of_mine, (i * kWaves + wave) / kEach);
+      uint32_t ra = above + (pre & 0xffffu), re = equal + (pre >> 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = key[4 * i + k];
+        ra = count_below(__ballot(x > border), ra);
+        re = count_below(__ballot(x && x == border), re);
       }
-      uint32_t ba = sa, be = se;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t ya = __shfl_up(ba, d), ye = __shfl_up(be, d);
-        if (lane >= d) {
-          ba += ya;
-          be += ye;
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = key[4 * i + k];
+        const bool a = x > border, e = x && x == border;
+        if (a || (e && re < need)) {
+          const uint32_t at = ra + min(re, need);
+          const int32_t t = base + 4 * (i * THREADS + tid) + k;
+          index[at] = t;
+          if (out_w) {
+            float w = __uint_as_float(x >> 31 ? x ^ 0x80000000u : ~x);
+            if (x == 1u || x == 0xffffffffu) w = t < P.length ? weights[t] : 0.0f;
+            out_w[at] = w;
+          }
         }
-      }
-      if (lane == 63) {
-        pick[2] = ba;
-        pick[3] = be;
-      }
-      ba -= sa;
-      be -= se;
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int at = lane * kEach + k;
-        if (at < KEYS * kWaves) {
-          more[at] = ba;
-          same[at] = be;
-        }
-        ba += a[k];
-        be += e[k];
+        ra += a;
+        re += e;
       }
     }
-    __syncthreads();
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < KEYS; ++i) {
-      const uint64_t in_a = __ballot(key[i] > border), in_e = __ballot(key[i] && key[i] == border);
-      const uint32_t ra = above + more[i * kWaves + wave] + (uint32_t)__popcll(in_a & below);
-      const uint32_t re = equal + same[i * kWaves + wave] + (uint32_t)__popcll(in_e & below);
-      if (key[i] > border || (key[i] && key[i] == border && re < need)) {
-        const uint32_t at = ra + min(re, need);
-        const int64_t t = base + (int64_t)i * THREADS + tid;
-        index[at] = (int32_t)t;
-        if (out_w) out_w[at] = t < P.length ? weights[t] : 0.0f;
-      }
-    }
-    above += pick[2];
-    equal += pick[3];
-    __syncthreads();
+    const uint32_t all = lane_of(upto, 63);
+    above += all & 0xffffu;
+    equal += all >> 16;
+    if (base + kStep < len) __syncthreads();
   }
   for (int64_t i = (int64_t)kept + tid; i < P.keep; i += THREADS) index[i] = -1;
   if (h == 0 && tid == 0) P.out_len[b] = (int32_t)kept;
@@ -1071,6 +1133,7 @@ hipError_t launch_kv_evict(const EvictParams& P, hipStream_t stream) {
   const dim3 heads(C.H, C.B);
   if (tokens <= 2048) k_evict_select<256, 8><<<heads, 256, 0, stream>>>(P);
   else if (tokens <= 8192) k_evict_select<1024, 8><<<heads, 1024, 0, stream>>>(P);
+  else if (tokens <= 16384) k_evict_select<1024, 16><<<heads, 1024, 0, stream>>>(P);
   else k_evict_select<1024, 32><<<heads, 1024, 0, stream>>>(P);
   if (C.D == 64) C.f8 ? move<64, true>(P, stream) : move<64, false>(P, stream);
   else if (C.D == 128) C.f8 ? move<128, true>(P, stream) : move<128, false>(P, stream);
