@@ -922,7 +922,9 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   // of 64, 23.9 / 19.7, of 16 x 8 rows to 4096 in e4m3, 8 heads of 128, 50.2 / 45.8;
   // 8 rows of 32 sequences behind 8192 in e4m3 107 / 97.)
   const int64_t most = std::max<int64_t>(
-      1, tokens / spc::kv_share_keys(L.tile_rows, f8, kind == spc::AttendKind::kPrefix));
+      1, tokens / spc::kv_share_keys(L.tile_rows, f8,
+                                     kind == spc::AttendKind::kPrefix ||
+                                         kind == spc::AttendKind::kBehindPrefix));
   const int64_t target = kind == spc::AttendKind::kOwnTokens ? 1024 : 512;
   L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                      (int64_t)spc::kKvShares, 65535 / B}));

@@ -46,10 +46,14 @@ enum AttendMode { kOwn, kBehind, kCross, kShared };
 
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512 (of a shared
-// prefix, which few workgroups take, 256).  (One token over 1500 bfloat16 tokens of
-// 8 heads: 13.9 us in shares of 512, 6.9 in shares of 128, and the join 4.4.)
+// prefix, which few workgroups take, and behind it, where the shares are joined
+// anyhow, 256).  (One token over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of
+// 512, 6.9 in shares of 128, and the join 4.4.  Behind a prefix, by 512 / 256: 40 rows
+// of 8 sequences with up to 1000 tokens of their own, 32/8 heads of 128 in e4m3, 87 /
+// 67; 64 rows of 4 with 1000, 16/4 heads of 256 in bfloat16, 120 / 103; where there
+// are enough workgroups, 600 rows of 2 with 548, 16/4 heads of 128, 68 / 72.)
 constexpr int share_keys(int tile_rows, bool f8, int mode = kOwn) {
-  return tile_rows > 64 ? (mode == kShared ? 256 : 512) : f8 ? 256 : 128;
+  return tile_rows > 64 ? (mode == kShared || mode == kBehind ? 256 : 512) : f8 ? 256 : 128;
 }
 
 // The tokens whose rows a launch is sized for, a sequence.
@@ -973,10 +977,8 @@ void attend_shares(const KvParams& P, hipStream_t stream) {
   const dim3 grid(attend_blocks<MODE>(P));
   const dim3 block(64 * kAttendWaves);
   if (P.tile_rows == 128) k_kv_attend_rows<D, F8, MODE><<<grid, block, 0, stream>>>(P);
-  else if constexpr (MODE != kShared) {  // (few rows behind a prefix: k_shared_both)
-    if (P.tile_rows == 16) k_kv_attend<D, F8, 1, MODE><<<grid, block, 0, stream>>>(P);
-    else if constexpr (!F8 || D == 64) k_kv_attend<D, F8, 2, MODE><<<grid, block, 0, stream>>>(P);
-  }
+  else if (P.tile_rows == 16) k_kv_attend<D, F8, 1, MODE><<<grid, block, 0, stream>>>(P);
+  else if constexpr (!F8 || D == 64) k_kv_attend<D, F8, 2, MODE><<<grid, block, 0, stream>>>(P);
 }
 
 template <int D, bool F8, int MODE>

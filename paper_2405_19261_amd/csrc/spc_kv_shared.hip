@@ -104,10 +104,14 @@ __global__ void __launch_bounds__(256) k_shared_join(KvParams own, KvParams pre,
 // Both attentions in one launch, the prefix's workgroups first: apart, the card
 // drains between them, and neither fills it (32 sequences of one token behind 8192,
 // 260 of their own on average, 32/8 heads of 128, bfloat16: 25 and 15 us apart, 22
-// together, at 3.1 TB/s: the few tiles of each workgroup do not cover its start).
+// together, at 3.1 TB/s: the few tiles of each workgroup do not cover its start; 64
+// rows of 4 sequences behind 4000 with 1000 of their own, 16/4 heads of 256, 140 a
+// call apart, 120 together; 256 rows of 4 behind 2048, up to 2048 of their own, 32/8
+// heads of 128, 118 and 99).
 template <int D, bool F8, int PRE, int OWN>
 __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1)
     k_shared_both(KvParams own, KvParams pre, uint32_t pre_blocks) {
+  static_assert(OWN <= 2 || PRE > 2, "many rows of a sequence are many of all");
   constexpr size_t kRows = PRE > 2 ? sizeof(RowsLds<D, F8>) : 0;
   constexpr size_t kBytes = kRows > sizeof(AttendLds<D>) ? kRows : sizeof(AttendLds<D>);
   __shared__ __align__(16) char lds[kBytes];
@@ -116,13 +120,16 @@ __global__ void __launch_bounds__(64 * kAttendWaves, D <= 128 ? 2 : 1)
       attend_many<D, F8, kShared>(pre, blockIdx.x, *reinterpret_cast<RowsLds<D, F8>*>(lds));
     else
       attend_few<D, F8, PRE, kShared>(pre, blockIdx.x, *reinterpret_cast<AttendLds<D>*>(lds));
+  } else if constexpr (OWN > 2) {
+    attend_many<D, F8, kBehind>(own, blockIdx.x - pre_blocks,
+                                *reinterpret_cast<RowsLds<D, F8>*>(lds));
   } else {
     attend_few<D, F8, OWN, kBehind>(own, blockIdx.x - pre_blocks,
                                     *reinterpret_cast<AttendLds<D>*>(lds));
   }
 }
 
-// Rows of a workgroup in sixteens: 1 or 8 of the prefix, 1 or 2 of the others.
+// Rows of a workgroup in sixteens: 1 or 8 of the prefix, 1, 2 or 8 of the others.
 template <int D, bool F8, int PRE, int OWN>
 void both(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   const uint32_t pre_blocks = attend_blocks<kShared>(pre);
@@ -133,9 +140,8 @@ void both(const KvParams& own, const KvParams& pre, hipStream_t stream) {
 
 template <int D, bool F8>
 void shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
-  if (own.tile_rows == 128) {  // (many rows a sequence: each fills the card)
-    attend_shares<D, F8, kShared>(pre, stream);
-    if (own.splits) attend_shares<D, F8, kBehind>(own, stream);
+  if (own.tile_rows == 128) {
+    both<D, F8, 8, 8>(own, pre, stream);
   } else if (pre.tile_rows == 128) {
     if (own.tile_rows == 16) both<D, F8, 8, 1>(own, pre, stream);
     else if constexpr (!F8 || D == 64) both<D, F8, 8, 2>(own, pre, stream);
@@ -146,7 +152,7 @@ void shared(const KvParams& own, const KvParams& pre, hipStream_t stream) {
   }
   const int64_t rows = (int64_t)own.n * (own.heads / own.H);
   k_shared_join<D><<<dim3((uint32_t)((rows + 3) / 4), own.H, own.B), 256, 0, stream>>>(
-      own, pre, tile_keys(D, F8, own.tile_rows), share_keys(own.tile_rows, F8),
+      own, pre, tile_keys(D, F8, own.tile_rows), share_keys(own.tile_rows, F8, kBehind),
       tile_keys(D, F8, pre.tile_rows), share_keys(pre.tile_rows, F8, kShared));
 }
 
