@@ -272,7 +272,10 @@ hipError_t launch_cross_attend(const KvParams& P, hipStream_t stream);
 // one's (tile_rows, splits, part of its own).
 hipError_t launch_kv_attend_shared(const KvParams& own, const KvParams& pre, hipStream_t stream);
 constexpr int kWeighRows = 32;     // rows of a key/value head whose scores a call may keep
-constexpr int kWeighShare = 512;   // keys that a share of more rows has at least
+// Keys that a share of more rows has at least.  (us by 512 / 256 / 128: 100 rows of 8
+// sequences over up to 2048 keys, 16/4 heads of 64, 38 / 29 / 29; 64 of 1 over 8000, 8
+// heads of 64, 22 / 21 / 24; 100 of 6 over up to 1500, 16/4 heads of 256, 60 / 50 / 47.)
+constexpr int kWeighShare = 256;
 constexpr int kWeighStats = 1024;  // rows whose statistics the second step holds
 hipError_t launch_kv_weigh(const KvParams& P, hipStream_t stream);
 
