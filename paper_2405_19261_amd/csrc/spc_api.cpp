@@ -921,10 +921,17 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   // (us by four / two: cross attention of 32 x 6 rows to up to 1024 tokens, 16 heads
   // of 64, 23.9 / 19.7, of 16 x 8 rows to 4096 in e4m3, 8 heads of 128, 50.2 / 45.8;
   // 8 rows of 32 sequences behind 8192 in e4m3 107 / 97.)
-  const int64_t most = std::max<int64_t>(
-      1, tokens / spc::kv_share_keys(L.tile_rows, f8,
-                                     kind == spc::AttendKind::kPrefix ||
-                                         kind == spc::AttendKind::kBehindPrefix));
+  int64_t most = std::max<int64_t>(
+      1, tokens / spc::kv_share_keys(L.tile_rows, f8, kind != spc::AttendKind::kOwnTokens));
+  // Many rows of an encoder's states: shares under 512 keys where there is no workgroup
+  // for each compute unit, up to eight.  (us by 512 / 256 keys: 9 rows of 16 sequences
+  // to 1686 tokens, 8/2 heads of 256, 48 / 32, 100 of 4 to up to 2000, 16/2 heads of 64,
+  // 25 / 20; but 600 of 4 to 900, 16/4 heads of 128, 54 / 82, and 50 of 2 to up to
+  // 4000, 32/4 heads of 256, in fifteen 56 / 62.)
+  if (kind == spc::AttendKind::kCrossTokens && L.tile_rows == 128) {
+    const int64_t whole = std::max<int64_t>(1, tokens / 512);
+    most = groups < 256 ? std::max(whole, std::min<int64_t>(8, most)) : whole;
+  }
   const int64_t target = kind == spc::AttendKind::kOwnTokens ? 1024 : 512;
   L.splits = (int32_t)std::max<int64_t>(1, std::min({most, (target + groups - 1) / groups,
                                                      (int64_t)spc::kKvShares, 65535 / B}));

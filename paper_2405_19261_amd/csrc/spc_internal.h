@@ -261,7 +261,7 @@ struct KvParams {
 hipError_t launch_kv_write(const KvParams& P, int dtype, hipStream_t stream);
 hipError_t launch_kv_read(const KvParams& P, int dtype, hipStream_t stream);
 constexpr int kKvShares = 128;                // shares the keys of a row are cut into, at most
-// Keys that a share of them has at least (shared: of a prefix, or behind one).
+// Keys that a share of them has at least (shared: of any but a sequence's own).
 int kv_share_keys(int tile_rows, bool f8, bool shared);
 hipError_t launch_kv_attend(const KvParams& P, hipStream_t stream);
 // What an attention's workgroups take, for how it is cut.

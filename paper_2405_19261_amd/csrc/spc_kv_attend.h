@@ -47,13 +47,13 @@ enum AttendMode { kOwn, kBehind, kCross, kShared };
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512 (of a shared
 // prefix, which few workgroups take, and behind it, where the shares are joined
-// anyhow, 256).  (One token over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of
+// anyhow, 256; of an encoder's states 256 where workgroups are few).  (One token over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of
 // 512, 6.9 in shares of 128, and the join 4.4.  Behind a prefix, by 512 / 256: 40 rows
 // of 8 sequences with up to 1000 tokens of their own, 32/8 heads of 128 in e4m3, 87 /
 // 67; 64 rows of 4 with 1000, 16/4 heads of 256 in bfloat16, 120 / 103; where there
 // are enough workgroups, 600 rows of 2 with 548, 16/4 heads of 128, 68 / 72.)
 constexpr int share_keys(int tile_rows, bool f8, int mode = kOwn) {
-  return tile_rows > 64 ? (mode == kShared || mode == kBehind ? 256 : 512) : f8 ? 256 : 128;
+  return tile_rows > 64 ? (mode != kOwn ? 256 : 512) : f8 ? 256 : 128;
 }
 
 // The tokens whose rows a launch is sized for, a sequence.
@@ -988,7 +988,7 @@ void attend(const KvParams& P, hipStream_t stream) {
     const int64_t rows = (int64_t)P.n * (P.heads / P.H);
     const dim3 join((uint32_t)((rows + 3) / 4), P.H, P.B);
     k_kv_join<D, MODE><<<join, 256, 0, stream>>>(P, P.tile_rows, tile_keys(D, F8, P.tile_rows),
-                                                 share_keys(P.tile_rows, F8));
+                                                 share_keys(P.tile_rows, F8, MODE));
   }
 }
 
