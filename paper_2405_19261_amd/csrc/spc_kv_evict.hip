@@ -19,9 +19,10 @@ namespace {
 // Each weight is one workgroup's, its rows always added in one order: no atomics.
 // Few rows are bound by the bytes of the keys (one token of 32 sequences over 4096, 8
 // heads of 128 in bfloat16: 48 us, 5.6 TB/s, and 7 for the second step), many by the
-// vector instructions of two softmaxes and the start of workgroups that have few
-// tiles (32 tokens of 4 sequences over up to 16384 in e4m3: 30 and 29 us, where the
-// products are 5 and the bytes 9; 600 tokens of 2 over 2048: 26, 27 and 4).
+// vector instructions of two softmaxes (42 % of the cycles) and uneven lengths, with
+// the start of workgroups that have few tiles (32 tokens of 4 sequences over up to
+// 16384 in e4m3: 29 and 30 us, where the products are 5 and the bytes 9; 600 tokens of
+// 2 over 2048: 22, 27 and 5).
 
 // The first step: as k_kv_attend, without values.
 template <int D, bool F8, int MT>
@@ -1131,6 +1132,9 @@ hipError_t launch_kv_evict(const EvictParams& P, hipStream_t stream) {
   const KvParams& C = P.cache;
   const int64_t tokens = (int64_t)C.width * C.S;
   const dim3 heads(C.H, C.B);
+  // As many threads as hold the positions, and no more registers.  (us a call by 256 /
+  // 1024 threads, 32 sequences of 1500, 16 heads 36 / 42, of 64 of 2000, 32 heads 60 /
+  // 108; by 16 / 32 positions, 12000 20 / 27.)
   if (tokens <= 2048) k_evict_select<256, 8><<<heads, 256, 0, stream>>>(P);
   else if (tokens <= 8192) k_evict_select<1024, 8><<<heads, 1024, 0, stream>>>(P);
   else if (tokens <= 16384) k_evict_select<1024, 16><<<heads, 1024, 0, stream>>>(P);
