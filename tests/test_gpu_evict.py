@@ -243,6 +243,18 @@ def test_evict_long(L, keep, kind):
     check_evict(cache, [L], weights_of(kind, 1, 1, L), keep, 4 if keep > 1 else 0, keep // 9)
 
 
+@pytest.mark.parametrize("kind", ["plain", "ties", "odd"])
+@pytest.mark.parametrize("L", [1, 2, 3, 5, 2047, 2050, 8191, 8194, 12001, 16384, 16387])
+def test_evict_ends(L, kind):
+    """Rows that end inside a lane's four positions, of every size that a workgroup holds;
+    weights that end at once, with the row, inside its last positions and behind it."""
+    for n in sorted({1, 3, max(L - 2, 1), L, L + 1}):
+        for keep in sorted({1, max(L // 3, 1), max(L - 1, 1)}):
+            S = 16
+            cache = cache_of([L, max(L - 1, 0)], 1, 64, S, True, more=2 * ((keep + S - 1) // S))
+            check_evict(cache, [L, max(L - 1, 0)], weights_of(kind, 2, 1, n, L), keep)
+
+
 @pytest.mark.parametrize("f8", [False, True])
 def test_evict_pages_that_are_none(f8):
     """Tokens that are in no page are never kept; pages that are none take nothing."""
