@@ -3,7 +3,10 @@
 Argument marshalling only: every step of the verify path runs in the gfx950
 kernels of ``libspeccascade.so``.  Functions carry the C names; tensors are
 torch tensors on the current HIP device (PyTorch supplies device memory and
-streams, nothing else).  A missing or unloadable library raises -- there is no
+streams, nothing else).  ``stream`` is the stream a call runs on (None: the
+current one), and the stream of the tensors it makes: as with any work on
+another stream, inputs are ready there before the call, and outputs are used
+behind it.  A missing or unloadable library raises -- there is no
 fallback implementation.
 """
 import ctypes
@@ -180,10 +183,27 @@ def _check(status):
         raise SpcError(status, lib().spc_last_error().decode())
 
 
-def _outputs(dev, B, gamma):
-    return (torch.empty(B, dtype=torch.int32, device=dev),
-            torch.empty(B, dtype=torch.int32, device=dev),
-            torch.empty((B, gamma + 1), dtype=torch.uint8, device=dev))
+# What a call makes itself belongs to the stream that its kernels run on: a fill is
+# then ahead of them, and the memory is not one that kernels of the current stream
+# still use.  The caller holds it on the current stream, which may read it (behind
+# the other) after the tensor is dropped: it is kept for that one too.
+def _new(make, shape, dtype, device, stream):
+    """make(shape), torch.empty or torch.zeros, for a call on ``stream``."""
+    if stream is None or stream.cuda_stream == _stream(None):
+        return make(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    current = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = make(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
+def _outputs(dev, B, gamma, stream):
+    return (_new(torch.empty, B, torch.int32, dev, stream),
+            _new(torch.empty, B, torch.int32, dev, stream),
+            _new(torch.empty, (B, gamma + 1), torch.uint8, dev, stream))
 
 
 def _shape(q, p, draft):
@@ -243,7 +263,7 @@ def spc_verify(q, p, draft, uniforms, rule, alpha, temperature, out=None, stream
     """One verify step; returns (accept_len [B], next_token [B], defer_mask [B, gamma+1])."""
     B, gamma, V, dev = _shape(q, p, draft)
     _check_arg("uniforms", uniforms, torch.float32, dev, (B, gamma + 1))
-    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma)
+    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma, stream)
     _check(lib().spc_verify(_ptr(q), _ptr(p), _dtype_code(q), _ptr(draft), _ptr(uniforms), B,
                             gamma, V, int(rule), float(alpha), float(temperature), _ptr(acc),
                             _ptr(tok), _ptr(dm), _stream(stream)))
@@ -253,7 +273,7 @@ def spc_verify(q, p, draft, uniforms, rule, alpha, temperature, out=None, stream
 def spc_greedy_verify(q, p, draft, rule, alpha, out=None, stream=None):
     """The temperature-0 step; returns (accept_len, next_token, defer_mask)."""
     B, gamma, V, dev = _shape(q, p, draft)
-    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma)
+    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma, stream)
     _check(lib().spc_greedy_verify(_ptr(q), _ptr(p), _dtype_code(q), _ptr(draft), B, gamma, V,
                                    int(rule), float(alpha), _ptr(acc), _ptr(tok), _ptr(dm),
                                    _stream(stream)))
@@ -276,7 +296,7 @@ def _verify_ex(entry, q, p, draft, uniforms, rule, alpha, temperature, rule_per_
     _check_arg("out_row_stats", out_row_stats, torch.float32, dev, (B, gamma + 1, 8))
     _check_arg("out_argmax", out_argmax, torch.int32, dev, (B, gamma + 1, 2))
     _check_arg("out_sample_norm", out_sample_norm, torch.float32, dev, (B,))
-    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma)
+    acc, tok, dm = out if out is not None else _outputs(dev, B, gamma, stream)
     if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous tensor on the logits' device")
     ex = ExArgs(_ptr(rule_per_seq), _ptr(alpha_per_seq), _ptr(temp_per_seq), _ptr(out_row_stats),
@@ -324,7 +344,7 @@ def spc_draft_sample(logits, temperature, uniforms=None, temp_per_seq=None, out=
     dev = logits.device
     _check_arg("uniforms", uniforms, torch.float32, dev, (B,))
     _check_arg("temp_per_seq", temp_per_seq, torch.float32, dev, (B,))
-    tok = out if out is not None else torch.empty(B, dtype=torch.int32, device=dev)
+    tok = out if out is not None else _new(torch.empty, B, torch.int32, dev, stream)
     _check_arg("out", tok, torch.int32, dev, (B,))
     if workspace is None:
         _check(lib().spc_draft_sample(_ptr(logits), _dtype_code(logits), B, V, float(temperature),
@@ -385,7 +405,7 @@ def spc_sample(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.0, min_p
     _expect("out_kept", out_kept, torch.int32, logits, (B,))
     cut = _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq,
                       top_p_per_seq, min_p_per_seq, logits, B)
-    tok = out if out is not None else torch.empty(B, dtype=torch.int32, device=logits.device)
+    tok = out if out is not None else _new(torch.empty, B, torch.int32, logits.device, stream)
     _expect("out", tok, torch.int32, logits, (B,))
     code = _dtype_code(logits)
     ws, nbytes = _workspace(workspace, logits)
@@ -412,7 +432,7 @@ def spc_truncate(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, *, temp
     cut = _truncation(temperature, top_k, top_p, min_p, temp_per_seq, top_k_per_seq,
                       top_p_per_seq, min_p_per_seq, logits, B)
     if out is None:
-        out = torch.empty_like(logits)
+        out = _new(torch.empty, logits.shape, logits.dtype, logits.device, stream)
     _expect("out", out, logits.dtype, logits, logits.shape)
     code = _dtype_code(logits)
     ws, nbytes = _workspace(workspace, logits)
@@ -521,7 +541,7 @@ def spc_kv_read(k_pages, v_pages, page_table, kv_len, length=None, *, k_scale=No
         if length is None:
             raise ValueError("length or out must be given")
         shape = (cache.B, length, cache.kv_heads, cache.head_dim)
-        out = tuple(torch.zeros(shape, dtype=dtype, device=k_pages.device) for _ in range(2))
+        out = tuple(_new(torch.zeros, shape, dtype, k_pages.device, stream) for _ in range(2))
     k, v = out
     if length is None:
         length = _int32("length", k.shape[1])
@@ -545,11 +565,11 @@ def _queries(q, cache, k_pages, q_start, scale):
     return rows, heads, stride, dim ** -0.5 if scale is None else float(scale)
 
 
-def _answers(out, q, cache, k_pages, q_start):
+def _answers(out, q, cache, k_pages, q_start, stream):
     """(out, its row stride) of an attention."""
     if out is None:  # (rows of no sequence stay zero)
-        out = (torch.empty if q_start is None else torch.zeros)(q.shape, dtype=q.dtype,
-                                                                device=q.device)
+        out = _new(torch.empty if q_start is None else torch.zeros, q.shape, q.dtype, q.device,
+                   stream)
     if out.shape != q.shape or out.dtype is not q.dtype:
         raise ValueError("out must have the shape and type of q")
     return out, _kv_rows("out", out, k_pages, cache.B, q_start, cache.head_dim)[2]
@@ -564,7 +584,7 @@ def spc_kv_attend(q, k_pages, v_pages, page_table, kv_len, *, scale=None, window
     only the last ``window`` tokens.  Returns ``out`` (as ``q``)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
     rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
-    out, os_ = _answers(out, q, cache, k_pages, q_start)
+    out, os_ = _answers(out, q, cache, k_pages, q_start, stream)
     ws, nbytes = _workspace(workspace, k_pages)
     window = _int32("window", window)
     most = rows if max_q is None else _int32("max_q", max_q)
@@ -587,7 +607,7 @@ def spc_kv_attend_shared(q, k_pages, v_pages, page_table, kv_len, shared, *, sha
     are; ``kv_len`` counts the shared tokens.  Returns ``out`` (as ``q``)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
     rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
-    out, os_ = _answers(out, q, cache, k_pages, q_start)
+    out, os_ = _answers(out, q, cache, k_pages, q_start, stream)
     ws, nbytes = _workspace(workspace, k_pages)
     window, shared = _int32("window", window), _int32("shared", shared)
     most = rows if max_q is None else _int32("max_q", max_q)
@@ -616,7 +636,7 @@ def spc_cross_attend(q, k_pages, v_pages, page_table, kv_len, *, key_mask=None, 
     ``q``); a row that sees nothing is zero."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
     rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
-    out, os_ = _answers(out, q, cache, k_pages, q_start)
+    out, os_ = _answers(out, q, cache, k_pages, q_start, stream)
     ws, nbytes = _workspace(workspace, k_pages)
     most = rows if max_q is None else _int32("max_q", max_q)
     mask, mask_stride, mask_width = None, 0, 0
@@ -672,7 +692,7 @@ def spc_kv_weigh(q, k_pages, v_pages, page_table, kv_len, weights=None, *, scale
     if weights is not None:
         shape = weights.shape
     if out is None:
-        out = torch.zeros(shape, dtype=torch.float32, device=k_pages.device)
+        out = _new(torch.zeros, shape, torch.float32, k_pages.device, stream)
     stride = _weight_rows("out", out, cache, k_pages)
     if weights is not None and weights is not out:
         if _weight_rows("weights", weights, cache, k_pages, out.shape[2]) != stride:
@@ -707,11 +727,11 @@ def spc_kv_evict(k_pages, v_pages, page_table, kv_len, weights, keep, out_table,
     if keep < 1:
         raise ValueError(f"keep must be at least 1, not {keep}")
     if out_len is None:
-        out_len = torch.empty(B, dtype=torch.int32, device=dev)
+        out_len = _new(torch.empty, B, torch.int32, dev, stream)
     if out_index is None:
-        out_index = torch.empty((B, H, keep), dtype=torch.int32, device=dev)
+        out_index = _new(torch.empty, (B, H, keep), torch.int32, dev, stream)
     if out_weights is None:
-        out_weights = torch.zeros((B, H, keep), device=dev)
+        out_weights = _new(torch.zeros, (B, H, keep), torch.float32, dev, stream)
     _expect("out_len", out_len, torch.int32, k_pages, (B,))
     _expect("out_index", out_index, torch.int32, k_pages, (B, H, keep))
     out_stride = _weight_rows("out_weights", out_weights, cache, k_pages, keep)
