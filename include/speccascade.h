@@ -508,8 +508,8 @@ size_t spc_kv_shared_workspace_bytes(const spc_kv_cache* cache, int32_t shared, 
  * rows of one sequence here.
  *
  *   key_mask     bytes, row b at key_mask + b * mask_stride (0: one row for all), of
- *                mask_width tokens (those from there on are masked); NULL: nothing
- *                is masked
+ *                mask_width tokens (at least 1; those from there on are masked); NULL:
+ *                nothing is masked
  * The keys and values of masked tokens may be anything.  Other arguments and types
  * as for spc_kv_attend.
  *   workspace    of spc_cross_workspace_bytes(...) bytes, or NULL, as there

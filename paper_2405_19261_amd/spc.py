@@ -647,6 +647,8 @@ def spc_cross_attend(q, k_pages, v_pages, page_table, kv_len, *, key_mask=None, 
             raise ValueError("key_mask must be [B, width], the bytes of a row contiguous")
         if key_mask.get_device() != k_pages.get_device():
             raise ValueError(f"key_mask must be on {k_pages.device}, not {key_mask.device}")
+        if key_mask.shape[1] == 0:  # masks all (its address is NULL, which is no mask)
+            key_mask = _new(torch.zeros, (1, 1), torch.uint8, k_pages.device, stream).expand(cache.B, 1)
         mask, mask_stride = key_mask.data_ptr(), key_mask.stride(0)
         mask_width = _int32("the width of key_mask", key_mask.shape[1])
     if rows == 0:
