@@ -537,8 +537,8 @@ size_t spc_cross_workspace_bytes(const spc_kv_cache* cache, int32_t heads, int64
  *   weights      [B][kv_heads] rows of `length` float32, row (b, h) at element
  *                (b * kv_heads + h) * weights_stride (at least length), or NULL:
  *                all begin at 0.  length is at most 2^26
- *   out          the same; may be `weights` itself, but not overlap it otherwise.
- *                Positions at or past length get none; those at or past kv_len
+ *   out          the same; may be `weights` itself, but not overlap it otherwise
+ *                (SPC_E_PARAM).  Positions at or past length get none; those at or past kv_len
  *                (or the table's last slot) are left as they are
  *   max_rows     as for spc_kv_attend; rows past it are not counted
  * Scores, statistics and sums are in 32 bits, and sums over rows always in one
@@ -571,13 +571,14 @@ size_t spc_kv_weigh_workspace_bytes(const spc_kv_cache* cache, int32_t heads, in
  *                `keep` tokens may be given its own pages.  A page id out of
  *                range takes nothing
  *   out_len      [B] int32: the tokens kept, min(keep, those in the cache), the
- *                same for every head (kv_len of later calls; not this call's:
- *                SPC_E_PARAM)
+ *                same for every head (kv_len of later calls; it may not overlap
+ *                this call's: SPC_E_PARAM)
  *   out_index    [B][kv_heads][keep] int32: the positions they had, ascending, -1
  *                behind the last
  *   out_weights  [B][kv_heads] rows of keep float32, out_stride apart (at least
  *                keep), or NULL: their weights, entries behind the last one left
- *                as they are.  Not `weights` itself (SPC_E_PARAM), nor overlapping it
+ *                as they are.  No row of them may overlap one of `weights`
+ *                (SPC_E_PARAM)
  * The pages they came from, and page_table, are left as they are.  Positions are
  * the caller's to follow (out_index): queries and keys that encode them stay as
  * they were written, and the next new token is at out_len.  No workspace.

@@ -1165,6 +1165,29 @@ spc_status weight_rows(const void* weights, int64_t stride, int32_t length) {
   return SPC_OK;
 }
 
+// Whether `count` rows of n elements of 4 bytes, a stride apart, have one in common
+// with as many of m.
+bool rows_meet(const void* a, int64_t a_stride, int64_t n, const void* b, int64_t b_stride,
+               int64_t m, int64_t count) {
+  __int128 x = 0, y = ((__int128)(intptr_t)b - (intptr_t)a) / 4;  // where the next rows begin
+  for (int64_t i = 0, j = 0; i < count && j < count;) {
+    if (x + n <= y) {  // (all rows that end before y at once)
+      const __int128 skip = 1 + (y - x - n) / a_stride;
+      if (skip > count - i) return false;
+      i += (int64_t)skip;
+      x += skip * a_stride;
+    } else if (y + m <= x) {
+      const __int128 skip = 1 + (x - y - m) / b_stride;
+      if (skip > count - j) return false;
+      j += (int64_t)skip;
+      y += skip * b_stride;
+    } else {
+      return true;
+    }
+  }
+  return false;
+}
+
 spc_status kv_weigh_impl(const spc_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride,
                          int32_t heads, int64_t rows, const int32_t* row_start, int32_t max_rows,
                          float scale, int32_t window, const float* weights, float* out,
@@ -1177,6 +1200,9 @@ spc_status kv_weigh_impl(const spc_kv_cache* cache, const void* q, int32_t dtype
   if (st == SPC_OK) st = weight_rows(out, weights_stride, length);
   if (st != SPC_OK) return st;
   if ((uintptr_t)weights % 4 != 0) return fail(SPC_E_ALIGN, "weights must be 4-byte aligned");
+  if (weights && out != weights &&
+      rows_meet(weights, weights_stride, length, out, weights_stride, length, (int64_t)P.B * P.H))
+    return fail(SPC_E_PARAM, "out must be weights, or not overlap them");
   const WeighLayout L =
       weigh_layout(P.B, P.H, heads, P.n, (int64_t)P.width * P.S, P.f8);
   st = kv_launch_size(P.B, P.H, (int64_t)P.n * (heads / P.H), L.cut, row_start);
@@ -1222,8 +1248,11 @@ spc_status kv_evict_impl(const spc_kv_cache* cache, const float* weights, int64_
     return fail(SPC_E_SHAPE, "out_stride must be at least keep (got %lld)", (long long)out_stride);
   if (((uintptr_t)out_table | (uintptr_t)out_len | (uintptr_t)out_index | (uintptr_t)out_weights) % 4)
     return fail(SPC_E_ALIGN, "arrays must be 4-byte aligned");
-  if (out_len == cache->kv_len || out_weights == weights)
-    return fail(SPC_E_PARAM, "outputs must not be inputs of the call");
+  const int64_t B = P.cache.B;
+  if (rows_meet(cache->kv_len, B, B, out_len, B, B, 1) ||
+      (out_weights && rows_meet(weights, weights_stride, length, out_weights, out_stride, keep,
+                                B * P.cache.H)))
+    return fail(SPC_E_PARAM, "outputs must not overlap kv_len or weights, inputs of the call");
   P.weights = weights;
   P.weights_stride = weights_stride;
   P.out_stride = out_stride;
