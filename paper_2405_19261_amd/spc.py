@@ -699,8 +699,10 @@ def spc_kv_weigh(q, k_pages, v_pages, page_table, kv_len, weights=None, *, scale
     if weights is not None and weights is not out:
         if _weight_rows("weights", weights, cache, k_pages, out.shape[2]) != stride:
             raise ValueError("weights and out must have rows at one stride")
-    if rows == 0:
-        raise ValueError("there must be a new token")
+    if rows == 0:  # the weights as they were: a call whose only row is no sequence's
+        q = _new(torch.zeros, (1, heads, cache.head_dim), q.dtype, k_pages.device, stream)
+        q_start = _new(torch.zeros, cache.B + 1, torch.int32, k_pages.device, stream)
+        rows, qs, most = 1, heads * cache.head_dim, 1
     _on_current_device(k_pages)
     _check(lib().spc_kv_weigh(cache, q.data_ptr(), SPC_BF16, qs, heads, rows, _ptr(q_start), most,
                               scale, window, _ptr(weights), out.data_ptr(), stride, out.shape[2],
@@ -781,6 +783,8 @@ def spc_kv_weigh_workspace_bytes(k_pages, v_pages, page_table, kv_len, heads, ro
                                  k_scale=None, v_scale=None, q_start=None):
     """As ``spc_kv_workspace_bytes``, for ``spc_kv_weigh``."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
+    if rows == 0:
+        rows = max_q = 1
     if max_q is None:
         max_q = 0 if q_start is None else rows
     return lib().spc_kv_weigh_workspace_bytes(cache, _int32("heads", heads), rows,
