@@ -683,18 +683,20 @@ def spc_kv_weigh(q, k_pages, v_pages, page_table, kv_len, weights=None, *, scale
     of ``weights`` (float32 [B, kv_heads, length]; None: nothing), summed over
     the new tokens and the query heads of a key/value head; the chunk's own
     tokens begin at zero.  Rows and positions as for ``spc_kv_attend``.
-    Returns ``out``, which may be ``weights`` (None: a new tensor, zero from
-    ``kv_len`` on, of ``length`` or, without weights, of the table's tokens)."""
+    Returns ``out``, which may be ``weights`` and has its rows at their stride
+    (None: a new tensor, zero from ``kv_len`` on, of ``length`` or, without
+    weights, of the table's tokens)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
     rows, heads, qs, scale = _queries(q, cache, k_pages, q_start, scale)
     ws, nbytes = _workspace(workspace, k_pages)
     window = _int32("window", window)
     most = rows if max_q is None else _int32("max_q", max_q)
-    shape = (cache.B, cache.kv_heads, cache.table_width * cache.page_size)
-    if weights is not None:
-        shape = weights.shape
-    if out is None:
-        out = _new(torch.zeros, shape, torch.float32, k_pages.device, stream)
+    if out is None:  # (rows at the stride of those of weights)
+        length = row = cache.table_width * cache.page_size
+        if weights is not None:
+            row, length = _weight_rows("weights", weights, cache, k_pages), weights.shape[2]
+        out = _new(torch.zeros, (cache.B, cache.kv_heads, row), torch.float32, k_pages.device,
+                   stream)[..., :length]
     stride = _weight_rows("out", out, cache, k_pages)
     if weights is not None and weights is not out:
         if _weight_rows("weights", weights, cache, k_pages, out.shape[2]) != stride:

@@ -40,3 +40,19 @@ def test_no_new_token(ragged, calls):
     w = torch.rand((3, 2, 50))
     out = spc.spc_kv_weigh(q.flatten(0, 1) if ragged else q, *cache(), w, **kw)
     assert calls == [(1, [0, 0, 0, 0], 1, w.data_ptr(), out.data_ptr(), 50, 50)]
+
+
+@pytest.mark.parametrize("B,H", [(3, 2), (3, 1), (1, 2), (1, 1)])
+def test_weights_that_are_part_of_wider_rows(B, H, calls):
+    """A new `out` has its rows at their stride."""
+    q = torch.zeros((B, 1, 4, 64), dtype=torch.bfloat16)
+    w = torch.rand((B, H, 70))[..., 3:53]
+    out = spc.spc_kv_weigh(q, *cache(B, H), w)
+    assert out.shape == w.shape and not bool(out.any())
+    _, _, _, weights, to, stride, length = calls[0]
+    assert (weights, to, length) == (w.data_ptr(), out.data_ptr(), 50)
+    if B * H > 1:
+        assert stride == 70 and (out.stride(1) if H > 1 else out.stride(0)) == 70
+    # with weights of whole rows it is whole, as without any
+    assert spc.spc_kv_weigh(q, *cache(B, H), w.contiguous()).is_contiguous()
+    assert spc.spc_kv_weigh(q, *cache(B, H)).is_contiguous()

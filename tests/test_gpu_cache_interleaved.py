@@ -53,3 +53,18 @@ def test_evict(at, to):
     n2, index2, _ = spc.spc_kv_evict(*cache.args(lens), src, 48, other, recent=5, out_weights=out)
     assert torch.equal(n, n2) and torch.equal(index, index2) and torch.equal(out, kept)
     assert torch.equal(src, w)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_weigh_part_of_wider_rows(n):
+    """Weights between others in wider rows, without an `out`."""
+    cache, lens, _, w = setup()
+    q = randn((3, n, 4, 64), 1).to(DEV)
+    want = spc.spc_kv_weigh(q, *cache.args(lens), w)
+    wide = torch.full((3, 2, 200), 5.0, device=DEV)
+    wide[..., 31:161] = w
+    got = spc.spc_kv_weigh(q, *cache.args(lens), wide[..., 31:161])
+    assert torch.equal(got, want) and torch.equal(wide[..., 31:161], w)
+    # and they can be the next call's
+    again = spc.spc_kv_weigh(q, *cache.args(lens), got, out=got)
+    assert again is got and torch.equal(got, spc.spc_kv_weigh(q, *cache.args(lens), want))
