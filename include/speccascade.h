@@ -566,9 +566,12 @@ size_t spc_kv_weigh_workspace_bytes(const spc_kv_cache* cache, int32_t heads, in
  *   out_table    [B][out_width] int32 device array: the pages of the same pools
  *                that receive the tokens of sequence b, at positions 0, 1, ...;
  *                out_width * page_size at least keep.  They are pages that no
- *                sequence of the call holds tokens in, but that a token which
- *                comes to lie where it was is not moved: a sequence of at most
- *                `keep` tokens may be given its own pages.  A page id out of
+ *                sequence of the call holds tokens in, each for one sequence
+ *                alone (not checked), but that a token which comes to lie where
+ *                it was is not moved: a sequence of at most `keep` tokens, each
+ *                of them in a page, may be given its own pages.  (Not one with a
+ *                page that is none before its last token: the tokens behind that
+ *                would go to places which are still read.)  A page id out of
  *                range takes nothing
  *   out_len      [B] int32: the tokens kept, min(keep, those in the cache), the
  *                same for every head (kv_len of later calls; it may not overlap

@@ -719,7 +719,9 @@ def spc_kv_evict(k_pages, v_pages, page_table, kv_len, weights, keep, out_table,
     order, into the pages of ``out_table`` (int32 [B, pages], of the same
     pools): the first ``first``, the last ``recent`` and, of the others, those
     of the largest ``weights`` (float32 [B, kv_heads, length], as
-    ``spc_kv_weigh`` leaves them).  Returns (the tokens kept [B] int32, the
+    ``spc_kv_weigh`` leaves them).  The pages are ones that no sequence holds
+    tokens in, or a sequence's own where it has at most ``keep`` tokens and all
+    of them in pages: then none moves.  Returns (the tokens kept [B] int32, the
     positions they had [B, kv_heads, keep] int32, -1 behind the last, their
     weights [B, kv_heads, keep], new ones zero behind the last)."""
     cache = _kv_cache(k_pages, v_pages, page_table, kv_len, k_scale, v_scale)
