@@ -124,7 +124,7 @@ class ContextLM:
         self.encoder = None
         if encoder_lens is not None:
             lens = [int(x) for x in encoder_lens]
-            w = (max(lens) + page_size - 1) // page_size
+            w = (max(1, *lens) + page_size - 1) // page_size  # (of no states too, a page)
             pages = torch.randperm(B * w, generator=g).view(B, w).to(self.device, torch.int32)
             k, v, scales = self._pages(B * w, page_size, cache_dtype)
             self._write(g, k, v, pages, lens, scales)
