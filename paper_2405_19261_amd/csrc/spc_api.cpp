@@ -902,17 +902,19 @@ AttendLayout attend_layout(int64_t B, int64_t H, int64_t heads, int64_t n, int64
   //     145, 128: 238 / 233 / 157; of 256: 32 rows 182 / 246 / 306, 64: 282 / 378 /
   //     324, 128: 525 / 594 / 365; of 64: 32 rows 46 / 44 / 94, 128: 110 / 94 / 115,
   //     256: 205 / 179 / 211
-  // (64 rows of bfloat16 would gain by 128; the border stays where such chunks keep
-  // the answers they gave, bit for bit.)
+  // (64 rows of bfloat16 would gain by 128; a sequence's own tokens keep the border
+  // where such chunks keep the answers they gave, bit for bit.  Tokens behind a prefix,
+  // and an encoder's states with heads of 64, have the same border; for them 33 to 64
+  // rows are not measured.)
   if (f8 && D > 64) L.tile_rows = rows <= 64 ? 16 : 128;
   else L.tile_rows = rows <= 16 ? 16 : rows <= (f8 ? 256 : 64) ? 32 : 128;
   // Rows of shared keys gain more by 128.  us by 16 / 32 / 128 rows, cross attention
   // of 32 sequences to 4096 tokens, 8 heads of 128, bfloat16: 32 rows 142 / 111 / 115,
   // 64: 251 / 145 / 122; 16 sequences, 4 heads of 256: 32 rows 82 / 72 / 85, 64: 140 /
   // 106 / 90.  A prefix is read at the rate that few workgroups reach, by 16 rows
-  // each sooner: of 8192 tokens, bfloat16, heads of 128, 32 rows 25 / 30 / 24, 64: 30 /
-  // 30 / 26 (of 1000: 32 rows 12 / 15 / 21), heads of 64, 64 rows 19 / 20 / 21, of 256
-  // 41 / 50 / 33.
+  // each sooner (measured in bfloat16; 8 bits take the same): of 8192 tokens, heads of
+  // 128, 32 rows 25 / 30 / 24, 64: 30 / 30 / 26 (of 1000: 32 rows 12 / 15 / 21), heads
+  // of 64, 64 rows 19 / 20 / 21, of 256 41 / 50 / 33.
   if (kind == spc::AttendKind::kCrossTokens && !f8 && D > 64 && rows > 32) L.tile_rows = 128;
   if (kind == spc::AttendKind::kPrefix)
     L.tile_rows = rows <= 32 || (rows <= 64 && D <= 128) ? 16 : 128;

@@ -46,12 +46,13 @@ enum AttendMode { kOwn, kBehind, kCross, kShared };
 
 // A share of the keys has at least as many: a tile for each wavefront, or in
 // k_kv_attend_rows, whose wavefronts take every tile together, 512 (of a shared
-// prefix, which few workgroups take, and behind it, where the shares are joined
-// anyhow, 256; of an encoder's states 256 where workgroups are few).  (One token over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of
-// 512, 6.9 in shares of 128, and the join 4.4.  Behind a prefix, by 512 / 256: 40 rows
-// of 8 sequences with up to 1000 tokens of their own, 32/8 heads of 128 in e4m3, 87 /
-// 67; 64 rows of 4 with 1000, 16/4 heads of 256 in bfloat16, 120 / 103; where there
-// are enough workgroups, 600 rows of 2 with 548, 16/4 heads of 128, 68 / 72.)
+// prefix, which few workgroups take, behind it, where the shares are joined anyhow,
+// and of an encoder's states, whose number the launch bounds instead, 256).  (One token
+// over 1500 bfloat16 tokens of 8 heads: 13.9 us in shares of 512, 6.9 in shares of 128,
+// and the join 4.4.  Behind a prefix, by 512 / 256: 40 rows of 8 sequences with up to
+// 1000 tokens of their own, 32/8 heads of 128 in e4m3, 87 / 67; 64 rows of 4 with 1000,
+// 16/4 heads of 256 in bfloat16, 120 / 103; where there are enough workgroups, 600 rows
+// of 2 with 548, 16/4 heads of 128, 68 / 72.)
 constexpr int share_keys(int tile_rows, bool f8, int mode = kOwn) {
   return tile_rows > 64 ? (mode != kOwn ? 256 : 512) : f8 ? 256 : 128;
 }

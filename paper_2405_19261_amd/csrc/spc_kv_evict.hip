@@ -19,10 +19,10 @@ namespace {
 // Each weight is one workgroup's, its rows always added in one order: no atomics.
 // Few rows are bound by the bytes of the keys (one token of 32 sequences over 4096, 8
 // heads of 128 in bfloat16: 48 us, 5.6 TB/s, and 7 for the second step), many by the
-// vector instructions of two softmaxes (42 % of the cycles) and uneven lengths, with
-// the start of workgroups that have few tiles (32 tokens of 4 sequences over up to
-// 16384 in e4m3: 29 and 30 us, where the products are 5 and the bytes 9; 600 tokens of
-// 2 over 2048: 22, 27 and 5).
+// vector instructions of two softmaxes (34 to 43 % of the cycles) and uneven lengths,
+// with the start of workgroups that have few tiles (up to 32 tokens of 4 sequences over
+// up to 16384 in e4m3: 29 and 30 us at 1.5 wavefronts a SIMD, where the products are 5
+// and the bytes 9; 600 tokens of 2 over 2048: 22, 27 and 5).
 
 // The first step: as k_kv_attend, without values.
 template <int D, bool F8, int MT>

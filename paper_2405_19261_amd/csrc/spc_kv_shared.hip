@@ -4,8 +4,8 @@
 // Cross attention is the cache's attention with one limit for all rows and a byte a
 // key that may mask it: bits a lane, taken once a tile; a masked key's score is minus
 // infinity and its value zero, whatever the page holds.  Bound by the bytes of the
-// cache where rows are few (6 rows of 32 sequences to 622 tokens on average, 16 heads
-// of 64: 19 us, 3.8 TB/s), in 8 bits by widening them (8 rows of 16 sequences to 4096
+// cache where rows are few (up to 6 rows of 32 sequences to 544 tokens on average, 16
+// heads of 64: 19 us, 3.8 TB/s), in 8 bits by widening them (8 rows of 16 sequences to 4096
 // masked tokens, 32/8 heads of 128: 39 us, 3.6 TB/s), and by the matrix unit and the
 // softmax together where rows are many (even chunks of 1024 rows 717 to 862 TFLOP/s).
 //
