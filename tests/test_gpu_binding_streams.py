@@ -63,3 +63,27 @@ def test_on_another_stream(name, handle):
     for x, y, z in zip(want, first, got if isinstance(got, tuple) else (got,)):
         assert torch.equal(x.cpu().view(torch.uint8), y.view(torch.uint8))
         assert torch.equal(x.view(torch.uint8), z.view(torch.uint8))
+
+
+@pytest.mark.parametrize("name", ["attend", "cross", "evict", "read", "shared", "truncate", "weigh"])
+def test_on_a_captured_branch(name):
+    """A call on a stream that a capture forks to and joins: what it makes is filled in the branch,
+    every replay again."""
+    def outputs(x):
+        return x if isinstance(x, tuple) else (x,)
+
+    call = calls()[name]
+    want = [t.clone() for t in outputs(call())]
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        side.wait_stream(torch.cuda.current_stream())
+        got = outputs(call(stream=side))
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        for t in got:
+            t.fill_(3)
+        call()  # (eager work between the replays)
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(want, got):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
